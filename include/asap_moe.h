@@ -334,6 +334,22 @@ int asap_moe_layer(asap_moe_t h, const void* x, int32_t n, void* out, void* ws,
 int asap_moe_layer_dyn(asap_moe_t h, const int32_t* layer_id, const void* x, int32_t n,
                        void* out, void* ws, size_t ws_bytes, void* stream);
 
+/* The whole layer for a few tokens (decode): route, expert FFN and combine of
+ * 0 <= n <= ASAP_MOE_FEW_MAX_TOKENS tokens in two kernel launches on a handle
+ * that serves asap_moe_layer too (same packed weights, both dtypes, every
+ * gating rule).  layer_id: NULL (layer 0) or a device int32 with the rules of
+ * asap_moe_layer_dyn.
+ *  - The function of asap_moe_layer with fewer roundings, so not the same
+ *    bits: logits are summed in another order; BF16 layers keep h as the sum of
+ *    two bf16 and expert outputs in fp32 until the final rounding; FP8 layers
+ *    quantise x and h with correctly rounded quotients and keep expert outputs
+ *    in fp32.  The same call gives the same bits each time.
+ *  - The workspace is asap_moe_workspace_size for n tokens; its contents
+ *    before the call do not matter. */
+#define ASAP_MOE_FEW_MAX_TOKENS 64
+int asap_moe_layer_few(asap_moe_t h, const int32_t* layer_id, const void* x, int32_t n, void* out,
+                       void* ws, size_t ws_bytes, void* stream);
+
 /* Timing hook: the next asap_moe_layer or asap_moe_layer_dyn call made by
  * this thread records events[0] (a cudaEvent_t; NULL entries are skipped) on
  * its stream before its first kernel and events[i] after its i-th step:

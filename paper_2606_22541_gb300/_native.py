@@ -57,6 +57,7 @@ SIGNATURES = {
     "asap_moe_combine": [_P, _P, _P, _P, _P, _I, _P, _P],
     "asap_moe_layer": [_P, _P, _I, _P, _P, _SZ, _P],
     "asap_moe_route_noalloc": [_P, _P, _I, _P, _P, _P, _P, _P],
+    "asap_moe_layer_few": [_P, _P, _P, _I, _P, _P, _SZ, _P],
     "asap_moe_layer_batched": [_P, _I, ctypes.POINTER(_P), ctypes.POINTER(_I), ctypes.POINTER(_P), _P, _SZ, _P],
     "asap_moe_layer_dyn": [_P, _P, _P, _I, _P, _P, _SZ, _P],
     "asap_moe_layer_batched_dyn": [_P, _P, _I, ctypes.POINTER(_P), ctypes.POINTER(_I), ctypes.POINTER(_P), _P, _SZ,

@@ -185,6 +185,18 @@ def asap_moe_layer(h, x, out, ws, stream=None):
         _timing.events = None   # the call has taken this thread's timing request
 
 
+FEW_MAX_TOKENS = 64
+
+
+def asap_moe_layer_few(h, x, out, ws, stream=None, layer_id=None):
+    """The whole layer for 1 to FEW_MAX_TOKENS tokens in two kernels (the
+    decode steps of a handle whose prompt batches go through asap_moe_layer).
+    layer_id: None (layer 0) or a one-element int32 CUDA tensor."""
+    p, n = _ws(ws)
+    check("asap_moe_layer_few", lib().asap_moe_layer_few(h.ptr, _ptr(layer_id), _ptr(x), x.shape[0], _ptr(out), p, n,
+                                                         _stream(stream)))
+
+
 def asap_moe_layer_batched(h, xs, outs, ws, stream=None):
     """Serve several ready micro-batches in one pass (one grouped GEMM per
     weight matrix); outs[i] equals asap_moe_layer on xs[i] bit for bit."""

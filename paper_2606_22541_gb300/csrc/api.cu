@@ -3,6 +3,7 @@
 // than create / destroy / status only enqueues kernels on the caller's stream.
 #include "../../include/asap_moe.h"
 #include "common.cuh"
+#include "few.h"
 #include "internal.h"
 #include "gemm_config.h"
 
@@ -124,6 +125,77 @@ Layout layout(const asap_moe_config& c, long long n) {
   }
   L.total = off;
   return L;
+}
+
+// ------------------------------------------------------------ few tokens
+// K slices of a tile so that a launch of ``tiles`` tiles has at least
+// kFewItemsPerSm work items per SM (of a GB300: the size of a workspace needs no
+// GPU), with at least kFewMinSteps k-steps each.
+constexpr int kFewItemsPerSm = 8, kFewSms = 152, kFewMinSteps = 4;
+int few_slices(long long tiles, int k_steps) {
+  const long long want = (static_cast<long long>(kFewItemsPerSm) * kFewSms + tiles - 1) / tiles;
+  return static_cast<int>(std::max<long long>(1, std::min<long long>(want, k_steps / kFewMinSteps)));
+}
+
+// Sizes and workspace offsets of a few-token call of n tokens (1 .. kFewTokens).
+struct FewLayout {
+  asap::FewArgs a{};
+  size_t meta, counters, ximg, himg, p1, p1s, y, ys, total;
+};
+
+FewLayout few_layout(const asap_moe_config& c, int n) {
+  FewLayout L{};
+  asap::FewArgs& a = L.a;
+  const bool fp8 = c.dtype == ASAP_FP8_E4M3_BLOCK128;
+  const int step = fp8 ? 128 : 64, k = c.top_k;
+  a.n = n;
+  a.H = c.hidden;
+  a.I = c.inter;
+  a.Is = c.n_shared ? c.shared_inter : 0;
+  a.max_active = std::min(c.n_experts, n * k);
+  const int tI = a.I / 128, tS = a.Is / 128, tH = a.H / 256;
+  a.s1 = few_slices(tS + static_cast<long long>(a.max_active) * tI, a.H / step);
+  const long long down = static_cast<long long>(a.max_active + (a.Is ? 1 : 0)) * tH;
+  a.s2 = few_slices(down, a.I / step);
+  a.s2s = a.Is ? few_slices(down, a.Is / step) : 0;
+  a.down_tickets = 1 + tS + a.max_active * tI;
+  a.h_ready = a.down_tickets + tH;
+  a.n_counters = a.h_ready + 1 + a.max_active;
+  // rings: 32 KB of weights a stage; operand rows (e4m3: and their scales) of the widest k-step, BF16 h rows twice
+  const int m8 = asap::round_up_dev(n, 8);
+  const int rows = fp8 ? asap::round_up_dev(n, 16) : 2 * m8;
+  a.x_slot = asap::round_up_dev(std::max(rows * 128, fp8 ? m8 * 132 : 0), 1024);
+  const int room = static_cast<int>(asap::kFewSmem - asap::kFewSmemState);
+  a.stages_w = 6;
+  while ((room - a.stages_w * 32768) / a.x_slot < std::min(a.stages_w, 4)) --a.stages_w;
+  a.stages_x = std::min(asap::kFewMaxStages, (room - a.stages_w * 32768) / a.x_slot);
+  a.smem = asap::kFewSmemState + static_cast<size_t>(a.stages_w) * 32768 + static_cast<size_t>(a.stages_x) * a.x_slot;
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    const size_t o = off;
+    off = (off + bytes + 255) & ~static_cast<size_t>(255);
+    return o;
+  };
+  const size_t nk = static_cast<size_t>(n) * k;
+  // groups of 8 rows of the active experts: at most one per row, and the rows over 8 plus one per expert
+  const size_t groups = std::min<size_t>(nk, nk / 8 + a.max_active);
+  const size_t row = fp8 ? 132 : 128, hrows = fp8 ? 8 : 16;
+  L.meta = take(sizeof(asap::FewMeta));
+  L.counters = take(a.n_counters * sizeof(int));
+  L.ximg = take(a.H / step * m8 * row);
+  L.himg = take((a.Is / step * (m8 / 8) + a.I / step * groups) * hrows * row);
+  L.p1 = take(a.s1 * nk * 2 * a.I * 4);
+  L.p1s = take(static_cast<size_t>(a.s1) * n * 2 * a.Is * 4);
+  L.y = take(a.s2 * nk * a.H * 4);
+  L.ys = take(static_cast<size_t>(a.s2s) * n * a.H * 4);
+  L.total = off;
+  return L;
+}
+
+// Bytes of workspace that serve every enqueuing call of n tokens.
+size_t workspace_bytes(const asap_moe_config& c, int n) {
+  const size_t b = layout(c, n).total;
+  return n <= asap::kFewTokens ? std::max(b, few_layout(c, n).total) : b;
 }
 
 template <typename T>
@@ -683,7 +755,7 @@ ASAP_API int asap_moe_workspace_size(const asap_moe_config* cfg, int32_t n_token
   if (r != ASAP_OK) return r;
   if (!bytes) return fail(ASAP_ERR_INVALID, "NULL bytes");
   if (n_tokens < 0 || n_tokens > cfg->max_tokens) return fail(ASAP_ERR_INVALID, "n_tokens outside [0, max_tokens]");
-  *bytes = n_tokens == 0 ? 0 : layout(*cfg, n_tokens).total;
+  *bytes = n_tokens == 0 ? 0 : workspace_bytes(*cfg, n_tokens);
   return ASAP_OK;
 }
 
@@ -874,6 +946,7 @@ ASAP_API int asap_moe_create_layers(const asap_moe_config* cfg, const asap_moe_w
   if (e == cudaSuccess) e = asap::pair_gemm_set_attributes();
   if (e == cudaSuccess) e = asap::fp8_gemm_set_attributes();
   if (e == cudaSuccess) e = asap::route_fused_set_attributes();
+  if (e == cudaSuccess) e = asap::few_set_attributes();
   if (e != cudaSuccess) return bail(cuda_fail(e, "GEMM attributes"));
   h->fp8 = c.dtype == ASAP_FP8_E4M3_BLOCK128;
   h->tc_router = (c.n_experts == asap::kGemmBN);
@@ -1316,6 +1389,40 @@ ASAP_API int asap_moe_layer_dyn(asap_moe_t h, const int32_t* layer_id, const voi
   if (!h) return fail(ASAP_ERR_INVALID, "NULL handle");
   if (!valid_layer_ptr(layer_id)) return fail(ASAP_ERR_INVALID, "layer_id must be a non-NULL 4-byte aligned device pointer");
   return run_layer(h, x, n, out, ws, ws_bytes, layer_id, stream, tev);
+}
+
+ASAP_API int asap_moe_layer_few(asap_moe_t h, const int32_t* layer_id, const void* x, int32_t n, void* out, void* ws,
+                                size_t ws_bytes, void* stream) {
+  if (!h) return fail(ASAP_ERR_INVALID, "NULL handle");
+  const int most = std::min(h->cfg.max_tokens, asap::kFewTokens);
+  if (n < 0 || n > most)
+    return fail(ASAP_ERR_INVALID, "n = " + std::to_string(n) + " outside [0, " + std::to_string(most) + "]");
+  if (layer_id && (reinterpret_cast<uintptr_t>(layer_id) & 3u) != 0)
+    return fail(ASAP_ERR_INVALID, "layer_id must be 4-byte aligned");
+  if (n == 0) return ASAP_OK;
+  if (!x || !out || !aligned16(x) || !aligned16(out)) return fail(ASAP_ERR_INVALID, "NULL or unaligned tensor");
+  if (!ws) return fail(ASAP_ERR_WORKSPACE, "NULL workspace");
+  if ((reinterpret_cast<uintptr_t>(ws) & 255u) != 0) return fail(ASAP_ERR_INVALID, "workspace must be 256-byte aligned");
+  const FewLayout L = few_layout(h->cfg, n);
+  if (ws_bytes < L.total)
+    return fail(ASAP_ERR_WORKSPACE,
+                "workspace has " + std::to_string(ws_bytes) + " bytes, needs " + std::to_string(L.total));
+  asap::FewArgs a = L.a;
+  a.gate = gate_params(h, layer_id ? layer_id : h->layer_ids);
+  a.lref = a.gate.lref;
+  a.status = h->status;
+  a.x = x;
+  a.out = out;
+  a.meta = at<asap::FewMeta>(ws, L.meta);
+  a.counters = at<int>(ws, L.counters);
+  a.ximg = at<uint8_t>(ws, L.ximg);
+  a.himg = at<uint8_t>(ws, L.himg);
+  a.p1 = at<float>(ws, L.p1);
+  a.p1s = at<float>(ws, L.p1s);
+  a.y = at<float>(ws, L.y);
+  a.ys = at<float>(ws, L.ys);
+  CU_TRY(asap::few_launch(a, h->fp8, h->num_sms, S(stream)), "few-token layer launch");
+  return ASAP_OK;
 }
 
 ASAP_API int asap_moe_layer_batched(asap_moe_t h, int32_t count, const void* const* xs, const int32_t* ns,

@@ -1,0 +1,1015 @@
+// The whole MoE layer for a few tokens (1 .. kFewTokens): two kernels.
+//
+//   out[t] = sum_j w[t,j] Wd_e (silu(Wg_e x_t) * (Wu_e x_t)) + shared expert,  e = idx[t,j]
+//
+// With one to a few rows per expert every weight is used once, so the layer is a
+// stream of the active experts' matrices (three of H x I each) and nothing else
+// matters but that this stream never stops.
+//
+// few_route_kernel (one cluster): router logits with mma.sync, K split over the
+// CTAs and added in rank order through distributed shared memory; gating, one
+// warp per token; the list of active experts, each with the set of its tokens
+// as a 64-bit mask (so a row's place in its expert is a popcount); the hidden
+// states as an image of the operand tiles (128-byte rows, 128-byte swizzle; e4m3
+// with scales for FP8), which the second kernel copies to shared memory as they
+// are; and zeroed counters.
+//
+// few_ffn_kernel (one CTA per SM): a list of work items, gate/up tiles of all
+// experts and then down tiles, claimed one by one from a counter.  An item is a
+// 256-row weight tile (a box per k-step, 32 KB, as the handle packs them) over
+// a slice of K.  The weights are the M operand of the MMA and all tokens the N
+// operand, so a tile costs the same whatever its rows; the tensor core is idle
+// most of the time.
+//  - gate/up: the partial sums of a K slice go to the workspace in fp32; the
+//    last slice of a tile to arrive adds them in slice order, applies SwiGLU
+//    and writes h as an operand image: e4m3 with scales, or, for BF16, as the
+//    sum of two bf16 (the value and what its rounding left), since N has room:
+//    h keeps 16 bits at no cost.
+//  - down: a tile waits until its expert's h is complete.  Partial sums are
+//    fp32; the last arrival of an output tile adds the experts in slot order.
+// Sums are taken in a fixed order, so a call gives the same bits each time.
+// An item waits only for items claimed before it, by CTAs that are running,
+// so the launch needs no co-residency to make progress.
+#include "common.cuh"
+#include "few.h"
+#include "internal.h"
+
+#include <cuda_fp8.h>
+#include <math_constants.h>
+
+namespace asap {
+
+namespace {
+
+constexpr unsigned kFull = 0xffffffffu;
+
+__device__ __forceinline__ uint32_t rank_in_cluster() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ uint32_t map_rank(uint32_t addr, uint32_t rank) {
+  uint32_t d;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(d) : "r"(addr), "r"(rank));
+  return d;
+}
+__device__ __forceinline__ float ld_rank_f32(uint32_t addr) {
+  float v;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ void st_rank_u32(uint32_t addr, uint32_t v) {
+  asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+}
+
+// ------------------------------------------------------------ operand images
+// A k-step's rows: R rows of 128 bytes, 16-byte chunk c of row r at chunk
+// c ^ (r % 8) (the 128-byte swizzle of a tile that starts on a 1024-byte
+// boundary), then, for FP8, R fp32 scales.
+template <bool FP8>
+__host__ __device__ constexpr int step_bytes(int rows) {
+  return rows * (FP8 ? 132 : 128);
+}
+__device__ __forceinline__ int swizzled(int row, int byte) {
+  return row * 128 + ((((byte >> 4) ^ (row & 7)) << 4) | (byte & 15));
+}
+
+// e4m3 of v / s.  The quotient is the correctly rounded one (Markstein 1990: one
+// correction of v * (1/s) by its residual), as a division gives it: bf16
+// values over amax / 448 fall exactly between two e4m3 values for about one
+// element in 500, and those must not depend on how the quotient was taken.
+__device__ __forceinline__ float quotient(float v, float s, float inv) {
+  const float q = v * inv;
+  return fmaf(fmaf(-q, s, v), inv, q);
+}
+__device__ __forceinline__ uint32_t e4m3x4(float a, float b, float c, float d) {
+  const __nv_fp8x2_storage_t lo = __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
+  const __nv_fp8x2_storage_t hi = __nv_cvt_float2_to_fp8x2(make_float2(c, d), __NV_SATFINITE, __NV_E4M3);
+  return static_cast<uint32_t>(lo) | (static_cast<uint32_t>(hi) << 16);
+}
+
+// ------------------------------------------------------------ route
+constexpr int kRouteWarps = 16;
+constexpr int kRouteThreads = 32 * kRouteWarps;
+
+// Float as an unsigned that orders the same way (-0 as +0).
+__device__ __forceinline__ uint32_t ordered(float f) {
+  const uint32_t u = __float_as_uint(f + 0.0f);
+  return (u >> 31) ? ~u : u | 0x80000000u;
+}
+
+// Gating of one token by a warp, from its logits (lane l: experts l, l + 32,
+// ...): expert and weight of slot j in lane j.  The rules and tie-breaks of
+// gate_kernel (route.cu); a round's winner is found with two warp reductions.
+// scratch: n_groups * (group size + 1) floats.
+__device__ __forceinline__ void gate_token(const GateParams& p, const float* bias, const float (&logit)[8], float* scratch,
+                                           int lane, int& my_e, float& my_w) {
+  const int E = p.n_experts;
+  const bool grouped = p.gating == 2;
+  float key[8], val[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int e = lane + 32 * i;
+    val[i] = grouped ? gate_sigmoid(logit[i]) : logit[i];
+    key[i] = val[i] + (grouped && bias && e < E ? __ldg(bias + e) : 0.f);
+  }
+  uint32_t open = 0;  // experts of this lane that may be chosen
+  if (grouped) {
+    const int gsz = E / p.n_groups;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int e = lane + 32 * i;
+      if (e < E) scratch[e + e / gsz] = key[i];
+    }
+    __syncwarp();
+    float score = -CUDART_INF_F;
+    if (lane < p.n_groups) {
+      float m1 = -CUDART_INF_F, m2 = -CUDART_INF_F;
+      for (int j = 0; j < gsz; ++j) {
+        const float v = scratch[lane * (gsz + 1) + j];
+        m2 = fmaxf(m2, fminf(m1, v));
+        m1 = fmaxf(m1, v);
+      }
+      score = m1 + m2;
+    }
+    int rank = 0;  // groups in front of this lane's
+    for (int g = 0; g < p.n_groups; ++g) {
+      const float o = __shfl_sync(kFull, score, g);
+      rank += (o > score || (o == score && g < lane)) ? 1 : 0;
+    }
+    const uint32_t kept = __ballot_sync(kFull, lane < p.n_groups && rank < p.topk_groups);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int e = lane + 32 * i;
+      if (e < E && ((kept >> (e / gsz)) & 1u)) open |= 1u << i;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (lane + 32 * i < E) open |= 1u << i;
+  }
+  my_e = -1;
+  float my_v = 0.f;
+  float top = 0.f;  // the first slot's value
+  for (int j = 0; j < p.top_k; ++j) {
+    uint32_t best = 0;
+    int be = 0x7fffffff;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t o = ordered(key[i]);
+      if (((open >> i) & 1u) && (be == 0x7fffffff || o > best)) {
+        best = o;
+        be = lane + 32 * i;
+      }
+    }
+    const uint32_t mx = __reduce_max_sync(kFull, best);
+    const int win = __reduce_min_sync(kFull, best == mx ? be : 0x7fffffff);
+    if (win == 0x7fffffff) break;
+    float v = 0.f;
+    if ((win & 31) == lane) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (i == (win >> 5)) v = val[i];
+      open &= ~(1u << (win >> 5));
+    }
+    v = __shfl_sync(kFull, v, win & 31);
+    if (j == 0) top = v;
+    if (lane == j) {
+      my_e = win;
+      my_v = v;
+    }
+  }
+  // lanes 0 .. k-1 hold the slots; sums in slot order
+  float num = lane < p.top_k && my_e >= 0 ? (grouped ? my_v : expf(my_v - top)) : 0.f;
+  float den = 0.f;
+  for (int j = 0; j < p.top_k; ++j) den += __shfl_sync(kFull, num, j);
+  if (p.gating == 0) {
+    den = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (lane + 32 * i < E) den += expf(logit[i] - top);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) den += __shfl_xor_sync(kFull, den, o);
+  }
+  my_w = num / den * (grouped ? p.route_scale : 1.0f);
+}
+
+// Hidden states as operand image: rows n .. are zero.
+template <bool FP8>
+__device__ __forceinline__ void write_image(const FewArgs& a, int rows, long long thread, long long threads) {
+  const int V = a.H / 8;  // 16-byte vectors of a row
+  const uint4* x = static_cast<const uint4*>(a.x);
+  if constexpr (!FP8) {
+    for (long long i = thread; i < static_cast<long long>(rows) * V; i += threads) {
+      const int t = static_cast<int>(i / V), v = static_cast<int>(i % V);
+      const uint4 d = t < a.n ? ld_dep(x + static_cast<long long>(t) * V + v) : make_uint4(0, 0, 0, 0);
+      *reinterpret_cast<uint4*>(a.ximg + static_cast<long long>(v >> 3) * step_bytes<false>(rows) +
+                                swizzled(t, (v & 7) * 16)) = d;
+    }
+  } else {
+    // 16 threads a group of 128 channels (rows * V and the stride are multiples of 32: a warp stays together)
+    for (long long i = thread; i < static_cast<long long>(rows) * V; i += threads) {
+      const int t = static_cast<int>(i / V), v = static_cast<int>(i % V);
+      const uint4 d = t < a.n ? ld_dep(x + static_cast<long long>(t) * V + v) : make_uint4(0, 0, 0, 0);
+      const float f[8] = {bf16_lo(d.x), bf16_hi(d.x), bf16_lo(d.y), bf16_hi(d.y),
+                          bf16_lo(d.z), bf16_hi(d.z), bf16_lo(d.w), bf16_hi(d.w)};
+      float am = 0.f;
+#pragma unroll
+      for (int u = 0; u < 8; ++u) am = fmaxf(am, fabsf(f[u]));
+#pragma unroll
+      for (int o = 8; o > 0; o >>= 1) am = fmaxf(am, __shfl_xor_sync(kFull, am, o));
+      const float s = am > 0.f ? am / 448.0f : 1.0f, inv = 1.0f / s;
+      uint2 q;
+      q.x = e4m3x4(quotient(f[0], s, inv), quotient(f[1], s, inv), quotient(f[2], s, inv), quotient(f[3], s, inv));
+      q.y = e4m3x4(quotient(f[4], s, inv), quotient(f[5], s, inv), quotient(f[6], s, inv), quotient(f[7], s, inv));
+      uint8_t* step = a.ximg + static_cast<long long>(v >> 4) * step_bytes<true>(rows);
+      *reinterpret_cast<uint2*>(step + swizzled(t, (v & 15) * 8)) = q;
+      if ((v & 15) == 0) *reinterpret_cast<float*>(step + rows * 128 + t * 4) = s;
+    }
+  }
+}
+
+template <bool FP8>
+__global__ void __launch_bounds__(kRouteThreads) few_route_kernel(const FewArgs a) {
+  pdl_launch();  // the second kernel may come up and fetch weights meanwhile
+  pdl_wait();
+  extern __shared__ float smem_f[];
+  __shared__ int sel_e[kFewTokens * kMaxTopK];
+  __shared__ float sel_w[kFewTokens * kMaxTopK];
+  __shared__ unsigned long long mask[kMaxExperts];
+  __shared__ int packed_before[kMaxExperts];  // rows, row groups and actives before expert e
+  __shared__ int warp_total[kMaxExperts / 32];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = static_cast<int>(rank_in_cluster());
+  const int E = a.gate.n_experts, k = a.gate.top_k, n = a.n;
+  const int tiles = (E + 15) / 16, Ep = 16 * tiles;
+  const int subs = kRouteWarps / tiles;          // K parts inside the CTA
+  const int per = ceil_div_dev(n, kFewCluster);  // tokens gated by a CTA at most
+  float* part = smem_f;                          // [subs][n][Ep]
+  float* gat = smem_f + subs * n * Ep;           // [per][kFewCluster][Ep]
+  const LayerEntry& le =
+      a.lref.table[load_layer(a.lref.layer, a.lref.n_layers, a.status, rank == 0 && threadIdx.x == 0)];
+
+  // ---- partial logits: expert tile (16 rows, M) x tokens (8 per MMA, N); thread (g, q) feeds 16 bytes of a
+  // row to two MMAs whose K order both operands share
+  const int tile = warp % tiles, sub = warp / tiles;
+  if (sub < subs) {
+    const uint4* __restrict__ wr = static_cast<const uint4*>(le.router_w);
+    const uint4* x = static_cast<const uint4*>(a.x);
+    const int V = a.H / 8, units = a.H / 32;
+    const int u0 = units * rank / kFewCluster, u1 = units * (rank + 1) / kFewCluster;
+    const int g = lane >> 2, q = lane & 3;
+    const int e0 = tile * 16 + g, e1 = e0 + 8;
+    const uint4 zero = make_uint4(0, 0, 0, 0);
+    float c[kFewTokens / 8][4];
+#pragma unroll
+    for (int j = 0; j < kFewTokens / 8; ++j) c[j][0] = c[j][1] = c[j][2] = c[j][3] = 0.f;
+#pragma unroll 4
+    for (int u = u0 + sub; u < u1; u += subs) {
+      const int v = 4 * u + q;
+      const uint4 w0 = e0 < E ? __ldg(wr + static_cast<long long>(e0) * V + v) : zero;
+      const uint4 w1 = e1 < E ? __ldg(wr + static_cast<long long>(e1) * V + v) : zero;
+#pragma unroll
+      for (int j = 0; j < kFewTokens / 8; ++j) {
+        if (8 * j < n) {
+          const int t = 8 * j + g;
+          const uint4 xv = t < n ? ld_dep(x + static_cast<long long>(t) * V + v) : zero;
+          mma_bf16_16816(c[j], w0.x, w1.x, w0.y, w1.y, xv.x, xv.y);
+          mma_bf16_16816(c[j], w0.z, w1.z, w0.w, w1.w, xv.z, xv.w);
+        }
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < kFewTokens / 8; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int t = 8 * j + 2 * q + (i & 1);
+        if (t < n) part[(sub * n + t) * Ep + tile * 16 + g + 8 * (i >> 1)] = c[j][i];
+      }
+  }
+  // ---- what the second kernel needs besides the routing
+  const long long thread = static_cast<long long>(rank) * kRouteThreads + threadIdx.x;
+  constexpr long long kThreadsAll = static_cast<long long>(kFewCluster) * kRouteThreads;
+  for (long long i = thread; i < a.n_counters; i += kThreadsAll) a.counters[i] = 0;
+  write_image<FP8>(a, round_up_dev(n, 8), thread, kThreadsAll);
+  for (int e = threadIdx.x; e < kMaxExperts; e += kRouteThreads) mask[e] = 0;
+  __syncthreads();
+  if (subs > 1) {  // parts in order
+    for (int i = threadIdx.x; i < n * Ep; i += kRouteThreads) {
+      float s = part[i];
+      for (int u = 1; u < subs; ++u) s += part[u * n * Ep + i];
+      part[i] = s;
+    }
+  }
+  cluster_sync();
+  // ---- this CTA's tokens rank, rank + kFewCluster, ...: every warp fetches some ranks' partial logits
+  const int mine = rank < n ? ceil_div_dev(n - rank, kFewCluster) : 0;
+  for (int i = warp; i < mine * kFewCluster; i += kRouteWarps) {
+    const int src = i % kFewCluster, ti = i / kFewCluster;
+    const uint32_t from = map_rank(smem_u32(part + (rank + ti * kFewCluster) * Ep), src);
+    for (int e = lane; e < E; e += 32) gat[i * Ep + e] = ld_rank_f32(from + 4u * e);
+  }
+  __syncthreads();
+  if (warp < mine) {
+    const int t = rank + warp * kFewCluster;
+    float logit[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int e = lane + 32 * i;
+      float l = 0.f;
+      if (e < E) {
+        const float* src = gat + warp * kFewCluster * Ep + e;
+        l = src[0];
+#pragma unroll
+        for (int s = 1; s < kFewCluster; ++s) l += src[s * Ep];
+      }
+      logit[i] = l;
+    }
+    __syncwarp();
+    int e;
+    float w;
+    // the gathered logits are in registers: their place holds the group scores (E + 32 floats of at least 8 Ep)
+    gate_token(a.gate, le.router_bias, logit, gat + warp * kFewCluster * Ep, lane, e, w);
+    if (lane < k) {
+      st_rank_u32(map_rank(smem_u32(&sel_e[t * k + lane]), 0), static_cast<uint32_t>(e));
+      st_rank_u32(map_rank(smem_u32(&sel_w[t * k + lane]), 0), __float_as_uint(w));
+    }
+  }
+  cluster_sync();  // all choices are in rank 0, and no CTA's shared memory is read any more
+  if (rank != 0) return;
+  // ---- active experts in order, their tokens, rows and row groups
+  for (int p = threadIdx.x; p < n * k; p += kRouteThreads) {
+    const int e = sel_e[p];
+    if (e >= 0 && e < E) atomicOr(&mask[e], 1ull << (p / k));
+    else record_status(a.status, ST_BAD_EXPERT_INDEX);
+  }
+  __syncthreads();
+  int v = 0, incl = 0;
+  if (threadIdx.x < kMaxExperts) {
+    const int m = __popcll(mask[threadIdx.x]);
+    v = m ? 1 | (m << 10) | (((m + 7) / 8) << 20) : 0;  // at most 256, 512 and 512 in all
+    incl = v;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int b = __shfl_up_sync(kFull, incl, o);
+      if (lane >= o) incl += b;
+    }
+    if (lane == 31) warp_total[warp] = incl;
+  }
+  __syncthreads();
+  FewMeta* meta = a.meta;
+  if (threadIdx.x < kMaxExperts) {
+    int before = 0;
+    for (int w2 = 0; w2 < warp; ++w2) before += warp_total[w2];
+    before += incl - v;
+    packed_before[threadIdx.x] = before;
+    if (v) {
+      const int j = before & 1023;
+      meta->expert[j] = threadIdx.x;
+      meta->start[j] = (before >> 10) & 1023;
+      meta->row8[j] = before >> 20;
+      meta->mask[j] = mask[threadIdx.x];
+    }
+    if (threadIdx.x == kMaxExperts - 1) meta->active = (before + v) & 1023;
+  }
+  __syncthreads();
+  for (int p = threadIdx.x; p < n * k; p += kRouteThreads) {
+    const int e = sel_e[p], t = p / k;
+    const bool ok = e >= 0 && e < E;
+    meta->pos[p] = ok ? ((packed_before[e] >> 10) & 1023) + __popcll(mask[e] & ((1ull << t) - 1)) : -1;
+    meta->w[p] = sel_w[p];
+  }
+}
+
+// ------------------------------------------------------------ expert FFN
+constexpr int kWBytes = 256 * 128;  // weight box
+constexpr int kEpiWarps = 8;
+constexpr int kEpiThreads = 32 * kEpiWarps;
+constexpr int kThreads = 32 * (4 + kEpiWarps);
+constexpr int kQ = 6;               // items in flight in a CTA
+constexpr int kQReaders = 2 + kEpiWarps;
+constexpr uint32_t kTmemCols = 512;
+constexpr int kPartials = 4;        // FP8: TMEM partials of 2 x 64 columns
+constexpr int kAccs = 2;            // BF16: accumulators of 2 x 128 columns
+
+struct FewItem {
+  bool down, shared;
+  int j;           // index among the active experts
+  int tile;        // 256-row weight tile of the expert's matrix
+  int slice, kb0, kb1;
+  int tokens;      // of the expert
+  int rows;        // operand rows of a k-step
+  int n;           // N of the MMA
+  int start;       // the expert's first row among the routed rows
+  int ticket;      // counter of the output tile
+  int slices;      // arrivals that complete the tile
+  unsigned long long mask;
+};
+
+struct FewSmem {  // behind the rings
+  uint64_t bar[2 * kFewMaxStages + 2 * kFewMaxStages + 2 * kPartials + 2 * kQ + 1];
+  int q[kQ];
+  uint32_t tmem;
+  int abort;
+  int layer;
+  int last;
+  int active;
+  int expert[kMaxExperts], start[kMaxExperts], row8[kMaxExperts];
+  unsigned long long mask[kMaxExperts];
+  int pos[kFewTokens * kMaxTopK];
+  float w[kFewTokens * kMaxTopK];
+};
+static_assert(sizeof(FewSmem) <= kFewSmemState, "shared memory budget");
+
+template <bool FP8>
+__device__ __forceinline__ FewItem decode(const FewArgs& a, const FewSmem& s, int item) {
+  FewItem T;
+  const int tI = a.I / 128, tS = a.Is / 128, tH = a.H / 256;
+  const int gu = (tS + s.active * tI) * a.s1;  // gate/up items
+  T.down = item >= gu;
+  int kit;
+  if (!T.down) {
+    const int t = item / a.s1;
+    T.slice = item - t * a.s1;
+    T.shared = t < tS;
+    T.j = T.shared ? 0 : (t - tS) / tI;
+    T.tile = T.shared ? t : (t - tS) - T.j * tI;
+    T.slices = a.s1;
+    T.ticket = 1 + t;
+    kit = a.H / (FP8 ? 128 : 64);
+  } else {
+    int u = item - gu;
+    const int sh = a.Is ? tH * a.s2s : 0;
+    T.shared = u < sh;
+    if (!T.shared) u -= sh;
+    const int sl = T.shared ? a.s2s : a.s2;
+    T.j = T.shared ? 0 : u / (tH * sl);
+    u -= T.j * tH * sl;
+    T.tile = u / sl;
+    T.slice = u - T.tile * sl;
+    T.slices = s.active * a.s2 + (a.Is ? a.s2s : 0);
+    T.ticket = a.down_tickets + T.tile;
+    kit = (T.shared ? a.Is : a.I) / (FP8 ? 128 : 64);
+  }
+  const int sl = T.down ? (T.shared ? a.s2s : a.s2) : a.s1;
+  T.kb0 = kit * T.slice / sl;
+  T.kb1 = kit * (T.slice + 1) / sl;
+  T.mask = T.shared ? (a.n == 64 ? ~0ull : (1ull << a.n) - 1) : s.mask[T.j];
+  T.tokens = T.shared ? a.n : __popcll(T.mask);
+  T.start = T.shared ? 0 : s.start[T.j];
+  const int m8 = round_up_dev(T.down ? T.tokens : a.n, 8);
+  T.rows = T.down && !FP8 ? 2 * m8 : m8;
+  T.n = round_up_dev(T.rows, 16);
+  return T;
+}
+
+// The h image of an expert: its first byte (m8 row groups before it, the shared expert's rows first).
+template <bool FP8>
+__device__ __forceinline__ uint8_t* h_image(const FewArgs& a, const FewSmem& s, const FewItem& T) {
+  const int kit = a.I / (FP8 ? 128 : 64), kits = a.Is / (FP8 ? 128 : 64);
+  constexpr int group = FP8 ? 8 : 16;  // rows per group of 8 tokens
+  const long long shared = static_cast<long long>(kits) * step_bytes<FP8>(round_up_dev(a.n, 8) / 8 * group);
+  return a.himg + (T.shared ? 0 : shared + static_cast<long long>(kit) * step_bytes<FP8>(s.row8[T.j] * group));
+}
+
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
+               "l"(src), "r"(bytes), "r"(bar)
+               : "memory");
+}
+__device__ __forceinline__ void prefetch_box(const CUtensorMap* m, int y) {
+  asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global.tile [%0, {%1, %2}];" ::"l"(reinterpret_cast<uint64_t>(m)),
+               "r"(0), "r"(y)
+               : "memory");
+}
+__device__ __forceinline__ void fence_proxy_async_all() { asm volatile("fence.proxy.async;" ::: "memory"); }
+__device__ __forceinline__ int ld_acquire(const int* p) {
+  int v;
+  asm volatile("ld.acquire.gpu.global.b32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+  return v;
+}
+__device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t (&r)[8]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "r"(taddr)
+               : "memory");
+}
+__device__ __forceinline__ void mma_e4m3(uint32_t d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t acc) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+      "l"(adesc), "l"(bdesc), "r"(idesc), "r"(acc)
+      : "memory");
+}
+__device__ __forceinline__ void epi_sync() {
+  __syncwarp();
+  asm volatile("bar.sync 1, 256;" ::: "memory");
+}
+// Whether ok holds in every thread of the epilogue warps (a barrier too).
+__device__ __forceinline__ bool epi_all(bool ok) {
+  uint32_t r;
+  __syncwarp();
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.u32 p, %1, 0;\n\t"
+      "bar.red.and.pred q, 2, 256, p;\n\t"
+      "selp.u32 %0, 1, 0, q;\n\t}"
+      : "=r"(r)
+      : "r"(ok ? 1u : 0u)
+      : "memory");
+  return r != 0;
+}
+
+// The last slice of a gate/up tile: the slices' sums, SwiGLU and the tile's 128
+// channels of h into the expert's image.  Warp w takes tokens w, w + 8, ...; lane l
+// channels 4l .. 4l + 3.
+template <bool FP8>
+__device__ __forceinline__ void write_h(const FewArgs& a, const FewSmem& s, const FewItem& T, int warp, int lane) {
+  const int W = 2 * (T.shared ? a.Is : a.I);
+  const long long plane = static_cast<long long>(T.shared ? a.n : a.n * a.gate.top_k) * W;
+  const float* p = (T.shared ? a.p1s : a.p1) + T.tile * 256;
+  // packed rows: gate and up alternate in eights (bf16) or by 128
+  const int grow = FP8 ? 4 * lane : 16 * (lane >> 1) + 4 * (lane & 1);
+  constexpr int up = FP8 ? 128 : 8;
+  uint8_t* img = h_image<FP8>(a, s, T);
+  const int m8 = round_up_dev(T.tokens, 8);
+  for (int c = warp; c < T.tokens; c += kEpiWarps) {
+    const float* src = p + static_cast<long long>(T.start + c) * W + grow;
+    float4 g = make_float4(0.f, 0.f, 0.f, 0.f), u = g;
+    for (int i = 0; i < a.s1; ++i) {
+      const float4 gi = __ldcg(reinterpret_cast<const float4*>(src + i * plane));
+      const float4 ui = __ldcg(reinterpret_cast<const float4*>(src + i * plane + up));
+      g.x += gi.x, g.y += gi.y, g.z += gi.z, g.w += gi.w;
+      u.x += ui.x, u.y += ui.y, u.z += ui.z, u.w += ui.w;
+    }
+    float h[4] = {g.x / (1.0f + expf(-g.x)) * u.x, g.y / (1.0f + expf(-g.y)) * u.y,
+                  g.z / (1.0f + expf(-g.z)) * u.z, g.w / (1.0f + expf(-g.w)) * u.w};
+    if constexpr (FP8) {
+      float am = fmaxf(fmaxf(fabsf(h[0]), fabsf(h[1])), fmaxf(fabsf(h[2]), fabsf(h[3])));
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) am = fmaxf(am, __shfl_xor_sync(kFull, am, o));
+      const float sc = am > 0.f ? am / 448.0f : 1.0f, inv = 1.0f / sc;
+      uint8_t* step = img + static_cast<long long>(T.tile) * step_bytes<true>(m8);
+      *reinterpret_cast<uint32_t*>(step + swizzled(c, 4 * lane)) =
+          e4m3x4(quotient(h[0], sc, inv), quotient(h[1], sc, inv), quotient(h[2], sc, inv), quotient(h[3], sc, inv));
+      if (lane == 0) *reinterpret_cast<float*>(step + m8 * 128 + c * 4) = sc;
+    } else {
+      uint8_t* step = img + static_cast<long long>(2 * T.tile + (lane >> 4)) * step_bytes<false>(2 * m8);
+      const uint32_t a0 = pack_bf16x2(h[0], h[1]), a1 = pack_bf16x2(h[2], h[3]);
+      const uint32_t b0 = pack_bf16x2(h[0] - bf16_lo(a0), h[1] - bf16_hi(a0));
+      const uint32_t b1 = pack_bf16x2(h[2] - bf16_lo(a1), h[3] - bf16_hi(a1));
+      *reinterpret_cast<uint2*>(step + swizzled(c, 8 * (lane & 15))) = make_uint2(a0, a1);
+      *reinterpret_cast<uint2*>(step + swizzled(m8 + c, 8 * (lane & 15))) = make_uint2(b0, b1);
+    }
+  }
+}
+
+// The last arrival of an output tile: 256 channels of every token, one thread a
+// channel.  A token's terms are its slots' partial sums, slot by slot, then the
+// shared expert's; kAhead of them are on their way at a time.
+__device__ __forceinline__ void write_out(const FewArgs& a, const FewSmem& s, const FewItem& T, int tid) {
+  constexpr int kAhead = 16;
+  const int k = a.gate.top_k, H = a.H;
+  const long long plane = static_cast<long long>(a.n) * k * H, plane_s = static_cast<long long>(a.n) * H;
+  const int ch = T.tile * 256 + tid;
+  __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out);
+  for (int t = 0; t < a.n; ++t) {
+    float acc = 0.f;
+    int j = 0, i = 0;  // the next term: slot j (k: the shared expert), slice i
+    const int slots = k + (a.Is ? 1 : 0);
+    while (j < slots) {
+      float w[kAhead], v[kAhead];
+#pragma unroll
+      for (int b = 0; b < kAhead; ++b) {
+        w[b] = v[b] = 0.f;
+        if (j < slots) {
+          const bool sh = j == k;
+          const int pos = sh ? t : s.pos[t * k + j];
+          if (pos >= 0) {
+            w[b] = sh ? 1.0f : s.w[t * k + j];
+            v[b] = __ldcg((sh ? a.ys + i * plane_s : a.y + i * plane) + static_cast<long long>(pos) * H + ch);
+          }
+          if (++i == (sh ? a.s2s : a.s2)) i = 0, ++j;
+        }
+      }
+#pragma unroll
+      for (int b = 0; b < kAhead; ++b) acc = fmaf(w[b], v[b], acc);
+    }
+    out[static_cast<long long>(t) * H + ch] = __float2bfloat16_rn(acc);
+  }
+}
+
+// NT: columns (tokens) the FP8 epilogue keeps in registers; unused for BF16.
+template <bool FP8, int NT>
+__global__ void __launch_bounds__(kThreads, 1) few_ffn_kernel(const FewArgs a) {
+  extern __shared__ __align__(1024) uint8_t smem_raw[];
+  const uint32_t base = smem_u32(smem_raw);
+  if (base & 1023u) {  // uniform for the CTA: nothing is initialised yet
+    pdl_wait();
+    if (threadIdx.x == 0) record_status(a.status, ST_SMEM_ALIGN);
+    return;
+  }
+  const int SW = a.stages_w, SX = a.stages_x;
+  const uint32_t sW = base, sX = base + SW * kWBytes;
+  FewSmem& s = *reinterpret_cast<FewSmem*>(smem_raw + SW * kWBytes + SX * a.x_slot);
+  auto bar = [&](int i) { return smem_u32(&s.bar[i]); };
+  constexpr int B_FW = 0, B_EW = kFewMaxStages, B_FX = 2 * kFewMaxStages, B_EX = 3 * kFewMaxStages,
+                B_PF = 4 * kFewMaxStages, B_PE = B_PF + kPartials, B_QF = B_PE + kPartials, B_QE = B_QF + kQ,
+                B_DR = B_QE + kQ;
+  volatile int* abort_flag = &s.abort;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  if (warp == 0) {
+    if (lane == 0) {
+      for (int i = 0; i < kFewMaxStages; ++i) {
+        mbar_init(bar(B_FW + i), 1);
+        mbar_init(bar(B_EW + i), 1);
+        mbar_init(bar(B_FX + i), 1);
+        mbar_init(bar(B_EX + i), FP8 ? 1 + kEpiWarps : 1);  // FP8: the epilogue reads its scales
+      }
+      for (int i = 0; i < kPartials; ++i) {
+        mbar_init(bar(B_PF + i), 1);
+        mbar_init(bar(B_PE + i), kEpiWarps);
+      }
+      for (int i = 0; i < kQ; ++i) {
+        mbar_init(bar(B_QF + i), 1);
+        mbar_init(bar(B_QE + i), kQReaders);
+      }
+      mbar_init(bar(B_DR), 1);
+      s.abort = 0;
+      fence_barrier_init();
+    }
+  } else if (warp == 1) {
+    tmem_alloc(smem_u32(&s.tmem), kTmemCols);
+    tmem_relinquish();
+  } else if (warp == 2 && a.Is && lane == 0) {
+    // The shared expert's gate/up weights are needed whatever the router says: fetched into L2 while it
+    // works.  (A layer id that is still being written would only fetch another layer's weights.)
+    const int l = load_layer(a.lref.layer, a.lref.n_layers, a.status, false);
+    const CUtensorMap* m = &a.lref.table[l].map[MAP_SH_GATE_UP];
+    tensormap_acquire(m);
+    const int boxes = a.Is / 128 * (a.H / (FP8 ? 128 : 64));
+    for (int b = blockIdx.x; b < boxes; b += gridDim.x) prefetch_box(m, b * 256);
+  }
+  pdl_wait();
+  if (threadIdx.x < kMaxExperts) {
+    s.expert[threadIdx.x] = ld_dep(&a.meta->expert[threadIdx.x]);
+    s.start[threadIdx.x] = ld_dep(&a.meta->start[threadIdx.x]);
+    s.row8[threadIdx.x] = ld_dep(&a.meta->row8[threadIdx.x]);
+    s.mask[threadIdx.x] = *reinterpret_cast<const volatile unsigned long long*>(&a.meta->mask[threadIdx.x]);
+  } else if (threadIdx.x == kMaxExperts) {
+    s.active = min(max(ld_dep(&a.meta->active), 0), a.max_active);
+    s.layer = load_layer(a.lref.layer, a.lref.n_layers, a.status, false);
+  }
+  for (int p = threadIdx.x; p < a.n * a.gate.top_k; p += kThreads) {
+    s.pos[p] = ld_dep(&a.meta->pos[p]);
+    s.w[p] = ld_dep(&a.meta->w[p]);
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = s.tmem;
+  const LayerEntry& le = a.lref.table[s.layer];
+  const int items = (a.Is / 128 + s.active * (a.I / 128)) * a.s1 +
+                    a.H / 256 * (s.active * a.s2 + (a.Is ? a.s2s : 0));
+  auto give_up = [&]() {
+    *abort_flag = 1;
+    record_status(a.status, ST_WAIT_TIMEOUT);
+  };
+  // the next item of a reader of the queue (-1: none left); false: gave up
+  auto pop = [&](Ring<kQ>& r, int& item) {
+    if (!__all_sync(kFull, mbar_wait(bar(B_QF + r.s), r.phase, abort_flag))) return false;
+    item = *reinterpret_cast<volatile int*>(&s.q[r.s]);
+    __syncwarp();
+    if (lane == 0) mbar_arrive(bar(B_QE + r.s));
+    r.advance();
+    return true;
+  };
+
+  if (warp == 0) {
+    // -------------------------------------------------------- claims and weights
+    if (lane == 0) {
+      bool ok = true;
+      int st = 0, issued = 0;
+      uint32_t ph = 0;
+      Ring<kQ> rq;
+      const uint64_t pol = l2_policy(1);
+      tensormap_acquire(&le.map[MAP_GATE_UP]);
+      tensormap_acquire(&le.map[MAP_DOWN]);
+      if (a.Is) {
+        tensormap_acquire(&le.map[MAP_SH_GATE_UP]);
+        tensormap_acquire(&le.map[MAP_SH_DOWN]);
+      }
+      int next = atomicAdd(&a.counters[0], 1);
+      while (ok) {
+        const int item = next < items ? next : -1;
+        ok = mbar_wait(bar(B_QE + rq.s), rq.phase ^ 1u, abort_flag);
+        if (!ok) break;
+        s.q[rq.s] = item;
+        mbar_arrive(bar(B_QF + rq.s));
+        rq.advance();
+        if (item < 0) break;
+        next = atomicAdd(&a.counters[0], 1);
+        const FewItem T = decode<FP8>(a, s, item);
+        const CUtensorMap* m = &le.map[T.down ? (T.shared ? MAP_SH_DOWN : MAP_DOWN)
+                                              : (T.shared ? MAP_SH_GATE_UP : MAP_GATE_UP)];
+        const int tiles = T.down ? a.H / 256 : a.I / 128;
+        const int kit = (T.down ? (T.shared ? a.Is : a.I) : a.H) / (FP8 ? 128 : 64);
+        const int box0 = ((T.shared ? 0 : s.expert[T.j] * tiles) + T.tile) * kit;
+        for (int kb = T.kb0; kb < T.kb1; ++kb) {
+          ok = mbar_wait(bar(B_EW + st), ph ^ 1u, abort_flag);
+          if (!ok) break;
+          mbar_arrive_expect_tx(bar(B_FW + st), kWBytes);
+          tma_load_2d(sW + st * kWBytes, m, bar(B_FW + st), 0, (box0 + kb) * 256, pol);
+          issued = min(issued + 1, SW);
+          if (++st == SW) st = 0, ph ^= 1u;
+        }
+      }
+      pdl_launch();  // no items left for this CTA
+      if (!ok) {
+        give_up();
+        // the copies in flight land before the CTA's memory goes away
+        int dummy = 0;
+        for (int i = issued; i > 0; --i) {
+          const int b = st - i;
+          mbar_wait(bar(B_FW + (b < 0 ? b + SW : b)), b < 0 ? ph ^ 1u : ph, &dummy);
+        }
+      }
+    }
+  } else if (warp == 2) {
+    // -------------------------------------------------------- operand rows
+    Ring<kQ> rq;
+    bool ok = true;
+    int st = 0, issued = 0, item;
+    uint32_t ph = 0;
+    if (lane == 0) fence_proxy_async_all();
+    while (ok) {
+      ok = pop(rq, item);
+      if (!ok || item < 0) break;
+      if (lane == 0) {
+        const FewItem T = decode<FP8>(a, s, item);
+        const uint32_t bytes = step_bytes<FP8>(T.rows);
+        const uint8_t* img = T.down ? h_image<FP8>(a, s, T) : a.ximg;
+        if (T.down) {
+          const int* ready = a.counters + a.h_ready + (T.shared ? 0 : 1 + T.j);
+          const int want = (T.shared ? a.Is : a.I) / 128;
+          ok = bounded_wait([&]() { return ld_acquire(ready) >= want; }, abort_flag);
+          fence_proxy_async_all();
+        }
+        for (int kb = T.kb0; ok && kb < T.kb1; ++kb) {
+          ok = mbar_wait(bar(B_EX + st), ph ^ 1u, abort_flag);
+          if (!ok) break;
+          mbar_arrive_expect_tx(bar(B_FX + st), bytes);
+          bulk_load(sX + st * a.x_slot, img + static_cast<long long>(kb) * bytes, bytes, bar(B_FX + st));
+          issued = min(issued + 1, SX);
+          if (++st == SX) st = 0, ph ^= 1u;
+        }
+      }
+      ok = __all_sync(kFull, ok);
+    }
+    if (!ok && lane == 0) {
+      give_up();
+      int dummy = 0;
+      for (int i = issued; i > 0; --i) {
+        const int b = st - i;
+        mbar_wait(bar(B_FX + (b < 0 ? b + SX : b)), b < 0 ? ph ^ 1u : ph, &dummy);
+      }
+    }
+  } else if (warp == 1) {
+    // -------------------------------------------------------- MMA
+    const bool issuer = elect_one();
+    Ring<kQ> rq;
+    Ring<FP8 ? kPartials : kAccs> p;
+    int sw = 0, sx = 0, item;
+    uint32_t pw = 0, px = 0;
+    bool ok = true, issued = false;
+    const uint64_t wdesc = smem_desc_sw128(sW), xdesc = smem_desc_sw128(sX);
+    while (ok) {
+      ok = pop(rq, item);
+      if (!ok || item < 0) break;
+      const FewItem T = decode<FP8>(a, s, item);
+      const uint32_t id = FP8 ? (1u << 4) | (static_cast<uint32_t>(T.n >> 3) << 17) | (8u << 24) : idesc_bf16_f32(128, T.n);
+      for (int kb = T.kb0; kb < T.kb1; ++kb) {
+        ok = mbar_wait(bar(B_FX + sx), px, abort_flag) && mbar_wait(bar(B_FW + sw), pw, abort_flag);
+        if (FP8 || kb == T.kb0) ok = ok && mbar_wait(bar(B_PE + p.s), p.phase ^ 1u, abort_flag);
+        ok = __all_sync(kFull, ok);
+        if (!ok) break;
+        tc_fence_after();
+        if (issuer) {
+          const uint64_t wd = wdesc + static_cast<uint32_t>(sw * (kWBytes >> 4));
+          const uint64_t xd = xdesc + static_cast<uint32_t>(sx * (a.x_slot >> 4));
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            const uint32_t d = tmem_base + p.s * (FP8 ? 128 : 256) + half * (FP8 ? 64 : 128);
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk) {
+              const uint64_t w = wd + half * (16384 >> 4) + 2 * kk, x = xd + 2 * kk;
+              if constexpr (FP8) mma_e4m3(d, w, x, id, kk > 0 ? 1u : 0u);
+              else tc_mma_bf16(d, w, x, id, kb > T.kb0 || kk > 0 ? 1u : 0u);
+            }
+          }
+          if (FP8 || kb == T.kb1 - 1) tc_commit(bar(B_PF + p.s));
+          tc_commit(bar(B_EW + sw));
+          tc_commit(bar(B_EX + sx));
+        }
+        __syncwarp();
+        issued = true;
+        if (FP8 || kb == T.kb1 - 1) p.advance();
+        if (++sw == SW) sw = 0, pw ^= 1u;
+        if (++sx == SX) sx = 0, px ^= 1u;
+      }
+    }
+    if (!ok) {
+      if (lane == 0) give_up();
+      if (issued) {
+        int dummy = 0;
+        if (elect_one()) tc_commit(bar(B_DR));
+        __syncwarp();
+        mbar_wait(bar(B_DR), 0, &dummy);
+      }
+    }
+  } else if (warp >= 4) {
+    // -------------------------------------------------------- epilogue
+    // warp w: TMEM lanes 32 (w % 4) .. of row half (w - 4) / 4
+    const int q = warp & 3, half = (warp - 4) >> 2;
+    const int tid = threadIdx.x - 128;
+    const uint32_t lanes = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + half * (FP8 ? 64 : 128);
+    const int row = half * 128 + q * 32 + lane;  // of the weight tile
+    Ring<kQ> rq;
+    Ring<FP8 ? kPartials : kAccs> p;
+    int sx = 0, item;
+    uint32_t px = 0;
+    bool ok = true;
+    while (true) {
+      ok = pop(rq, item);
+      if (!epi_all(ok)) {  // the warps share barriers: all go on or none does
+        ok = false;
+        break;
+      }
+      if (item < 0) break;
+      const FewItem T = decode<FP8>(a, s, item);
+      // the item's sums of this thread's row go to plane ``slice`` of the workspace, row start + c for the
+      // expert's c-th token
+      const long long rows_all = T.shared ? a.n : a.n * a.gate.top_k;
+      const long long ld = T.down ? a.H : 2 * (T.shared ? a.Is : a.I);
+      float* dst = (T.down ? (T.shared ? a.ys : a.y) : (T.shared ? a.p1s : a.p1)) +
+                   (T.slice * rows_all + T.start) * ld + T.tile * 256 + row;
+      if constexpr (FP8) {
+        float acc[NT];
+#pragma unroll
+        for (int i = 0; i < NT; ++i) acc[i] = 0.f;
+        // (gate/up computes every token's column; 16 columns without a token of this expert are left out)
+        uint32_t live = 0;
+#pragma unroll
+        for (int ch = 0; ch < NT / 16; ++ch)
+          live |= (T.down ? 16 * ch < T.tokens : ((T.mask >> (16 * ch)) & 0xffffull) != 0) ? 1u << ch : 0u;
+        const int scale_rows = T.down ? a.H / 128 : 2 * a.I / 128;
+        const int kit = (T.down ? (T.shared ? a.Is : a.I) : a.H) / 128;
+        const float* bs_lo =
+            le.scale[T.down ? (T.shared ? MAP_SH_DOWN : MAP_DOWN) : (T.shared ? MAP_SH_GATE_UP : MAP_GATE_UP)] +
+            (static_cast<long long>(T.shared ? 0 : s.expert[T.j]) * scale_rows + 2 * T.tile + half) * kit;
+        float next = __ldg(bs_lo + T.kb0);
+        for (int kb = T.kb0; kb < T.kb1; ++kb) {
+          const float ws = next;
+          if (kb + 1 < T.kb1) next = __ldg(bs_lo + kb + 1);
+          ok = __all_sync(kFull, mbar_wait(bar(B_FX + sx), px, abort_flag) &&
+                                     mbar_wait(bar(B_PF + p.s), p.phase, abort_flag));
+          if (!ok) break;
+          tc_fence_after();
+          const float4* sc = reinterpret_cast<const float4*>(smem_raw + SW * kWBytes + sx * a.x_slot + T.rows * 128);
+#pragma unroll
+          for (int ch = 0; ch < NT / 16; ++ch) {
+            if ((live >> ch) & 1u) {
+              uint32_t v[16];
+              tmem_ld16(lanes + p.s * 128 + 16 * ch, v);
+              tmem_ld_wait();
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const float4 f = sc[4 * ch + i];
+                acc[16 * ch + 4 * i] = fmaf(ws * f.x, __uint_as_float(v[4 * i]), acc[16 * ch + 4 * i]);
+                acc[16 * ch + 4 * i + 1] = fmaf(ws * f.y, __uint_as_float(v[4 * i + 1]), acc[16 * ch + 4 * i + 1]);
+                acc[16 * ch + 4 * i + 2] = fmaf(ws * f.z, __uint_as_float(v[4 * i + 2]), acc[16 * ch + 4 * i + 2]);
+                acc[16 * ch + 4 * i + 3] = fmaf(ws * f.w, __uint_as_float(v[4 * i + 3]), acc[16 * ch + 4 * i + 3]);
+              }
+            }
+          }
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) {
+            mbar_arrive(bar(B_EX + sx));
+            mbar_arrive(bar(B_PE + p.s));
+          }
+          p.advance();
+          if (++sx == SX) sx = 0, px ^= 1u;
+        }
+        if (ok) {
+          int c = 0;
+#pragma unroll
+          for (int i = 0; i < NT; ++i)
+            if (T.down ? i < T.tokens : (T.mask >> i) & 1ull) dst[ld * c++] = acc[i];
+        }
+      } else {
+        ok = __all_sync(kFull, mbar_wait(bar(B_PF + p.s), p.phase, abort_flag));
+        if (ok) {
+          tc_fence_after();
+          const uint32_t t0 = lanes + p.s * 256;
+          const int cols = T.down ? T.rows / 2 : T.rows;  // down: the columns of the roundings follow
+          int c = 0;
+          for (int c0 = 0; c0 < cols; c0 += 8) {
+            const uint32_t some = T.down ? (c0 + 8 <= T.tokens ? 0xffu : (1u << (T.tokens - c0)) - 1u)
+                                         : static_cast<uint32_t>(T.mask >> c0) & 0xffu;
+            if (!some) continue;
+            uint32_t v[8], r[8];
+            tmem_ld8(t0 + c0, v);
+            if (T.down) tmem_ld8(t0 + cols + c0, r);
+            tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              if ((some >> i) & 1u)
+                dst[ld * c++] = T.down ? __uint_as_float(v[i]) + __uint_as_float(r[i]) : __uint_as_float(v[i]);
+          }
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(B_PE + p.s));
+          p.advance();
+        }
+      }
+      __threadfence();
+      if (!epi_all(ok)) {
+        ok = false;
+        break;
+      }
+      if (tid == 0) {
+        __threadfence();
+        s.last = atomicAdd(&a.counters[T.ticket], 1) == T.slices - 1;
+        __threadfence();
+      }
+      epi_sync();
+      const bool last = *reinterpret_cast<volatile int*>(&s.last) != 0;
+      if (last) {
+        if (T.down) {
+          write_out(a, s, T, tid);
+        } else {
+          write_h<FP8>(a, s, T, warp - 4, lane);
+          fence_proxy_async_all();
+          __threadfence();
+          epi_sync();
+          if (tid == 0) {
+            __threadfence();
+            atomicAdd(a.counters + a.h_ready + (T.shared ? 0 : 1 + T.j), 1);
+          }
+        }
+      }
+      // (s.last is written again only after the next item's epi_all)
+    }
+    if (!ok && lane == 0) give_up();
+  }
+
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem_base, kTmemCols);
+  }
+}
+
+template <bool FP8, int NT>
+cudaError_t launch_ffn(const FewArgs& a, int grid, cudaStream_t st) {
+  return launch_pdl(few_ffn_kernel<FP8, NT>, dim3(grid), dim3(kThreads), a.smem, st, 1, a);
+}
+
+}  // namespace
+
+cudaError_t few_set_attributes() {
+  cudaError_t e = cudaSuccess;
+  auto set = [&](auto* f, size_t bytes) {
+    if (e == cudaSuccess)
+      e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes));
+  };
+  set(few_route_kernel<false>, kFewRouteSmem);
+  set(few_route_kernel<true>, kFewRouteSmem);
+  set(few_ffn_kernel<false, 16>, kFewSmem);
+  set(few_ffn_kernel<true, 16>, kFewSmem);
+  set(few_ffn_kernel<true, 64>, kFewSmem);
+  return e;
+}
+
+cudaError_t few_launch(const FewArgs& a, bool fp8, int grid, cudaStream_t st) {
+  const int tiles = ceil_div(a.gate.n_experts, 16);
+  const size_t smem = sizeof(float) * 16 * tiles *
+                      (static_cast<size_t>(kRouteWarps / tiles) * a.n + ceil_div(a.n, kFewCluster) * kFewCluster);
+  const cudaError_t e =
+      fp8 ? launch_pdl(few_route_kernel<true>, dim3(kFewCluster), dim3(kRouteThreads), smem, st, kFewCluster, a)
+          : launch_pdl(few_route_kernel<false>, dim3(kFewCluster), dim3(kRouteThreads), smem, st, kFewCluster, a);
+  if (e != cudaSuccess) return e;
+  if (!fp8) return launch_ffn<false, 16>(a, grid, st);
+  return a.n <= 16 ? launch_ffn<true, 16>(a, grid, st) : launch_ffn<true, 64>(a, grid, st);
+}
+
+}  // namespace asap

@@ -101,15 +101,6 @@ __global__ void __launch_bounds__(256) router_small_kernel(const uint4* x, Layer
 constexpr int kRmmaWarps = 8;
 constexpr int kRmmaTokens = 16;
 
-__device__ __forceinline__ void mma_bf16_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
-                                               uint32_t b0, uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
-      "{%0, %1, %2, %3};"
-      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-
 template <int NB>  // E = 8 NB experts
 __global__ void __launch_bounds__(kRmmaWarps * 32) router_mma_kernel(const uint4* x, LayerRef lref,
                                                                      uint32_t* status, int n, int V,
