@@ -15,7 +15,7 @@
 // are; and zeroed counters.
 //
 // few_ffn_kernel (one CTA per SM): a list of work items, gate/up tiles of all
-// experts and then down tiles, claimed one by one from a counter.  An item is a
+// experts, then down tiles, then the outputs, claimed one by one from a counter.  An item is a
 // 256-row weight tile (a box per k-step, 32 KB, as the handle packs them) over
 // a slice of K.  The weights are the M operand of the MMA and all tokens the N
 // operand, so a tile costs the same whatever its rows; the tensor core is idle
@@ -25,8 +25,10 @@
 //    and writes h as an operand image: e4m3 with scales, or, for BF16, as the
 //    sum of two bf16 (the value and what its rounding left), since N has room:
 //    h keeps 16 bits at no cost.
-//  - down: a tile waits until its expert's h is complete.  Partial sums are
-//    fp32; the last arrival of an output tile adds the experts in slot order.
+//  - down: a tile waits until its expert's h is complete; its partial sums are
+//    fp32.
+//  - combine: 256 channels of one token, once the output tile's partial sums
+//    are complete: the experts' in slot order, then the shared expert's.
 // Sums are taken in a fixed order, so a call gives the same bits each time.
 // An item waits only for items claimed before it, by CTAs that are running,
 // so the launch needs no co-residency to make progress.
@@ -36,6 +38,8 @@
 
 #include <cuda_fp8.h>
 #include <math_constants.h>
+
+#include <cstddef>
 
 namespace asap {
 
@@ -52,11 +56,6 @@ __device__ __forceinline__ uint32_t map_rank(uint32_t addr, uint32_t rank) {
   uint32_t d;
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(d) : "r"(addr), "r"(rank));
   return d;
-}
-__device__ __forceinline__ float ld_rank_f32(uint32_t addr) {
-  float v;
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
-  return v;
 }
 __device__ __forceinline__ void st_rank_u32(uint32_t addr, uint32_t v) {
   asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
@@ -78,6 +77,8 @@ __device__ __forceinline__ int swizzled(int row, int byte) {
   return row * 128 + ((((byte >> 4) ^ (row & 7)) << 4) | (byte & 15));
 }
 
+// Scale of a group: amax times the fp32 reciprocal of 448.
+__device__ __forceinline__ float group_scale(float amax) { return amax > 0.f ? amax * (1.0f / 448.0f) : 1.0f; }
 // e4m3 of v / s.  The quotient is the correctly rounded one (Markstein 1990: one
 // correction of v * (1/s) by its residual), as a division gives it: bf16
 // values over amax / 448 fall exactly between two e4m3 values for about one
@@ -126,16 +127,23 @@ __device__ __forceinline__ void gate_token(const GateParams& p, const float* bia
       if (e < E) scratch[e + e / gsz] = key[i];
     }
     __syncwarp();
-    float score = -CUDART_INF_F;
-    if (lane < p.n_groups) {
-      float m1 = -CUDART_INF_F, m2 = -CUDART_INF_F;
-      for (int j = 0; j < gsz; ++j) {
-        const float v = scratch[lane * (gsz + 1) + j];
+    // a team of lanes (the largest power of two that gives every group one) finds a group's two best
+    int team = 1;
+    while (2 * team * p.n_groups <= 32) team *= 2;
+    const int grp = lane / team;
+    float m1 = -CUDART_INF_F, m2 = -CUDART_INF_F;
+    if (grp < p.n_groups)
+      for (int j = lane % team; j < gsz; j += team) {
+        const float v = scratch[grp * (gsz + 1) + j];
         m2 = fmaxf(m2, fminf(m1, v));
         m1 = fmaxf(m1, v);
       }
-      score = m1 + m2;
+    for (int o = 1; o < team; o *= 2) {
+      const float o1 = __shfl_xor_sync(kFull, m1, o), o2 = __shfl_xor_sync(kFull, m2, o);
+      m2 = fmaxf(fmaxf(m2, o2), fminf(m1, o1));
+      m1 = fmaxf(m1, o1);
     }
+    const float score = __shfl_sync(kFull, m1 + m2, min(lane * team, 31));  // lane g: group g's
     int rank = 0;  // groups in front of this lane's
     for (int g = 0; g < p.n_groups; ++g) {
       const float o = __shfl_sync(kFull, score, g);
@@ -200,44 +208,55 @@ __device__ __forceinline__ void gate_token(const GateParams& p, const float* bia
 
 // Hidden states as operand image: rows n .. are zero.
 template <bool FP8>
-__device__ __forceinline__ void write_image(const FewArgs& a, int rows, long long thread, long long threads) {
+__device__ __forceinline__ void write_image(const FewArgs& a, int rows, int thread, int threads) {
+  constexpr int kAhead = 4;
   const int V = a.H / 8;  // 16-byte vectors of a row
+  const int total = rows * V;
   const uint4* x = static_cast<const uint4*>(a.x);
-  if constexpr (!FP8) {
-    for (long long i = thread; i < static_cast<long long>(rows) * V; i += threads) {
-      const int t = static_cast<int>(i / V), v = static_cast<int>(i % V);
-      const uint4 d = t < a.n ? ld_dep(x + static_cast<long long>(t) * V + v) : make_uint4(0, 0, 0, 0);
-      *reinterpret_cast<uint4*>(a.ximg + static_cast<long long>(v >> 3) * step_bytes<false>(rows) +
-                                swizzled(t, (v & 7) * 16)) = d;
+  // FP8: 16 threads a group of 128 channels (total and the stride are multiples of 32: a warp stays together)
+  for (int i0 = thread; i0 < total; i0 += kAhead * threads) {
+    uint4 d[kAhead];
+#pragma unroll
+    for (int r = 0; r < kAhead; ++r) {
+      const int i = i0 + r * threads;
+      d[r] = i < a.n * V ? ld_dep(x + i) : make_uint4(0, 0, 0, 0);  // (rows follow one another)
     }
-  } else {
-    // 16 threads a group of 128 channels (rows * V and the stride are multiples of 32: a warp stays together)
-    for (long long i = thread; i < static_cast<long long>(rows) * V; i += threads) {
-      const int t = static_cast<int>(i / V), v = static_cast<int>(i % V);
-      const uint4 d = t < a.n ? ld_dep(x + static_cast<long long>(t) * V + v) : make_uint4(0, 0, 0, 0);
-      const float f[8] = {bf16_lo(d.x), bf16_hi(d.x), bf16_lo(d.y), bf16_hi(d.y),
-                          bf16_lo(d.z), bf16_hi(d.z), bf16_lo(d.w), bf16_hi(d.w)};
-      float am = 0.f;
 #pragma unroll
-      for (int u = 0; u < 8; ++u) am = fmaxf(am, fabsf(f[u]));
+    for (int r = 0; r < kAhead; ++r) {
+      const int i = i0 + r * threads;
+      if (i >= total) break;
+      const int t = i / V, v = i - t * V;
+      if constexpr (!FP8) {
+        *reinterpret_cast<uint4*>(a.ximg + static_cast<long long>(v >> 3) * step_bytes<false>(rows) +
+                                  swizzled(t, (v & 7) * 16)) = d[r];
+      } else {
+        const float f[8] = {bf16_lo(d[r].x), bf16_hi(d[r].x), bf16_lo(d[r].y), bf16_hi(d[r].y),
+                            bf16_lo(d[r].z), bf16_hi(d[r].z), bf16_lo(d[r].w), bf16_hi(d[r].w)};
+        float am = 0.f;
 #pragma unroll
-      for (int o = 8; o > 0; o >>= 1) am = fmaxf(am, __shfl_xor_sync(kFull, am, o));
-      const float s = am > 0.f ? am / 448.0f : 1.0f, inv = 1.0f / s;
-      uint2 q;
-      q.x = e4m3x4(quotient(f[0], s, inv), quotient(f[1], s, inv), quotient(f[2], s, inv), quotient(f[3], s, inv));
-      q.y = e4m3x4(quotient(f[4], s, inv), quotient(f[5], s, inv), quotient(f[6], s, inv), quotient(f[7], s, inv));
-      uint8_t* step = a.ximg + static_cast<long long>(v >> 4) * step_bytes<true>(rows);
-      *reinterpret_cast<uint2*>(step + swizzled(t, (v & 15) * 8)) = q;
-      if ((v & 15) == 0) *reinterpret_cast<float*>(step + rows * 128 + t * 4) = s;
+        for (int u = 0; u < 8; ++u) am = fmaxf(am, fabsf(f[u]));
+#pragma unroll
+        for (int o = 8; o > 0; o >>= 1) am = fmaxf(am, __shfl_xor_sync(kFull, am, o));
+        const float s = group_scale(am), inv = 1.0f / s;
+        uint2 q;
+        q.x = e4m3x4(quotient(f[0], s, inv), quotient(f[1], s, inv), quotient(f[2], s, inv), quotient(f[3], s, inv));
+        q.y = e4m3x4(quotient(f[4], s, inv), quotient(f[5], s, inv), quotient(f[6], s, inv), quotient(f[7], s, inv));
+        uint8_t* step = a.ximg + static_cast<long long>(v >> 4) * step_bytes<true>(rows);
+        *reinterpret_cast<uint2*>(step + swizzled(t, (v & 15) * 8)) = q;
+        if ((v & 15) == 0) *reinterpret_cast<float*>(step + rows * 128 + t * 4) = s;
+      }
     }
   }
 }
 
+// K units (32 channels) of the router that a warp has on their way at a time; a
+// row of them in shared memory is 28 vectors, so that the 8 lanes of a 128-bit
+// access phase (two rows) meet every bank once.
+constexpr int kUnits = 7;
+
 template <bool FP8>
 __global__ void __launch_bounds__(kRouteThreads) few_route_kernel(const FewArgs a) {
-  pdl_launch();  // the second kernel may come up and fetch weights meanwhile
-  pdl_wait();
-  extern __shared__ float smem_f[];
+  extern __shared__ __align__(16) float smem_f[];
   __shared__ int sel_e[kFewTokens * kMaxTopK];
   __shared__ float sel_w[kFewTokens * kMaxTopK];
   __shared__ unsigned long long mask[kMaxExperts];
@@ -248,98 +267,120 @@ __global__ void __launch_bounds__(kRouteThreads) few_route_kernel(const FewArgs 
   const int E = a.gate.n_experts, k = a.gate.top_k, n = a.n;
   const int tiles = (E + 15) / 16, Ep = 16 * tiles;
   const int subs = kRouteWarps / tiles;          // K parts inside the CTA
-  const int per = ceil_div_dev(n, kFewCluster);  // tokens gated by a CTA at most
-  float* part = smem_f;                          // [subs][n][Ep]
-  float* gat = smem_f + subs * n * Ep;           // [per][kFewCluster][Ep]
+  const int V = a.H / 8, units = a.H / 32;
+  const int u0 = units * rank / kFewCluster, u1 = units * (rank + 1) / kFewCluster;
+  // this rank's columns of the router weights are asked for before the second kernel, which comes up
+  // meanwhile, asks for its own
+  {
+    const uint8_t* w = static_cast<const uint8_t*>(
+        a.lref.table[load_layer(a.lref.layer, a.lref.n_layers, a.status, false)].router_w);
+    const int bytes = (u1 - u0) * 64, lines = (bytes + 127) / 128;
+    for (int i = threadIdx.x; i < E * lines; i += kRouteThreads)
+      asm volatile("prefetch.global.L2 [%0];" ::"l"(w + (static_cast<long long>(i / lines) * V + u0 * 4) * 16 +
+                                                    min(i % lines * 128, bytes - 64)));
+  }
+  pdl_launch();
+  pdl_wait();
+  uint4* xs = reinterpret_cast<uint4*>(smem_f);                          // [n][4 kUnits]
+  float* part = smem_f + n * kUnits * 16;                                // [subs][n][Ep]
+  float* gat = part + subs * n * Ep;                                     // [tokens][kFewCluster][Ep]
   const LayerEntry& le =
       a.lref.table[load_layer(a.lref.layer, a.lref.n_layers, a.status, rank == 0 && threadIdx.x == 0)];
+
+  // ---- what the second kernel needs besides the routing
+  const int thread = rank * kRouteThreads + threadIdx.x;
+  constexpr int kThreadsAll = kFewCluster * kRouteThreads;
+  for (int i = thread; i < a.n_counters; i += kThreadsAll) a.counters[i] = 0;
+  write_image<FP8>(a, round_up_dev(n, 8), thread, kThreadsAll);
+  for (int e = threadIdx.x; e < kMaxExperts; e += kRouteThreads) mask[e] = 0;
 
   // ---- partial logits: expert tile (16 rows, M) x tokens (8 per MMA, N); thread (g, q) feeds 16 bytes of a
   // row to two MMAs whose K order both operands share
   const int tile = warp % tiles, sub = warp / tiles;
-  if (sub < subs) {
+  const int g = lane >> 2, q = lane & 3;
+  {
     const uint4* __restrict__ wr = static_cast<const uint4*>(le.router_w);
     const uint4* x = static_cast<const uint4*>(a.x);
-    const int V = a.H / 8, units = a.H / 32;
-    const int u0 = units * rank / kFewCluster, u1 = units * (rank + 1) / kFewCluster;
-    const int g = lane >> 2, q = lane & 3;
     const int e0 = tile * 16 + g, e1 = e0 + 8;
     const uint4 zero = make_uint4(0, 0, 0, 0);
     float c[kFewTokens / 8][4];
 #pragma unroll
     for (int j = 0; j < kFewTokens / 8; ++j) c[j][0] = c[j][1] = c[j][2] = c[j][3] = 0.f;
-#pragma unroll 4
-    for (int u = u0 + sub; u < u1; u += subs) {
-      const int v = 4 * u + q;
-      const uint4 w0 = e0 < E ? __ldg(wr + static_cast<long long>(e0) * V + v) : zero;
-      const uint4 w1 = e1 < E ? __ldg(wr + static_cast<long long>(e1) * V + v) : zero;
+    for (int ub = u0; ub < u1; ub += kUnits) {
+      const int cnt = sub < subs ? min(kUnits, u1 - ub) : 0;
+      uint4 w0[kUnits], w1[kUnits];
 #pragma unroll
-      for (int j = 0; j < kFewTokens / 8; ++j) {
-        if (8 * j < n) {
+      for (int i = 0; i < kUnits; ++i) {
+        const int u = i * subs + sub, v = 4 * (ub + u) + q;
+        w0[i] = u < cnt && e0 < E ? __ldg(wr + static_cast<long long>(e0) * V + v) : zero;
+        w1[i] = u < cnt && e1 < E ? __ldg(wr + static_cast<long long>(e1) * V + v) : zero;
+      }
+      const int vecs = 4 * min(kUnits, u1 - ub);
+      for (int i = threadIdx.x; i < n * vecs; i += kRouteThreads) {
+        const int t = i / vecs, v = i - t * vecs;
+        xs[t * 4 * kUnits + v] = ld_dep(x + static_cast<long long>(t) * V + 4 * ub + v);
+      }
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < kUnits; ++i) {
+        const int u = i * subs + sub;
+        if (u >= cnt) break;
+#pragma unroll
+        for (int j = 0; j < kFewTokens / 8; ++j) {
+          if (8 * j >= n) break;
           const int t = 8 * j + g;
-          const uint4 xv = t < n ? ld_dep(x + static_cast<long long>(t) * V + v) : zero;
-          mma_bf16_16816(c[j], w0.x, w1.x, w0.y, w1.y, xv.x, xv.y);
-          mma_bf16_16816(c[j], w0.z, w1.z, w0.w, w1.w, xv.z, xv.w);
+          const uint4 xv = t < n ? xs[t * 4 * kUnits + 4 * u + q] : zero;
+          mma_bf16_16816(c[j], w0[i].x, w1[i].x, w0[i].y, w1[i].y, xv.x, xv.y);
+          mma_bf16_16816(c[j], w0[i].z, w1[i].z, w0[i].w, w1[i].w, xv.z, xv.w);
         }
       }
+      __syncthreads();
     }
+    if (sub < subs)
 #pragma unroll
-    for (int j = 0; j < kFewTokens / 8; ++j)
+      for (int j = 0; j < kFewTokens / 8; ++j)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int t = 8 * j + 2 * q + (i & 1);
-        if (t < n) part[(sub * n + t) * Ep + tile * 16 + g + 8 * (i >> 1)] = c[j][i];
-      }
+        for (int i = 0; i < 4; ++i) {
+          const int t = 8 * j + 2 * q + (i & 1);
+          if (t < n) part[(sub * n + t) * Ep + tile * 16 + g + 8 * (i >> 1)] = c[j][i];
+        }
   }
-  // ---- what the second kernel needs besides the routing
-  const long long thread = static_cast<long long>(rank) * kRouteThreads + threadIdx.x;
-  constexpr long long kThreadsAll = static_cast<long long>(kFewCluster) * kRouteThreads;
-  for (long long i = thread; i < a.n_counters; i += kThreadsAll) a.counters[i] = 0;
-  write_image<FP8>(a, round_up_dev(n, 8), thread, kThreadsAll);
-  for (int e = threadIdx.x; e < kMaxExperts; e += kRouteThreads) mask[e] = 0;
-  __syncthreads();
-  if (subs > 1) {  // parts in order
-    for (int i = threadIdx.x; i < n * Ep; i += kRouteThreads) {
-      float s = part[i];
-      for (int u = 1; u < subs; ++u) s += part[u * n * Ep + i];
-      part[i] = s;
+  cluster_sync();  // (every CTA has started; and the CTA's own barrier)
+  // ---- token t's partial logits go to CTA t % kFewCluster, which adds the ranks' in order
+  for (int t = warp; t < n; t += kRouteWarps) {
+    const uint32_t to =
+        map_rank(smem_u32(gat + (t / kFewCluster * kFewCluster + rank) * Ep), static_cast<uint32_t>(t % kFewCluster));
+    for (int e = lane; e < Ep; e += 32) {
+      float v = part[t * Ep + e];
+      for (int u = 1; u < subs; ++u) v += part[(u * n + t) * Ep + e];
+      st_rank_u32(to + 4u * e, __float_as_uint(v));
     }
   }
   cluster_sync();
-  // ---- this CTA's tokens rank, rank + kFewCluster, ...: every warp fetches some ranks' partial logits
   const int mine = rank < n ? ceil_div_dev(n - rank, kFewCluster) : 0;
-  for (int i = warp; i < mine * kFewCluster; i += kRouteWarps) {
-    const int src = i % kFewCluster, ti = i / kFewCluster;
-    const uint32_t from = map_rank(smem_u32(part + (rank + ti * kFewCluster) * Ep), src);
-    for (int e = lane; e < E; e += 32) gat[i * Ep + e] = ld_rank_f32(from + 4u * e);
+  for (int i = threadIdx.x; i < mine * Ep; i += kRouteThreads) {
+    const float* src = gat + (i / Ep * kFewCluster) * Ep + i % Ep;
+    float l = src[0];
+#pragma unroll
+    for (int r = 1; r < kFewCluster; ++r) l += src[r * Ep];
+    part[i] = l;
   }
   __syncthreads();
   if (warp < mine) {
     const int t = rank + warp * kFewCluster;
     float logit[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int e = lane + 32 * i;
-      float l = 0.f;
-      if (e < E) {
-        const float* src = gat + warp * kFewCluster * Ep + e;
-        l = src[0];
-#pragma unroll
-        for (int s = 1; s < kFewCluster; ++s) l += src[s * Ep];
-      }
-      logit[i] = l;
-    }
-    __syncwarp();
+    for (int i = 0; i < 8; ++i) logit[i] = lane + 32 * i < E ? part[warp * Ep + lane + 32 * i] : 0.f;
     int e;
     float w;
-    // the gathered logits are in registers: their place holds the group scores (E + 32 floats of at least 8 Ep)
+    // the gathered logits have been added: their place holds the selection scores
     gate_token(a.gate, le.router_bias, logit, gat + warp * kFewCluster * Ep, lane, e, w);
     if (lane < k) {
       st_rank_u32(map_rank(smem_u32(&sel_e[t * k + lane]), 0), static_cast<uint32_t>(e));
       st_rank_u32(map_rank(smem_u32(&sel_w[t * k + lane]), 0), __float_as_uint(w));
     }
   }
-  cluster_sync();  // all choices are in rank 0, and no CTA's shared memory is read any more
+  cluster_sync();  // all choices are in rank 0
   if (rank != 0) return;
   // ---- active experts in order, their tokens, rows and row groups
   for (int p = threadIdx.x; p < n * k; p += kRouteThreads) {
@@ -390,6 +431,7 @@ constexpr int kWBytes = 256 * 128;  // weight box
 constexpr int kEpiWarps = 8;
 constexpr int kEpiThreads = 32 * kEpiWarps;
 constexpr int kThreads = 32 * (4 + kEpiWarps);
+constexpr int kPrefetchBoxes = 1792;  // at most 56 MB of the 129 MB L2
 constexpr int kQ = 6;               // items in flight in a CTA
 constexpr int kQReaders = 2 + kEpiWarps;
 constexpr uint32_t kTmemCols = 512;
@@ -397,7 +439,7 @@ constexpr int kPartials = 4;        // FP8: TMEM partials of 2 x 64 columns
 constexpr int kAccs = 2;            // BF16: accumulators of 2 x 128 columns
 
 struct FewItem {
-  bool down, shared;
+  bool down, combine, shared;
   int j;           // index among the active experts
   int tile;        // 256-row weight tile of the expert's matrix
   int slice, kb0, kb1;
@@ -405,13 +447,14 @@ struct FewItem {
   int rows;        // operand rows of a k-step
   int n;           // N of the MMA
   int start;       // the expert's first row among the routed rows
-  int ticket;      // counter of the output tile
-  int slices;      // arrivals that complete the tile
+  int ticket;      // counter of the gate/up or output tile
+  int arrivals;    // that complete it
+  int token;       // combine
   unsigned long long mask;
 };
 
 struct FewSmem {  // behind the rings
-  uint64_t bar[2 * kFewMaxStages + 2 * kFewMaxStages + 2 * kPartials + 2 * kQ + 1];
+  alignas(16) uint64_t bar[2 * kFewMaxStages + 2 * kFewMaxStages + 2 * kPartials + 2 * kQ + 1];
   int q[kQ];
   uint32_t tmem;
   int abort;
@@ -422,40 +465,52 @@ struct FewSmem {  // behind the rings
   unsigned long long mask[kMaxExperts];
   int pos[kFewTokens * kMaxTopK];
   float w[kFewTokens * kMaxTopK];
+  alignas(16) float sum[kEpiWarps][256];  // combine; accessed as float4
 };
 static_assert(sizeof(FewSmem) <= kFewSmemState, "shared memory budget");
+static_assert(offsetof(FewSmem, sum) % 16 == 0, "float4 accesses");
 
 template <bool FP8>
 __device__ __forceinline__ FewItem decode(const FewArgs& a, const FewSmem& s, int item) {
-  FewItem T;
+  FewItem T{};
   const int tI = a.I / 128, tS = a.Is / 128, tH = a.H / 256;
   const int gu = (tS + s.active * tI) * a.s1;  // gate/up items
+  const int arrivals = s.active * a.s2 + (a.Is ? a.s2s : 0);
+  const int dn = tH * arrivals;                // down items
   T.down = item >= gu;
-  int kit;
+  int kit, sl;
   if (!T.down) {
     const int t = item / a.s1;
     T.slice = item - t * a.s1;
     T.shared = t < tS;
     T.j = T.shared ? 0 : (t - tS) / tI;
     T.tile = T.shared ? t : (t - tS) - T.j * tI;
-    T.slices = a.s1;
+    T.arrivals = a.s1;
     T.ticket = 1 + t;
     kit = a.H / (FP8 ? 128 : 64);
+    sl = a.s1;
   } else {
     int u = item - gu;
+    T.arrivals = arrivals;
+    if (u >= dn) {
+      u -= dn;
+      T.combine = true;
+      T.token = u / tH;
+      T.tile = u - T.token * tH;
+      T.ticket = a.down_tickets + T.tile;
+      return T;
+    }
     const int sh = a.Is ? tH * a.s2s : 0;
     T.shared = u < sh;
     if (!T.shared) u -= sh;
-    const int sl = T.shared ? a.s2s : a.s2;
+    sl = T.shared ? a.s2s : a.s2;
     T.j = T.shared ? 0 : u / (tH * sl);
     u -= T.j * tH * sl;
     T.tile = u / sl;
     T.slice = u - T.tile * sl;
-    T.slices = s.active * a.s2 + (a.Is ? a.s2s : 0);
     T.ticket = a.down_tickets + T.tile;
     kit = (T.shared ? a.Is : a.I) / (FP8 ? 128 : 64);
   }
-  const int sl = T.down ? (T.shared ? a.s2s : a.s2) : a.s1;
   T.kb0 = kit * T.slice / sl;
   T.kb1 = kit * (T.slice + 1) / sl;
   T.mask = T.shared ? (a.n == 64 ? ~0ull : (1ull << a.n) - 1) : s.mask[T.j];
@@ -490,6 +545,15 @@ __device__ __forceinline__ void fence_proxy_async_all() { asm volatile("fence.pr
 __device__ __forceinline__ int ld_acquire(const int* p) {
   int v;
   asm volatile("ld.acquire.gpu.global.b32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+  return v;
+}
+// One arrival on a counter, after everything this thread has seen done (by its CTA's barriers: by the CTA).
+__device__ __forceinline__ void arrive_release(int* p) {
+  asm volatile("red.release.gpu.global.add.s32 [%0], 1;" ::"l"(p) : "memory");
+}
+__device__ __forceinline__ int arrive_acq_rel(int* p) {
+  int v;
+  asm volatile("atom.acq_rel.gpu.global.add.s32 %0, [%1], 1;" : "=r"(v) : "l"(p) : "memory");
   return v;
 }
 __device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t (&r)[8]) {
@@ -553,7 +617,7 @@ __device__ __forceinline__ void write_h(const FewArgs& a, const FewSmem& s, cons
       float am = fmaxf(fmaxf(fabsf(h[0]), fabsf(h[1])), fmaxf(fabsf(h[2]), fabsf(h[3])));
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) am = fmaxf(am, __shfl_xor_sync(kFull, am, o));
-      const float sc = am > 0.f ? am / 448.0f : 1.0f, inv = 1.0f / sc;
+      const float sc = group_scale(am), inv = 1.0f / sc;
       uint8_t* step = img + static_cast<long long>(T.tile) * step_bytes<true>(m8);
       *reinterpret_cast<uint32_t*>(step + swizzled(c, 4 * lane)) =
           e4m3x4(quotient(h[0], sc, inv), quotient(h[1], sc, inv), quotient(h[2], sc, inv), quotient(h[3], sc, inv));
@@ -569,39 +633,53 @@ __device__ __forceinline__ void write_h(const FewArgs& a, const FewSmem& s, cons
   }
 }
 
-// The last arrival of an output tile: 256 channels of every token, one thread a
-// channel.  A token's terms are its slots' partial sums, slot by slot, then the
-// shared expert's; kAhead of them are on their way at a time.
-__device__ __forceinline__ void write_out(const FewArgs& a, const FewSmem& s, const FewItem& T, int tid) {
-  constexpr int kAhead = 16;
-  const int k = a.gate.top_k, H = a.H;
+// 256 channels of a token: its terms are the slots' partial sums, slot by slot,
+// then the shared expert's; warp w adds terms w, w + 8, ... (lane l channels 4l ..
+// and 128 + 4l ..), then the warps' sums are added in order.
+__device__ __forceinline__ void write_out(const FewArgs& a, FewSmem& s, const FewItem& T, int warp, int lane, int tid) {
+  constexpr int kAhead = 4;
+  const int k = a.gate.top_k, H = a.H, t = T.token;
   const long long plane = static_cast<long long>(a.n) * k * H, plane_s = static_cast<long long>(a.n) * H;
-  const int ch = T.tile * 256 + tid;
-  __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out);
-  for (int t = 0; t < a.n; ++t) {
-    float acc = 0.f;
-    int j = 0, i = 0;  // the next term: slot j (k: the shared expert), slice i
-    const int slots = k + (a.Is ? 1 : 0);
-    while (j < slots) {
-      float w[kAhead], v[kAhead];
+  const int routed = k * a.s2, terms = routed + (a.Is ? a.s2s : 0);
+  const int ch = T.tile * 256 + 4 * lane;
+  float4 lo = make_float4(0.f, 0.f, 0.f, 0.f), hi = lo;
+  for (int i0 = warp; i0 < terms; i0 += kEpiWarps * kAhead) {
+    float w[kAhead];
+    float4 l[kAhead], h[kAhead];
 #pragma unroll
-      for (int b = 0; b < kAhead; ++b) {
-        w[b] = v[b] = 0.f;
-        if (j < slots) {
-          const bool sh = j == k;
-          const int pos = sh ? t : s.pos[t * k + j];
-          if (pos >= 0) {
-            w[b] = sh ? 1.0f : s.w[t * k + j];
-            v[b] = __ldcg((sh ? a.ys + i * plane_s : a.y + i * plane) + static_cast<long long>(pos) * H + ch);
-          }
-          if (++i == (sh ? a.s2s : a.s2)) i = 0, ++j;
-        }
+    for (int r = 0; r < kAhead; ++r) {
+      const int i = i0 + r * kEpiWarps;
+      w[r] = 0.f;
+      l[r] = h[r] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (i >= terms) continue;
+      const float* src;
+      if (i < routed) {
+        const int j = i / a.s2, pos = s.pos[t * k + j];
+        if (pos < 0) continue;
+        w[r] = s.w[t * k + j];
+        src = a.y + (i - j * a.s2) * plane + static_cast<long long>(pos) * H + ch;
+      } else {
+        w[r] = 1.0f;
+        src = a.ys + (i - routed) * plane_s + static_cast<long long>(t) * H + ch;
       }
-#pragma unroll
-      for (int b = 0; b < kAhead; ++b) acc = fmaf(w[b], v[b], acc);
+      l[r] = __ldcg(reinterpret_cast<const float4*>(src));
+      h[r] = __ldcg(reinterpret_cast<const float4*>(src + 128));
     }
-    out[static_cast<long long>(t) * H + ch] = __float2bfloat16_rn(acc);
+#pragma unroll
+    for (int r = 0; r < kAhead; ++r) {
+      lo.x = fmaf(w[r], l[r].x, lo.x), lo.y = fmaf(w[r], l[r].y, lo.y);
+      lo.z = fmaf(w[r], l[r].z, lo.z), lo.w = fmaf(w[r], l[r].w, lo.w);
+      hi.x = fmaf(w[r], h[r].x, hi.x), hi.y = fmaf(w[r], h[r].y, hi.y);
+      hi.z = fmaf(w[r], h[r].z, hi.z), hi.w = fmaf(w[r], h[r].w, hi.w);
+    }
   }
+  *reinterpret_cast<float4*>(&s.sum[warp][4 * lane]) = lo;
+  *reinterpret_cast<float4*>(&s.sum[warp][128 + 4 * lane]) = hi;
+  epi_sync();
+  float acc = s.sum[0][tid];
+#pragma unroll
+  for (int w2 = 1; w2 < kEpiWarps; ++w2) acc += s.sum[w2][tid];
+  static_cast<__nv_bfloat16*>(a.out)[static_cast<long long>(t) * H + T.tile * 256 + tid] = __float2bfloat16_rn(acc);
 }
 
 // NT: columns (tokens) the FP8 epilogue keeps in registers; unused for BF16.
@@ -647,16 +725,24 @@ __global__ void __launch_bounds__(kThreads, 1) few_ffn_kernel(const FewArgs a) {
   } else if (warp == 1) {
     tmem_alloc(smem_u32(&s.tmem), kTmemCols);
     tmem_relinquish();
-  } else if (warp == 2 && a.Is && lane == 0) {
-    // The shared expert's gate/up weights are needed whatever the router says: fetched into L2 while it
-    // works.  (A layer id that is still being written would only fetch another layer's weights.)
-    const int l = load_layer(a.lref.layer, a.lref.n_layers, a.status, false);
-    const CUtensorMap* m = &a.lref.table[l].map[MAP_SH_GATE_UP];
-    tensormap_acquire(m);
-    const int boxes = a.Is / 128 * (a.H / (FP8 ? 128 : 64));
-    for (int b = blockIdx.x; b < boxes; b += gridDim.x) prefetch_box(m, b * 256);
+  }
+  // Before the router is done: the weight maps are acquired, and the shared expert's weights, which are needed
+  // whatever it says, are fetched into L2.  (A layer id that is still being written would only acquire and
+  // fetch another layer's.)
+  const int early = load_layer(a.lref.layer, a.lref.n_layers, a.status, false);
+  auto acquire_maps = [&](int l) {
+    for (int m = MAP_GATE_UP; m <= (a.Is ? MAP_SH_DOWN : MAP_DOWN); ++m) tensormap_acquire(&a.lref.table[l].map[m]);
+  };
+  if ((warp == 0 || warp == 2) && lane == 0) acquire_maps(early);
+  if (warp == 2 && a.Is && lane == 0) {
+    const int kx = FP8 ? 128 : 64;
+    const int gu = a.Is / 128 * (a.H / kx), all = gu + a.H / 256 * (a.Is / kx);
+    for (int b = blockIdx.x; b < min(all, kPrefetchBoxes); b += gridDim.x)
+      prefetch_box(&a.lref.table[early].map[b < gu ? MAP_SH_GATE_UP : MAP_SH_DOWN], (b < gu ? b : b - gu) * 256);
   }
   pdl_wait();
+  int claim = 0;
+  if (threadIdx.x == 0) claim = atomicAdd(&a.counters[0], 1);
   if (threadIdx.x < kMaxExperts) {
     s.expert[threadIdx.x] = ld_dep(&a.meta->expert[threadIdx.x]);
     s.start[threadIdx.x] = ld_dep(&a.meta->start[threadIdx.x]);
@@ -676,7 +762,7 @@ __global__ void __launch_bounds__(kThreads, 1) few_ffn_kernel(const FewArgs a) {
   const uint32_t tmem_base = s.tmem;
   const LayerEntry& le = a.lref.table[s.layer];
   const int items = (a.Is / 128 + s.active * (a.I / 128)) * a.s1 +
-                    a.H / 256 * (s.active * a.s2 + (a.Is ? a.s2s : 0));
+                    a.H / 256 * (s.active * a.s2 + (a.Is ? a.s2s : 0) + a.n);
   auto give_up = [&]() {
     *abort_flag = 1;
     record_status(a.status, ST_WAIT_TIMEOUT);
@@ -699,13 +785,8 @@ __global__ void __launch_bounds__(kThreads, 1) few_ffn_kernel(const FewArgs a) {
       uint32_t ph = 0;
       Ring<kQ> rq;
       const uint64_t pol = l2_policy(1);
-      tensormap_acquire(&le.map[MAP_GATE_UP]);
-      tensormap_acquire(&le.map[MAP_DOWN]);
-      if (a.Is) {
-        tensormap_acquire(&le.map[MAP_SH_GATE_UP]);
-        tensormap_acquire(&le.map[MAP_SH_DOWN]);
-      }
-      int next = atomicAdd(&a.counters[0], 1);
+      if (s.layer != early) acquire_maps(s.layer);
+      int next = claim;
       while (ok) {
         const int item = next < items ? next : -1;
         ok = mbar_wait(bar(B_QE + rq.s), rq.phase ^ 1u, abort_flag);
@@ -716,6 +797,7 @@ __global__ void __launch_bounds__(kThreads, 1) few_ffn_kernel(const FewArgs a) {
         if (item < 0) break;
         next = atomicAdd(&a.counters[0], 1);
         const FewItem T = decode<FP8>(a, s, item);
+        if (T.combine) continue;
         const CUtensorMap* m = &le.map[T.down ? (T.shared ? MAP_SH_DOWN : MAP_DOWN)
                                               : (T.shared ? MAP_SH_GATE_UP : MAP_GATE_UP)];
         const int tiles = T.down ? a.H / 256 : a.I / 128;
@@ -755,7 +837,7 @@ __global__ void __launch_bounds__(kThreads, 1) few_ffn_kernel(const FewArgs a) {
         const FewItem T = decode<FP8>(a, s, item);
         const uint32_t bytes = step_bytes<FP8>(T.rows);
         const uint8_t* img = T.down ? h_image<FP8>(a, s, T) : a.ximg;
-        if (T.down) {
+        if (T.down && !T.combine) {
           const int* ready = a.counters + a.h_ready + (T.shared ? 0 : 1 + T.j);
           const int want = (T.shared ? a.Is : a.I) / 128;
           ok = bounded_wait([&]() { return ld_acquire(ready) >= want; }, abort_flag);
@@ -842,24 +924,42 @@ __global__ void __launch_bounds__(kThreads, 1) few_ffn_kernel(const FewArgs a) {
     const int row = half * 128 + q * 32 + lane;  // of the weight tile
     Ring<kQ> rq;
     Ring<FP8 ? kPartials : kAccs> p;
-    int sx = 0, item;
+    int sx = 0, item = -1;
     uint32_t px = 0;
-    bool ok = true;
-    while (true) {
-      ok = pop(rq, item);
-      if (!epi_all(ok)) {  // the warps share barriers: all go on or none does
-        ok = false;
-        break;
+    FewItem T{};
+    // FP8: the scales of this warp's 128 weight rows, k-step kb0 + l in lane l (32 steps at a time), on their
+    // way before the item in front is finished
+    const float* bs_lo = nullptr;
+    float scales = 0.f;
+    auto load_scales = [&](int kb) {
+      if (kb + lane < T.kb1) scales = __ldg(bs_lo + kb + lane);
+    };
+    auto next_item = [&]() {
+      if (!pop(rq, item)) return false;
+      if (item < 0) return true;
+      T = decode<FP8>(a, s, item);
+      if (FP8 && !T.combine) {
+        const int scale_rows = T.down ? a.H / 128 : 2 * a.I / 128;
+        const int kit = (T.down ? (T.shared ? a.Is : a.I) : a.H) / 128;
+        bs_lo = le.scale[T.down ? (T.shared ? MAP_SH_DOWN : MAP_DOWN) : (T.shared ? MAP_SH_GATE_UP : MAP_GATE_UP)] +
+                (static_cast<long long>(T.shared ? 0 : s.expert[T.j]) * scale_rows + 2 * T.tile + half) * kit;
+        load_scales(T.kb0);
       }
-      if (item < 0) break;
-      const FewItem T = decode<FP8>(a, s, item);
+      return true;
+    };
+    bool ok = next_item();
+    while (true) {
+      const bool work = ok && item >= 0;
       // the item's sums of this thread's row go to plane ``slice`` of the workspace, row start + c for the
       // expert's c-th token
       const long long rows_all = T.shared ? a.n : a.n * a.gate.top_k;
       const long long ld = T.down ? a.H : 2 * (T.shared ? a.Is : a.I);
       float* dst = (T.down ? (T.shared ? a.ys : a.y) : (T.shared ? a.p1s : a.p1)) +
                    (T.slice * rows_all + T.start) * ld + T.tile * 256 + row;
-      if constexpr (FP8) {
+      if (work && T.combine) {
+        const int* done = a.counters + T.ticket;
+        ok = tid != 0 || bounded_wait([&]() { return ld_acquire(done) == T.arrivals; }, abort_flag);
+      } else if (FP8 && work) {
         float acc[NT];
 #pragma unroll
         for (int i = 0; i < NT; ++i) acc[i] = 0.f;
@@ -868,15 +968,10 @@ __global__ void __launch_bounds__(kThreads, 1) few_ffn_kernel(const FewArgs a) {
 #pragma unroll
         for (int ch = 0; ch < NT / 16; ++ch)
           live |= (T.down ? 16 * ch < T.tokens : ((T.mask >> (16 * ch)) & 0xffffull) != 0) ? 1u << ch : 0u;
-        const int scale_rows = T.down ? a.H / 128 : 2 * a.I / 128;
-        const int kit = (T.down ? (T.shared ? a.Is : a.I) : a.H) / 128;
-        const float* bs_lo =
-            le.scale[T.down ? (T.shared ? MAP_SH_DOWN : MAP_DOWN) : (T.shared ? MAP_SH_GATE_UP : MAP_GATE_UP)] +
-            (static_cast<long long>(T.shared ? 0 : s.expert[T.j]) * scale_rows + 2 * T.tile + half) * kit;
-        float next = __ldg(bs_lo + T.kb0);
         for (int kb = T.kb0; kb < T.kb1; ++kb) {
-          const float ws = next;
-          if (kb + 1 < T.kb1) next = __ldg(bs_lo + kb + 1);
+          const int at = (kb - T.kb0) & 31;
+          if (at == 0 && kb > T.kb0) load_scales(kb);
+          const float ws = __shfl_sync(kFull, scales, at);
           ok = __all_sync(kFull, mbar_wait(bar(B_FX + sx), px, abort_flag) &&
                                      mbar_wait(bar(B_PF + p.s), p.phase, abort_flag));
           if (!ok) break;
@@ -913,7 +1008,7 @@ __global__ void __launch_bounds__(kThreads, 1) few_ffn_kernel(const FewArgs a) {
           for (int i = 0; i < NT; ++i)
             if (T.down ? i < T.tokens : (T.mask >> i) & 1ull) dst[ld * c++] = acc[i];
         }
-      } else {
+      } else if (work) {
         ok = __all_sync(kFull, mbar_wait(bar(B_PF + p.s), p.phase, abort_flag));
         if (ok) {
           tc_fence_after();
@@ -939,33 +1034,32 @@ __global__ void __launch_bounds__(kThreads, 1) few_ffn_kernel(const FewArgs a) {
           p.advance();
         }
       }
-      __threadfence();
+      // the warps share barriers: all go on or none does, and each passes this one before it leaves
       if (!epi_all(ok)) {
         ok = false;
         break;
       }
-      if (tid == 0) {
-        __threadfence();
-        s.last = atomicAdd(&a.counters[T.ticket], 1) == T.slices - 1;
-        __threadfence();
-      }
-      epi_sync();
-      const bool last = *reinterpret_cast<volatile int*>(&s.last) != 0;
-      if (last) {
-        if (T.down) {
-          write_out(a, s, T, tid);
-        } else {
-          write_h<FP8>(a, s, T, warp - 4, lane);
+      if (item < 0) break;
+      if (T.combine) {
+        write_out(a, s, T, warp - 4, lane, tid);
+        ok = next_item();
+      } else if (T.down) {
+        if (tid == 0) arrive_release(a.counters + T.ticket);
+        ok = next_item();
+      } else {
+        const FewItem D = T;
+        int before = 0;
+        if (tid == 0) before = arrive_acq_rel(a.counters + D.ticket);
+        ok = next_item();
+        if (tid == 0) s.last = before == D.arrivals - 1;
+        epi_sync();
+        if (*reinterpret_cast<volatile int*>(&s.last)) {  // (written again only after the next epi_all)
+          write_h<FP8>(a, s, D, warp - 4, lane);
           fence_proxy_async_all();
-          __threadfence();
           epi_sync();
-          if (tid == 0) {
-            __threadfence();
-            atomicAdd(a.counters + a.h_ready + (T.shared ? 0 : 1 + T.j), 1);
-          }
+          if (tid == 0) arrive_release(a.counters + a.h_ready + (D.shared ? 0 : 1 + D.j));
         }
       }
-      // (s.last is written again only after the next item's epi_all)
     }
     if (!ok && lane == 0) give_up();
   }
@@ -994,6 +1088,8 @@ cudaError_t few_set_attributes() {
   };
   set(few_route_kernel<false>, kFewRouteSmem);
   set(few_route_kernel<true>, kFewRouteSmem);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(few_route_kernel<false>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(few_route_kernel<true>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
   set(few_ffn_kernel<false, 16>, kFewSmem);
   set(few_ffn_kernel<true, 16>, kFewSmem);
   set(few_ffn_kernel<true, 64>, kFewSmem);
@@ -1002,8 +1098,9 @@ cudaError_t few_set_attributes() {
 
 cudaError_t few_launch(const FewArgs& a, bool fp8, int grid, cudaStream_t st) {
   const int tiles = ceil_div(a.gate.n_experts, 16);
-  const size_t smem = sizeof(float) * 16 * tiles *
-                      (static_cast<size_t>(kRouteWarps / tiles) * a.n + ceil_div(a.n, kFewCluster) * kFewCluster);
+  const size_t smem =
+      sizeof(float) * (static_cast<size_t>(a.n) * kUnits * 16 +
+                       16 * tiles * (static_cast<size_t>(kRouteWarps / tiles) * a.n + round_up_dev(a.n, kFewCluster)));
   const cudaError_t e =
       fp8 ? launch_pdl(few_route_kernel<true>, dim3(kFewCluster), dim3(kRouteThreads), smem, st, kFewCluster, a)
           : launch_pdl(few_route_kernel<false>, dim3(kFewCluster), dim3(kRouteThreads), smem, st, kFewCluster, a);

@@ -7,11 +7,11 @@
 namespace asap {
 
 constexpr int kFewTokens = 64;                // tokens of a call at most (one bit each in a 64-bit mask)
-constexpr int kFewCluster = 8;                // CTAs of the route kernel
+constexpr int kFewCluster = 16;               // CTAs of the route kernel
 constexpr int kFewMaxStages = 8;              // ring stages of either operand at most
-constexpr size_t kFewSmemState = 10752;       // barriers, queue and metadata behind the rings
+constexpr size_t kFewSmemState = 18944;       // barriers, queue and metadata behind the rings
 constexpr size_t kFewSmem = 227 * 1024;       // dynamic shared memory of a few_ffn_kernel CTA at most
-constexpr size_t kFewRouteSmem = 2 * 4 * 256 * kFewTokens;  // partial and gathered logits at most
+constexpr size_t kFewRouteSmem = (448 + 2 * 4 * 256) * kFewTokens;  // rows, partial and gathered logits at most
 
 // Routing as the second kernel reads it.  Active experts are in increasing
 // order; expert j's tokens are the bits of mask[j], its rows start[j] .. of the
