@@ -140,7 +140,7 @@ int few_slices(long long tiles, int k_steps) {
 // Sizes and workspace offsets of a few-token call of n tokens (1 .. kFewTokens).
 struct FewLayout {
   asap::FewArgs a{};
-  size_t meta, counters, ximg, himg, p1, p1s, y, ys, total;
+  size_t logits, counters, ximg, himg, p1, p1s, y, ys, total;
 };
 
 FewLayout few_layout(const asap_moe_config& c, int n) {
@@ -158,6 +158,15 @@ FewLayout few_layout(const asap_moe_config& c, int n) {
   const long long down = static_cast<long long>(a.max_active + (a.Is ? 1 : 0)) * tH;
   a.s2 = few_slices(down, a.I / step);
   a.s2s = a.Is ? few_slices(down, a.Is / step) : 0;
+  a.first_routed = tS * a.s1;
+  a.r_s1 = 1.0f / a.s1;
+  a.r_s2 = 1.0f / a.s2;
+  a.r_s2s = a.Is ? 1.0f / a.s2s : 0.f;
+  a.r_tI = 1.0f / tI;
+  a.r_tH = 1.0f / tH;
+  a.r_down = 1.0f / (tH * a.s2);
+  // every CTA of the second kernel adds the slices of all logits: fewer where there are many tokens
+  a.logit_slices = n <= 8 ? 8 : 4;
   a.down_tickets = 1 + tS + a.max_active * tI;
   a.h_ready = a.down_tickets + tH;
   a.n_counters = a.h_ready + 1 + a.max_active;
@@ -180,7 +189,7 @@ FewLayout few_layout(const asap_moe_config& c, int n) {
   // groups of 8 rows of the active experts: at most one per row, and the rows over 8 plus one per expert
   const size_t groups = std::min<size_t>(nk, nk / 8 + a.max_active);
   const size_t row = fp8 ? 132 : 128, hrows = fp8 ? 8 : 16;
-  L.meta = take(sizeof(asap::FewMeta));
+  L.logits = take(static_cast<size_t>(a.logit_slices) * n * c.n_experts * 4);
   L.counters = take(a.n_counters * sizeof(int));
   L.ximg = take(a.H / step * m8 * row);
   L.himg = take((a.Is / step * (m8 / 8) + a.I / step * groups) * hrows * row);
@@ -1413,7 +1422,7 @@ ASAP_API int asap_moe_layer_few(asap_moe_t h, const int32_t* layer_id, const voi
   a.status = h->status;
   a.x = x;
   a.out = out;
-  a.meta = at<asap::FewMeta>(ws, L.meta);
+  a.logits = at<float>(ws, L.logits);
   a.counters = at<int>(ws, L.counters);
   a.ximg = at<uint8_t>(ws, L.ximg);
   a.himg = at<uint8_t>(ws, L.himg);

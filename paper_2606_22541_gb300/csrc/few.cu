@@ -6,20 +6,20 @@
 // stream of the active experts' matrices (three of H x I each) and nothing else
 // matters but that this stream never stops.
 //
-// few_route_kernel (one cluster): router logits with mma.sync, K split over the
-// CTAs and added in rank order through distributed shared memory; gating, one
-// warp per token; the list of active experts, each with the set of its tokens
-// as a 64-bit mask (so a row's place in its expert is a popcount); the hidden
-// states as an image of the operand tiles (128-byte rows, 128-byte swizzle; e4m3
-// with scales for FP8), which the second kernel copies to shared memory as they
-// are; and zeroed counters.
+// few_logits_kernel: router logits with mma.sync, 16 experts and a slice of K per
+// CTA, as planes of partial sums; the hidden states as an image of the operand
+// tiles (128-byte rows, 128-byte swizzle; e4m3 with scales for FP8), which the
+// second kernel copies to shared memory as they are; and zeroed counters.
 //
 // few_ffn_kernel (one CTA per SM): a list of work items, gate/up tiles of all
 // experts, then down tiles, then the outputs, claimed one by one from a counter.  An item is a
 // 256-row weight tile (a box per k-step, 32 KB, as the handle packs them) over
 // a slice of K.  The weights are the M operand of the MMA and all tokens the N
 // operand, so a tile costs the same whatever its rows; the tensor core is idle
-// most of the time.
+// most of the time.  The shared expert, which every token meets, comes first:
+// while its weights stream, every CTA gates all tokens for itself (one warp per
+// token) and lists the active experts, each with the set of its tokens as a
+// 64-bit mask, so that a row's place in its expert is a popcount.
 //  - gate/up: the partial sums of a K slice go to the workspace in fp32; the
 //    last slice of a tile to arrive adds them in slice order, applies SwiGLU
 //    and writes h as an operand image: e4m3 with scales, or, for BF16, as the
@@ -39,6 +39,7 @@
 #include <cuda_fp8.h>
 #include <math_constants.h>
 
+#include <algorithm>
 #include <cstddef>
 
 namespace asap {
@@ -46,24 +47,6 @@ namespace asap {
 namespace {
 
 constexpr unsigned kFull = 0xffffffffu;
-
-__device__ __forceinline__ uint32_t rank_in_cluster() {
-  uint32_t r;
-  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-  return r;
-}
-__device__ __forceinline__ uint32_t map_rank(uint32_t addr, uint32_t rank) {
-  uint32_t d;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(d) : "r"(addr), "r"(rank));
-  return d;
-}
-__device__ __forceinline__ void st_rank_u32(uint32_t addr, uint32_t v) {
-  asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
-}
-__device__ __forceinline__ void cluster_sync() {
-  asm volatile("barrier.cluster.arrive.release;" ::: "memory");
-  asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
-}
 
 // ------------------------------------------------------------ operand images
 // A k-step's rows: R rows of 128 bytes, 16-byte chunk c of row r at chunk
@@ -93,10 +76,7 @@ __device__ __forceinline__ uint32_t e4m3x4(float a, float b, float c, float d) {
   return static_cast<uint32_t>(lo) | (static_cast<uint32_t>(hi) << 16);
 }
 
-// ------------------------------------------------------------ route
-constexpr int kRouteWarps = 16;
-constexpr int kRouteThreads = 32 * kRouteWarps;
-
+// ------------------------------------------------------------ gating
 // Float as an unsigned that orders the same way (-0 as +0).
 __device__ __forceinline__ uint32_t ordered(float f) {
   const uint32_t u = __float_as_uint(f + 0.0f);
@@ -104,36 +84,35 @@ __device__ __forceinline__ uint32_t ordered(float f) {
 }
 
 // Gating of one token by a warp, from its logits (lane l: experts l, l + 32,
-// ...): expert and weight of slot j in lane j.  The rules and tie-breaks of
-// gate_kernel (route.cu); a round's winner is found with two warp reductions.
-// scratch: n_groups * (group size + 1) floats.
-__device__ __forceinline__ void gate_token(const GateParams& p, const float* bias, const float (&logit)[8], float* scratch,
-                                           int lane, int& my_e, float& my_w) {
+// ...): expert and weight of slot j in lane j (expert -1: none left).  The rules
+// and tie-breaks of gate_kernel (route.cu); a round's winner is found with two
+// warp reductions over the lanes' best.  scratch: E + n_groups floats.
+__device__ __forceinline__ void gate_token(const GateParams& p, const float (&logit)[8], const float (&biases)[8],
+                                           float* scratch, int lane, int& my_e, float& my_w) {
   const int E = p.n_experts;
   const bool grouped = p.gating == 2;
-  float key[8], val[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int e = lane + 32 * i;
-    val[i] = grouped ? gate_sigmoid(logit[i]) : logit[i];
-    key[i] = val[i] + (grouped && bias && e < E ? __ldg(bias + e) : 0.f);
-  }
-  uint32_t open = 0;  // experts of this lane that may be chosen
+  float val[8];
+  uint32_t key[8];  // 0: may not be chosen
   if (grouped) {
     const int gsz = E / p.n_groups;
+    const float per = 1.0f / static_cast<float>(gsz);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const int e = lane + 32 * i;
-      if (e < E) scratch[e + e / gsz] = key[i];
+      const int e = lane + 32 * i, g = static_cast<int>((e + 0.5f) * per);
+      val[i] = gate_sigmoid(logit[i]);
+      const float sel = val[i] + biases[i];
+      key[i] = e < E ? ordered(sel) : 0u;
+      if (e < E) scratch[e + g] = sel;
     }
     __syncwarp();
     // a team of lanes (the largest power of two that gives every group one) finds a group's two best
-    int team = 1;
-    while (2 * team * p.n_groups <= 32) team *= 2;
-    const int grp = lane / team;
+    int log_team = 0;
+    while ((2 << log_team) * p.n_groups <= 32) ++log_team;
+    const int team = 1 << log_team, grp = lane >> log_team;
     float m1 = -CUDART_INF_F, m2 = -CUDART_INF_F;
     if (grp < p.n_groups)
-      for (int j = lane % team; j < gsz; j += team) {
+#pragma unroll 4
+      for (int j = lane & (team - 1); j < gsz; j += team) {
         const float v = scratch[grp * (gsz + 1) + j];
         m2 = fmaxf(m2, fminf(m1, v));
         m1 = fmaxf(m1, v);
@@ -143,8 +122,9 @@ __device__ __forceinline__ void gate_token(const GateParams& p, const float* bia
       m2 = fmaxf(fmaxf(m2, o2), fminf(m1, o1));
       m1 = fmaxf(m1, o1);
     }
-    const float score = __shfl_sync(kFull, m1 + m2, min(lane * team, 31));  // lane g: group g's
+    const float score = __shfl_sync(kFull, m1 + m2, min(lane << log_team, 31));  // lane g: group g's
     int rank = 0;  // groups in front of this lane's
+#pragma unroll 4
     for (int g = 0; g < p.n_groups; ++g) {
       const float o = __shfl_sync(kFull, score, g);
       rank += (o > score || (o == score && g < lane)) ? 1 : 0;
@@ -152,47 +132,46 @@ __device__ __forceinline__ void gate_token(const GateParams& p, const float* bia
     const uint32_t kept = __ballot_sync(kFull, lane < p.n_groups && rank < p.topk_groups);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const int e = lane + 32 * i;
-      if (e < E && ((kept >> (e / gsz)) & 1u)) open |= 1u << i;
+      const int g = static_cast<int>((lane + 32 * i + 0.5f) * per);
+      if (!((kept >> (g & 31)) & 1u)) key[i] = 0u;
     }
+    __syncwarp();
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (lane + 32 * i < E) open |= 1u << i;
-  }
-  my_e = -1;
-  float my_v = 0.f;
-  float top = 0.f;  // the first slot's value
-  for (int j = 0; j < p.top_k; ++j) {
-    uint32_t best = 0;
-    int be = 0x7fffffff;
-#pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const uint32_t o = ordered(key[i]);
-      if (((open >> i) & 1u) && (be == 0x7fffffff || o > best)) {
-        best = o;
-        be = lane + 32 * i;
-      }
+      val[i] = logit[i];
+      key[i] = lane + 32 * i < E ? ordered(logit[i]) : 0u;
     }
+  }
+  uint32_t best = 0;  // the lane's best, of equal ones the first
+  int be = 0x7fffffff;
+  float bv = 0.f;
+  auto take_best = [&]() {
+    best = 0, be = 0x7fffffff;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (key[i] > best) best = key[i], be = lane + 32 * i, bv = val[i];
+  };
+  take_best();
+  my_e = -1;
+  float my_v = 0.f, top = 0.f;  // top: the first slot's value
+  for (int j = 0; j < p.top_k; ++j) {
     const uint32_t mx = __reduce_max_sync(kFull, best);
     const int win = __reduce_min_sync(kFull, best == mx ? be : 0x7fffffff);
     if (win == 0x7fffffff) break;
-    float v = 0.f;
+    const float v = __shfl_sync(kFull, bv, win & 31);
+    if (j == 0) top = v;
+    if (lane == j) my_e = win, my_v = v;
     if ((win & 31) == lane) {
 #pragma unroll
       for (int i = 0; i < 8; ++i)
-        if (i == (win >> 5)) v = val[i];
-      open &= ~(1u << (win >> 5));
+        if (i == (win >> 5)) key[i] = 0u;
+      take_best();
     }
-    v = __shfl_sync(kFull, v, win & 31);
-    if (j == 0) top = v;
-    if (lane == j) {
-      my_e = win;
-      my_v = v;
-    }
+    __syncwarp();
   }
   // lanes 0 .. k-1 hold the slots; sums in slot order
-  float num = lane < p.top_k && my_e >= 0 ? (grouped ? my_v : expf(my_v - top)) : 0.f;
+  const float num = lane < p.top_k && my_e >= 0 ? (grouped ? my_v : expf(my_v - top)) : 0.f;
   float den = 0.f;
   for (int j = 0; j < p.top_k; ++j) den += __shfl_sync(kFull, num, j);
   if (p.gating == 0) {
@@ -206,6 +185,7 @@ __device__ __forceinline__ void gate_token(const GateParams& p, const float* bia
   my_w = num / den * (grouped ? p.route_scale : 1.0f);
 }
 
+// ------------------------------------------------------------ logits
 // Hidden states as operand image: rows n .. are zero.
 template <bool FP8>
 __device__ __forceinline__ void write_image(const FewArgs& a, int rows, int thread, int threads) {
@@ -249,181 +229,92 @@ __device__ __forceinline__ void write_image(const FewArgs& a, int rows, int thre
   }
 }
 
-// K units (32 channels) of the router that a warp has on their way at a time; a
-// row of them in shared memory is 28 vectors, so that the 8 lanes of a 128-bit
-// access phase (two rows) meet every bank once.
-constexpr int kUnits = 7;
+constexpr int kLogitWarps = 8;
+constexpr int kLogitThreads = 32 * kLogitWarps;
+constexpr int kUnits = 7;  // K units (32 channels) of a warp on their way at a time
+constexpr int kPrefetchBoxes = 1024;  // of 32 KB, what HBM delivers until the second kernel asks for more
 
+__device__ __forceinline__ void prefetch_box(const CUtensorMap* m, int y) {
+  asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global.tile [%0, {%1, %2}];" ::"l"(reinterpret_cast<uint64_t>(m)),
+               "r"(0), "r"(y)
+               : "memory");
+}
+
+// CTA (tile, slice): logits of 16 experts (M) over a slice of K for all tokens (8 per MMA, N).  Its warps take
+// every eighth K unit; thread (g, q) feeds 16 bytes of a row to two MMAs, whose K order both operands share.
+// CTAs past the router's help with the rest.
 template <bool FP8>
-__global__ void __launch_bounds__(kRouteThreads) few_route_kernel(const FewArgs a) {
-  extern __shared__ __align__(16) float smem_f[];
-  __shared__ int sel_e[kFewTokens * kMaxTopK];
-  __shared__ float sel_w[kFewTokens * kMaxTopK];
-  __shared__ unsigned long long mask[kMaxExperts];
-  __shared__ int packed_before[kMaxExperts];  // rows, row groups and actives before expert e
-  __shared__ int warp_total[kMaxExperts / 32];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int rank = static_cast<int>(rank_in_cluster());
-  const int E = a.gate.n_experts, k = a.gate.top_k, n = a.n;
-  const int tiles = (E + 15) / 16, Ep = 16 * tiles;
-  const int subs = kRouteWarps / tiles;          // K parts inside the CTA
-  const int V = a.H / 8, units = a.H / 32;
-  const int u0 = units * rank / kFewCluster, u1 = units * (rank + 1) / kFewCluster;
-  // this rank's columns of the router weights are asked for before the second kernel, which comes up
-  // meanwhile, asks for its own
-  {
-    const uint8_t* w = static_cast<const uint8_t*>(
-        a.lref.table[load_layer(a.lref.layer, a.lref.n_layers, a.status, false)].router_w);
-    const int bytes = (u1 - u0) * 64, lines = (bytes + 127) / 128;
-    for (int i = threadIdx.x; i < E * lines; i += kRouteThreads)
-      asm volatile("prefetch.global.L2 [%0];" ::"l"(w + (static_cast<long long>(i / lines) * V + u0 * 4) * 16 +
-                                                    min(i % lines * 128, bytes - 64)));
-  }
-  pdl_launch();
+__global__ void __launch_bounds__(kLogitThreads) few_logits_kernel(const FewArgs a) {
+  pdl_launch();  // the second kernel may come up and fetch weights meanwhile
+  __shared__ float part[kLogitWarps][kFewTokens][16];
   pdl_wait();
-  uint4* xs = reinterpret_cast<uint4*>(smem_f);                          // [n][4 kUnits]
-  float* part = smem_f + n * kUnits * 16;                                // [subs][n][Ep]
-  float* gat = part + subs * n * Ep;                                     // [tokens][kFewCluster][Ep]
-  const LayerEntry& le =
-      a.lref.table[load_layer(a.lref.layer, a.lref.n_layers, a.status, rank == 0 && threadIdx.x == 0)];
-
-  // ---- what the second kernel needs besides the routing
-  const int thread = rank * kRouteThreads + threadIdx.x;
-  constexpr int kThreadsAll = kFewCluster * kRouteThreads;
-  for (int i = thread; i < a.n_counters; i += kThreadsAll) a.counters[i] = 0;
-  write_image<FP8>(a, round_up_dev(n, 8), thread, kThreadsAll);
-  for (int e = threadIdx.x; e < kMaxExperts; e += kRouteThreads) mask[e] = 0;
-
-  // ---- partial logits: expert tile (16 rows, M) x tokens (8 per MMA, N); thread (g, q) feeds 16 bytes of a
-  // row to two MMAs whose K order both operands share
-  const int tile = warp % tiles, sub = warp / tiles;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int E = a.gate.n_experts, n = a.n;
+  const int slice = blockIdx.x % a.logit_slices, tile = blockIdx.x / a.logit_slices;
   const int g = lane >> 2, q = lane & 3;
-  {
-    const uint4* __restrict__ wr = static_cast<const uint4*>(le.router_w);
+  if (tile * 16 < E) {
+    const int layer = load_layer(a.lref.layer, a.lref.n_layers, a.status, blockIdx.x == 0 && threadIdx.x == 0);
+    const uint4* __restrict__ wr = static_cast<const uint4*>(a.lref.table[layer].router_w);
     const uint4* x = static_cast<const uint4*>(a.x);
+    const int V = a.H / 8, units = a.H / 32;
+    const int u0 = units * slice / a.logit_slices, u1 = units * (slice + 1) / a.logit_slices;
     const int e0 = tile * 16 + g, e1 = e0 + 8;
     const uint4 zero = make_uint4(0, 0, 0, 0);
     float c[kFewTokens / 8][4];
 #pragma unroll
     for (int j = 0; j < kFewTokens / 8; ++j) c[j][0] = c[j][1] = c[j][2] = c[j][3] = 0.f;
-    for (int ub = u0; ub < u1; ub += kUnits) {
-      const int cnt = sub < subs ? min(kUnits, u1 - ub) : 0;
+    for (int ub = u0 + warp; ub < u1; ub += kLogitWarps * kUnits) {
       uint4 w0[kUnits], w1[kUnits];
 #pragma unroll
       for (int i = 0; i < kUnits; ++i) {
-        const int u = i * subs + sub, v = 4 * (ub + u) + q;
-        w0[i] = u < cnt && e0 < E ? __ldg(wr + static_cast<long long>(e0) * V + v) : zero;
-        w1[i] = u < cnt && e1 < E ? __ldg(wr + static_cast<long long>(e1) * V + v) : zero;
+        const int u = ub + kLogitWarps * i, v = 4 * u + q;
+        w0[i] = u < u1 && e0 < E ? __ldg(wr + static_cast<long long>(e0) * V + v) : zero;
+        w1[i] = u < u1 && e1 < E ? __ldg(wr + static_cast<long long>(e1) * V + v) : zero;
       }
-      const int vecs = 4 * min(kUnits, u1 - ub);
-      for (int i = threadIdx.x; i < n * vecs; i += kRouteThreads) {
-        const int t = i / vecs, v = i - t * vecs;
-        xs[t * 4 * kUnits + v] = ld_dep(x + static_cast<long long>(t) * V + 4 * ub + v);
+      // The shared expert's gate/up weights are needed whatever the router says: fetched into L2, behind the
+      // router's own.
+      if (threadIdx.x == 0 && ub == u0 && a.Is) {
+        const CUtensorMap* m = &a.lref.table[layer].map[MAP_SH_GATE_UP];
+        tensormap_acquire(m);
+        const int boxes = min(kPrefetchBoxes, a.Is / 128 * (a.H / (FP8 ? 128 : 64)));
+        for (int b = blockIdx.x; b < boxes; b += gridDim.x) prefetch_box(m, b * 256);
       }
-      __syncthreads();
 #pragma unroll
-      for (int i = 0; i < kUnits; ++i) {
-        const int u = i * subs + sub;
-        if (u >= cnt) break;
+      for (int j = 0; j < kFewTokens / 8; ++j) {
+        if (8 * j >= n) break;
+        const int t = 8 * j + g;
+        uint4 xv[kUnits];
 #pragma unroll
-        for (int j = 0; j < kFewTokens / 8; ++j) {
-          if (8 * j >= n) break;
-          const int t = 8 * j + g;
-          const uint4 xv = t < n ? xs[t * 4 * kUnits + 4 * u + q] : zero;
-          mma_bf16_16816(c[j], w0[i].x, w1[i].x, w0[i].y, w1[i].y, xv.x, xv.y);
-          mma_bf16_16816(c[j], w0[i].z, w1[i].z, w0[i].w, w1[i].w, xv.z, xv.w);
+        for (int i = 0; i < kUnits; ++i) {
+          const int u = ub + kLogitWarps * i;
+          xv[i] = u < u1 && t < n ? ld_dep(x + static_cast<long long>(t) * V + 4 * u + q) : zero;
+        }
+#pragma unroll
+        for (int i = 0; i < kUnits; ++i) {
+          mma_bf16_16816(c[j], w0[i].x, w1[i].x, w0[i].y, w1[i].y, xv[i].x, xv[i].y);
+          mma_bf16_16816(c[j], w0[i].z, w1[i].z, w0[i].w, w1[i].w, xv[i].z, xv[i].w);
         }
       }
-      __syncthreads();
     }
-    if (sub < subs)
 #pragma unroll
-      for (int j = 0; j < kFewTokens / 8; ++j)
+    for (int j = 0; j < kFewTokens / 8; ++j)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int t = 8 * j + 2 * q + (i & 1);
-          if (t < n) part[(sub * n + t) * Ep + tile * 16 + g + 8 * (i >> 1)] = c[j][i];
-        }
-  }
-  cluster_sync();  // (every CTA has started; and the CTA's own barrier)
-  // ---- token t's partial logits go to CTA t % kFewCluster, which adds the ranks' in order
-  for (int t = warp; t < n; t += kRouteWarps) {
-    const uint32_t to =
-        map_rank(smem_u32(gat + (t / kFewCluster * kFewCluster + rank) * Ep), static_cast<uint32_t>(t % kFewCluster));
-    for (int e = lane; e < Ep; e += 32) {
-      float v = part[t * Ep + e];
-      for (int u = 1; u < subs; ++u) v += part[(u * n + t) * Ep + e];
-      st_rank_u32(to + 4u * e, __float_as_uint(v));
+      for (int i = 0; i < 4; ++i) {
+        const int t = 8 * j + 2 * q + (i & 1);
+        if (t < n) part[warp][t][g + 8 * (i >> 1)] = c[j][i];
+      }
+    __syncthreads();
+    for (int i = threadIdx.x; i < n * 16; i += kLogitThreads) {
+      const int t = i / 16, e = tile * 16 + i % 16;
+      float sum = part[0][t][i % 16];
+#pragma unroll
+      for (int w = 1; w < kLogitWarps; ++w) sum += part[w][t][i % 16];
+      if (e < E) a.logits[(slice * n + t) * E + e] = sum;
     }
   }
-  cluster_sync();
-  const int mine = rank < n ? ceil_div_dev(n - rank, kFewCluster) : 0;
-  for (int i = threadIdx.x; i < mine * Ep; i += kRouteThreads) {
-    const float* src = gat + (i / Ep * kFewCluster) * Ep + i % Ep;
-    float l = src[0];
-#pragma unroll
-    for (int r = 1; r < kFewCluster; ++r) l += src[r * Ep];
-    part[i] = l;
-  }
-  __syncthreads();
-  if (warp < mine) {
-    const int t = rank + warp * kFewCluster;
-    float logit[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) logit[i] = lane + 32 * i < E ? part[warp * Ep + lane + 32 * i] : 0.f;
-    int e;
-    float w;
-    // the gathered logits have been added: their place holds the selection scores
-    gate_token(a.gate, le.router_bias, logit, gat + warp * kFewCluster * Ep, lane, e, w);
-    if (lane < k) {
-      st_rank_u32(map_rank(smem_u32(&sel_e[t * k + lane]), 0), static_cast<uint32_t>(e));
-      st_rank_u32(map_rank(smem_u32(&sel_w[t * k + lane]), 0), __float_as_uint(w));
-    }
-  }
-  cluster_sync();  // all choices are in rank 0
-  if (rank != 0) return;
-  // ---- active experts in order, their tokens, rows and row groups
-  for (int p = threadIdx.x; p < n * k; p += kRouteThreads) {
-    const int e = sel_e[p];
-    if (e >= 0 && e < E) atomicOr(&mask[e], 1ull << (p / k));
-    else record_status(a.status, ST_BAD_EXPERT_INDEX);
-  }
-  __syncthreads();
-  int v = 0, incl = 0;
-  if (threadIdx.x < kMaxExperts) {
-    const int m = __popcll(mask[threadIdx.x]);
-    v = m ? 1 | (m << 10) | (((m + 7) / 8) << 20) : 0;  // at most 256, 512 and 512 in all
-    incl = v;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int b = __shfl_up_sync(kFull, incl, o);
-      if (lane >= o) incl += b;
-    }
-    if (lane == 31) warp_total[warp] = incl;
-  }
-  __syncthreads();
-  FewMeta* meta = a.meta;
-  if (threadIdx.x < kMaxExperts) {
-    int before = 0;
-    for (int w2 = 0; w2 < warp; ++w2) before += warp_total[w2];
-    before += incl - v;
-    packed_before[threadIdx.x] = before;
-    if (v) {
-      const int j = before & 1023;
-      meta->expert[j] = threadIdx.x;
-      meta->start[j] = (before >> 10) & 1023;
-      meta->row8[j] = before >> 20;
-      meta->mask[j] = mask[threadIdx.x];
-    }
-    if (threadIdx.x == kMaxExperts - 1) meta->active = (before + v) & 1023;
-  }
-  __syncthreads();
-  for (int p = threadIdx.x; p < n * k; p += kRouteThreads) {
-    const int e = sel_e[p], t = p / k;
-    const bool ok = e >= 0 && e < E;
-    meta->pos[p] = ok ? ((packed_before[e] >> 10) & 1023) + __popcll(mask[e] & ((1ull << t) - 1)) : -1;
-    meta->w[p] = sel_w[p];
-  }
+  const int thread = blockIdx.x * kLogitThreads + threadIdx.x, threads = gridDim.x * kLogitThreads;
+  for (int i = thread; i < a.n_counters; i += threads) a.counters[i] = 0;
+  write_image<FP8>(a, round_up_dev(n, 8), thread, threads);
 }
 
 // ------------------------------------------------------------ expert FFN
@@ -431,7 +322,6 @@ constexpr int kWBytes = 256 * 128;  // weight box
 constexpr int kEpiWarps = 8;
 constexpr int kEpiThreads = 32 * kEpiWarps;
 constexpr int kThreads = 32 * (4 + kEpiWarps);
-constexpr int kPrefetchBoxes = 1792;  // at most 56 MB of the 129 MB L2
 constexpr int kQ = 6;               // items in flight in a CTA
 constexpr int kQReaders = 2 + kEpiWarps;
 constexpr uint32_t kTmemCols = 512;
@@ -454,36 +344,45 @@ struct FewItem {
 };
 
 struct FewSmem {  // behind the rings
-  alignas(16) uint64_t bar[2 * kFewMaxStages + 2 * kFewMaxStages + 2 * kPartials + 2 * kQ + 1];
+  alignas(16) uint64_t bar[2 * kFewMaxStages + 2 * kFewMaxStages + 2 * kPartials + 2 * kQ + 2];
   int q[kQ];
   uint32_t tmem;
   int abort;
   int layer;
   int last;
   int active;
+  int items;
+  int warp_total[kEpiWarps];
   int expert[kMaxExperts], start[kMaxExperts], row8[kMaxExperts];
   unsigned long long mask[kMaxExperts];
   int pos[kFewTokens * kMaxTopK];
   float w[kFewTokens * kMaxTopK];
-  alignas(16) float sum[kEpiWarps][256];  // combine; accessed as float4
+  alignas(16) float sum[kEpiWarps][288];  // combine (accessed as float4); gating: selection scores and ranks
 };
 static_assert(sizeof(FewSmem) <= kFewSmemState, "shared memory budget");
 static_assert(offsetof(FewSmem, sum) % 16 == 0, "float4 accesses");
+
+// u / d for 0 <= u < 2^21 from r = 1 / d rounded to fp32 (u + 1/2 is at least 1/(2 d) from a multiple of d, in
+// units of d, and the product's error is below 2^-23 u / d).
+__device__ __forceinline__ int quick_div(int u, float r) { return static_cast<int>((u + 0.5f) * r); }
 
 template <bool FP8>
 __device__ __forceinline__ FewItem decode(const FewArgs& a, const FewSmem& s, int item) {
   FewItem T{};
   const int tI = a.I / 128, tS = a.Is / 128, tH = a.H / 256;
-  const int gu = (tS + s.active * tI) * a.s1;  // gate/up items
-  const int arrivals = s.active * a.s2 + (a.Is ? a.s2s : 0);
-  const int dn = tH * arrivals;                // down items
-  T.down = item >= gu;
+  // (items below first_routed do not need the routing, which may not be there yet)
+  const bool early = item < a.first_routed;
+  const int active = early ? 0 : s.active;
+  const int gu = (tS + active * tI) * a.s1;  // gate/up items
+  const int arrivals = active * a.s2 + (a.Is ? a.s2s : 0);
+  const int dn = tH * arrivals;              // down items
+  T.down = !early && item >= gu;
   int kit, sl;
   if (!T.down) {
-    const int t = item / a.s1;
+    const int t = quick_div(item, a.r_s1);
     T.slice = item - t * a.s1;
     T.shared = t < tS;
-    T.j = T.shared ? 0 : (t - tS) / tI;
+    T.j = T.shared ? 0 : quick_div(t - tS, a.r_tI);
     T.tile = T.shared ? t : (t - tS) - T.j * tI;
     T.arrivals = a.s1;
     T.ticket = 1 + t;
@@ -495,7 +394,7 @@ __device__ __forceinline__ FewItem decode(const FewArgs& a, const FewSmem& s, in
     if (u >= dn) {
       u -= dn;
       T.combine = true;
-      T.token = u / tH;
+      T.token = quick_div(u, a.r_tH);
       T.tile = u - T.token * tH;
       T.ticket = a.down_tickets + T.tile;
       return T;
@@ -504,15 +403,16 @@ __device__ __forceinline__ FewItem decode(const FewArgs& a, const FewSmem& s, in
     T.shared = u < sh;
     if (!T.shared) u -= sh;
     sl = T.shared ? a.s2s : a.s2;
-    T.j = T.shared ? 0 : u / (tH * sl);
+    T.j = T.shared ? 0 : quick_div(u, a.r_down);
     u -= T.j * tH * sl;
-    T.tile = u / sl;
+    T.tile = quick_div(u, T.shared ? a.r_s2s : a.r_s2);
     T.slice = u - T.tile * sl;
     T.ticket = a.down_tickets + T.tile;
     kit = (T.shared ? a.Is : a.I) / (FP8 ? 128 : 64);
   }
-  T.kb0 = kit * T.slice / sl;
-  T.kb1 = kit * (T.slice + 1) / sl;
+  const float r_sl = T.down ? (T.shared ? a.r_s2s : a.r_s2) : a.r_s1;
+  T.kb0 = quick_div(kit * T.slice, r_sl);
+  T.kb1 = quick_div(kit * (T.slice + 1), r_sl);
   T.mask = T.shared ? (a.n == 64 ? ~0ull : (1ull << a.n) - 1) : s.mask[T.j];
   T.tokens = T.shared ? a.n : __popcll(T.mask);
   T.start = T.shared ? 0 : s.start[T.j];
@@ -534,11 +434,6 @@ __device__ __forceinline__ uint8_t* h_image(const FewArgs& a, const FewSmem& s, 
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
                "l"(src), "r"(bytes), "r"(bar)
-               : "memory");
-}
-__device__ __forceinline__ void prefetch_box(const CUtensorMap* m, int y) {
-  asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global.tile [%0, {%1, %2}];" ::"l"(reinterpret_cast<uint64_t>(m)),
-               "r"(0), "r"(y)
                : "memory");
 }
 __device__ __forceinline__ void fence_proxy_async_all() { asm volatile("fence.proxy.async;" ::: "memory"); }
@@ -587,6 +482,78 @@ __device__ __forceinline__ bool epi_all(bool ok) {
       : "r"(ok ? 1u : 0u)
       : "memory");
   return r != 0;
+}
+
+// The routing of the call, by the epilogue warps of every CTA for themselves:
+// active experts in increasing order, their tokens, first rows and row groups,
+// the row and weight of every slot, and the number of work items.
+__device__ __forceinline__ void list_experts(const FewArgs& a, FewSmem& s, const float* bias, int warp, int lane, int tid) {
+  const int E = a.gate.n_experts, k = a.gate.top_k, n = a.n;
+  s.mask[tid] = 0ull;
+  float biases[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) biases[i] = bias && lane + 32 * i < E ? __ldg(bias + lane + 32 * i) : 0.f;
+  epi_sync();
+  for (int t = warp; t < n; t += kEpiWarps) {
+    float logit[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) logit[i] = 0.f;
+#pragma unroll 4
+    for (int r = 0; r < a.logit_slices; ++r) {
+      float l[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        l[i] = lane + 32 * i < E ? __ldcg(a.logits + (r * n + t) * E + lane + 32 * i) : 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) logit[i] += l[i];
+    }
+    int e;
+    float w;
+    gate_token(a.gate, logit, biases, s.sum[warp], lane, e, w);
+    if (lane < k) {
+      s.pos[t * k + lane] = e;  // the expert, for now
+      s.w[t * k + lane] = w;
+      if (e >= 0) atomicOr(&s.mask[e], 1ull << t);
+      else if (blockIdx.x == 0) record_status(a.status, ST_BAD_EXPERT_INDEX);
+    }
+  }
+  epi_sync();
+  const unsigned long long mask = s.mask[tid];  // thread e: expert e
+  const int m = __popcll(mask);
+  const int v = m ? 1 | (m << 10) | (((m + 7) / 8) << 20) : 0;  // at most 256, 512 and 512 in all
+  int incl = v;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int b = __shfl_up_sync(kFull, incl, o);
+    if (lane >= o) incl += b;
+  }
+  if (lane == 31) s.warp_total[warp] = incl;
+  epi_sync();
+  int before = incl - v;
+  for (int w = 0; w < warp; ++w) before += s.warp_total[w];
+  int* first_row = reinterpret_cast<int*>(&s.sum[0][0]);  // of expert e (the scores are done with)
+  first_row[tid] = (before >> 10) & 1023;
+  unsigned long long* mask_of = reinterpret_cast<unsigned long long*>(&s.sum[2][0]);
+  mask_of[tid] = mask;
+  epi_sync();  // every mask has been read: the list takes their place
+  if (v) {
+    const int j = before & 1023;
+    s.expert[j] = tid;
+    s.start[j] = (before >> 10) & 1023;
+    s.row8[j] = before >> 20;
+    s.mask[j] = mask;
+  }
+  if (tid == kMaxExperts - 1) {
+    const int active = (before + v) & 1023;
+    s.active = active;
+    s.items = (a.Is / 128 + active * (a.I / 128)) * a.s1 +
+              a.H / 256 * (active * a.s2 + (a.Is ? a.s2s : 0) + n);
+  }
+  for (int p = tid; p < n * k; p += kEpiThreads) {
+    const int e = s.pos[p], t = p / k;
+    s.pos[p] = e >= 0 ? first_row[e] + __popcll(mask_of[e] & ((1ull << t) - 1)) : -1;
+  }
+  epi_sync();
 }
 
 // The last slice of a gate/up tile: the slices' sums, SwiGLU and the tile's 128
@@ -698,7 +665,7 @@ __global__ void __launch_bounds__(kThreads, 1) few_ffn_kernel(const FewArgs a) {
   auto bar = [&](int i) { return smem_u32(&s.bar[i]); };
   constexpr int B_FW = 0, B_EW = kFewMaxStages, B_FX = 2 * kFewMaxStages, B_EX = 3 * kFewMaxStages,
                 B_PF = 4 * kFewMaxStages, B_PE = B_PF + kPartials, B_QF = B_PE + kPartials, B_QE = B_QF + kQ,
-                B_DR = B_QE + kQ;
+                B_DR = B_QE + kQ, B_META = B_DR + 1;
   volatile int* abort_flag = &s.abort;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
@@ -719,6 +686,7 @@ __global__ void __launch_bounds__(kThreads, 1) few_ffn_kernel(const FewArgs a) {
         mbar_init(bar(B_QE + i), kQReaders);
       }
       mbar_init(bar(B_DR), 1);
+      mbar_init(bar(B_META), kEpiThreads);
       s.abort = 0;
       fence_barrier_init();
     }
@@ -726,43 +694,22 @@ __global__ void __launch_bounds__(kThreads, 1) few_ffn_kernel(const FewArgs a) {
     tmem_alloc(smem_u32(&s.tmem), kTmemCols);
     tmem_relinquish();
   }
-  // Before the router is done: the weight maps are acquired, and the shared expert's weights, which are needed
-  // whatever it says, are fetched into L2.  (A layer id that is still being written would only acquire and
-  // fetch another layer's.)
+  // the weight maps are acquired while the logits are computed (a layer id that is still being written would
+  // only acquire another layer's)
   const int early = load_layer(a.lref.layer, a.lref.n_layers, a.status, false);
   auto acquire_maps = [&](int l) {
     for (int m = MAP_GATE_UP; m <= (a.Is ? MAP_SH_DOWN : MAP_DOWN); ++m) tensormap_acquire(&a.lref.table[l].map[m]);
   };
-  if ((warp == 0 || warp == 2) && lane == 0) acquire_maps(early);
-  if (warp == 2 && a.Is && lane == 0) {
-    const int kx = FP8 ? 128 : 64;
-    const int gu = a.Is / 128 * (a.H / kx), all = gu + a.H / 256 * (a.Is / kx);
-    for (int b = blockIdx.x; b < min(all, kPrefetchBoxes); b += gridDim.x)
-      prefetch_box(&a.lref.table[early].map[b < gu ? MAP_SH_GATE_UP : MAP_SH_DOWN], (b < gu ? b : b - gu) * 256);
-  }
+  if (warp == 0 && lane == 0) acquire_maps(early);
   pdl_wait();
   int claim = 0;
   if (threadIdx.x == 0) claim = atomicAdd(&a.counters[0], 1);
-  if (threadIdx.x < kMaxExperts) {
-    s.expert[threadIdx.x] = ld_dep(&a.meta->expert[threadIdx.x]);
-    s.start[threadIdx.x] = ld_dep(&a.meta->start[threadIdx.x]);
-    s.row8[threadIdx.x] = ld_dep(&a.meta->row8[threadIdx.x]);
-    s.mask[threadIdx.x] = *reinterpret_cast<const volatile unsigned long long*>(&a.meta->mask[threadIdx.x]);
-  } else if (threadIdx.x == kMaxExperts) {
-    s.active = min(max(ld_dep(&a.meta->active), 0), a.max_active);
-    s.layer = load_layer(a.lref.layer, a.lref.n_layers, a.status, false);
-  }
-  for (int p = threadIdx.x; p < a.n * a.gate.top_k; p += kThreads) {
-    s.pos[p] = ld_dep(&a.meta->pos[p]);
-    s.w[p] = ld_dep(&a.meta->w[p]);
-  }
+  if (threadIdx.x == 32) s.layer = load_layer(a.lref.layer, a.lref.n_layers, a.status, false);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem_base = s.tmem;
   const LayerEntry& le = a.lref.table[s.layer];
-  const int items = (a.Is / 128 + s.active * (a.I / 128)) * a.s1 +
-                    a.H / 256 * (s.active * a.s2 + (a.Is ? a.s2s : 0) + a.n);
   auto give_up = [&]() {
     *abort_flag = 1;
     record_status(a.status, ST_WAIT_TIMEOUT);
@@ -777,6 +724,12 @@ __global__ void __launch_bounds__(kThreads, 1) few_ffn_kernel(const FewArgs a) {
     return true;
   };
 
+  bool routed = false;  // the routing has been waited for
+  auto wait_routing = [&](int item) {
+    if (!routed && item >= a.first_routed) routed = mbar_wait(bar(B_META), 0, abort_flag);
+    return routed || item < a.first_routed;
+  };
+
   if (warp == 0) {
     // -------------------------------------------------------- claims and weights
     if (lane == 0) {
@@ -788,7 +741,9 @@ __global__ void __launch_bounds__(kThreads, 1) few_ffn_kernel(const FewArgs a) {
       if (s.layer != early) acquire_maps(s.layer);
       int next = claim;
       while (ok) {
-        const int item = next < items ? next : -1;
+        ok = wait_routing(next);
+        if (!ok) break;
+        const int item = next < a.first_routed || next < s.items ? next : -1;
         ok = mbar_wait(bar(B_QE + rq.s), rq.phase ^ 1u, abort_flag);
         if (!ok) break;
         s.q[rq.s] = item;
@@ -832,6 +787,7 @@ __global__ void __launch_bounds__(kThreads, 1) few_ffn_kernel(const FewArgs a) {
     if (lane == 0) fence_proxy_async_all();
     while (ok) {
       ok = pop(rq, item);
+      ok = ok && (item < 0 || __all_sync(kFull, wait_routing(item)));
       if (!ok || item < 0) break;
       if (lane == 0) {
         const FewItem T = decode<FP8>(a, s, item);
@@ -873,6 +829,7 @@ __global__ void __launch_bounds__(kThreads, 1) few_ffn_kernel(const FewArgs a) {
     const uint64_t wdesc = smem_desc_sw128(sW), xdesc = smem_desc_sw128(sX);
     while (ok) {
       ok = pop(rq, item);
+      ok = ok && (item < 0 || __all_sync(kFull, wait_routing(item)));
       if (!ok || item < 0) break;
       const FewItem T = decode<FP8>(a, s, item);
       const uint32_t id = FP8 ? (1u << 4) | (static_cast<uint32_t>(T.n >> 3) << 17) | (8u << 24) : idesc_bf16_f32(128, T.n);
@@ -922,6 +879,8 @@ __global__ void __launch_bounds__(kThreads, 1) few_ffn_kernel(const FewArgs a) {
     const int tid = threadIdx.x - 128;
     const uint32_t lanes = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + half * (FP8 ? 64 : 128);
     const int row = half * 128 + q * 32 + lane;  // of the weight tile
+    list_experts(a, s, le.router_bias, warp - 4, lane, tid);
+    mbar_arrive(bar(B_META));
     Ring<kQ> rq;
     Ring<FP8 ? kPartials : kAccs> p;
     int sx = 0, item = -1;
@@ -1086,10 +1045,6 @@ cudaError_t few_set_attributes() {
     if (e == cudaSuccess)
       e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes));
   };
-  set(few_route_kernel<false>, kFewRouteSmem);
-  set(few_route_kernel<true>, kFewRouteSmem);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(few_route_kernel<false>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(few_route_kernel<true>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
   set(few_ffn_kernel<false, 16>, kFewSmem);
   set(few_ffn_kernel<true, 16>, kFewSmem);
   set(few_ffn_kernel<true, 64>, kFewSmem);
@@ -1097,13 +1052,11 @@ cudaError_t few_set_attributes() {
 }
 
 cudaError_t few_launch(const FewArgs& a, bool fp8, int grid, cudaStream_t st) {
-  const int tiles = ceil_div(a.gate.n_experts, 16);
-  const size_t smem =
-      sizeof(float) * (static_cast<size_t>(a.n) * kUnits * 16 +
-                       16 * tiles * (static_cast<size_t>(kRouteWarps / tiles) * a.n + round_up_dev(a.n, kFewCluster)));
+  // (a CTA more for every two tokens than the router has use for, up to a third of the GPU)
+  const int ctas = std::max(ceil_div(a.gate.n_experts, 16) * a.logit_slices, std::min(48, a.n / 2));
   const cudaError_t e =
-      fp8 ? launch_pdl(few_route_kernel<true>, dim3(kFewCluster), dim3(kRouteThreads), smem, st, kFewCluster, a)
-          : launch_pdl(few_route_kernel<false>, dim3(kFewCluster), dim3(kRouteThreads), smem, st, kFewCluster, a);
+      fp8 ? launch_pdl(few_logits_kernel<true>, dim3(ctas), dim3(kLogitThreads), 0, st, 1, a)
+          : launch_pdl(few_logits_kernel<false>, dim3(ctas), dim3(kLogitThreads), 0, st, 1, a);
   if (e != cudaSuccess) return e;
   if (!fp8) return launch_ffn<false, 16>(a, grid, st);
   return a.n <= 16 ? launch_ffn<true, 16>(a, grid, st) : launch_ffn<true, 64>(a, grid, st);
