@@ -129,18 +129,18 @@ Layout layout(const asap_moe_config& c, long long n) {
 
 // ------------------------------------------------------------ few tokens
 // K slices of a tile so that a launch of ``tiles`` tiles has at least
-// kFewItemsPerSm work items per SM (of a GB300: the size of a workspace needs no
+// kFewItems work items (2.5 per SM of a GB300: the size of a workspace needs no
 // GPU), with at least kFewMinSteps k-steps each.
-constexpr int kFewItemsPerSm = 8, kFewSms = 152, kFewMinSteps = 4;
+constexpr int kFewItems = 380, kFewMinSteps = 4;
 int few_slices(long long tiles, int k_steps) {
-  const long long want = (static_cast<long long>(kFewItemsPerSm) * kFewSms + tiles - 1) / tiles;
+  const long long want = (kFewItems + tiles - 1) / tiles;
   return static_cast<int>(std::max<long long>(1, std::min<long long>(want, k_steps / kFewMinSteps)));
 }
 
 // Sizes and workspace offsets of a few-token call of n tokens (1 .. kFewTokens).
 struct FewLayout {
   asap::FewArgs a{};
-  size_t logits, counters, ximg, himg, p1, p1s, y, ys, total;
+  size_t logits, counters, sel_e, sel_w, ximg, himg, p1, p1s, y, ys, total;
 };
 
 FewLayout few_layout(const asap_moe_config& c, int n) {
@@ -165,17 +165,16 @@ FewLayout few_layout(const asap_moe_config& c, int n) {
   a.r_tI = 1.0f / tI;
   a.r_tH = 1.0f / tH;
   a.r_down = 1.0f / (tH * a.s2);
-  // every CTA of the second kernel adds the slices of all logits: fewer where there are many tokens
-  a.logit_slices = n <= 8 ? 8 : 4;
   a.down_tickets = 1 + tS + a.max_active * tI;
   a.h_ready = a.down_tickets + tH;
-  a.n_counters = a.h_ready + 1 + a.max_active;
+  a.gate_claims = a.h_ready + 1 + a.max_active;
+  a.n_counters = a.gate_claims + 2;
   // rings: 32 KB of weights a stage; operand rows (e4m3: and their scales) of the widest k-step, BF16 h rows twice
   const int m8 = asap::round_up_dev(n, 8);
   const int rows = fp8 ? asap::round_up_dev(n, 16) : 2 * m8;
   a.x_slot = asap::round_up_dev(std::max(rows * 128, fp8 ? m8 * 132 : 0), 1024);
   const int room = static_cast<int>(asap::kFewSmem - asap::kFewSmemState);
-  a.stages_w = 6;
+  a.stages_w = 4;
   while ((room - a.stages_w * 32768) / a.x_slot < std::min(a.stages_w, 4)) --a.stages_w;
   a.stages_x = std::min(asap::kFewMaxStages, (room - a.stages_w * 32768) / a.x_slot);
   a.smem = asap::kFewSmemState + static_cast<size_t>(a.stages_w) * 32768 + static_cast<size_t>(a.stages_x) * a.x_slot;
@@ -189,8 +188,10 @@ FewLayout few_layout(const asap_moe_config& c, int n) {
   // groups of 8 rows of the active experts: at most one per row, and the rows over 8 plus one per expert
   const size_t groups = std::min<size_t>(nk, nk / 8 + a.max_active);
   const size_t row = fp8 ? 132 : 128, hrows = fp8 ? 8 : 16;
-  L.logits = take(static_cast<size_t>(a.logit_slices) * n * c.n_experts * 4);
+  L.logits = take(static_cast<size_t>(8) * n * c.n_experts * 4);
   L.counters = take(a.n_counters * sizeof(int));
+  L.sel_e = take(static_cast<size_t>(n) * k * 4);
+  L.sel_w = take(static_cast<size_t>(n) * k * 4);
   L.ximg = take(a.H / step * m8 * row);
   L.himg = take((a.Is / step * (m8 / 8) + a.I / step * groups) * hrows * row);
   L.p1 = take(a.s1 * nk * 2 * a.I * 4);
@@ -1424,6 +1425,8 @@ ASAP_API int asap_moe_layer_few(asap_moe_t h, const int32_t* layer_id, const voi
   a.out = out;
   a.logits = at<float>(ws, L.logits);
   a.counters = at<int>(ws, L.counters);
+  a.sel_e = at<int>(ws, L.sel_e);
+  a.sel_w = at<float>(ws, L.sel_w);
   a.ximg = at<uint8_t>(ws, L.ximg);
   a.himg = at<uint8_t>(ws, L.himg);
   a.p1 = at<float>(ws, L.p1);

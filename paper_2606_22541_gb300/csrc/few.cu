@@ -83,14 +83,25 @@ __device__ __forceinline__ uint32_t ordered(float f) {
   return (u >> 31) ? ~u : u | 0x80000000u;
 }
 
-// Gating of one token by a warp, from its logits (lane l: experts l, l + 32,
-// ...): expert and weight of slot j in lane j (expert -1: none left).  The rules
+// Gating of one token by a warp, from its logits in row (E + n_groups floats,
+// overwritten): expert (-1: none left) and weight of slot j in lane j.  The rules
 // and tie-breaks of gate_kernel (route.cu); a round's winner is found with two
-// warp reductions over the lanes' best.  scratch: E + n_groups floats.
-__device__ __forceinline__ void gate_token(const GateParams& p, const float (&logit)[8], const float (&biases)[8],
-                                           float* scratch, int lane, int& my_e, float& my_w) {
+// warp reductions over the lanes' best.  bias: E selection biases.  Not inlined: a
+// CTA runs it on anything while it waits for the logits, so that the instructions
+// are in the caches when they count (us per token-gating, cold 7, warm 4).
+struct Slot {
+  int e;
+  float w;
+};
+__device__ __noinline__ Slot gate_token(const GateParams& p, float* row, const float* bias, int lane) {
   const int E = p.n_experts;
   const bool grouped = p.gating == 2;
+  float logit[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) logit[i] = lane + 32 * i < E ? row[lane + 32 * i] : 0.f;
+  __syncwarp();
+  float* scratch = row;
+  int my_e = -1;
   float val[8];
   uint32_t key[8];  // 0: may not be chosen
   if (grouped) {
@@ -100,7 +111,7 @@ __device__ __forceinline__ void gate_token(const GateParams& p, const float (&lo
     for (int i = 0; i < 8; ++i) {
       const int e = lane + 32 * i, g = static_cast<int>((e + 0.5f) * per);
       val[i] = gate_sigmoid(logit[i]);
-      const float sel = val[i] + biases[i];
+      const float sel = val[i] + (e < E ? bias[e] : 0.f);
       key[i] = e < E ? ordered(sel) : 0u;
       if (e < E) scratch[e + g] = sel;
     }
@@ -153,7 +164,6 @@ __device__ __forceinline__ void gate_token(const GateParams& p, const float (&lo
       if (key[i] > best) best = key[i], be = lane + 32 * i, bv = val[i];
   };
   take_best();
-  my_e = -1;
   float my_v = 0.f, top = 0.f;  // top: the first slot's value
   for (int j = 0; j < p.top_k; ++j) {
     const uint32_t mx = __reduce_max_sync(kFull, best);
@@ -182,7 +192,7 @@ __device__ __forceinline__ void gate_token(const GateParams& p, const float (&lo
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) den += __shfl_xor_sync(kFull, den, o);
   }
-  my_w = num / den * (grouped ? p.route_scale : 1.0f);
+  return Slot{my_e, num / den * (grouped ? p.route_scale : 1.0f)};
 }
 
 // ------------------------------------------------------------ logits
@@ -231,8 +241,9 @@ __device__ __forceinline__ void write_image(const FewArgs& a, int rows, int thre
 
 constexpr int kLogitWarps = 8;
 constexpr int kLogitThreads = 32 * kLogitWarps;
-constexpr int kUnits = 7;  // K units (32 channels) of a warp on their way at a time
-constexpr int kPrefetchBoxes = 1024;  // of 32 KB, what HBM delivers until the second kernel asks for more
+constexpr int kUnits = 4;    // K units (32 channels) of a warp on their way at a time
+constexpr int kLogitSlices = 8;
+constexpr int kPrefetchBoxes = 1344;  // of 32 KB: 44 MB, what HBM delivers until the routed experts are known
 
 __device__ __forceinline__ void prefetch_box(const CUtensorMap* m, int y) {
   asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global.tile [%0, {%1, %2}];" ::"l"(reinterpret_cast<uint64_t>(m)),
@@ -243,61 +254,74 @@ __device__ __forceinline__ void prefetch_box(const CUtensorMap* m, int y) {
 // CTA (tile, slice): logits of 16 experts (M) over a slice of K for all tokens (8 per MMA, N).  Its warps take
 // every eighth K unit; thread (g, q) feeds 16 bytes of a row to two MMAs, whose K order both operands share.
 // CTAs past the router's help with the rest.
-template <bool FP8>
-__global__ void __launch_bounds__(kLogitThreads) few_logits_kernel(const FewArgs a) {
-  pdl_launch();  // the second kernel may come up and fetch weights meanwhile
-  __shared__ float part[kLogitWarps][kFewTokens][16];
-  pdl_wait();
+// NJ: groups of 8 tokens at most.
+template <bool FP8, int NJ>
+__global__ void __launch_bounds__(kLogitThreads) few_logits_kernel(const __grid_constant__ FewArgs a) {
+  pdl_launch();  // the second kernel may come up meanwhile
+  __shared__ float part[kLogitWarps][8 * NJ][16];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int E = a.gate.n_experts, n = a.n;
-  const int slice = blockIdx.x % a.logit_slices, tile = blockIdx.x / a.logit_slices;
+  const int slice = blockIdx.x % kLogitSlices, tile = blockIdx.x / kLogitSlices;
   const int g = lane >> 2, q = lane & 3;
+  const int V = a.H / 8, units = a.H / 32;
+  const int u0 = units * slice / kLogitSlices, u1 = units * (slice + 1) / kLogitSlices;
+  const int e0 = tile * 16 + g, e1 = e0 + 8;
+  const uint4 zero = make_uint4(0, 0, 0, 0);
+  uint4 w0[kUnits], w1[kUnits];
+  auto load_weights = [&](int layer, int ub) {
+    const uint4* __restrict__ wr = static_cast<const uint4*>(a.lref.table[layer].router_w);
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i) {
+      const int u = ub + kLogitWarps * i, v = 4 * u + q;
+      w0[i] = u < u1 && e0 < E ? __ldg(wr + static_cast<long long>(e0) * V + v) : zero;
+      w1[i] = u < u1 && e1 < E ? __ldg(wr + static_cast<long long>(e1) * V + v) : zero;
+    }
+  };
+  // The first weights are on their way before what the kernels in front write may be read; a layer id that
+  // turns out to have been written since has them loaded again.
+  const int early = load_layer(a.lref.layer, a.lref.n_layers, a.status, false);
+  load_weights(early, u0 + warp);
+  // The shared expert's weights are needed whatever the router says: fetched into L2, behind the router's own.
+  if (threadIdx.x == 0 && a.Is) {
+    const LayerEntry& le = a.lref.table[early];
+    tensormap_acquire(&le.map[MAP_SH_GATE_UP]);
+    tensormap_acquire(&le.map[MAP_SH_DOWN]);
+    constexpr int kx = FP8 ? 128 : 64;
+    const int gu = a.Is / 128 * (a.H / kx), all = gu + a.H / 256 * (a.Is / kx);
+    for (int b = blockIdx.x; b < min(all, kPrefetchBoxes); b += gridDim.x)
+      prefetch_box(&le.map[b < gu ? MAP_SH_GATE_UP : MAP_SH_DOWN], (b < gu ? b : b - gu) * 256);
+  }
+  pdl_wait();
   if (tile * 16 < E) {
     const int layer = load_layer(a.lref.layer, a.lref.n_layers, a.status, blockIdx.x == 0 && threadIdx.x == 0);
-    const uint4* __restrict__ wr = static_cast<const uint4*>(a.lref.table[layer].router_w);
     const uint4* x = static_cast<const uint4*>(a.x);
-    const int V = a.H / 8, units = a.H / 32;
-    const int u0 = units * slice / a.logit_slices, u1 = units * (slice + 1) / a.logit_slices;
-    const int e0 = tile * 16 + g, e1 = e0 + 8;
-    const uint4 zero = make_uint4(0, 0, 0, 0);
-    float c[kFewTokens / 8][4];
+    float c[NJ][4];
 #pragma unroll
-    for (int j = 0; j < kFewTokens / 8; ++j) c[j][0] = c[j][1] = c[j][2] = c[j][3] = 0.f;
+    for (int j = 0; j < NJ; ++j) c[j][0] = c[j][1] = c[j][2] = c[j][3] = 0.f;
     for (int ub = u0 + warp; ub < u1; ub += kLogitWarps * kUnits) {
-      uint4 w0[kUnits], w1[kUnits];
+      if (layer != early || ub != u0 + warp) load_weights(layer, ub);
+      constexpr int kGroups = NJ < 4 ? NJ : 4;  // token groups on their way at a time
 #pragma unroll
-      for (int i = 0; i < kUnits; ++i) {
-        const int u = ub + kLogitWarps * i, v = 4 * u + q;
-        w0[i] = u < u1 && e0 < E ? __ldg(wr + static_cast<long long>(e0) * V + v) : zero;
-        w1[i] = u < u1 && e1 < E ? __ldg(wr + static_cast<long long>(e1) * V + v) : zero;
-      }
-      // The shared expert's gate/up weights are needed whatever the router says: fetched into L2, behind the
-      // router's own.
-      if (threadIdx.x == 0 && ub == u0 && a.Is) {
-        const CUtensorMap* m = &a.lref.table[layer].map[MAP_SH_GATE_UP];
-        tensormap_acquire(m);
-        const int boxes = min(kPrefetchBoxes, a.Is / 128 * (a.H / (FP8 ? 128 : 64)));
-        for (int b = blockIdx.x; b < boxes; b += gridDim.x) prefetch_box(m, b * 256);
-      }
+      for (int j0 = 0; j0 < NJ; j0 += kGroups) {
+        uint4 xv[kGroups][kUnits];
 #pragma unroll
-      for (int j = 0; j < kFewTokens / 8; ++j) {
-        if (8 * j >= n) break;
-        const int t = 8 * j + g;
-        uint4 xv[kUnits];
+        for (int j = 0; j < kGroups; ++j)
 #pragma unroll
-        for (int i = 0; i < kUnits; ++i) {
-          const int u = ub + kLogitWarps * i;
-          xv[i] = u < u1 && t < n ? ld_dep(x + static_cast<long long>(t) * V + 4 * u + q) : zero;
-        }
+          for (int i = 0; i < kUnits; ++i) {
+            const int t = 8 * (j0 + j) + g, u = ub + kLogitWarps * i;
+            xv[j][i] = u < u1 && t < n ? ld_dep(x + static_cast<long long>(t) * V + 4 * u + q) : zero;
+          }
 #pragma unroll
-        for (int i = 0; i < kUnits; ++i) {
-          mma_bf16_16816(c[j], w0[i].x, w1[i].x, w0[i].y, w1[i].y, xv[i].x, xv[i].y);
-          mma_bf16_16816(c[j], w0[i].z, w1[i].z, w0[i].w, w1[i].w, xv[i].z, xv[i].w);
-        }
+        for (int j = 0; j < kGroups; ++j)
+#pragma unroll
+          for (int i = 0; i < kUnits; ++i) {
+            mma_bf16_16816(c[j0 + j], w0[i].x, w1[i].x, w0[i].y, w1[i].y, xv[j][i].x, xv[j][i].y);
+            mma_bf16_16816(c[j0 + j], w0[i].z, w1[i].z, w0[i].w, w1[i].w, xv[j][i].z, xv[j][i].w);
+          }
       }
     }
 #pragma unroll
-    for (int j = 0; j < kFewTokens / 8; ++j)
+    for (int j = 0; j < NJ; ++j)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int t = 8 * j + 2 * q + (i & 1);
@@ -323,9 +347,9 @@ constexpr int kEpiWarps = 8;
 constexpr int kEpiThreads = 32 * kEpiWarps;
 constexpr int kThreads = 32 * (4 + kEpiWarps);
 constexpr int kQ = 6;               // items in flight in a CTA
-constexpr int kQReaders = 2 + kEpiWarps;
+constexpr int kQReaders = 3 + kEpiWarps;
 constexpr uint32_t kTmemCols = 512;
-constexpr int kPartials = 4;        // FP8: TMEM partials of 2 x 64 columns
+constexpr int kMaxPartials = 8;     // FP8: TMEM partials of 2 x NT columns
 constexpr int kAccs = 2;            // BF16: accumulators of 2 x 128 columns
 
 struct FewItem {
@@ -344,12 +368,10 @@ struct FewItem {
 };
 
 struct FewSmem {  // behind the rings
-  alignas(16) uint64_t bar[2 * kFewMaxStages + 2 * kFewMaxStages + 2 * kPartials + 2 * kQ + 2];
+  alignas(16) uint64_t bar[2 * kFewMaxStages + 2 * kFewMaxStages + 2 * kMaxPartials + 3 * kQ + 2];
   int q[kQ];
   uint32_t tmem;
   int abort;
-  int layer;
-  int last;
   int active;
   int items;
   int warp_total[kEpiWarps];
@@ -357,6 +379,7 @@ struct FewSmem {  // behind the rings
   unsigned long long mask[kMaxExperts];
   int pos[kFewTokens * kMaxTopK];
   float w[kFewTokens * kMaxTopK];
+  float bias[kMaxExperts];  // of the router's selection
   alignas(16) float sum[kEpiWarps][288];  // combine (accessed as float4); gating: selection scores and ranks
 };
 static_assert(sizeof(FewSmem) <= kFewSmemState, "shared memory budget");
@@ -484,39 +507,64 @@ __device__ __forceinline__ bool epi_all(bool ok) {
   return r != 0;
 }
 
-// The routing of the call, by the epilogue warps of every CTA for themselves:
-// active experts in increasing order, their tokens, first rows and row groups,
-// the row and weight of every slot, and the number of work items.
-__device__ __forceinline__ void list_experts(const FewArgs& a, FewSmem& s, const float* bias, int warp, int lane, int tid) {
-  const int E = a.gate.n_experts, k = a.gate.top_k, n = a.n;
-  s.mask[tid] = 0ull;
-  float biases[8];
+// Gating of token t by a warp from the planes of its logits; row: E + n_groups floats.
+__device__ __forceinline__ Slot gate_logits(const FewArgs& a, const float* bias, float* row, int t, int lane) {
+  const int E = a.gate.n_experts;
+  float l[kLogitSlices][8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) biases[i] = bias && lane + 32 * i < E ? __ldg(bias + lane + 32 * i) : 0.f;
-  epi_sync();
-  for (int t = warp; t < n; t += kEpiWarps) {
-    float logit[8];
+  for (int r = 0; r < kLogitSlices; ++r)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) logit[i] = 0.f;
-#pragma unroll 4
-    for (int r = 0; r < a.logit_slices; ++r) {
-      float l[8];
+    for (int i = 0; i < 8; ++i)
+      l[r][i] = lane + 32 * i < E ? __ldcg(a.logits + (r * a.n + t) * E + lane + 32 * i) : 0.f;
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        l[i] = lane + 32 * i < E ? __ldcg(a.logits + (r * n + t) * E + lane + 32 * i) : 0.f;
+  for (int i = 0; i < 8; ++i) {
+    float sum = l[0][i];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) logit[i] += l[i];
-    }
-    int e;
-    float w;
-    gate_token(a.gate, logit, biases, s.sum[warp], lane, e, w);
-    if (lane < k) {
-      s.pos[t * k + lane] = e;  // the expert, for now
-      s.w[t * k + lane] = w;
-      if (e >= 0) atomicOr(&s.mask[e], 1ull << t);
-      else if (blockIdx.x == 0) record_status(a.status, ST_BAD_EXPERT_INDEX);
-    }
+    for (int r = 1; r < kLogitSlices; ++r) sum += l[r][i];
+    if (lane + 32 * i < E) row[lane + 32 * i] = sum;
   }
+  __syncwarp();
+  const Slot slot = gate_token(a.gate, row, bias, lane);
+  if (lane < a.gate.top_k && slot.e < 0) record_status(a.status, ST_BAD_EXPERT_INDEX);
+  return slot;
+}
+
+// The routing of the call in every CTA, by its epilogue warps: active experts in
+// increasing order, their tokens, first rows and row groups, the row and weight
+// of every slot, and the number of work items.  Up to kOwnGate tokens every CTA
+// gates all of them, one warp each (a warp takes about 4 us); more are gated
+// once, claimed one by one, and read by every CTA when all are done.
+constexpr int kOwnGate = kEpiWarps;
+__device__ __forceinline__ bool list_experts(const FewArgs& a, FewSmem& s, int warp, int lane, int tid,
+                                             volatile int* abort_flag) {
+  const int k = a.gate.top_k, n = a.n;
+  s.mask[tid] = 0ull;
+  if (n <= kOwnGate) {
+    if (warp < n) {
+      const Slot slot = gate_logits(a, s.bias, s.sum[warp], warp, lane);
+      if (lane < k) s.pos[warp * k + lane] = slot.e, s.w[warp * k + lane] = slot.w;  // (pos: the expert, for now)
+    }
+    epi_sync();
+  } else {
+    int* claims = a.counters + a.gate_claims;
+    if (warp == 0) {
+      while (true) {
+        int t = 0;
+        if (lane == 0) t = atomicAdd(claims, 1);
+        t = __shfl_sync(kFull, t, 0);
+        if (t >= n) break;
+        const Slot slot = gate_logits(a, s.bias, s.sum[0], t, lane);
+        if (lane < k) a.sel_e[t * k + lane] = slot.e, a.sel_w[t * k + lane] = slot.w;
+        __syncwarp();
+        if (lane == 0) arrive_release(claims + 1);
+      }
+    }
+    if (!epi_all(tid != 0 || bounded_wait([&]() { return ld_acquire(claims + 1) >= n; }, abort_flag))) return false;
+    for (int p = tid; p < n * k; p += kEpiThreads) s.pos[p] = __ldcg(a.sel_e + p), s.w[p] = __ldcg(a.sel_w + p);
+    epi_sync();
+  }
+  for (int p = tid; p < n * k; p += kEpiThreads)
+    if (s.pos[p] >= 0) atomicOr(&s.mask[s.pos[p]], 1ull << (p / k));
   epi_sync();
   const unsigned long long mask = s.mask[tid];  // thread e: expert e
   const int m = __popcll(mask);
@@ -550,52 +598,68 @@ __device__ __forceinline__ void list_experts(const FewArgs& a, FewSmem& s, const
               a.H / 256 * (active * a.s2 + (a.Is ? a.s2s : 0) + n);
   }
   for (int p = tid; p < n * k; p += kEpiThreads) {
-    const int e = s.pos[p], t = p / k;
-    s.pos[p] = e >= 0 ? first_row[e] + __popcll(mask_of[e] & ((1ull << t) - 1)) : -1;
+    const int ex = s.pos[p], t = p / k;
+    s.pos[p] = ex >= 0 ? first_row[ex] + __popcll(mask_of[ex] & ((1ull << t) - 1)) : -1;
   }
   epi_sync();
+  return true;
 }
 
 // The last slice of a gate/up tile: the slices' sums, SwiGLU and the tile's 128
-// channels of h into the expert's image.  Warp w takes tokens w, w + 8, ...; lane l
-// channels 4l .. 4l + 3.
+// channels of h into the expert's image, by a warp; lane l has channels 4l ..
+// 4l + 3 and kAhead tokens on their way.
 template <bool FP8>
-__device__ __forceinline__ void write_h(const FewArgs& a, const FewSmem& s, const FewItem& T, int warp, int lane) {
+__device__ __forceinline__ void write_h(const FewArgs& a, const FewSmem& s, const FewItem& T, int lane) {
+  constexpr int kAhead = 4;
   const int W = 2 * (T.shared ? a.Is : a.I);
   const long long plane = static_cast<long long>(T.shared ? a.n : a.n * a.gate.top_k) * W;
-  const float* p = (T.shared ? a.p1s : a.p1) + T.tile * 256;
   // packed rows: gate and up alternate in eights (bf16) or by 128
   const int grow = FP8 ? 4 * lane : 16 * (lane >> 1) + 4 * (lane & 1);
   constexpr int up = FP8 ? 128 : 8;
+  const float* src = (T.shared ? a.p1s : a.p1) + static_cast<long long>(T.start) * W + T.tile * 256 + grow;
   uint8_t* img = h_image<FP8>(a, s, T);
   const int m8 = round_up_dev(T.tokens, 8);
-  for (int c = warp; c < T.tokens; c += kEpiWarps) {
-    const float* src = p + static_cast<long long>(T.start + c) * W + grow;
-    float4 g = make_float4(0.f, 0.f, 0.f, 0.f), u = g;
-    for (int i = 0; i < a.s1; ++i) {
-      const float4 gi = __ldcg(reinterpret_cast<const float4*>(src + i * plane));
-      const float4 ui = __ldcg(reinterpret_cast<const float4*>(src + i * plane + up));
-      g.x += gi.x, g.y += gi.y, g.z += gi.z, g.w += gi.w;
-      u.x += ui.x, u.y += ui.y, u.z += ui.z, u.w += ui.w;
-    }
-    float h[4] = {g.x / (1.0f + expf(-g.x)) * u.x, g.y / (1.0f + expf(-g.y)) * u.y,
-                  g.z / (1.0f + expf(-g.z)) * u.z, g.w / (1.0f + expf(-g.w)) * u.w};
-    if constexpr (FP8) {
-      float am = fmaxf(fmaxf(fabsf(h[0]), fabsf(h[1])), fmaxf(fabsf(h[2]), fabsf(h[3])));
+  for (int c0 = 0; c0 < T.tokens; c0 += kAhead) {
+    float4 g[kAhead], u[kAhead];
 #pragma unroll
-      for (int o = 16; o > 0; o >>= 1) am = fmaxf(am, __shfl_xor_sync(kFull, am, o));
-      const float sc = group_scale(am), inv = 1.0f / sc;
-      uint8_t* step = img + static_cast<long long>(T.tile) * step_bytes<true>(m8);
-      *reinterpret_cast<uint32_t*>(step + swizzled(c, 4 * lane)) =
-          e4m3x4(quotient(h[0], sc, inv), quotient(h[1], sc, inv), quotient(h[2], sc, inv), quotient(h[3], sc, inv));
-      if (lane == 0) *reinterpret_cast<float*>(step + m8 * 128 + c * 4) = sc;
-    } else {
-      uint8_t* step = img + static_cast<long long>(2 * T.tile + (lane >> 4)) * step_bytes<false>(2 * m8);
-      const uint32_t a0 = pack_bf16x2(h[0], h[1]), a1 = pack_bf16x2(h[2], h[3]);
-      const uint32_t b0 = pack_bf16x2(h[0] - bf16_lo(a0), h[1] - bf16_hi(a0));
-      const uint32_t b1 = pack_bf16x2(h[2] - bf16_lo(a1), h[3] - bf16_hi(a1));
-      *reinterpret_cast<uint2*>(step + swizzled(c, 8 * (lane & 15))) = make_uint2(a0, a1);
-      *reinterpret_cast<uint2*>(step + swizzled(m8 + c, 8 * (lane & 15))) = make_uint2(b0, b1);
+    for (int r = 0; r < kAhead; ++r) g[r] = u[r] = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int i = 0; i < a.s1; ++i) {
+      float4 gi[kAhead], ui[kAhead];
+#pragma unroll
+      for (int r = 0; r < kAhead; ++r) {
+        const float* at = src + i * plane + static_cast<long long>(min(c0 + r, T.tokens - 1)) * W;
+        gi[r] = __ldcg(reinterpret_cast<const float4*>(at));
+        ui[r] = __ldcg(reinterpret_cast<const float4*>(at + up));
+      }
+#pragma unroll
+      for (int r = 0; r < kAhead; ++r) {
+        g[r].x += gi[r].x, g[r].y += gi[r].y, g[r].z += gi[r].z, g[r].w += gi[r].w;
+        u[r].x += ui[r].x, u[r].y += ui[r].y, u[r].z += ui[r].z, u[r].w += ui[r].w;
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < kAhead; ++r) {
+      const int c = c0 + r;
+      if (c >= T.tokens) break;
+      const float h[4] = {g[r].x / (1.0f + expf(-g[r].x)) * u[r].x, g[r].y / (1.0f + expf(-g[r].y)) * u[r].y,
+                          g[r].z / (1.0f + expf(-g[r].z)) * u[r].z, g[r].w / (1.0f + expf(-g[r].w)) * u[r].w};
+      if constexpr (FP8) {
+        float am = fmaxf(fmaxf(fabsf(h[0]), fabsf(h[1])), fmaxf(fabsf(h[2]), fabsf(h[3])));
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) am = fmaxf(am, __shfl_xor_sync(kFull, am, o));
+        const float sc = group_scale(am), inv = 1.0f / sc;
+        uint8_t* step = img + static_cast<long long>(T.tile) * step_bytes<true>(m8);
+        *reinterpret_cast<uint32_t*>(step + swizzled(c, 4 * lane)) =
+            e4m3x4(quotient(h[0], sc, inv), quotient(h[1], sc, inv), quotient(h[2], sc, inv), quotient(h[3], sc, inv));
+        if (lane == 0) *reinterpret_cast<float*>(step + m8 * 128 + c * 4) = sc;
+      } else {
+        uint8_t* step = img + static_cast<long long>(2 * T.tile + (lane >> 4)) * step_bytes<false>(2 * m8);
+        const uint32_t a0 = pack_bf16x2(h[0], h[1]), a1 = pack_bf16x2(h[2], h[3]);
+        const uint32_t b0 = pack_bf16x2(h[0] - bf16_lo(a0), h[1] - bf16_hi(a0));
+        const uint32_t b1 = pack_bf16x2(h[2] - bf16_lo(a1), h[3] - bf16_hi(a1));
+        *reinterpret_cast<uint2*>(step + swizzled(c, 8 * (lane & 15))) = make_uint2(a0, a1);
+        *reinterpret_cast<uint2*>(step + swizzled(m8 + c, 8 * (lane & 15))) = make_uint2(b0, b1);
+      }
     }
   }
 }
@@ -650,8 +714,9 @@ __device__ __forceinline__ void write_out(const FewArgs& a, FewSmem& s, const Fe
 }
 
 // NT: columns (tokens) the FP8 epilogue keeps in registers; unused for BF16.
+// (Bounded to 512 threads' registers where that suffices: the next call's logits kernel then fits beside it.)
 template <bool FP8, int NT>
-__global__ void __launch_bounds__(kThreads, 1) few_ffn_kernel(const FewArgs a) {
+__global__ void __launch_bounds__(FP8 && NT == 64 ? kThreads : 512, 1) few_ffn_kernel(const __grid_constant__ FewArgs a) {
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   const uint32_t base = smem_u32(smem_raw);
   if (base & 1023u) {  // uniform for the CTA: nothing is initialised yet
@@ -664,8 +729,11 @@ __global__ void __launch_bounds__(kThreads, 1) few_ffn_kernel(const FewArgs a) {
   FewSmem& s = *reinterpret_cast<FewSmem*>(smem_raw + SW * kWBytes + SX * a.x_slot);
   auto bar = [&](int i) { return smem_u32(&s.bar[i]); };
   constexpr int B_FW = 0, B_EW = kFewMaxStages, B_FX = 2 * kFewMaxStages, B_EX = 3 * kFewMaxStages,
-                B_PF = 4 * kFewMaxStages, B_PE = B_PF + kPartials, B_QF = B_PE + kPartials, B_QE = B_QF + kQ,
-                B_DR = B_QE + kQ, B_META = B_DR + 1;
+                B_PF = 4 * kFewMaxStages, B_PE = B_PF + kMaxPartials, B_QF = B_PE + kMaxPartials, B_QE = B_QF + kQ,
+                B_QD = B_QE + kQ, B_DR = B_QD + kQ, B_META = B_DR + 1;
+  constexpr int kPartials = FP8 ? (NT == 16 ? 8 : 4) : kAccs;
+  constexpr int kHalf = FP8 ? NT : 128;  // columns of a row half
+  static_assert(2 * kHalf * kPartials <= kTmemCols, "tensor memory budget");
   volatile int* abort_flag = &s.abort;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
@@ -677,13 +745,14 @@ __global__ void __launch_bounds__(kThreads, 1) few_ffn_kernel(const FewArgs a) {
         mbar_init(bar(B_FX + i), 1);
         mbar_init(bar(B_EX + i), FP8 ? 1 + kEpiWarps : 1);  // FP8: the epilogue reads its scales
       }
-      for (int i = 0; i < kPartials; ++i) {
+      for (int i = 0; i < kMaxPartials; ++i) {
         mbar_init(bar(B_PF + i), 1);
         mbar_init(bar(B_PE + i), kEpiWarps);
       }
       for (int i = 0; i < kQ; ++i) {
         mbar_init(bar(B_QF + i), 1);
         mbar_init(bar(B_QE + i), kQReaders);
+        mbar_init(bar(B_QD + i), kEpiWarps);
       }
       mbar_init(bar(B_DR), 1);
       mbar_init(bar(B_META), kEpiThreads);
@@ -700,16 +769,24 @@ __global__ void __launch_bounds__(kThreads, 1) few_ffn_kernel(const FewArgs a) {
   auto acquire_maps = [&](int l) {
     for (int m = MAP_GATE_UP; m <= (a.Is ? MAP_SH_DOWN : MAP_DOWN); ++m) tensormap_acquire(&a.lref.table[l].map[m]);
   };
+  auto load_bias = [&](int l) {
+    const float* bias = a.lref.table[l].router_bias;
+    if (bias && threadIdx.x < a.gate.n_experts) s.bias[threadIdx.x] = __ldg(bias + threadIdx.x);
+    else if (threadIdx.x < kMaxExperts) s.bias[threadIdx.x] = 0.f;
+  };
   if (warp == 0 && lane == 0) acquire_maps(early);
+  load_bias(early);
+  if (warp >= 4) gate_token(a.gate, s.sum[warp - 4], s.bias, lane);  // (see there: the result is not used)
   pdl_wait();
   int claim = 0;
   if (threadIdx.x == 0) claim = atomicAdd(&a.counters[0], 1);
-  if (threadIdx.x == 32) s.layer = load_layer(a.lref.layer, a.lref.n_layers, a.status, false);
+  const int layer = load_layer(a.lref.layer, a.lref.n_layers, a.status, false);
+  if (layer != early) load_bias(layer);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem_base = s.tmem;
-  const LayerEntry& le = a.lref.table[s.layer];
+  const LayerEntry& le = a.lref.table[layer];
   auto give_up = [&]() {
     *abort_flag = 1;
     record_status(a.status, ST_WAIT_TIMEOUT);
@@ -738,7 +815,7 @@ __global__ void __launch_bounds__(kThreads, 1) few_ffn_kernel(const FewArgs a) {
       uint32_t ph = 0;
       Ring<kQ> rq;
       const uint64_t pol = l2_policy(1);
-      if (s.layer != early) acquire_maps(s.layer);
+      if (layer != early) acquire_maps(layer);
       int next = claim;
       while (ok) {
         ok = wait_routing(next);
@@ -822,7 +899,7 @@ __global__ void __launch_bounds__(kThreads, 1) few_ffn_kernel(const FewArgs a) {
     // -------------------------------------------------------- MMA
     const bool issuer = elect_one();
     Ring<kQ> rq;
-    Ring<FP8 ? kPartials : kAccs> p;
+    Ring<kPartials> p;
     int sw = 0, sx = 0, item;
     uint32_t pw = 0, px = 0;
     bool ok = true, issued = false;
@@ -844,7 +921,7 @@ __global__ void __launch_bounds__(kThreads, 1) few_ffn_kernel(const FewArgs a) {
           const uint64_t xd = xdesc + static_cast<uint32_t>(sx * (a.x_slot >> 4));
 #pragma unroll
           for (int half = 0; half < 2; ++half) {
-            const uint32_t d = tmem_base + p.s * (FP8 ? 128 : 256) + half * (FP8 ? 64 : 128);
+            const uint32_t d = tmem_base + (2 * p.s + half) * kHalf;
 #pragma unroll
             for (int kk = 0; kk < 4; ++kk) {
               const uint64_t w = wd + half * (16384 >> 4) + 2 * kk, x = xd + 2 * kk;
@@ -872,17 +949,55 @@ __global__ void __launch_bounds__(kThreads, 1) few_ffn_kernel(const FewArgs a) {
         mbar_wait(bar(B_DR), 0, &dummy);
       }
     }
-  } else if (warp >= 4) {
+  } else if (warp == 3) {
+    // -------------------------------------------------------- finisher
+    // An item whose partial sums are stored is counted; the arrival that completes a gate/up tile makes its h.
+    // (A warp of its own: under the weight stream a release and the counter's answer take microseconds.)
+    Ring<kQ> rq;
+    bool ok = true;
+    while (ok) {
+      ok = __all_sync(kFull, mbar_wait(bar(B_QF + rq.s), rq.phase, abort_flag));
+      if (!ok) break;
+      const int item = *reinterpret_cast<volatile int*>(&s.q[rq.s]);
+      if (item < 0) break;
+      ok = __all_sync(kFull, wait_routing(item));
+      if (!ok) break;
+      const FewItem T = decode<FP8>(a, s, item);
+      // (an output's place is left as it is: the epilogue does not arrive there, so its phase is made up for)
+      if (T.combine) {
+        if (lane < kEpiWarps) mbar_arrive(bar(B_QD + rq.s));
+      } else {
+        ok = __all_sync(kFull, mbar_wait(bar(B_QD + rq.s), rq.phase, abort_flag));
+        if (!ok) break;
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(B_QE + rq.s));
+      rq.advance();
+      if (T.combine) continue;
+      if (T.down) {
+        if (lane == 0) arrive_release(a.counters + T.ticket);
+        continue;
+      }
+      int last = 0;
+      if (lane == 0) last = arrive_acq_rel(a.counters + T.ticket) == T.arrivals - 1;
+      if (!__shfl_sync(kFull, last, 0)) continue;
+      write_h<FP8>(a, s, T, lane);
+      fence_proxy_async_all();
+      __syncwarp();
+      if (lane == 0) arrive_release(a.counters + a.h_ready + (T.shared ? 0 : 1 + T.j));
+    }
+    if (!ok && lane == 0) give_up();
+  } else {
     // -------------------------------------------------------- epilogue
     // warp w: TMEM lanes 32 (w % 4) .. of row half (w - 4) / 4
     const int q = warp & 3, half = (warp - 4) >> 2;
     const int tid = threadIdx.x - 128;
-    const uint32_t lanes = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + half * (FP8 ? 64 : 128);
+    const uint32_t lanes = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + half * kHalf;
     const int row = half * 128 + q * 32 + lane;  // of the weight tile
-    list_experts(a, s, le.router_bias, warp - 4, lane, tid);
-    mbar_arrive(bar(B_META));
+    bool ok = list_experts(a, s, warp - 4, lane, tid, abort_flag);
+    if (ok) mbar_arrive(bar(B_META));
     Ring<kQ> rq;
-    Ring<FP8 ? kPartials : kAccs> p;
+    Ring<kPartials> p;
     int sx = 0, item = -1;
     uint32_t px = 0;
     FewItem T{};
@@ -893,7 +1008,9 @@ __global__ void __launch_bounds__(kThreads, 1) few_ffn_kernel(const FewArgs a) {
     auto load_scales = [&](int kb) {
       if (kb + lane < T.kb1) scales = __ldg(bs_lo + kb + lane);
     };
+    int at = 0;  // the item's place in the queue
     auto next_item = [&]() {
+      at = rq.s;
       if (!pop(rq, item)) return false;
       if (item < 0) return true;
       T = decode<FP8>(a, s, item);
@@ -906,7 +1023,7 @@ __global__ void __launch_bounds__(kThreads, 1) few_ffn_kernel(const FewArgs a) {
       }
       return true;
     };
-    bool ok = next_item();
+    ok = ok && next_item();
     while (true) {
       const bool work = ok && item >= 0;
       // the item's sums of this thread's row go to plane ``slice`` of the workspace, row start + c for the
@@ -928,9 +1045,9 @@ __global__ void __launch_bounds__(kThreads, 1) few_ffn_kernel(const FewArgs a) {
         for (int ch = 0; ch < NT / 16; ++ch)
           live |= (T.down ? 16 * ch < T.tokens : ((T.mask >> (16 * ch)) & 0xffffull) != 0) ? 1u << ch : 0u;
         for (int kb = T.kb0; kb < T.kb1; ++kb) {
-          const int at = (kb - T.kb0) & 31;
-          if (at == 0 && kb > T.kb0) load_scales(kb);
-          const float ws = __shfl_sync(kFull, scales, at);
+          const int l = (kb - T.kb0) & 31;
+          if (l == 0 && kb > T.kb0) load_scales(kb);
+          const float ws = __shfl_sync(kFull, scales, l);
           ok = __all_sync(kFull, mbar_wait(bar(B_FX + sx), px, abort_flag) &&
                                      mbar_wait(bar(B_PF + p.s), p.phase, abort_flag));
           if (!ok) break;
@@ -940,7 +1057,7 @@ __global__ void __launch_bounds__(kThreads, 1) few_ffn_kernel(const FewArgs a) {
           for (int ch = 0; ch < NT / 16; ++ch) {
             if ((live >> ch) & 1u) {
               uint32_t v[16];
-              tmem_ld16(lanes + p.s * 128 + 16 * ch, v);
+              tmem_ld16(lanes + p.s * 2 * kHalf + 16 * ch, v);
               tmem_ld_wait();
 #pragma unroll
               for (int i = 0; i < 4; ++i) {
@@ -971,7 +1088,7 @@ __global__ void __launch_bounds__(kThreads, 1) few_ffn_kernel(const FewArgs a) {
         ok = __all_sync(kFull, mbar_wait(bar(B_PF + p.s), p.phase, abort_flag));
         if (ok) {
           tc_fence_after();
-          const uint32_t t0 = lanes + p.s * 256;
+          const uint32_t t0 = lanes + p.s * 2 * kHalf;
           const int cols = T.down ? T.rows / 2 : T.rows;  // down: the columns of the roundings follow
           int c = 0;
           for (int c0 = 0; c0 < cols; c0 += 8) {
@@ -993,32 +1110,21 @@ __global__ void __launch_bounds__(kThreads, 1) few_ffn_kernel(const FewArgs a) {
           p.advance();
         }
       }
-      // the warps share barriers: all go on or none does, and each passes this one before it leaves
+      if (work && ok && !T.combine) {  // the finisher takes it from here
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(B_QD + at));
+        ok = next_item();
+        continue;
+      }
+      // An output, the end or a failure.  The outputs' barriers are shared: all warps go on or none does, and
+      // each passes this one before it leaves.
       if (!epi_all(ok)) {
         ok = false;
         break;
       }
       if (item < 0) break;
-      if (T.combine) {
-        write_out(a, s, T, warp - 4, lane, tid);
-        ok = next_item();
-      } else if (T.down) {
-        if (tid == 0) arrive_release(a.counters + T.ticket);
-        ok = next_item();
-      } else {
-        const FewItem D = T;
-        int before = 0;
-        if (tid == 0) before = arrive_acq_rel(a.counters + D.ticket);
-        ok = next_item();
-        if (tid == 0) s.last = before == D.arrivals - 1;
-        epi_sync();
-        if (*reinterpret_cast<volatile int*>(&s.last)) {  // (written again only after the next epi_all)
-          write_h<FP8>(a, s, D, warp - 4, lane);
-          fence_proxy_async_all();
-          epi_sync();
-          if (tid == 0) arrive_release(a.counters + a.h_ready + (D.shared ? 0 : 1 + D.j));
-        }
-      }
+      write_out(a, s, T, warp - 4, lane, tid);
+      ok = next_item();
     }
     if (!ok && lane == 0) give_up();
   }
@@ -1053,10 +1159,15 @@ cudaError_t few_set_attributes() {
 
 cudaError_t few_launch(const FewArgs& a, bool fp8, int grid, cudaStream_t st) {
   // (a CTA more for every two tokens than the router has use for, up to a third of the GPU)
-  const int ctas = std::max(ceil_div(a.gate.n_experts, 16) * a.logit_slices, std::min(48, a.n / 2));
-  const cudaError_t e =
-      fp8 ? launch_pdl(few_logits_kernel<true>, dim3(ctas), dim3(kLogitThreads), 0, st, 1, a)
-          : launch_pdl(few_logits_kernel<false>, dim3(ctas), dim3(kLogitThreads), 0, st, 1, a);
+  const int ctas = std::max(ceil_div(a.gate.n_experts, 16) * kLogitSlices, std::min(48, a.n / 2));
+  const dim3 grid_l(ctas), block_l(kLogitThreads);
+  cudaError_t e;
+  if (a.n <= 8)
+    e = fp8 ? launch_pdl(few_logits_kernel<true, 1>, grid_l, block_l, 0, st, 1, a)
+            : launch_pdl(few_logits_kernel<false, 1>, grid_l, block_l, 0, st, 1, a);
+  else
+    e = fp8 ? launch_pdl(few_logits_kernel<true, kFewTokens / 8>, grid_l, block_l, 0, st, 1, a)
+            : launch_pdl(few_logits_kernel<false, kFewTokens / 8>, grid_l, block_l, 0, st, 1, a);
   if (e != cudaSuccess) return e;
   if (!fp8) return launch_ffn<false, 16>(a, grid, st);
   return a.n <= 16 ? launch_ffn<true, 16>(a, grid, st) : launch_ffn<true, 64>(a, grid, st);
