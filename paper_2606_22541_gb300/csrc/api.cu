@@ -1420,6 +1420,7 @@ ASAP_API int asap_moe_layer_few(asap_moe_t h, const int32_t* layer_id, const voi
   asap::FewArgs a = L.a;
   a.gate = gate_params(h, layer_id ? layer_id : h->layer_ids);
   a.lref = a.gate.lref;
+  a.fixed_layer = layer_id == nullptr;
   a.status = h->status;
   a.x = x;
   a.out = out;

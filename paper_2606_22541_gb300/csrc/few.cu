@@ -17,8 +17,8 @@
 // a slice of K.  The weights are the M operand of the MMA and all tokens the N
 // operand, so a tile costs the same whatever its rows; the tensor core is idle
 // most of the time.  The shared expert, which every token meets, comes first:
-// while its weights stream, every CTA gates all tokens for itself (one warp per
-// token) and lists the active experts, each with the set of its tokens as a
+// while its weights stream, every CTA learns the routing (it gates a few tokens
+// for itself, one thread per expert) and lists the active experts, each with the set of its tokens as a
 // 64-bit mask, so that a row's place in its expert is a popcount.
 //  - gate/up: the partial sums of a K slice go to the workspace in fp32; the
 //    last slice of a tile to arrive adds them in slice order, applies SwiGLU
@@ -76,124 +76,16 @@ __device__ __forceinline__ uint32_t e4m3x4(float a, float b, float c, float d) {
   return static_cast<uint32_t>(lo) | (static_cast<uint32_t>(hi) << 16);
 }
 
-// ------------------------------------------------------------ gating
+// u / d for 0 <= u < 2^21 from r = 1 / d rounded to fp32 (u + 1/2 is at least 1/(2 d) from a multiple of d, in
+// units of d, and the product's error is below 2^-23 u / d).
+__device__ __forceinline__ int quick_div(int u, float r) { return static_cast<int>((u + 0.5f) * r); }
+
 // Float as an unsigned that orders the same way (-0 as +0).
 __device__ __forceinline__ uint32_t ordered(float f) {
   const uint32_t u = __float_as_uint(f + 0.0f);
   return (u >> 31) ? ~u : u | 0x80000000u;
 }
-
-// Gating of one token by a warp, from its logits in row (E + n_groups floats,
-// overwritten): expert (-1: none left) and weight of slot j in lane j.  The rules
-// and tie-breaks of gate_kernel (route.cu); a round's winner is found with two
-// warp reductions over the lanes' best.  bias: E selection biases.  Not inlined: a
-// CTA runs it on anything while it waits for the logits, so that the instructions
-// are in the caches when they count (us per token-gating, cold 7, warm 4).
-struct Slot {
-  int e;
-  float w;
-};
-__device__ __noinline__ Slot gate_token(const GateParams& p, float* row, const float* bias, int lane) {
-  const int E = p.n_experts;
-  const bool grouped = p.gating == 2;
-  float logit[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) logit[i] = lane + 32 * i < E ? row[lane + 32 * i] : 0.f;
-  __syncwarp();
-  float* scratch = row;
-  int my_e = -1;
-  float val[8];
-  uint32_t key[8];  // 0: may not be chosen
-  if (grouped) {
-    const int gsz = E / p.n_groups;
-    const float per = 1.0f / static_cast<float>(gsz);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int e = lane + 32 * i, g = static_cast<int>((e + 0.5f) * per);
-      val[i] = gate_sigmoid(logit[i]);
-      const float sel = val[i] + (e < E ? bias[e] : 0.f);
-      key[i] = e < E ? ordered(sel) : 0u;
-      if (e < E) scratch[e + g] = sel;
-    }
-    __syncwarp();
-    // a team of lanes (the largest power of two that gives every group one) finds a group's two best
-    int log_team = 0;
-    while ((2 << log_team) * p.n_groups <= 32) ++log_team;
-    const int team = 1 << log_team, grp = lane >> log_team;
-    float m1 = -CUDART_INF_F, m2 = -CUDART_INF_F;
-    if (grp < p.n_groups)
-#pragma unroll 4
-      for (int j = lane & (team - 1); j < gsz; j += team) {
-        const float v = scratch[grp * (gsz + 1) + j];
-        m2 = fmaxf(m2, fminf(m1, v));
-        m1 = fmaxf(m1, v);
-      }
-    for (int o = 1; o < team; o *= 2) {
-      const float o1 = __shfl_xor_sync(kFull, m1, o), o2 = __shfl_xor_sync(kFull, m2, o);
-      m2 = fmaxf(fmaxf(m2, o2), fminf(m1, o1));
-      m1 = fmaxf(m1, o1);
-    }
-    const float score = __shfl_sync(kFull, m1 + m2, min(lane << log_team, 31));  // lane g: group g's
-    int rank = 0;  // groups in front of this lane's
-#pragma unroll 4
-    for (int g = 0; g < p.n_groups; ++g) {
-      const float o = __shfl_sync(kFull, score, g);
-      rank += (o > score || (o == score && g < lane)) ? 1 : 0;
-    }
-    const uint32_t kept = __ballot_sync(kFull, lane < p.n_groups && rank < p.topk_groups);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int g = static_cast<int>((lane + 32 * i + 0.5f) * per);
-      if (!((kept >> (g & 31)) & 1u)) key[i] = 0u;
-    }
-    __syncwarp();
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      val[i] = logit[i];
-      key[i] = lane + 32 * i < E ? ordered(logit[i]) : 0u;
-    }
-  }
-  uint32_t best = 0;  // the lane's best, of equal ones the first
-  int be = 0x7fffffff;
-  float bv = 0.f;
-  auto take_best = [&]() {
-    best = 0, be = 0x7fffffff;
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (key[i] > best) best = key[i], be = lane + 32 * i, bv = val[i];
-  };
-  take_best();
-  float my_v = 0.f, top = 0.f;  // top: the first slot's value
-  for (int j = 0; j < p.top_k; ++j) {
-    const uint32_t mx = __reduce_max_sync(kFull, best);
-    const int win = __reduce_min_sync(kFull, best == mx ? be : 0x7fffffff);
-    if (win == 0x7fffffff) break;
-    const float v = __shfl_sync(kFull, bv, win & 31);
-    if (j == 0) top = v;
-    if (lane == j) my_e = win, my_v = v;
-    if ((win & 31) == lane) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (i == (win >> 5)) key[i] = 0u;
-      take_best();
-    }
-    __syncwarp();
-  }
-  // lanes 0 .. k-1 hold the slots; sums in slot order
-  const float num = lane < p.top_k && my_e >= 0 ? (grouped ? my_v : expf(my_v - top)) : 0.f;
-  float den = 0.f;
-  for (int j = 0; j < p.top_k; ++j) den += __shfl_sync(kFull, num, j);
-  if (p.gating == 0) {
-    den = 0.f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (lane + 32 * i < E) den += expf(logit[i] - top);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) den += __shfl_xor_sync(kFull, den, o);
-  }
-  return Slot{my_e, num / den * (grouped ? p.route_scale : 1.0f)};
-}
+__device__ __forceinline__ float unordered(uint32_t o) { return __uint_as_float((o >> 31) ? o & 0x7fffffffu : ~o); }
 
 // ------------------------------------------------------------ logits
 // Hidden states as operand image: rows n .. are zero.
@@ -243,14 +135,6 @@ constexpr int kLogitWarps = 8;
 constexpr int kLogitThreads = 32 * kLogitWarps;
 constexpr int kUnits = 4;    // K units (32 channels) of a warp on their way at a time
 constexpr int kLogitSlices = 8;
-constexpr int kPrefetchBoxes = 1344;  // of 32 KB: 44 MB, what HBM delivers until the routed experts are known
-
-__device__ __forceinline__ void prefetch_box(const CUtensorMap* m, int y) {
-  asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global.tile [%0, {%1, %2}];" ::"l"(reinterpret_cast<uint64_t>(m)),
-               "r"(0), "r"(y)
-               : "memory");
-}
-
 // CTA (tile, slice): logits of 16 experts (M) over a slice of K for all tokens (8 per MMA, N).  Its warps take
 // every eighth K unit; thread (g, q) feeds 16 bytes of a row to two MMAs, whose K order both operands share.
 // CTAs past the router's help with the rest.
@@ -281,19 +165,10 @@ __global__ void __launch_bounds__(kLogitThreads) few_logits_kernel(const __grid_
   // turns out to have been written since has them loaded again.
   const int early = load_layer(a.lref.layer, a.lref.n_layers, a.status, false);
   load_weights(early, u0 + warp);
-  // The shared expert's weights are needed whatever the router says: fetched into L2, behind the router's own.
-  if (threadIdx.x == 0 && a.Is) {
-    const LayerEntry& le = a.lref.table[early];
-    tensormap_acquire(&le.map[MAP_SH_GATE_UP]);
-    tensormap_acquire(&le.map[MAP_SH_DOWN]);
-    constexpr int kx = FP8 ? 128 : 64;
-    const int gu = a.Is / 128 * (a.H / kx), all = gu + a.H / 256 * (a.Is / kx);
-    for (int b = blockIdx.x; b < min(all, kPrefetchBoxes); b += gridDim.x)
-      prefetch_box(&le.map[b < gu ? MAP_SH_GATE_UP : MAP_SH_DOWN], (b < gu ? b : b - gu) * 256);
-  }
   pdl_wait();
   if (tile * 16 < E) {
-    const int layer = load_layer(a.lref.layer, a.lref.n_layers, a.status, blockIdx.x == 0 && threadIdx.x == 0);
+    const int layer = a.fixed_layer ? early
+                                    : load_layer(a.lref.layer, a.lref.n_layers, a.status, blockIdx.x == 0 && threadIdx.x == 0);
     const uint4* x = static_cast<const uint4*>(a.x);
     float c[NJ][4];
 #pragma unroll
@@ -367,6 +242,18 @@ struct FewItem {
   unsigned long long mask;
 };
 
+struct FewGate {  // of one token
+  uint32_t key[kMaxExperts];
+  float two[2][32];        // a group's two best selection scores
+  unsigned long long cand[kEpiWarps * kMaxTopK];
+  float val[kEpiWarps * kMaxTopK];
+  uint32_t top[kEpiWarps];
+  float sum[kEpiWarps];
+  int slot_e[kMaxTopK];
+  float slot_v[kMaxTopK];
+  int claim;
+};
+
 struct FewSmem {  // behind the rings
   alignas(16) uint64_t bar[2 * kFewMaxStages + 2 * kFewMaxStages + 2 * kMaxPartials + 3 * kQ + 2];
   int q[kQ];
@@ -380,14 +267,13 @@ struct FewSmem {  // behind the rings
   int pos[kFewTokens * kMaxTopK];
   float w[kFewTokens * kMaxTopK];
   float bias[kMaxExperts];  // of the router's selection
-  alignas(16) float sum[kEpiWarps][288];  // combine (accessed as float4); gating: selection scores and ranks
+  FewGate gate;
+  int first_row[kMaxExperts];               // of expert e
+  unsigned long long mask_of[kMaxExperts];
+  alignas(16) float sum[kEpiWarps][256];    // combine; accessed as float4
 };
 static_assert(sizeof(FewSmem) <= kFewSmemState, "shared memory budget");
 static_assert(offsetof(FewSmem, sum) % 16 == 0, "float4 accesses");
-
-// u / d for 0 <= u < 2^21 from r = 1 / d rounded to fp32 (u + 1/2 is at least 1/(2 d) from a multiple of d, in
-// units of d, and the product's error is below 2^-23 u / d).
-__device__ __forceinline__ int quick_div(int u, float r) { return static_cast<int>((u + 0.5f) * r); }
 
 template <bool FP8>
 __device__ __forceinline__ FewItem decode(const FewArgs& a, const FewSmem& s, int item) {
@@ -459,6 +345,14 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_
                "l"(src), "r"(bytes), "r"(bar)
                : "memory");
 }
+constexpr int kPrefetchBoxes = 1344;  // of 32 KB: 44 MB, what HBM delivers until the routed experts are known
+
+__device__ __forceinline__ void prefetch_box(const CUtensorMap* m, int y) {
+  asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global.tile [%0, {%1, %2}];" ::"l"(reinterpret_cast<uint64_t>(m)),
+               "r"(0), "r"(y)
+               : "memory");
+}
+
 __device__ __forceinline__ void fence_proxy_async_all() { asm volatile("fence.proxy.async;" ::: "memory"); }
 __device__ __forceinline__ int ld_acquire(const int* p) {
   int v;
@@ -507,54 +401,129 @@ __device__ __forceinline__ bool epi_all(bool ok) {
   return r != 0;
 }
 
-// Gating of token t by a warp from the planes of its logits; row: E + n_groups floats.
-__device__ __forceinline__ Slot gate_logits(const FewArgs& a, const float* bias, float* row, int t, int lane) {
-  const int E = a.gate.n_experts;
-  float l[kLogitSlices][8];
+// Gating of token t by the epilogue warps, one thread per expert, from the planes
+// of its logits: expert (-1: none left) and weight of slot j to e[j], w[j].  The
+// rules and tie-breaks of gate_kernel (route.cu).  No rounds: an expert's place is
+// the number of experts in front of it, counted in its group, for groups against
+// one another, in its warp, and among the warps' best.
+__device__ __forceinline__ void gate_token(const FewArgs& a, FewSmem& s, int t, int warp, int lane, int tid, int* e_out,
+                                           float* w_out) {
+  const GateParams& p = a.gate;
+  const int E = p.n_experts, k = p.top_k;
+  const bool grouped = p.gating == 2, in = tid < E;
+  float logit = 0.f;
+  if (in) {
+    float l[kLogitSlices];
 #pragma unroll
-  for (int r = 0; r < kLogitSlices; ++r)
+    for (int r = 0; r < kLogitSlices; ++r) l[r] = __ldcg(a.logits + (r * a.n + t) * E + tid);
+    logit = l[0];
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      l[r][i] = lane + 32 * i < E ? __ldcg(a.logits + (r * a.n + t) * E + lane + 32 * i) : 0.f;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    float sum = l[0][i];
-#pragma unroll
-    for (int r = 1; r < kLogitSlices; ++r) sum += l[r][i];
-    if (lane + 32 * i < E) row[lane + 32 * i] = sum;
+    for (int r = 1; r < kLogitSlices; ++r) logit += l[r];
   }
-  __syncwarp();
-  const Slot slot = gate_token(a.gate, row, bias, lane);
-  if (lane < a.gate.top_k && slot.e < 0) record_status(a.status, ST_BAD_EXPERT_INDEX);
-  return slot;
+  FewGate& g = s.gate;
+  const float val = grouped ? gate_sigmoid(logit) : logit;
+  const float sel = grouped ? val + s.bias[tid] : val;
+  uint32_t key = in ? ordered(sel) : 0u;  // 0: may not be chosen
+  if (grouped) {
+    const int gsz = E / p.n_groups;
+    const int grp = in ? quick_div(tid, 1.0f / static_cast<float>(gsz)) : 0, first = grp * gsz;
+    g.key[tid] = key;
+    epi_sync();
+    int rank = 0;  // members of the group in front of this one
+#pragma unroll 8
+    for (int m = first; m < first + gsz; ++m) {
+      const uint32_t o = g.key[m];
+      rank += (o > key || (o == key && m < tid)) ? 1 : 0;
+    }
+    if (in && rank < 2) g.two[rank][grp] = sel;
+    epi_sync();
+    const float score = g.two[0][grp] + g.two[1][grp];
+    int before = 0;  // groups in front of this one
+#pragma unroll 4
+    for (int m = 0; m < p.n_groups; ++m) {
+      const float o = g.two[0][m] + g.two[1][m];
+      before += (o > score || (o == score && m < grp)) ? 1 : 0;
+    }
+    if (before >= p.topk_groups) key = 0u;
+  }
+  if (p.gating == 0) {  // the softmax sum over all experts, from the largest logit
+    const uint32_t mx = __reduce_max_sync(kFull, key);
+    if (lane == 0) g.top[warp] = mx;
+    epi_sync();
+    uint32_t top = g.top[0];
+#pragma unroll
+    for (int w = 1; w < kEpiWarps; ++w) top = max(top, g.top[w]);
+    float z = in ? expf(logit - unordered(top)) : 0.f;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) z += __shfl_xor_sync(kFull, z, o);
+    if (lane == 0) g.sum[warp] = z;
+  }
+  int rank = 0;  // experts of this warp in front of this one
+#pragma unroll
+  for (int m = 0; m < 32; ++m) {
+    const uint32_t o = __shfl_sync(kFull, key, m);
+    rank += (o > key || (o == key && m < lane)) ? 1 : 0;
+  }
+  // the warps' first k are candidates: larger keys first, of equal ones the lower expert
+  if (rank < kMaxTopK) {
+    g.cand[warp * kMaxTopK + rank] =
+        key == 0u ? 0ull : (static_cast<unsigned long long>(key) << 32) | static_cast<uint32_t>(kMaxExperts - 1 - tid);
+    g.val[warp * kMaxTopK + rank] = val;
+  }
+  if (tid < kMaxTopK) g.slot_e[tid] = -1;
+  epi_sync();
+  if (tid < kEpiWarps * kMaxTopK) {
+    const unsigned long long mine = g.cand[tid];
+    int place = 0;
+#pragma unroll 16
+    for (int m = 0; m < kEpiWarps * kMaxTopK; ++m) place += g.cand[m] > mine ? 1 : 0;
+    if (mine != 0ull && place < k) {
+      g.slot_e[place] = kMaxExperts - 1 - static_cast<int>(mine & 0xffffffffu);
+      g.slot_v[place] = g.val[tid];
+    }
+  }
+  epi_sync();
+  if (warp == 0) {
+    const int e = lane < k ? g.slot_e[lane] : -1;
+    const float num = e >= 0 ? (grouped ? g.slot_v[lane] : expf(g.slot_v[lane] - g.slot_v[0])) : 0.f;
+    float den = 0.f;  // in slot order
+    if (p.gating == 0) {
+#pragma unroll
+      for (int w = 0; w < kEpiWarps; ++w) den += g.sum[w];
+    } else {
+#pragma unroll
+      for (int j = 0; j < kMaxTopK; ++j) den += __shfl_sync(kFull, num, j);
+    }
+    if (lane < k) {
+      e_out[lane] = e;
+      w_out[lane] = num / den * (grouped ? p.route_scale : 1.0f);
+      if (e < 0) record_status(a.status, ST_BAD_EXPERT_INDEX);
+    }
+  }
 }
 
 // The routing of the call in every CTA, by its epilogue warps: active experts in
 // increasing order, their tokens, first rows and row groups, the row and weight
 // of every slot, and the number of work items.  Up to kOwnGate tokens every CTA
-// gates all of them, one warp each (a warp takes about 4 us); more are gated
-// once, claimed one by one, and read by every CTA when all are done.
-constexpr int kOwnGate = kEpiWarps;
+// gates for itself (a token takes about 1.5 us); more are gated once, claimed one
+// by one, and read by every CTA when all are done (about 4 us for the round trips).
+constexpr int kOwnGate = 3;
 __device__ __forceinline__ bool list_experts(const FewArgs& a, FewSmem& s, int warp, int lane, int tid,
                                              volatile int* abort_flag) {
   const int k = a.gate.top_k, n = a.n;
   s.mask[tid] = 0ull;
   if (n <= kOwnGate) {
-    if (warp < n) {
-      const Slot slot = gate_logits(a, s.bias, s.sum[warp], warp, lane);
-      if (lane < k) s.pos[warp * k + lane] = slot.e, s.w[warp * k + lane] = slot.w;  // (pos: the expert, for now)
-    }
+    for (int t = 0; t < n; ++t) gate_token(a, s, t, warp, lane, tid, s.pos + t * k, s.w + t * k);  // (pos: the expert, for now)
     epi_sync();
   } else {
     int* claims = a.counters + a.gate_claims;
-    if (warp == 0) {
-      while (true) {
-        int t = 0;
-        if (lane == 0) t = atomicAdd(claims, 1);
-        t = __shfl_sync(kFull, t, 0);
-        if (t >= n) break;
-        const Slot slot = gate_logits(a, s.bias, s.sum[0], t, lane);
-        if (lane < k) a.sel_e[t * k + lane] = slot.e, a.sel_w[t * k + lane] = slot.w;
+    while (true) {
+      if (tid == 0) s.gate.claim = atomicAdd(claims, 1);
+      epi_sync();
+      const int t = *reinterpret_cast<volatile int*>(&s.gate.claim);
+      if (t >= n) break;
+      gate_token(a, s, t, warp, lane, tid, a.sel_e + t * k, a.sel_w + t * k);
+      if (warp == 0) {
         __syncwarp();
         if (lane == 0) arrive_release(claims + 1);
       }
@@ -579,10 +548,8 @@ __device__ __forceinline__ bool list_experts(const FewArgs& a, FewSmem& s, int w
   epi_sync();
   int before = incl - v;
   for (int w = 0; w < warp; ++w) before += s.warp_total[w];
-  int* first_row = reinterpret_cast<int*>(&s.sum[0][0]);  // of expert e (the scores are done with)
-  first_row[tid] = (before >> 10) & 1023;
-  unsigned long long* mask_of = reinterpret_cast<unsigned long long*>(&s.sum[2][0]);
-  mask_of[tid] = mask;
+  s.first_row[tid] = (before >> 10) & 1023;
+  s.mask_of[tid] = mask;
   epi_sync();  // every mask has been read: the list takes their place
   if (v) {
     const int j = before & 1023;
@@ -599,7 +566,7 @@ __device__ __forceinline__ bool list_experts(const FewArgs& a, FewSmem& s, int w
   }
   for (int p = tid; p < n * k; p += kEpiThreads) {
     const int ex = s.pos[p], t = p / k;
-    s.pos[p] = ex >= 0 ? first_row[ex] + __popcll(mask_of[ex] & ((1ull << t) - 1)) : -1;
+    s.pos[p] = ex >= 0 ? s.first_row[ex] + __popcll(s.mask_of[ex] & ((1ull << t) - 1)) : -1;
   }
   epi_sync();
   return true;
@@ -774,13 +741,22 @@ __global__ void __launch_bounds__(FP8 && NT == 64 ? kThreads : 512, 1) few_ffn_k
     if (bias && threadIdx.x < a.gate.n_experts) s.bias[threadIdx.x] = __ldg(bias + threadIdx.x);
     else if (threadIdx.x < kMaxExperts) s.bias[threadIdx.x] = 0.f;
   };
-  if (warp == 0 && lane == 0) acquire_maps(early);
+  if ((warp == 0 || warp == 2) && lane == 0) acquire_maps(early);
   load_bias(early);
-  if (warp >= 4) gate_token(a.gate, s.sum[warp - 4], s.bias, lane);  // (see there: the result is not used)
+  // The shared expert's weights are needed whatever the router says: fetched into L2 meanwhile.  (By the time
+  // this kernel comes up the logits kernel has asked for the router's, which would have to wait behind these:
+  // with these first its logits took 13 us instead of 5.)
+  if (warp == 2 && lane == 0 && a.Is) {
+    constexpr int kx = FP8 ? 128 : 64;
+    const CUtensorMap* m = a.lref.table[early].map;
+    const int gu = a.Is / 128 * (a.H / kx), all = gu + a.H / 256 * (a.Is / kx);
+    for (int b = blockIdx.x; b < min(all, kPrefetchBoxes); b += gridDim.x)
+      prefetch_box(m + (b < gu ? MAP_SH_GATE_UP : MAP_SH_DOWN), (b < gu ? b : b - gu) * 256);
+  }
   pdl_wait();
   int claim = 0;
   if (threadIdx.x == 0) claim = atomicAdd(&a.counters[0], 1);
-  const int layer = load_layer(a.lref.layer, a.lref.n_layers, a.status, false);
+  const int layer = a.fixed_layer ? early : load_layer(a.lref.layer, a.lref.n_layers, a.status, false);
   if (layer != early) load_bias(layer);
   tc_fence_before();
   __syncthreads();
@@ -1151,6 +1127,16 @@ cudaError_t few_set_attributes() {
     if (e == cudaSuccess)
       e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes));
   };
+  // the logits kernels leave their SM in the configuration that the FFN's shared memory needs, which can then
+  // come up beside them
+  auto carve = [&](auto* f) {
+    if (e == cudaSuccess)
+      e = cudaFuncSetAttribute(f, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
+  };
+  carve(few_logits_kernel<false, 1>);
+  carve(few_logits_kernel<true, 1>);
+  carve(few_logits_kernel<false, kFewTokens / 8>);
+  carve(few_logits_kernel<true, kFewTokens / 8>);
   set(few_ffn_kernel<false, 16>, kFewSmem);
   set(few_ffn_kernel<true, 16>, kFewSmem);
   set(few_ffn_kernel<true, 64>, kFewSmem);
@@ -1158,7 +1144,7 @@ cudaError_t few_set_attributes() {
 }
 
 cudaError_t few_launch(const FewArgs& a, bool fp8, int grid, cudaStream_t st) {
-  // (a CTA more for every two tokens than the router has use for, up to a third of the GPU)
+  // (at least a CTA for every two tokens, whose rows the image takes, up to a third of the GPU)
   const int ctas = std::max(ceil_div(a.gate.n_experts, 16) * kLogitSlices, std::min(48, a.n / 2));
   const dim3 grid_l(ctas), block_l(kLogitThreads);
   cudaError_t e;

@@ -8,10 +8,11 @@ namespace asap {
 
 constexpr int kFewTokens = 64;                // tokens of a call at most (one bit each in a 64-bit mask)
 constexpr int kFewMaxStages = 8;              // ring stages of either operand at most
-constexpr size_t kFewSmemState = 20992;       // barriers, queue and metadata behind the rings
+constexpr size_t kFewSmemState = 25600;       // barriers, queue and metadata behind the rings
 constexpr size_t kFewSmem = 227 * 1024;       // dynamic shared memory of a few_ffn_kernel CTA at most
 struct FewArgs {
   LayerRef lref;
+  int fixed_layer;               // *lref.layer never changes
   GateParams gate;
   uint32_t* status;
   const void* x;
