@@ -159,6 +159,7 @@ FewLayout few_layout(const asap_moe_config& c, int n) {
   a.s2 = few_slices(down, a.I / step);
   a.s2s = a.Is ? few_slices(down, a.Is / step) : 0;
   a.first_routed = tS * a.s1;
+  a.out_tokens = n >= 8 ? 8 : 1;  // (61 tokens one by one: 11 items a CTA, 20 us after the last weights)
   a.r_s1 = 1.0f / a.s1;
   a.r_s2 = 1.0f / a.s2;
   a.r_s2s = a.Is ? 1.0f / a.s2s : 0.f;

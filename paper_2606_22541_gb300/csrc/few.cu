@@ -165,6 +165,10 @@ __global__ void __launch_bounds__(kLogitThreads) few_logits_kernel(const __grid_
   // turns out to have been written since has them loaded again.
   const int early = load_layer(a.lref.layer, a.lref.n_layers, a.status, false);
   load_weights(early, u0 + warp);
+  // (and the hidden states in L2, in front of the expert weights that the second kernel fetches meanwhile:
+  // behind these the logits of 61 tokens took 19 us)
+  for (long long i = (blockIdx.x * kLogitThreads + threadIdx.x) * 128ll; i < 2ll * n * a.H; i += gridDim.x * kLogitThreads * 128ll)
+    asm volatile("prefetch.global.L2 [%0];" ::"l"(static_cast<const uint8_t*>(a.x) + i));
   pdl_wait();
   if (tile * 16 < E) {
     const int layer = a.fixed_layer ? early
@@ -303,8 +307,9 @@ __device__ __forceinline__ FewItem decode(const FewArgs& a, const FewSmem& s, in
     if (u >= dn) {
       u -= dn;
       T.combine = true;
-      T.token = quick_div(u, a.r_tH);
-      T.tile = u - T.token * tH;
+      const int group = quick_div(u, a.r_tH);
+      T.token = group * a.out_tokens;
+      T.tile = u - group * tH;
       T.ticket = a.down_tickets + T.tile;
       return T;
     }
@@ -562,7 +567,7 @@ __device__ __forceinline__ bool list_experts(const FewArgs& a, FewSmem& s, int w
     const int active = (before + v) & 1023;
     s.active = active;
     s.items = (a.Is / 128 + active * (a.I / 128)) * a.s1 +
-              a.H / 256 * (active * a.s2 + (a.Is ? a.s2s : 0) + n);
+              a.H / 256 * (active * a.s2 + (a.Is ? a.s2s : 0) + ceil_div_dev(n, a.out_tokens));
   }
   for (int p = tid; p < n * k; p += kEpiThreads) {
     const int ex = s.pos[p], t = p / k;
@@ -631,28 +636,29 @@ __device__ __forceinline__ void write_h(const FewArgs& a, const FewSmem& s, cons
   }
 }
 
-// 256 channels of a token: its terms are the slots' partial sums, slot by slot,
-// then the shared expert's; warp w adds terms w, w + 8, ... (lane l channels 4l ..
-// and 128 + 4l ..), then the warps' sums are added in order.
-__device__ __forceinline__ void write_out(const FewArgs& a, FewSmem& s, const FewItem& T, int warp, int lane, int tid) {
+// 256 channels of an item's tokens.  A token's terms are its slots' partial sums,
+// slot by slot, then the shared expert's; lane l adds channels 4l .. and 128 + 4l
+// .. of terms first, first + step, ...
+__device__ __forceinline__ void add_terms(const FewArgs& a, const FewSmem& s, int t, int tile, int first, int step,
+                                          int lane, float4& lo, float4& hi) {
   constexpr int kAhead = 4;
-  const int k = a.gate.top_k, H = a.H, t = T.token;
+  const int k = a.gate.top_k, H = a.H;
   const long long plane = static_cast<long long>(a.n) * k * H, plane_s = static_cast<long long>(a.n) * H;
   const int routed = k * a.s2, terms = routed + (a.Is ? a.s2s : 0);
-  const int ch = T.tile * 256 + 4 * lane;
-  float4 lo = make_float4(0.f, 0.f, 0.f, 0.f), hi = lo;
-  for (int i0 = warp; i0 < terms; i0 += kEpiWarps * kAhead) {
+  const int ch = tile * 256 + 4 * lane;
+  lo = hi = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int i0 = first; i0 < terms; i0 += step * kAhead) {
     float w[kAhead];
     float4 l[kAhead], h[kAhead];
 #pragma unroll
     for (int r = 0; r < kAhead; ++r) {
-      const int i = i0 + r * kEpiWarps;
+      const int i = i0 + r * step;
       w[r] = 0.f;
       l[r] = h[r] = make_float4(0.f, 0.f, 0.f, 0.f);
       if (i >= terms) continue;
       const float* src;
       if (i < routed) {
-        const int j = i / a.s2, pos = s.pos[t * k + j];
+        const int j = quick_div(i, a.r_s2), pos = s.pos[t * k + j];
         if (pos < 0) continue;
         w[r] = s.w[t * k + j];
         src = a.y + (i - j * a.s2) * plane + static_cast<long long>(pos) * H + ch;
@@ -671,13 +677,28 @@ __device__ __forceinline__ void write_out(const FewArgs& a, FewSmem& s, const Fe
       hi.z = fmaf(w[r], h[r].z, hi.z), hi.w = fmaf(w[r], h[r].w, hi.w);
     }
   }
+}
+// An item of one token: its terms over the warps, whose sums are then added in
+// order; of several: a token per warp.
+__device__ __forceinline__ void write_out(const FewArgs& a, FewSmem& s, const FewItem& T, int warp, int lane, int tid) {
+  float4 lo, hi;
+  __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) + static_cast<long long>(T.token) * a.H + T.tile * 256;
+  if (a.out_tokens > 1) {
+    if (T.token + warp >= a.n) return;
+    add_terms(a, s, T.token + warp, T.tile, 0, 1, lane, lo, hi);
+    uint2* o = reinterpret_cast<uint2*>(out + static_cast<long long>(warp) * a.H);
+    o[lane] = make_uint2(pack_bf16x2(lo.x, lo.y), pack_bf16x2(lo.z, lo.w));
+    o[32 + lane] = make_uint2(pack_bf16x2(hi.x, hi.y), pack_bf16x2(hi.z, hi.w));
+    return;
+  }
+  add_terms(a, s, T.token, T.tile, warp, kEpiWarps, lane, lo, hi);
   *reinterpret_cast<float4*>(&s.sum[warp][4 * lane]) = lo;
   *reinterpret_cast<float4*>(&s.sum[warp][128 + 4 * lane]) = hi;
   epi_sync();
   float acc = s.sum[0][tid];
 #pragma unroll
-  for (int w2 = 1; w2 < kEpiWarps; ++w2) acc += s.sum[w2][tid];
-  static_cast<__nv_bfloat16*>(a.out)[static_cast<long long>(t) * H + T.tile * 256 + tid] = __float2bfloat16_rn(acc);
+  for (int w = 1; w < kEpiWarps; ++w) acc += s.sum[w][tid];
+  out[tid] = __float2bfloat16_rn(acc);
 }
 
 // NT: columns (tokens) the FP8 epilogue keeps in registers; unused for BF16.

@@ -20,6 +20,7 @@ struct FewArgs {
   int n, H, I, Is;               // Is 0: no shared expert
   int max_active;                // min(E, n * k)
   int s1, s2, s2s;               // K slices of a gate/up, a down and a shared down tile
+  int out_tokens;                // tokens of an output item: 1, or one per epilogue warp
   int first_routed;              // work items in front of the first that needs the routing
   float r_s1, r_s2, r_s2s, r_tI, r_tH, r_down;  // reciprocals: of the slices, tiles and down items of an expert
   int stages_w, stages_x, x_slot;  // rings: stages, bytes of a stage of operand rows
