@@ -414,6 +414,46 @@ int asap_moe_layer_batched_dyn(asap_moe_t h, const int32_t* layer_id, int32_t co
                                void* ws, size_t ws_bytes, void* stream);
 
 /* ------------------------------------------------------------------------
+ * e4m3 operators on plain tensors: the dense layers around the MoE layers in
+ * the number format of ASAP_FP8_E4M3_BLOCK128.  No handle, no workspace; they
+ * launch on the caller's current device and only enqueue.  Strides (ld*) are in
+ * elements between rows.  m, n, rows or cols of 0 is a successful no-op.
+ * Outputs must not overlap inputs.
+ * ------------------------------------------------------------------------ */
+
+/* Activation rows to e4m3 with one fp32 scale per row per 128 columns (the
+ * last group of a row may be shorter):
+ *   amax = max |v| over the group,  s = amax * fl(1 / 448) (1 where that is 0),
+ *   q = e4m3(v / s), quotient correctly rounded, then nearest even, saturated.
+ * x [rows, cols] bf16; q [rows, cols] e4m3; scales [rows, ceil(cols/128)].
+ * Any column count, stride and alignment; rows of q that asap_moe_fp8_matmul
+ * reads start on 16-byte boundaries.  A NaN gives a NaN and leaves the group's
+ * scale alone; an infinity gives its group an infinite scale and NaNs. */
+int asap_moe_fp8_quantize(const void* x, int64_t ldx, int32_t rows, int32_t cols, void* q,
+                          int64_t ldq, float* scales, int64_t lds, void* stream);
+
+/* The same for v = silu(gate) * up in fp32 (silu(g) = g / (1 + exp(-g))): what
+ * stands between the two products of a SwiGLU layer.  gate, up [rows, cols]
+ * bf16 with one stride, e.g. the halves of a product's rows. */
+int asap_moe_fp8_swiglu_quantize(const void* gate, const void* up, int64_t ld, int32_t rows,
+                                 int32_t cols, void* q, int64_t ldq, float* scales, int64_t lds,
+                                 void* stream);
+
+/* Product of e4m3 matrices with block scales:
+ *   c[i, j] = bf16( sum_kb a_scales[i, kb] b_scales[j / 128, kb]
+ *                   sum_{l in block kb of 128} a[i, l] b[j, l] )
+ * in fp32 (the inner sums on the tensor core).
+ * a [m, k], b [n, k] e4m3, rows on 16-byte boundaries (lda, ldb multiples of
+ * 16); a_scales [m, ceil(k/128)], b_scales [ceil(n/128), ceil(k/128)] fp32;
+ * c [m, n] bf16.  Any m, n >= 0 and k >= 1.  The same call gives the same bits
+ * each time.  status: NULL, or a device word that gets the bits of
+ * asap_moe_status (4, 32) ORed in should a kernel fail. */
+int asap_moe_fp8_matmul(const void* a, int64_t lda, const float* a_scales, int64_t lds_a,
+                        const void* b, int64_t ldb, const float* b_scales, int64_t lds_b, void* c,
+                        int64_t ldc, int32_t m, int32_t n, int32_t k, uint32_t* status,
+                        void* stream);
+
+/* ------------------------------------------------------------------------
  * Mailbox: the device decides which micro-batches one grouped GEMM pass
  * serves.  The single-GPU form of the asynchronous primitives of Sections
  * 3.2.1 and 3.2.2 (Table 2: per DP group, regions for the token data and the

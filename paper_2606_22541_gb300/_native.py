@@ -35,6 +35,7 @@ class AsapMoeWeights(ctypes.Structure):
 
 _P = ctypes.c_void_p
 _I = ctypes.c_int32
+_L = ctypes.c_int64
 _SZ = ctypes.c_size_t
 
 SIGNATURES = {
@@ -58,6 +59,9 @@ SIGNATURES = {
     "asap_moe_layer": [_P, _P, _I, _P, _P, _SZ, _P],
     "asap_moe_route_noalloc": [_P, _P, _I, _P, _P, _P, _P, _P],
     "asap_moe_layer_few": [_P, _P, _P, _I, _P, _P, _SZ, _P],
+    "asap_moe_fp8_quantize": [_P, _L, _I, _I, _P, _L, _P, _L, _P],
+    "asap_moe_fp8_swiglu_quantize": [_P, _P, _L, _I, _I, _P, _L, _P, _L, _P],
+    "asap_moe_fp8_matmul": [_P, _L, _P, _L, _P, _L, _P, _L, _P, _L, _I, _I, _I, _P, _P],
     "asap_moe_layer_batched": [_P, _I, ctypes.POINTER(_P), ctypes.POINTER(_I), ctypes.POINTER(_P), _P, _SZ, _P],
     "asap_moe_layer_dyn": [_P, _P, _P, _I, _P, _P, _SZ, _P],
     "asap_moe_layer_batched_dyn": [_P, _P, _I, ctypes.POINTER(_P), ctypes.POINTER(_I), ctypes.POINTER(_P), _P, _SZ,

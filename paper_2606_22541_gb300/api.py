@@ -252,6 +252,76 @@ def asap_moe_route_noalloc(h, x, idx, w, counts, offsets, stream=None):
                                        _ptr(offsets), _stream(stream)))
 
 
+def _matrix(name, t, dtypes):
+    """Pointer and row stride of a 2-D tensor whose columns are contiguous."""
+    if t.dim() != 2 or t.dtype not in dtypes or not t.is_cuda:
+        raise ValueError(f"{name}: a 2-D CUDA tensor of {' or '.join(str(d) for d in dtypes)}, got "
+                         f"{tuple(t.shape)} {t.dtype} on {t.device}")
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name}: columns must be contiguous, got strides {tuple(t.stride())}")
+    # (a single row's stride says nothing: one that any row may have)
+    return _ptr(t), t.stride(0) if t.shape[0] > 1 else -(-t.shape[1] // 16) * 16
+
+
+_E4M3 = (torch.float8_e4m3fn, torch.uint8)
+_BF16 = (torch.bfloat16,)
+_F32 = (torch.float32,)
+
+
+def _shape(name, t, rows, cols):
+    if tuple(t.shape) != (rows, cols):
+        raise ValueError(f"{name}: shape ({rows}, {cols}) expected, got {tuple(t.shape)}")
+
+
+def asap_moe_fp8_quantize(x, q, scales, stream=None):
+    """bf16 rows x [n, c] to e4m3 q [n, c] with scales [n, ceil(c / 128)]
+    (fp32); any row strides."""
+    n, c = x.shape
+    _shape("q", q, n, c)
+    _shape("scales", scales, n, -(-c // 128))
+    px, ldx = _matrix("x", x, _BF16)
+    pq, ldq = _matrix("q", q, _E4M3)
+    ps, lds = _matrix("scales", scales, _F32)
+    check("asap_moe_fp8_quantize", lib().asap_moe_fp8_quantize(px, ldx, n, c, pq, ldq, ps, lds, _stream(stream)))
+
+
+def asap_moe_fp8_swiglu_quantize(gate, up, q, scales, stream=None):
+    """silu(gate) * up of bf16 [n, c] tensors with one row stride (the halves of
+    a product's rows) to e4m3 q [n, c] with scales [n, ceil(c / 128)]."""
+    n, c = gate.shape
+    _shape("up", up, n, c)
+    _shape("q", q, n, c)
+    _shape("scales", scales, n, -(-c // 128))
+    pg, ld = _matrix("gate", gate, _BF16)
+    pu, ldu = _matrix("up", up, _BF16)
+    if ldu != ld:
+        raise ValueError(f"gate and up must have one row stride, got {ld} and {ldu}")
+    pq, ldq = _matrix("q", q, _E4M3)
+    ps, lds = _matrix("scales", scales, _F32)
+    check("asap_moe_fp8_swiglu_quantize",
+          lib().asap_moe_fp8_swiglu_quantize(pg, pu, ld, n, c, pq, ldq, ps, lds, _stream(stream)))
+
+
+def asap_moe_fp8_matmul(a, a_scales, b, b_scales, out, stream=None, status=None):
+    """out [m, n] (bf16) = a b^T of e4m3 a [m, k], b [n, k] (rows on 16-byte
+    boundaries) with fp32 scales [m, ceil(k / 128)] and [ceil(n / 128),
+    ceil(k / 128)].  status: None or a one-element int32 CUDA tensor that gets
+    error bits."""
+    (m, k), n = a.shape, b.shape[0]
+    _shape("b", b, n, k)
+    _shape("out", out, m, n)
+    _shape("a_scales", a_scales, m, -(-k // 128))
+    _shape("b_scales", b_scales, -(-n // 128), -(-k // 128))
+    pa, lda = _matrix("a", a, _E4M3)
+    pb, ldb = _matrix("b", b, _E4M3)
+    psa, lsa = _matrix("a_scales", a_scales, _F32)
+    psb, lsb = _matrix("b_scales", b_scales, _F32)
+    pc, ldc = _matrix("out", out, _BF16)
+    check("asap_moe_fp8_matmul",
+          lib().asap_moe_fp8_matmul(pa, lda, psa, lsa, pb, ldb, psb, lsb, pc, ldc, m, n, k, _ptr(status),
+                                    _stream(stream)))
+
+
 class Mailbox:
     """Owns an asap_moe_mailbox_t (slots that DP-group streams post routed
     micro-batches into and that service rounds on the MoE stream claim on the

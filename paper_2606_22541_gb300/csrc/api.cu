@@ -1453,6 +1453,94 @@ ASAP_API int asap_moe_layer_batched_dyn(asap_moe_t h, const int32_t* layer_id, i
   return run_layer_batched(h, count, xs, ns, outs, ws, ws_bytes, layer_id, stream);
 }
 
+namespace {
+
+// Device the calls without a handle launch on: its SM count, and the kernels'
+// attributes set on it, once per device.
+int matmul_device(int* num_sms) {
+  static std::mutex lock;
+  static std::vector<int> sms;  // by device, 0: not looked at yet
+  int dev = 0;
+  CU_TRY(cudaGetDevice(&dev), "cudaGetDevice");
+  std::lock_guard<std::mutex> g(lock);
+  if (static_cast<size_t>(dev) >= sms.size()) sms.resize(dev + 1, 0);
+  if (sms[dev] == 0) {
+    int major = 0, minor = 0, n = 0;
+    CU_TRY(cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev), "compute capability");
+    CU_TRY(cudaDeviceGetAttribute(&minor, cudaDevAttrComputeCapabilityMinor, dev), "compute capability");
+    if (major != 10 || minor != 3)
+      return fail(ASAP_ERR_UNSUPPORTED, "libasap_moe is built for sm_103a (GB300) only; device is sm_" +
+                                            std::to_string(major) + std::to_string(minor));
+    CU_TRY(cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev), "SM count");
+    CU_TRY(asap::fp8_matmul_set_attributes(), "product attributes");
+    sms[dev] = n;
+  }
+  *num_sms = sms[dev];
+  return ASAP_OK;
+}
+
+int run_quantize(const void* x, const void* u, bool swiglu, int64_t ldx, int32_t rows, int32_t cols, void* q, int64_t ldq,
+                 float* scales, int64_t lds, void* stream) {
+  if (rows < 0 || cols < 0) return fail(ASAP_ERR_INVALID, "negative rows or cols");
+  if (rows == 0 || cols == 0) return ASAP_OK;
+  if (!x || (swiglu && !u) || !q || !scales) return fail(ASAP_ERR_INVALID, "NULL tensor");
+  if (ldx < cols || ldq < cols || lds < asap::ceil_div(cols, 128))
+    return fail(ASAP_ERR_INVALID, "a row stride is shorter than its rows");
+  if (((reinterpret_cast<uintptr_t>(x) | reinterpret_cast<uintptr_t>(u)) & 1u) != 0 ||
+      (reinterpret_cast<uintptr_t>(scales) & 3u) != 0)
+    return fail(ASAP_ERR_INVALID, "tensors must be aligned to their elements");
+  CU_TRY(asap::launch_fp8_quantize(x, u, rows, cols, ldx, q, ldq, scales, lds, S(stream)), "quantise launch");
+  return ASAP_OK;
+}
+
+}  // namespace
+
+ASAP_API int asap_moe_fp8_quantize(const void* x, int64_t ldx, int32_t rows, int32_t cols, void* q, int64_t ldq,
+                                   float* scales, int64_t lds, void* stream) {
+  return run_quantize(x, nullptr, false, ldx, rows, cols, q, ldq, scales, lds, stream);
+}
+
+ASAP_API int asap_moe_fp8_swiglu_quantize(const void* gate, const void* up, int64_t ld, int32_t rows, int32_t cols,
+                                          void* q, int64_t ldq, float* scales, int64_t lds, void* stream) {
+  return run_quantize(gate, up, true, ld, rows, cols, q, ldq, scales, lds, stream);
+}
+
+ASAP_API int asap_moe_fp8_matmul(const void* a, int64_t lda, const float* a_scales, int64_t lds_a, const void* b,
+                                 int64_t ldb, const float* b_scales, int64_t lds_b, void* c, int64_t ldc, int32_t m,
+                                 int32_t n, int32_t k, uint32_t* status, void* stream) {
+  if (m < 0 || n < 0 || k < 1) return fail(ASAP_ERR_INVALID, "m and n must be at least 0, k at least 1");
+  if (m == 0 || n == 0) return ASAP_OK;
+  if (!a || !a_scales || !b || !b_scales || !c) return fail(ASAP_ERR_INVALID, "NULL tensor");
+  if (!aligned16(a) || !aligned16(b) || lda % 16 != 0 || ldb % 16 != 0)
+    return fail(ASAP_ERR_INVALID, "rows of a and b must start on 16-byte boundaries");
+  if ((reinterpret_cast<uintptr_t>(c) & 1u) != 0 ||
+      ((reinterpret_cast<uintptr_t>(a_scales) | reinterpret_cast<uintptr_t>(b_scales) |
+        reinterpret_cast<uintptr_t>(status)) & 3u) != 0)
+    return fail(ASAP_ERR_INVALID, "tensors must be aligned to their elements");
+  const int blocks = asap::ceil_div(k, 128);
+  if (lda < k || ldb < k || ldc < n || lds_a < blocks || lds_b < blocks)
+    return fail(ASAP_ERR_INVALID, "a row stride is shorter than its rows");
+  int num_sms = 0;
+  const int r = matmul_device(&num_sms);
+  if (r != ASAP_OK) return r;
+  asap::Fp8MatmulArgs args{};
+  args.m = m;
+  args.n = n;
+  args.k = k;
+  args.sa = a_scales;
+  args.sb = b_scales;
+  args.lds_a = lds_a;
+  args.lds_b = lds_b;
+  args.c = c;
+  args.ldc = ldc;
+  args.status = status;
+  std::string err;
+  const cudaError_t e = asap::fp8_matmul_launch(a, lda, b, ldb, args, num_sms, S(stream), &err);
+  if (!err.empty()) return fail(ASAP_ERR_INVALID, err);
+  if (e != cudaSuccess) return cuda_fail(e, "product launch");
+  return ASAP_OK;
+}
+
 ASAP_API int asap_moe_n_layers(asap_moe_t h, int32_t* n_layers) {
   if (!h || !n_layers) return fail(ASAP_ERR_INVALID, "NULL handle or output");
   *n_layers = static_cast<int32_t>(h->layers.size());

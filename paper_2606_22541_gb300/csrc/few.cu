@@ -33,10 +33,10 @@
 // An item waits only for items claimed before it, by CTAs that are running,
 // so the launch needs no co-residency to make progress.
 #include "common.cuh"
+#include "e4m3.cuh"
 #include "few.h"
 #include "internal.h"
 
-#include <cuda_fp8.h>
 #include <math_constants.h>
 
 #include <algorithm>
@@ -58,22 +58,6 @@ __host__ __device__ constexpr int step_bytes(int rows) {
 }
 __device__ __forceinline__ int swizzled(int row, int byte) {
   return row * 128 + ((((byte >> 4) ^ (row & 7)) << 4) | (byte & 15));
-}
-
-// Scale of a group: amax times the fp32 reciprocal of 448.
-__device__ __forceinline__ float group_scale(float amax) { return amax > 0.f ? amax * (1.0f / 448.0f) : 1.0f; }
-// e4m3 of v / s.  The quotient is the correctly rounded one (Markstein 1990: one
-// correction of v * (1/s) by its residual), as a division gives it: bf16
-// values over amax / 448 fall exactly between two e4m3 values for about one
-// element in 500, and those must not depend on how the quotient was taken.
-__device__ __forceinline__ float quotient(float v, float s, float inv) {
-  const float q = v * inv;
-  return fmaf(fmaf(-q, s, v), inv, q);
-}
-__device__ __forceinline__ uint32_t e4m3x4(float a, float b, float c, float d) {
-  const __nv_fp8x2_storage_t lo = __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
-  const __nv_fp8x2_storage_t hi = __nv_cvt_float2_to_fp8x2(make_float2(c, d), __NV_SATFINITE, __NV_E4M3);
-  return static_cast<uint32_t>(lo) | (static_cast<uint32_t>(hi) << 16);
 }
 
 // u / d for 0 <= u < 2^21 from r = 1 / d rounded to fp32 (u + 1/2 is at least 1/(2 d) from a multiple of d, in
@@ -119,13 +103,11 @@ __device__ __forceinline__ void write_image(const FewArgs& a, int rows, int thre
         for (int u = 0; u < 8; ++u) am = fmaxf(am, fabsf(f[u]));
 #pragma unroll
         for (int o = 8; o > 0; o >>= 1) am = fmaxf(am, __shfl_xor_sync(kFull, am, o));
-        const float s = group_scale(am), inv = 1.0f / s;
-        uint2 q;
-        q.x = e4m3x4(quotient(f[0], s, inv), quotient(f[1], s, inv), quotient(f[2], s, inv), quotient(f[3], s, inv));
-        q.y = e4m3x4(quotient(f[4], s, inv), quotient(f[5], s, inv), quotient(f[6], s, inv), quotient(f[7], s, inv));
+        const GroupScale gs(am);
+        const uint2 q = make_uint2(e4m3x4(gs, f[0], f[1], f[2], f[3]), e4m3x4(gs, f[4], f[5], f[6], f[7]));
         uint8_t* step = a.ximg + static_cast<long long>(v >> 4) * step_bytes<true>(rows);
         *reinterpret_cast<uint2*>(step + swizzled(t, (v & 15) * 8)) = q;
-        if ((v & 15) == 0) *reinterpret_cast<float*>(step + rows * 128 + t * 4) = s;
+        if ((v & 15) == 0) *reinterpret_cast<float*>(step + rows * 128 + t * 4) = gs.s;
       }
     }
   }
@@ -619,11 +601,10 @@ __device__ __forceinline__ void write_h(const FewArgs& a, const FewSmem& s, cons
         float am = fmaxf(fmaxf(fabsf(h[0]), fabsf(h[1])), fmaxf(fabsf(h[2]), fabsf(h[3])));
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) am = fmaxf(am, __shfl_xor_sync(kFull, am, o));
-        const float sc = group_scale(am), inv = 1.0f / sc;
+        const GroupScale gs(am);
         uint8_t* step = img + static_cast<long long>(T.tile) * step_bytes<true>(m8);
-        *reinterpret_cast<uint32_t*>(step + swizzled(c, 4 * lane)) =
-            e4m3x4(quotient(h[0], sc, inv), quotient(h[1], sc, inv), quotient(h[2], sc, inv), quotient(h[3], sc, inv));
-        if (lane == 0) *reinterpret_cast<float*>(step + m8 * 128 + c * 4) = sc;
+        *reinterpret_cast<uint32_t*>(step + swizzled(c, 4 * lane)) = e4m3x4(gs, h[0], h[1], h[2], h[3]);
+        if (lane == 0) *reinterpret_cast<float*>(step + m8 * 128 + c * 4) = gs.s;
       } else {
         uint8_t* step = img + static_cast<long long>(2 * T.tile + (lane >> 4)) * step_bytes<false>(2 * m8);
         const uint32_t a0 = pack_bf16x2(h[0], h[1]), a1 = pack_bf16x2(h[2], h[3]);

@@ -536,18 +536,19 @@ cudaError_t fp8_gemm_launch(int epi, const CUtensorMap* maps, const Fp8Args& arg
 }
 
 bool encode_tmap_u8(CUtensorMap* map, const void* ptr, uint64_t rows, uint64_t cols, uint32_t box_rows,
-                    std::string* err) {
+                    std::string* err, uint64_t ld) {
+  if (ld == 0) ld = cols;
   EncodeFn fn = encode_fn();
   if (!fn) {
     if (err) *err = "cuTensorMapEncodeTiled is not available from the driver";
     return false;
   }
-  if ((reinterpret_cast<uintptr_t>(ptr) & 15u) != 0 || cols % 16 != 0 || rows == 0) {
+  if ((reinterpret_cast<uintptr_t>(ptr) & 15u) != 0 || ld % 16 != 0 || rows == 0) {
     if (err) *err = "tensor for TMA must be 16-byte aligned with 16-byte row stride and >= 1 row";
     return false;
   }
   const cuuint64_t dims[2] = {cols, rows};
-  const cuuint64_t strides[1] = {cols};
+  const cuuint64_t strides[1] = {ld};
   const cuuint32_t box[2] = {static_cast<cuuint32_t>(kFp8BK), box_rows};
   const cuuint32_t estr[2] = {1, 1};
   const CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(ptr), dims, strides, box, estr,

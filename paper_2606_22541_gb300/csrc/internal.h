@@ -156,13 +156,35 @@ constexpr int kFp8Boxes = 4;  // A maps of a problem: boxes of 32, 64, 96 and 12
 cudaError_t fp8_gemm_set_attributes();
 // maps: A0 and A1 (kFp8Boxes each; A1 may repeat A0 when m1 == 0).
 cudaError_t fp8_gemm_launch(int epi, const CUtensorMap* maps, const Fp8Args& args, int grid, cudaStream_t stream);
-// 2-D row-major byte tensor [rows, cols] for 128-byte-swizzled boxes of [box_rows, 128].
+// 2-D row-major byte tensor [rows, cols] for 128-byte-swizzled boxes of [box_rows, 128]; ld: bytes between rows
+// (0: cols).
 bool encode_tmap_u8(CUtensorMap* map, const void* ptr, uint64_t rows, uint64_t cols, uint32_t box_rows,
-                    std::string* err);
+                    std::string* err, uint64_t ld = 0);
 
 // Rows of bf16 -> e4m3 with one fp32 scale per row per 128 channels
 // (s = amax / 448, q = round-to-nearest-even of v / s, saturated).
 cudaError_t launch_quantize_rows(const void* x, int rows, int cols, void* q, float* s, cudaStream_t st);
+
+// ------------------------------------------------------------ FP8 matrix product and quantisers (fp8_ops.cu)
+// C [m, n] = A [m, k] B [n, k]^T, e4m3 with a scale per row per 128 columns (A:
+// sa [m][lds_a]) and per 128 x 128 block (B: sb [ceil(n/128)][lds_b]); C bf16.
+struct Fp8MatmulArgs {
+  int m, n, k;
+  const float* sa;
+  const float* sb;
+  long long lds_a, lds_b;
+  void* c;
+  long long ldc;
+  uint32_t* status;  // nullable
+};
+cudaError_t fp8_matmul_set_attributes();
+// The product; err names the operand that TMA cannot read.
+cudaError_t fp8_matmul_launch(const void* a, long long lda, const void* b, long long ldb, const Fp8MatmulArgs& args,
+                              int num_sms, cudaStream_t s, std::string* err);
+// Rows of bf16 (u: nullptr), or silu(x) * u, to e4m3 with an fp32 scale per row
+// per 128 columns.  Any alignment and strides.
+cudaError_t launch_fp8_quantize(const void* x, const void* u, int rows, int cols, long long ld, void* q,
+                                long long ldq, float* s, long long lds, cudaStream_t st);
 
 // ------------------------------------------------------------ routing
 struct GateParams {
