@@ -13,14 +13,16 @@ namespace {
 constexpr unsigned kFull = 0xffffffffu;
 
 // ------------------------------------------------------------ quantisers
-// A lane holds 8 consecutive columns, 16 lanes a group of 128; a warp works on
-// 256 columns of a row at a time, kAhead of them on their way.  W: columns per
-// load (8, 4 or 1, by the alignment of the rows).
-constexpr int kAhead = 4;
+// A lane holds 16 consecutive columns, 8 lanes a group of 128; a warp works on 512
+// columns of a row at a time, kAhead of them on their way.  W: columns per load
+// (8, 4 or 1, by the alignment of the rows).  The arithmetic per column would
+// bound a scalar kernel (45 us for 8045 rows of 7168), so quotients go in pairs
+// (f32x2) and bf16 magnitudes two to a register.
 constexpr int kQuantThreads = 256;
+constexpr int kQuantCols = 512;
 
 template <int W>
-__device__ __forceinline__ void load8(const uint16_t* p, int left, uint32_t (&v)[4]) {
+__device__ __forceinline__ void load8(const uint16_t* p, int left, uint32_t* v) {
   if constexpr (W == 8) {
     if (left >= 8) {
       asm volatile("ld.global.v4.b32 {%0, %1, %2, %3}, [%4];"
@@ -44,6 +46,33 @@ __device__ __forceinline__ void load8(const uint16_t* p, int left, uint32_t (&v)
   }
 }
 
+__device__ __forceinline__ uint64_t pair(float lo, float hi) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ float2 unpair(uint64_t p) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(p));
+  return r;
+}
+// The larger magnitude of each half (a NaN loses).
+__device__ __forceinline__ uint32_t max_abs2(uint32_t a, uint32_t b) {
+  const __nv_bfloat162 m = __hmax2(__habs2(*reinterpret_cast<const __nv_bfloat162*>(&a)),
+                                   __habs2(*reinterpret_cast<const __nv_bfloat162*>(&b)));
+  return *reinterpret_cast<const uint32_t*>(&m);
+}
+
 __device__ __forceinline__ float swiglu(float g, float u) { return g / (1.0f + __expf(-g)) * u; }
 
 template <bool SWIGLU, int W>
@@ -52,60 +81,99 @@ __global__ void __launch_bounds__(kQuantThreads) fp8_quantize_kernel(const uint1
                                                                     float* s, long long lds, bool wide_q) {
   pdl_wait();
   pdl_launch();
+  constexpr int kAhead = SWIGLU ? 2 : 3;
   const int lane = threadIdx.x & 31;
-  // (a tensor of 2^31 parts would not fit the GPU)
-  const uint32_t parts = (static_cast<uint32_t>(cols) + 255) / 256;  // of a row
-  const uint32_t total = static_cast<uint32_t>(rows) * parts;
-  const uint32_t warps = gridDim.x * (kQuantThreads / 32);
-  for (uint32_t i0 = blockIdx.x * (kQuantThreads / 32) + (threadIdx.x >> 5); i0 < total; i0 += warps * kAhead) {
-    uint32_t g[kAhead][4], up[kAhead][4];
+  const int parts = (cols + kQuantCols - 1) / kQuantCols;  // of a row
+  const int warps = gridDim.x * (kQuantThreads / 32);
+  const int first = blockIdx.x * (kQuantThreads / 32) + (threadIdx.x >> 5);
+  // the warp's units are first, first + warps, ... of rows * parts
+  const int dr = warps / parts, dp = warps % parts;
+  int row = first / parts, part = first % parts;
+  auto next = [&](int& r, int& p) {
+    r += dr;
+    p += dp;
+    if (p >= parts) p -= parts, ++r;
+  };
+  while (row < rows) {
+    uint32_t g[kAhead][8], up[SWIGLU ? kAhead : 1][8];
+    int r = row, p = part;
 #pragma unroll
-    for (int r = 0; r < kAhead; ++r) {
-      const uint32_t i = i0 + r * warps;
-      g[r][0] = g[r][1] = g[r][2] = g[r][3] = 0u;
-      up[r][0] = up[r][1] = up[r][2] = up[r][3] = 0u;
-      if (i < total) {
-        const long long row = i / parts;
-        const int c = static_cast<int>(i % parts) * 256 + lane * 8;
-        if (c < cols) {
-          load8<W>(x + row * ld + c, cols - c, g[r]);
-          if constexpr (SWIGLU) load8<W>(u + row * ld + c, cols - c, up[r]);
+    for (int i = 0; i < kAhead; ++i) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        g[i][j] = 0u;
+        if constexpr (SWIGLU) up[i][j] = 0u;
+      }
+      const int c = p * kQuantCols + lane * 16;
+      if (r < rows && c < cols) {
+        const long long at = r * ld + c;
+        load8<W>(x + at, cols - c, g[i]);
+        load8<W>(x + at + 8, cols - c - 8, g[i] + 4);
+        if constexpr (SWIGLU) {
+          load8<W>(u + at, cols - c, up[i]);
+          load8<W>(u + at + 8, cols - c - 8, up[i] + 4);
         }
       }
+      next(r, p);
     }
 #pragma unroll
-    for (int r = 0; r < kAhead; ++r) {
-      const uint32_t i = i0 + r * warps;
-      if (i >= total) break;
-      const long long row = i / parts;
-      const int c = static_cast<int>(i % parts) * 256 + lane * 8;
-      float f[8];
+    for (int i = 0; i < kAhead; ++i) {
+      if (row < rows) {
+        const int c = part * kQuantCols + lane * 16;
+        float f[16];
+        float am;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        f[2 * j] = bf16_lo(g[r][j]);
-        f[2 * j + 1] = bf16_hi(g[r][j]);
+        for (int j = 0; j < 8; ++j) {
+          f[2 * j] = bf16_lo(g[i][j]);
+          f[2 * j + 1] = bf16_hi(g[i][j]);
+        }
         if constexpr (SWIGLU) {
-          f[2 * j] = swiglu(f[2 * j], bf16_lo(up[r][j]));
-          f[2 * j + 1] = swiglu(f[2 * j + 1], bf16_hi(up[r][j]));
+          am = 0.f;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            f[2 * j] = swiglu(f[2 * j], bf16_lo(up[i][j]));
+            f[2 * j + 1] = swiglu(f[2 * j + 1], bf16_hi(up[i][j]));
+            am = fmaxf(am, fmaxf(fabsf(f[2 * j]), fabsf(f[2 * j + 1])));
+          }
+#pragma unroll
+          for (int o = 4; o > 0; o >>= 1) am = fmaxf(am, __shfl_xor_sync(kFull, am, o));
+        } else {
+          uint32_t m = max_abs2(max_abs2(max_abs2(g[i][0], g[i][1]), max_abs2(g[i][2], g[i][3])),
+                                max_abs2(max_abs2(g[i][4], g[i][5]), max_abs2(g[i][6], g[i][7])));
+#pragma unroll
+          for (int o = 4; o > 0; o >>= 1) m = max_abs2(m, __shfl_xor_sync(kFull, m, o));
+          am = fmaxf(fmaxf(bf16_lo(m), bf16_hi(m)), 0.f);  // (0 where there are only NaNs)
+        }
+        const GroupScale gs(am);
+        if (c < cols) {
+          const uint64_t inv = pair(gs.inv, gs.inv), neg = pair(-gs.scaled, -gs.scaled);
+          uint32_t w[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            uint64_t v0 = pair(f[4 * j], f[4 * j + 1]), v1 = pair(f[4 * j + 2], f[4 * j + 3]);
+            if (gs.up != 1.0f) {
+              const uint64_t by = pair(gs.up, gs.up);
+              v0 = mul2(v0, by);
+              v1 = mul2(v1, by);
+            }
+            uint64_t q0 = mul2(v0, inv), q1 = mul2(v1, inv);  // GroupScale's quotient, two at a time
+            q0 = fma2(fma2(q0, neg, v0), inv, q0);
+            q1 = fma2(fma2(q1, neg, v1), inv, q1);
+            const float2 a = unpair(q0), b = unpair(q1);
+            w[j] = e4m3x4(a.x, a.y, b.x, b.y);
+          }
+          uint8_t* out = q + row * ldq + c;
+          if (wide_q && cols - c >= 16) {
+            *reinterpret_cast<uint4*>(out) = make_uint4(w[0], w[1], w[2], w[3]);
+          } else {
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+              if (j < cols - c) out[j] = static_cast<uint8_t>(w[j >> 2] >> (8 * (j & 3)));
+          }
+          if ((lane & 7) == 0) s[row * lds + (c >> 7)] = gs.s;
         }
       }
-      float am = 0.f;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) am = fmaxf(am, fabsf(f[j]));
-#pragma unroll
-      for (int o = 8; o > 0; o >>= 1) am = fmaxf(am, __shfl_xor_sync(kFull, am, o));
-      const GroupScale gs(am);
-      if (c >= cols) continue;
-      const uint32_t w[2] = {e4m3x4(gs, f[0], f[1], f[2], f[3]), e4m3x4(gs, f[4], f[5], f[6], f[7])};
-      uint8_t* out = q + row * ldq + c;
-      if (wide_q && cols - c >= 8) {
-        *reinterpret_cast<uint2*>(out) = make_uint2(w[0], w[1]);
-      } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (j < cols - c) out[j] = static_cast<uint8_t>(w[j >> 2] >> (8 * (j & 3)));
-      }
-      if ((lane & 15) == 0) s[row * lds + (c >> 7)] = gs.s;
+      next(row, part);
     }
   }
 }
@@ -377,6 +445,301 @@ __global__ void __launch_bounds__(kThreads, 2)
   }
 }
 
+// ------------------------------------------------------------ product, rows of A as the M operand
+// A tile is 128 rows of A (M) and 256 of B (N).  Every 128-wide K block has one of
+// two TMEM partials of 256 columns, which eight epilogue warps add, times row and
+// block scale, into registers (warp w: TMEM lanes 32 (w % 4) .., one half of the
+// columns, i.e. one row of scale blocks), two 16-column chunks in turn, so that one
+// is on its way while the other is added.  Without K slices the CTAs are
+// persistent; otherwise a cluster of S CTAs shares a tile as above.
+//   warp 0: TMA producer; warp 1: TMEM and MMA; warps 4-11: epilogue, which takes
+//   registers from the first four warps (56 + 2 x 224 a thread).
+constexpr int kWideN = 256;
+constexpr int kWideStages = 4;
+constexpr int kWideStage = (kRows + kWideN) * kFp8BK;
+constexpr int kWidePartials = 2;
+constexpr int kWideThreads = 32 * 12;
+constexpr int kCtrlRegs = 56, kEpiRegs = 224;
+static_assert(kCtrlRegs + 2 * kEpiRegs <= 3 * 168, "the register split stays within the launch's registers");
+constexpr int kWideBars = 2 * kWideStages + 2 * kWidePartials + 1;
+constexpr int kStageWarp = 32 * 4 * 16;   // output staging of an epilogue warp
+constexpr int kSumPitch = kRows + 1;      // floats of a column of the slices' sums: rows and columns both meet every bank
+constexpr size_t kWideSmem = kWideStages * kWideStage + 8 * kStageWarp + 8 * kWideBars + 16;
+static_assert(kWideSmem <= 227 * 1024, "shared memory budget");
+static_assert(kWideN * kSumPitch * 4 <= kWideStages * kWideStage, "the sums fit the ring");
+
+struct WideArgs {
+  Fp8MatmulArgs p;
+  int split, m_tiles, tiles;
+  int wide_c;  // rows of c start on 16-byte boundaries
+};
+
+// Eight bf16 of row t from column n on, those of them that exist.
+__device__ __forceinline__ void store8(const Fp8MatmulArgs& p, int wide_c, int t, int n, const uint4& v) {
+  __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.c) + static_cast<long long>(t) * p.ldc + n;
+  if (t >= p.m) return;
+  if (wide_c && n + 8 <= p.n) {
+    *reinterpret_cast<uint4*>(out) = v;
+    return;
+  }
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+    if (n + j < p.n) reinterpret_cast<uint16_t*>(out)[j] = static_cast<uint16_t>(w[j >> 1] >> (16 * (j & 1)));
+}
+
+__device__ __forceinline__ void add16(float* acc, const uint32_t (&v)[16], float s) {
+#pragma unroll
+  for (int j = 0; j < 16; ++j) acc[j] = fmaf(s, __uint_as_float(v[j]), acc[j]);
+}
+
+__global__ void __launch_bounds__(kWideThreads, 1)
+    fp8_wide_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
+                    const WideArgs args) {
+  extern __shared__ __align__(1024) uint8_t smem_raw[];
+  const uint32_t base = smem_u32(smem_raw);
+  const Fp8MatmulArgs& p = args.p;
+  const bool aligned = (base & 1023u) == 0;  // the 128-byte swizzle needs it; the same in the cluster
+  const int S = args.split;
+  const int rank = blockIdx.x % S;
+  const int blocks = (p.k + kFp8BK - 1) / kFp8BK;
+  const int kb0 = static_cast<int>(static_cast<long long>(blocks) * rank / S);
+  const int kb1 = static_cast<int>(static_cast<long long>(blocks) * (rank + 1) / S);
+  const int step = gridDim.x / S;  // tiles between a CTA's
+  uint4* stage_all = reinterpret_cast<uint4*>(smem_raw + kWideStages * kWideStage);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem_raw + kWideStages * kWideStage + 8 * kStageWarp);
+  const uint32_t bar0 = smem_u32(bars);
+  auto full = [&](int i) { return bar0 + 8u * i; };
+  auto empty = [&](int i) { return bar0 + 8u * (kWideStages + i); };
+  auto pfull = [&](int i) { return bar0 + 8u * (2 * kWideStages + i); };
+  auto pempty = [&](int i) { return bar0 + 8u * (2 * kWideStages + kWidePartials + i); };
+  const uint32_t drain = bar0 + 8u * (kWideBars - 1);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + kWideBars);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < kWideStages; ++i) {
+      mbar_init(full(i), 1);
+      mbar_init(empty(i), 1);
+    }
+    for (int i = 0; i < kWidePartials; ++i) {
+      mbar_init(pfull(i), 1);
+      mbar_init(pempty(i), 8);
+    }
+    mbar_init(drain, 1);
+    *abort_flag = aligned ? 0 : 1;
+    fence_barrier_init();
+    tma_prefetch_desc(&tmA);
+    tma_prefetch_desc(&tmB);
+    if (!aligned) record_status(p.status, ST_SMEM_ALIGN);
+  } else if (warp == 1) {
+    tmem_alloc(smem_u32(tmem_slot), 512);
+    tmem_relinquish();
+  }
+  pdl_wait();
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  auto give_up = [&]() {
+    *abort_flag = 1;
+    record_status(p.status, ST_WAIT_TIMEOUT);
+  };
+
+  if (warp < 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kCtrlRegs));
+    if (warp == 0) {
+      const bool issuer = elect_one();
+      Ring<kWideStages> r;
+      const uint64_t pol = l2_policy(2);
+      int issued = 0;
+      bool ok = aligned;
+      for (int tile = blockIdx.x / S; ok && tile < args.tiles; tile += step) {
+        const int tok0 = tile % args.m_tiles * kRows, row0 = tile / args.m_tiles * kWideN;
+        for (int kb = kb0; kb < kb1; ++kb) {
+          ok = __all_sync(kFull, mbar_wait(empty(r.s), r.phase ^ 1u, abort_flag));
+          if (!ok) break;
+          if (issuer) {
+            const uint32_t st = base + r.s * kWideStage;
+            mbar_arrive_expect_tx(full(r.s), kWideStage);
+            tma_load_2d(st, &tmA, full(r.s), kb * kFp8BK, tok0, pol);
+            tma_load_2d(st + kRows * kFp8BK, &tmB, full(r.s), kb * kFp8BK, row0, pol);
+          }
+          issued = min(issued + 1, kWideStages);
+          r.advance();
+        }
+      }
+      if (issuer) pdl_launch();  // nothing left to load
+      if (!ok && aligned) {
+        if (issuer) give_up();
+        // the copies in flight land before the CTA's memory goes away
+        int dummy = 0;
+        for (int i = issued; i > 0; --i) {
+          const int b = r.s - i;
+          mbar_wait(full(b < 0 ? b + kWideStages : b), b < 0 ? r.phase ^ 1u : r.phase, &dummy);
+        }
+      }
+    } else if (warp == 1) {
+      const bool issuer = elect_one();
+      constexpr uint32_t id =
+          (1u << 4) | (static_cast<uint32_t>(kWideN >> 3) << 17) | (static_cast<uint32_t>(kRows >> 4) << 24);
+      Ring<kWideStages> r;
+      Ring<kWidePartials> t;
+      bool ok = aligned, issued = false;
+      for (int tile = blockIdx.x / S; ok && tile < args.tiles; tile += step) {
+        for (int kb = kb0; kb < kb1; ++kb) {
+          ok = mbar_wait_all(lane < 16 ? full(r.s) : pempty(t.s), lane < 16 ? r.phase : t.phase ^ 1u, abort_flag);
+          if (!ok) break;
+          tc_fence_after();
+          if (issuer) {
+            const uint64_t ad = smem_desc_sw128(base + r.s * kWideStage);
+            const uint64_t bd = smem_desc_sw128(base + r.s * kWideStage + kRows * kFp8BK);
+#pragma unroll
+            for (int kk = 0; kk < kFp8BK / 32; ++kk)
+              mma_e4m3(tmem_base + t.s * kWideN, ad + 2 * kk, bd + 2 * kk, id, kk > 0 ? 1u : 0u);
+            tc_commit(pfull(t.s));
+            tc_commit(empty(r.s));
+          }
+          __syncwarp();
+          issued = true;
+          r.advance();
+          t.advance();
+        }
+      }
+      if (!ok && aligned) {
+        if (lane == 0) give_up();
+        if (issued) {
+          int dummy = 0;
+          if (elect_one()) tc_commit(drain);
+          __syncwarp();
+          mbar_wait(drain, 0, &dummy);
+        }
+      }
+    }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kEpiRegs));
+    const int q = warp & 3, half = (warp - 4) >> 2;
+    const uint32_t col = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + half * 128;
+    uint4* stage = stage_all + (warp - 4) * (kStageWarp / 16);
+    Ring<kWidePartials> t;
+    bool ok = aligned;
+    for (int tile = blockIdx.x / S; tile < args.tiles; tile += step) {
+      const int tok0 = tile % args.m_tiles * kRows, row0 = tile / args.m_tiles * kWideN + half * 128;
+      float acc[128];
+#pragma unroll
+      for (int j = 0; j < 128; ++j) acc[j] = 0.f;
+      // (rows and columns that do not exist take the last one's scales; their products are zero)
+      const float* sa = p.sa + static_cast<long long>(min(tok0 + q * 32 + lane, p.m - 1)) * p.lds_a;
+      const float* sb = p.sb + static_cast<long long>(min(row0, p.n - 1) / 128) * p.lds_b;
+      float a0 = ld_dep(sa + kb0), b0 = ld_dep(sb + kb0), a1 = 0.f, b1 = 0.f;
+      if (kb0 + 1 < kb1) a1 = ld_dep(sa + kb0 + 1), b1 = ld_dep(sb + kb0 + 1);
+      uint32_t c0[16], c1[16];
+#pragma unroll
+      for (int j = 0; j < 16; ++j) c1[j] = 0u;
+      float s_prev = 0.f;
+      for (int kb = kb0; kb < kb1; ++kb) {
+        const float s = a0 * b0;
+        a0 = a1;
+        b0 = b1;
+        if (kb + 2 < kb1) a1 = ld_dep(sa + kb + 2), b1 = ld_dep(sb + kb + 2);
+        ok = ok && __all_sync(kFull, mbar_wait(pfull(t.s), t.phase, abort_flag));
+        if (!ok) break;
+        tc_fence_after();
+        const uint32_t ta = col + t.s * kWideN;
+        tmem_ld16(ta, c0);
+        add16(acc + 112, c1, s_prev);
+        tmem_ld_wait();
+        tmem_ld16(ta + 16, c1);
+        add16(acc + 0, c0, s);
+        tmem_ld_wait();
+        tmem_ld16(ta + 32, c0);
+        add16(acc + 16, c1, s);
+        tmem_ld_wait();
+        tmem_ld16(ta + 48, c1);
+        add16(acc + 32, c0, s);
+        tmem_ld_wait();
+        tmem_ld16(ta + 64, c0);
+        add16(acc + 48, c1, s);
+        tmem_ld_wait();
+        tmem_ld16(ta + 80, c1);
+        add16(acc + 64, c0, s);
+        tmem_ld_wait();
+        tmem_ld16(ta + 96, c0);
+        add16(acc + 80, c1, s);
+        tmem_ld_wait();
+        tmem_ld16(ta + 112, c1);
+        add16(acc + 96, c0, s);
+        tmem_ld_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(pempty(t.s));
+        s_prev = s;
+        t.advance();
+      }
+      if (!ok) break;
+      add16(acc + 112, c1, s_prev);
+      if (S == 1) {
+        // four rounds of 32 columns: a row's 64 bytes cross the warp's staging (chunk j of row r at slot
+        // j ^ ((r / 2) % 4): no bank conflicts) and leave as eight rows x 64 bytes per store instruction
+#pragma unroll
+        for (int rd = 0; rd < 4; ++rd) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float* v = acc + 32 * rd + 8 * j;
+            stage[lane * 4 + (j ^ ((lane >> 1) & 3))] = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]),
+                                                                   pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
+          }
+          __syncwarp();
+          const int cu = lane & 3;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int r = (lane >> 2) + 8 * i;
+            store8(p, args.wide_c, tok0 + q * 32 + r, row0 + 32 * rd + 8 * cu, stage[r * 4 + (cu ^ ((r >> 1) & 3))]);
+          }
+          __syncwarp();
+        }
+      } else {
+        cluster_sync();  // every CTA's ring is done with: the sums take its place
+        const int cols = kWideN / S;  // that a CTA adds
+        const int r = q * 32 + lane;
+        const float* sums = reinterpret_cast<const float*>(smem_raw);
+#pragma unroll
+        for (int j = 0; j < 128; ++j) {
+          const int c = half * 128 + j, to = c / cols;
+          const uint32_t at = map_rank(smem_u32(sums + (rank * cols + (c - to * cols)) * kSumPitch + r),
+                                       static_cast<uint32_t>(to));
+          asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at), "f"(acc[j]) : "memory");
+        }
+      }
+    }
+    if (!ok && aligned && lane == 0) give_up();
+    if (S > 1 && !ok) cluster_sync();  // (the barrier that the slices pass when all is well)
+  }
+  if (S > 1 && warp < 4) cluster_sync();
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem_base, 512);
+  }
+  if (S > 1) cluster_sync();
+  if (S > 1 && warp >= 4) {  // (the first warps' registers would not do)
+    const int tile = blockIdx.x / S, cols = kWideN / S;
+    const int tok0 = tile % args.m_tiles * kRows, n0 = tile / args.m_tiles * kWideN + rank * cols;
+    const float* sums = reinterpret_cast<const float*>(smem_raw);
+    __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.c);
+    for (int i = threadIdx.x - 128; i < cols * kRows; i += 256) {
+      const int c = i & (cols - 1), r = i / cols;
+      if (tok0 + r >= p.m || n0 + c >= p.n) continue;
+      float v = sums[c * kSumPitch + r];
+      for (int s = 1; s < S; ++s) v += sums[(s * cols + c) * kSumPitch + r];
+      out[static_cast<long long>(tok0 + r) * p.ldc + n0 + c] = __float2bfloat16_rn(v);
+    }
+  }
+}
+
 template <int NT>
 cudaError_t skinny(const CUtensorMap& tmA, const CUtensorMap& tmB, const Fp8MatmulArgs& args, int num_sms,
                    cudaStream_t s) {
@@ -387,6 +750,19 @@ cudaError_t skinny(const CUtensorMap& tmA, const CUtensorMap& tmB, const Fp8Matm
   while (a.split < kMaxSplit && tiles * a.split < 2 * num_sms && blocks / (2 * a.split) >= 4) a.split *= 2;
   return launch_pdl(fp8_skinny_kernel<NT>, dim3(static_cast<unsigned>(tiles * a.split)), dim3(kThreads),
                     Skinny<NT>::kSmem, s, a.split, tmA, tmB, a);
+}
+
+cudaError_t wide(const CUtensorMap& tmA, const CUtensorMap& tmB, const Fp8MatmulArgs& args, int num_sms,
+                 cudaStream_t s) {
+  const int blocks = ceil_div(args.k, kFp8BK);
+  WideArgs a{args, 1, ceil_div(args.m, kRows), 0, 0};
+  const long long tiles = static_cast<long long>(ceil_div(args.n, kWideN)) * a.m_tiles;
+  a.tiles = static_cast<int>(tiles);
+  a.wide_c = (reinterpret_cast<uintptr_t>(args.c) & 15u) == 0 && args.ldc % 8 == 0;
+  while (a.split < kMaxSplit && tiles * a.split * 2 <= num_sms && blocks / (2 * a.split) >= 4) a.split *= 2;
+  const long long grid = a.split > 1 ? tiles * a.split : std::min<long long>(tiles, num_sms);
+  return launch_pdl(fp8_wide_kernel, dim3(static_cast<unsigned>(grid)), dim3(kWideThreads), kWideSmem, s, a.split, tmA,
+                    tmB, a);
 }
 
 }  // namespace
@@ -400,19 +776,19 @@ cudaError_t fp8_matmul_set_attributes() {
   set(fp8_skinny_kernel<16>, Skinny<16>::kSmem);
   set(fp8_skinny_kernel<32>, Skinny<32>::kSmem);
   set(fp8_skinny_kernel<64>, Skinny<64>::kSmem);
-  set(fp8_skinny_kernel<128>, Skinny<128>::kSmem);
+  set(fp8_wide_kernel, kWideSmem);
   return e;
 }
 
 cudaError_t fp8_matmul_launch(const void* a, long long lda, const void* b, long long ldb, const Fp8MatmulArgs& args,
                               int num_sms, cudaStream_t s, std::string* err) {
   CUtensorMap tmA, tmB;
-  const int nt = args.m <= 16 ? 16 : args.m <= 32 ? 32 : args.m <= 64 ? 64 : 128;
+  const int nt = args.m <= 16 ? 16 : args.m <= 32 ? 32 : args.m <= 64 ? 64 : kRows;
   if (!encode_tmap_u8(&tmA, a, args.m, args.k, nt, err, lda)) {
     *err = "a: " + *err;
     return cudaErrorInvalidValue;
   }
-  if (!encode_tmap_u8(&tmB, b, args.n, args.k, kRows, err, ldb)) {
+  if (!encode_tmap_u8(&tmB, b, args.n, args.k, nt == kRows ? kWideN : kRows, err, ldb)) {
     *err = "b: " + *err;
     return cudaErrorInvalidValue;
   }
@@ -420,15 +796,15 @@ cudaError_t fp8_matmul_launch(const void* a, long long lda, const void* b, long 
     case 16: return skinny<16>(tmA, tmB, args, num_sms, s);
     case 32: return skinny<32>(tmA, tmB, args, num_sms, s);
     case 64: return skinny<64>(tmA, tmB, args, num_sms, s);
-    default: return skinny<128>(tmA, tmB, args, num_sms, s);
+    default: return wide(tmA, tmB, args, num_sms, s);
   }
 }
 
 cudaError_t launch_fp8_quantize(const void* x, const void* u, int rows, int cols, long long ld, void* q,
                                 long long ldq, float* s, long long lds, cudaStream_t st) {
   const uintptr_t at = reinterpret_cast<uintptr_t>(x) | reinterpret_cast<uintptr_t>(u) | static_cast<uintptr_t>(2 * ld);
-  const bool wide_q = ((reinterpret_cast<uintptr_t>(q) | static_cast<uintptr_t>(ldq)) & 7u) == 0;
-  const long long parts = static_cast<long long>(rows) * ceil_div(cols, 256);
+  const bool wide_q = ((reinterpret_cast<uintptr_t>(q) | static_cast<uintptr_t>(ldq)) & 15u) == 0;
+  const long long parts = static_cast<long long>(rows) * ceil_div(cols, kQuantCols);
   const unsigned grid = static_cast<unsigned>(std::min<long long>((parts + 7) / 8, 152 * 8));
   const uint16_t *xp = static_cast<const uint16_t*>(x), *up = static_cast<const uint16_t*>(u);
   uint8_t* qp = static_cast<uint8_t*>(q);
