@@ -417,7 +417,8 @@ int asap_moe_layer_batched_dyn(asap_moe_t h, const int32_t* layer_id, int32_t co
  * e4m3 operators on plain tensors: the dense layers around the MoE layers in
  * the number format of ASAP_FP8_E4M3_BLOCK128.  No handle, no workspace; they
  * launch on the caller's current device and only enqueue.  Strides (ld*) are in
- * elements between rows.  m, n, rows or cols of 0 is a successful no-op.
+ * elements between rows.  m, n, rows or cols of 0 is a successful no-op; none
+ * may exceed 2^30.
  * Outputs must not overlap inputs.
  * ------------------------------------------------------------------------ */
 

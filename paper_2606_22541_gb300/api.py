@@ -23,8 +23,9 @@ _timing = threading.local()
 
 
 def _stream(stream):
-    s = torch.cuda.current_stream() if stream is None else stream
-    return ctypes.c_void_p(s.cuda_stream)
+    if stream is None:  # (the current stream's handle without its Python object, which takes 3 us to make)
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    return stream.cuda_stream
 
 
 def make_config(cfg, max_tokens):
@@ -252,54 +253,55 @@ def asap_moe_route_noalloc(h, x, idx, w, counts, offsets, stream=None):
                                        _ptr(offsets), _stream(stream)))
 
 
-def _matrix(name, t, dtypes):
-    """Pointer and row stride of a 2-D tensor whose columns are contiguous."""
-    if t.dim() != 2 or t.dtype not in dtypes or not t.is_cuda:
-        raise ValueError(f"{name}: a 2-D CUDA tensor of {' or '.join(str(d) for d in dtypes)}, got "
-                         f"{tuple(t.shape)} {t.dtype} on {t.device}")
-    if t.shape[1] > 1 and t.stride(1) != 1:
-        raise ValueError(f"{name}: columns must be contiguous, got strides {tuple(t.stride())}")
-    # (a single row's stride says nothing: one that any row may have)
-    return _ptr(t), t.stride(0) if t.shape[0] > 1 else -(-t.shape[1] // 16) * 16
+def _e4m3(t):
+    return t.dtype is torch.float8_e4m3fn or t.dtype is torch.uint8
 
 
-_E4M3 = (torch.float8_e4m3fn, torch.uint8)
-_BF16 = (torch.bfloat16,)
-_F32 = (torch.float32,)
+def _ld(t):
+    """Row stride of a 2-D CUDA tensor whose columns are contiguous, else 0.  (A
+    single row's stride says nothing: one that any row may have.)"""
+    s0, s1 = t.stride()
+    rows, cols = t.shape
+    if not t.is_cuda or (s1 != 1 and cols > 1):
+        return 0
+    return s0 if rows > 1 else (cols + 15) // 16 * 16
 
 
-def _shape(name, t, rows, cols):
-    if tuple(t.shape) != (rows, cols):
-        raise ValueError(f"{name}: shape ({rows}, {cols}) expected, got {tuple(t.shape)}")
+def _refuse(what, **tensors):
+    raise ValueError(what + "; got " + ", ".join(
+        f"{k} {tuple(t.shape)} {t.dtype} strides {tuple(t.stride())} on {t.device}" for k, t in tensors.items()))
 
 
 def asap_moe_fp8_quantize(x, q, scales, stream=None):
     """bf16 rows x [n, c] to e4m3 q [n, c] with scales [n, ceil(c / 128)]
     (fp32); any row strides."""
+    if x.dim() != 2 or x.dtype is not torch.bfloat16 or q.shape != x.shape or not _e4m3(q) or \
+            scales.dtype is not torch.float32 or scales.shape != (x.shape[0], (x.shape[1] + 127) // 128):
+        _refuse("x [n, c] bf16, q [n, c] e4m3, scales [n, ceil(c / 128)] fp32", x=x, q=q, scales=scales)
     n, c = x.shape
-    _shape("q", q, n, c)
-    _shape("scales", scales, n, -(-c // 128))
-    px, ldx = _matrix("x", x, _BF16)
-    pq, ldq = _matrix("q", q, _E4M3)
-    ps, lds = _matrix("scales", scales, _F32)
-    check("asap_moe_fp8_quantize", lib().asap_moe_fp8_quantize(px, ldx, n, c, pq, ldq, ps, lds, _stream(stream)))
+    ld, ldq, lds = _ld(x), _ld(q), _ld(scales)
+    if not (ld and ldq and lds) and n and c:
+        _refuse("CUDA tensors with contiguous columns", x=x, q=q, scales=scales)
+    check("asap_moe_fp8_quantize", lib().asap_moe_fp8_quantize(x.data_ptr(), ld, n, c, q.data_ptr(), ldq,
+                                                               scales.data_ptr(), lds, _stream(stream)))
 
 
 def asap_moe_fp8_swiglu_quantize(gate, up, q, scales, stream=None):
     """silu(gate) * up of bf16 [n, c] tensors with one row stride (the halves of
     a product's rows) to e4m3 q [n, c] with scales [n, ceil(c / 128)]."""
+    if gate.dim() != 2 or gate.dtype is not torch.bfloat16 or up.shape != gate.shape or \
+            up.dtype is not torch.bfloat16 or q.shape != gate.shape or not _e4m3(q) or \
+            scales.dtype is not torch.float32 or scales.shape != (gate.shape[0], (gate.shape[1] + 127) // 128):
+        _refuse("gate, up [n, c] bf16, q [n, c] e4m3, scales [n, ceil(c / 128)] fp32", gate=gate, up=up, q=q,
+                scales=scales)
     n, c = gate.shape
-    _shape("up", up, n, c)
-    _shape("q", q, n, c)
-    _shape("scales", scales, n, -(-c // 128))
-    pg, ld = _matrix("gate", gate, _BF16)
-    pu, ldu = _matrix("up", up, _BF16)
-    if ldu != ld:
-        raise ValueError(f"gate and up must have one row stride, got {ld} and {ldu}")
-    pq, ldq = _matrix("q", q, _E4M3)
-    ps, lds = _matrix("scales", scales, _F32)
+    ld, ldu, ldq, lds = _ld(gate), _ld(up), _ld(q), _ld(scales)
+    if not (ld and ldu == ld and ldq and lds) and n and c:
+        _refuse("CUDA tensors with contiguous columns, gate and up with one row stride", gate=gate, up=up, q=q,
+                scales=scales)
     check("asap_moe_fp8_swiglu_quantize",
-          lib().asap_moe_fp8_swiglu_quantize(pg, pu, ld, n, c, pq, ldq, ps, lds, _stream(stream)))
+          lib().asap_moe_fp8_swiglu_quantize(gate.data_ptr(), up.data_ptr(), ld, n, c, q.data_ptr(), ldq,
+                                             scales.data_ptr(), lds, _stream(stream)))
 
 
 def asap_moe_fp8_matmul(a, a_scales, b, b_scales, out, stream=None, status=None):
@@ -307,19 +309,22 @@ def asap_moe_fp8_matmul(a, a_scales, b, b_scales, out, stream=None, status=None)
     boundaries) with fp32 scales [m, ceil(k / 128)] and [ceil(n / 128),
     ceil(k / 128)].  status: None or a one-element int32 CUDA tensor that gets
     error bits."""
+    if a.dim() != 2 or b.dim() != 2:
+        _refuse("a [m, k], b [n, k]", a=a, b=b)
     (m, k), n = a.shape, b.shape[0]
-    _shape("b", b, n, k)
-    _shape("out", out, m, n)
-    _shape("a_scales", a_scales, m, -(-k // 128))
-    _shape("b_scales", b_scales, -(-n // 128), -(-k // 128))
-    pa, lda = _matrix("a", a, _E4M3)
-    pb, ldb = _matrix("b", b, _E4M3)
-    psa, lsa = _matrix("a_scales", a_scales, _F32)
-    psb, lsb = _matrix("b_scales", b_scales, _F32)
-    pc, ldc = _matrix("out", out, _BF16)
+    blocks = (k + 127) // 128
+    if not _e4m3(a) or not _e4m3(b) or b.shape[1] != k or out.dtype is not torch.bfloat16 or out.shape != (m, n) or \
+            a_scales.dtype is not torch.float32 or a_scales.shape != (m, blocks) or \
+            b_scales.dtype is not torch.float32 or b_scales.shape != ((n + 127) // 128, blocks):
+        _refuse("a [m, k], b [n, k] e4m3, a_scales [m, ceil(k / 128)], b_scales [ceil(n / 128), ceil(k / 128)] fp32, "
+                "out [m, n] bf16", a=a, a_scales=a_scales, b=b, b_scales=b_scales, out=out)
+    lda, lsa, ldb, lsb, ldc = _ld(a), _ld(a_scales), _ld(b), _ld(b_scales), _ld(out)
+    if not (lda and lsa and ldb and lsb and ldc) and m and n and k:
+        _refuse("CUDA tensors with contiguous columns", a=a, a_scales=a_scales, b=b, b_scales=b_scales, out=out)
     check("asap_moe_fp8_matmul",
-          lib().asap_moe_fp8_matmul(pa, lda, psa, lsa, pb, ldb, psb, lsb, pc, ldc, m, n, k, _ptr(status),
-                                    _stream(stream)))
+          lib().asap_moe_fp8_matmul(a.data_ptr(), lda, a_scales.data_ptr(), lsa, b.data_ptr(), ldb,
+                                    b_scales.data_ptr(), lsb, out.data_ptr(), ldc, m, n, k,
+                                    None if status is None else status.data_ptr(), _stream(stream)))
 
 
 class Mailbox:

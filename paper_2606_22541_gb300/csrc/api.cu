@@ -1455,33 +1455,41 @@ ASAP_API int asap_moe_layer_batched_dyn(asap_moe_t h, const int32_t* layer_id, i
 
 namespace {
 
-// Device the calls without a handle launch on: its SM count, and the kernels'
-// attributes set on it, once per device.
-int matmul_device(int* num_sms) {
+// What the product needs to know of a device, found out once per device.
+struct MatmulDevice {
+  bool known = false;
+  int num_sms = 0;
+};
+
+int matmul_device(MatmulDevice* out) {
   static std::mutex lock;
-  static std::vector<int> sms;  // by device, 0: not looked at yet
+  static std::vector<MatmulDevice> devices;
   int dev = 0;
   CU_TRY(cudaGetDevice(&dev), "cudaGetDevice");
   std::lock_guard<std::mutex> g(lock);
-  if (static_cast<size_t>(dev) >= sms.size()) sms.resize(dev + 1, 0);
-  if (sms[dev] == 0) {
-    int major = 0, minor = 0, n = 0;
+  if (static_cast<size_t>(dev) >= devices.size()) devices.resize(dev + 1);
+  MatmulDevice& d = devices[dev];
+  if (!d.known) {
+    int major = 0, minor = 0;
     CU_TRY(cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev), "compute capability");
     CU_TRY(cudaDeviceGetAttribute(&minor, cudaDevAttrComputeCapabilityMinor, dev), "compute capability");
     if (major != 10 || minor != 3)
       return fail(ASAP_ERR_UNSUPPORTED, "libasap_moe is built for sm_103a (GB300) only; device is sm_" +
                                             std::to_string(major) + std::to_string(minor));
-    CU_TRY(cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev), "SM count");
+    CU_TRY(cudaDeviceGetAttribute(&d.num_sms, cudaDevAttrMultiProcessorCount, dev), "SM count");
     CU_TRY(asap::fp8_matmul_set_attributes(), "product attributes");
-    sms[dev] = n;
+    d.known = true;
   }
-  *num_sms = sms[dev];
+  *out = d;
   return ASAP_OK;
 }
 
+constexpr int kMaxExtent = 1 << 30;  // of a plain tensor: the kernels' 32-bit row indices run past it by a step
+
 int run_quantize(const void* x, const void* u, bool swiglu, int64_t ldx, int32_t rows, int32_t cols, void* q, int64_t ldq,
                  float* scales, int64_t lds, void* stream) {
-  if (rows < 0 || cols < 0) return fail(ASAP_ERR_INVALID, "negative rows or cols");
+  if (rows < 0 || cols < 0 || rows > kMaxExtent || cols > kMaxExtent)
+    return fail(ASAP_ERR_INVALID, "rows and cols must be in [0, 2^30]");
   if (rows == 0 || cols == 0) return ASAP_OK;
   if (!x || (swiglu && !u) || !q || !scales) return fail(ASAP_ERR_INVALID, "NULL tensor");
   if (ldx < cols || ldq < cols || lds < asap::ceil_div(cols, 128))
@@ -1508,7 +1516,8 @@ ASAP_API int asap_moe_fp8_swiglu_quantize(const void* gate, const void* up, int6
 ASAP_API int asap_moe_fp8_matmul(const void* a, int64_t lda, const float* a_scales, int64_t lds_a, const void* b,
                                  int64_t ldb, const float* b_scales, int64_t lds_b, void* c, int64_t ldc, int32_t m,
                                  int32_t n, int32_t k, uint32_t* status, void* stream) {
-  if (m < 0 || n < 0 || k < 1) return fail(ASAP_ERR_INVALID, "m and n must be at least 0, k at least 1");
+  if (m < 0 || n < 0 || k < 1 || m > kMaxExtent || n > kMaxExtent || k > kMaxExtent)
+    return fail(ASAP_ERR_INVALID, "m and n must be in [0, 2^30], k in [1, 2^30]");
   if (m == 0 || n == 0) return ASAP_OK;
   if (!a || !a_scales || !b || !b_scales || !c) return fail(ASAP_ERR_INVALID, "NULL tensor");
   if (!aligned16(a) || !aligned16(b) || lda % 16 != 0 || ldb % 16 != 0)
@@ -1520,8 +1529,8 @@ ASAP_API int asap_moe_fp8_matmul(const void* a, int64_t lda, const float* a_scal
   const int blocks = asap::ceil_div(k, 128);
   if (lda < k || ldb < k || ldc < n || lds_a < blocks || lds_b < blocks)
     return fail(ASAP_ERR_INVALID, "a row stride is shorter than its rows");
-  int num_sms = 0;
-  const int r = matmul_device(&num_sms);
+  MatmulDevice dev;
+  const int r = matmul_device(&dev);
   if (r != ASAP_OK) return r;
   asap::Fp8MatmulArgs args{};
   args.m = m;
@@ -1535,7 +1544,7 @@ ASAP_API int asap_moe_fp8_matmul(const void* a, int64_t lda, const float* a_scal
   args.ldc = ldc;
   args.status = status;
   std::string err;
-  const cudaError_t e = asap::fp8_matmul_launch(a, lda, b, ldb, args, num_sms, S(stream), &err);
+  const cudaError_t e = asap::fp8_matmul_launch(a, lda, b, ldb, args, dev.num_sms, S(stream), &err);
   if (!err.empty()) return fail(ASAP_ERR_INVALID, err);
   if (e != cudaSuccess) return cuda_fail(e, "product launch");
   return ASAP_OK;

@@ -13,13 +13,15 @@ namespace {
 constexpr unsigned kFull = 0xffffffffu;
 
 // ------------------------------------------------------------ quantisers
-// A lane holds 16 consecutive columns, 8 lanes a group of 128; a warp works on 512
-// columns of a row at a time, kAhead of them on their way.  W: columns per load
-// (8, 4 or 1, by the alignment of the rows).  The arithmetic per column would
-// bound a scalar kernel (45 us for 8045 rows of 7168), so quotients go in pairs
-// (f32x2) and bf16 magnitudes two to a register.
+// A team of 8 lanes takes a group of 128 columns, 16 to a lane; a warp's four teams
+// take groups that follow one another.  W: columns per load (8, 4 or 1, by the
+// alignment of the rows).  The arithmetic per column would bound a scalar kernel
+// (45 us for 8045 rows of 7168), so quotients go in pairs (f32x2) and bf16
+// magnitudes two to a register.  Loads are hidden by eight CTAs an SM rather than
+// by several groups of a team on their way, whose registers cost more (1, 2 and 4
+// groups: 29.5, 33 and 35 us; SwiGLU of 4014 rows of 4096: 16, 18 and 23).
 constexpr int kQuantThreads = 256;
-constexpr int kQuantCols = 512;
+constexpr int kTeam = 8;
 
 template <int W>
 __device__ __forceinline__ void load8(const uint16_t* p, int left, uint32_t* v) {
@@ -73,108 +75,92 @@ __device__ __forceinline__ uint32_t max_abs2(uint32_t a, uint32_t b) {
   return *reinterpret_cast<const uint32_t*>(&m);
 }
 
-__device__ __forceinline__ float swiglu(float g, float u) { return g / (1.0f + __expf(-g)) * u; }
+__device__ __forceinline__ float swiglu(float g, float u) { return __fdividef(g, 1.0f + __expf(-g)) * u; }
 
 template <bool SWIGLU, int W>
-__global__ void __launch_bounds__(kQuantThreads) fp8_quantize_kernel(const uint16_t* x, const uint16_t* u, int rows,
+__global__ void __launch_bounds__(kQuantThreads, 8) fp8_quantize_kernel(const uint16_t* x, const uint16_t* u, int rows,
                                                                     int cols, long long ld, uint8_t* q, long long ldq,
                                                                     float* s, long long lds, bool wide_q) {
   pdl_wait();
   pdl_launch();
-  constexpr int kAhead = SWIGLU ? 2 : 3;
-  const int lane = threadIdx.x & 31;
-  const int parts = (cols + kQuantCols - 1) / kQuantCols;  // of a row
-  const int warps = gridDim.x * (kQuantThreads / 32);
-  const int first = blockIdx.x * (kQuantThreads / 32) + (threadIdx.x >> 5);
-  // the warp's units are first, first + warps, ... of rows * parts
-  const int dr = warps / parts, dp = warps % parts;
-  int row = first / parts, part = first % parts;
-  auto next = [&](int& r, int& p) {
-    r += dr;
-    p += dp;
-    if (p >= parts) p -= parts, ++r;
-  };
-  while (row < rows) {
-    uint32_t g[kAhead][8], up[SWIGLU ? kAhead : 1][8];
-    int r = row, p = part;
+  const int lane = threadIdx.x & (kTeam - 1);
+  const int groups = (cols + 127) / 128;  // of a row
+  const int teams = gridDim.x * (kQuantThreads / kTeam);
+  const int first = blockIdx.x * (kQuantThreads / kTeam) + threadIdx.x / kTeam;
+  // the team's groups are first, first + teams, ... of rows * groups
+  const int dr = teams / groups, dg = teams % groups;
+  int row = first / groups, grp = first % groups;
+  // (a warp's teams leave together: their shuffles name the whole warp)
+  while (__any_sync(kFull, row < rows)) {
+    uint32_t g[8], up[8];
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
+    for (int j = 0; j < 8; ++j) g[j] = up[j] = 0u;
+    const int c = grp * 128 + lane * 16;
+    const bool in = row < rows && c < cols;
+    if (in) {
+      const long long at = row * ld + c;
+      load8<W>(x + at, cols - c, g);
+      load8<W>(x + at + 8, cols - c - 8, g + 4);
+      if constexpr (SWIGLU) {
+        load8<W>(u + at, cols - c, up);
+        load8<W>(u + at + 8, cols - c - 8, up + 4);
+      }
+    }
+    float f[16];
+    float am;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      f[2 * j] = bf16_lo(g[j]);
+      f[2 * j + 1] = bf16_hi(g[j]);
+    }
+    if constexpr (SWIGLU) {
+      am = 0.f;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        g[i][j] = 0u;
-        if constexpr (SWIGLU) up[i][j] = 0u;
+        f[2 * j] = swiglu(f[2 * j], bf16_lo(up[j]));
+        f[2 * j + 1] = swiglu(f[2 * j + 1], bf16_hi(up[j]));
+        am = fmaxf(am, fmaxf(fabsf(f[2 * j]), fabsf(f[2 * j + 1])));
       }
-      const int c = p * kQuantCols + lane * 16;
-      if (r < rows && c < cols) {
-        const long long at = r * ld + c;
-        load8<W>(x + at, cols - c, g[i]);
-        load8<W>(x + at + 8, cols - c - 8, g[i] + 4);
-        if constexpr (SWIGLU) {
-          load8<W>(u + at, cols - c, up[i]);
-          load8<W>(u + at + 8, cols - c - 8, up[i] + 4);
-        }
-      }
-      next(r, p);
+#pragma unroll
+      for (int o = kTeam / 2; o > 0; o >>= 1) am = fmaxf(am, __shfl_xor_sync(kFull, am, o));
+    } else {
+      uint32_t m = max_abs2(max_abs2(max_abs2(g[0], g[1]), max_abs2(g[2], g[3])),
+                            max_abs2(max_abs2(g[4], g[5]), max_abs2(g[6], g[7])));
+#pragma unroll
+      for (int o = kTeam / 2; o > 0; o >>= 1) m = max_abs2(m, __shfl_xor_sync(kFull, m, o));
+      am = fmaxf(fmaxf(bf16_lo(m), bf16_hi(m)), 0.f);  // (0 where there are only NaNs)
     }
+    const GroupScale gs(am);
+    if (in) {
+      const uint64_t inv = pair(gs.inv, gs.inv), neg = pair(-gs.scaled, -gs.scaled);
+      uint32_t w[4];
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
-      if (row < rows) {
-        const int c = part * kQuantCols + lane * 16;
-        float f[16];
-        float am;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          f[2 * j] = bf16_lo(g[i][j]);
-          f[2 * j + 1] = bf16_hi(g[i][j]);
+      for (int j = 0; j < 4; ++j) {
+        uint64_t v0 = pair(f[4 * j], f[4 * j + 1]), v1 = pair(f[4 * j + 2], f[4 * j + 3]);
+        if (gs.up != 1.0f) {
+          const uint64_t by = pair(gs.up, gs.up);
+          v0 = mul2(v0, by);
+          v1 = mul2(v1, by);
         }
-        if constexpr (SWIGLU) {
-          am = 0.f;
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            f[2 * j] = swiglu(f[2 * j], bf16_lo(up[i][j]));
-            f[2 * j + 1] = swiglu(f[2 * j + 1], bf16_hi(up[i][j]));
-            am = fmaxf(am, fmaxf(fabsf(f[2 * j]), fabsf(f[2 * j + 1])));
-          }
-#pragma unroll
-          for (int o = 4; o > 0; o >>= 1) am = fmaxf(am, __shfl_xor_sync(kFull, am, o));
-        } else {
-          uint32_t m = max_abs2(max_abs2(max_abs2(g[i][0], g[i][1]), max_abs2(g[i][2], g[i][3])),
-                                max_abs2(max_abs2(g[i][4], g[i][5]), max_abs2(g[i][6], g[i][7])));
-#pragma unroll
-          for (int o = 4; o > 0; o >>= 1) m = max_abs2(m, __shfl_xor_sync(kFull, m, o));
-          am = fmaxf(fmaxf(bf16_lo(m), bf16_hi(m)), 0.f);  // (0 where there are only NaNs)
-        }
-        const GroupScale gs(am);
-        if (c < cols) {
-          const uint64_t inv = pair(gs.inv, gs.inv), neg = pair(-gs.scaled, -gs.scaled);
-          uint32_t w[4];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            uint64_t v0 = pair(f[4 * j], f[4 * j + 1]), v1 = pair(f[4 * j + 2], f[4 * j + 3]);
-            if (gs.up != 1.0f) {
-              const uint64_t by = pair(gs.up, gs.up);
-              v0 = mul2(v0, by);
-              v1 = mul2(v1, by);
-            }
-            uint64_t q0 = mul2(v0, inv), q1 = mul2(v1, inv);  // GroupScale's quotient, two at a time
-            q0 = fma2(fma2(q0, neg, v0), inv, q0);
-            q1 = fma2(fma2(q1, neg, v1), inv, q1);
-            const float2 a = unpair(q0), b = unpair(q1);
-            w[j] = e4m3x4(a.x, a.y, b.x, b.y);
-          }
-          uint8_t* out = q + row * ldq + c;
-          if (wide_q && cols - c >= 16) {
-            *reinterpret_cast<uint4*>(out) = make_uint4(w[0], w[1], w[2], w[3]);
-          } else {
-#pragma unroll
-            for (int j = 0; j < 16; ++j)
-              if (j < cols - c) out[j] = static_cast<uint8_t>(w[j >> 2] >> (8 * (j & 3)));
-          }
-          if ((lane & 7) == 0) s[row * lds + (c >> 7)] = gs.s;
-        }
+        uint64_t q0 = mul2(v0, inv), q1 = mul2(v1, inv);  // GroupScale's quotient, two at a time
+        q0 = fma2(fma2(q0, neg, v0), inv, q0);
+        q1 = fma2(fma2(q1, neg, v1), inv, q1);
+        const float2 a = unpair(q0), b = unpair(q1);
+        w[j] = e4m3x4(a.x, a.y, b.x, b.y);
       }
-      next(row, part);
+      uint8_t* out = q + row * ldq + c;
+      if (wide_q && cols - c >= 16) {
+        *reinterpret_cast<uint4*>(out) = make_uint4(w[0], w[1], w[2], w[3]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+          if (j < cols - c) out[j] = static_cast<uint8_t>(w[j >> 2] >> (8 * (j & 3)));
+      }
+      if (lane == 0) s[row * lds + grp] = gs.s;
     }
+    row += dr;
+    grp += dg;
+    if (grp >= groups) grp -= groups, ++row;
   }
 }
 
@@ -183,7 +169,13 @@ __global__ void __launch_bounds__(kQuantThreads) fp8_quantize_kernel(const uint1
 // cluster of S CTAs shares a tile, each with a slice of K.  Every 128-wide K block
 // is multiplied into one of the TMEM partials, which the epilogue warps add, times
 // the block's scales, into registers; the slices' sums meet in distributed shared
-// memory, each CTA adding those of NT / S columns in rank order.
+// memory, each CTA adding those of 128 / S rows in rank order.  They travel by
+// st.async, counted by the receiver's mbarrier (with plain stores between cluster
+// barriers one row x 4096 x 7168 took 10 us on eight slices, 8 so).  Two CTAs an
+// SM, so that one's start and end pass beside the other's stream; persistent
+// CTAs, one an SM with a ring twice as deep and the sums of a tile exchanged while
+// the next one streams, took 8.9 us there and 30 instead of 24 for 45 rows x 28672
+// x 4096: their four epilogue warps are a CTA's only ones.
 //   warp 0: TMA producer; warp 1: TMEM and MMA; warps 2-5: epilogue, one TMEM
 //   lane quarter (32 rows of B) each.
 constexpr int kRows = 128;
@@ -195,14 +187,14 @@ constexpr int kMaxSplit = 8;
 template <int NT>
 struct Skinny {
   static constexpr int kStage = kBBytes + NT * kFp8BK;
-  static constexpr int kStages = NT <= 32 ? 5 : NT == 64 ? 4 : 3;  // about 100 KB: two CTAs an SM
-  static constexpr int kPartials = NT <= 32 ? 4 : 256 / NT;
+  static constexpr int kStages = NT == 16 ? 5 : NT == 32 ? 4 : 3;  // about 100 KB
+  static constexpr int kPartials = 4;
   static constexpr uint32_t kTmem = NT * kPartials;
-  static constexpr bool kAlias = NT >= 64;  // the slices' sums take the ring's place
-  static constexpr int kSums = kRows * NT * 4;
-  static constexpr int kBars = 2 * kStages + 2 * kPartials + 1;
-  static constexpr size_t kSmem = kStages * kStage + (kAlias ? 0 : kSums) + 2 * NT * 4 + 8 * kBars + 16;
-  static_assert(!kAlias || kSums <= kStages * kStage, "the sums fit the ring");
+  static constexpr int kPitch = NT + 4;  // floats of a row of the slices' sums
+  static constexpr int kSums = kRows * kPitch;
+  static constexpr int kBars = 2 * kStages + 2 * kPartials + 2;
+  static constexpr size_t kSmem = kStages * kStage + 4 * kSums + 2 * NT * 4 + 8 * kBars + 16;
+  static_assert(2 * (kSmem + 1024) <= 228 * 1024, "two CTAs an SM");
 };
 
 struct SkinnyArgs {
@@ -215,9 +207,23 @@ __device__ __forceinline__ uint32_t map_rank(uint32_t addr, uint32_t rank) {
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(d) : "r"(addr), "r"(rank));
   return d;
 }
-__device__ __forceinline__ void cluster_sync() {
-  asm volatile("barrier.cluster.arrive.release;" ::: "memory");
-  asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+// Barrier of the cluster's threads; the first orders no memory (barriers are
+// initialised with a fence of their own).
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory"); }
+__device__ __forceinline__ void cluster_arrive_release() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait;" ::: "memory"); }
+// Arrive on a barrier of the cluster's CTA that addr names (map_rank).  Neither
+// this nor the waits take cluster scope, which stalls a thread for thousands of
+// cycles behind the loads in flight: what they order is counted in bytes or has
+// been seen to be done.
+__device__ __forceinline__ void mbar_arrive_remote(uint32_t addr) {
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(addr) : "memory");
+}
+// 16 bytes into a CTA of the cluster; its barrier counts them when they are visible there.
+__device__ __forceinline__ void send4(uint32_t addr, uint32_t bar, float a, float b, float c, float d) {
+  asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%2, %3, %4, %5}, [%1];" ::"r"(addr),
+               "r"(bar), "f"(a), "f"(b), "f"(c), "f"(d)
+               : "memory");
 }
 __device__ __forceinline__ void mma_e4m3(uint32_t d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t acc) {
   asm volatile(
@@ -245,15 +251,17 @@ __global__ void __launch_bounds__(kThreads, 2)
   const int blocks = (p.k + kFp8BK - 1) / kFp8BK;
   const int kb0 = static_cast<int>(static_cast<long long>(blocks) * rank / S);
   const int kb1 = static_cast<int>(static_cast<long long>(blocks) * (rank + 1) / S);
-  float* sums = reinterpret_cast<float*>(smem_raw + (C::kAlias ? 0 : C::kStages * C::kStage));  // [src][column][row]
-  float* scales = reinterpret_cast<float*>(smem_raw + C::kStages * C::kStage + (C::kAlias ? 0 : C::kSums));  // [2][NT]
+  float* sums = reinterpret_cast<float*>(smem_raw + C::kStages * C::kStage);  // [slice][row][column]
+  float* scales = sums + C::kSums;                                            // [2][NT]
   uint64_t* bars = reinterpret_cast<uint64_t*>(scales + 2 * NT);
   const uint32_t bar0 = smem_u32(bars);
   auto full = [&](int i) { return bar0 + 8u * i; };
   auto empty = [&](int i) { return bar0 + 8u * (C::kStages + i); };
   auto pfull = [&](int i) { return bar0 + 8u * (2 * C::kStages + i); };
   auto pempty = [&](int i) { return bar0 + 8u * (2 * C::kStages + C::kPartials + i); };
-  const uint32_t drain = bar0 + 8u * (C::kBars - 1);
+  const uint32_t drain = bar0 + 8u * (C::kBars - 2), received = drain + 8u;
+  const int rows = kRows / S;                        // whose sums this CTA adds
+  const int cols4 = (min(NT, p.m - tok0) + 3) / 4;   // groups of columns that travel
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + C::kBars);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -268,16 +276,20 @@ __global__ void __launch_bounds__(kThreads, 2)
       mbar_init(pempty(i), 4);
     }
     mbar_init(drain, 1);
+    mbar_init(received, 1);
     *abort_flag = aligned ? 0 : 1;
     fence_barrier_init();
+    if (S > 1) mbar_arrive_expect_tx(received, static_cast<uint32_t>(kRows * cols4 * 16));
     tma_prefetch_desc(&tmA);
     tma_prefetch_desc(&tmB);
-    if (!aligned) record_status(p.status, ST_SMEM_ALIGN);
   } else if (warp == 1) {
     tmem_alloc(smem_u32(tmem_slot), C::kTmem);
     tmem_relinquish();
   }
+  __syncwarp();
+  if (S > 1) cluster_arrive();  // this CTA's barriers stand
   pdl_wait();
+  if (!aligned && threadIdx.x == 0) record_status(p.status, ST_SMEM_ALIGN);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -286,10 +298,6 @@ __global__ void __launch_bounds__(kThreads, 2)
     *abort_flag = 1;
     record_status(p.status, ST_WAIT_TIMEOUT);
   };
-  float acc[NT];
-#pragma unroll
-  for (int i = 0; i < NT; ++i) acc[i] = 0.f;
-
   if (warp == 0) {
     if (lane == 0 && aligned) {
       Ring<C::kStages> r;
@@ -353,9 +361,18 @@ __global__ void __launch_bounds__(kThreads, 2)
       }
     }
   } else {
+    // (a warp whose wait has failed goes on through the barriers that the four share)
     const int q = warp & 3;
     const int tid = threadIdx.x - 64;
+    const int r = q * 32 + lane;  // row of the tile
     const uint32_t lanes = tmem_base + (static_cast<uint32_t>(q * 32) << 16);
+    auto epi_sync = [&]() {
+      __syncwarp();
+      asm volatile("bar.sync 1, 128;" ::: "memory");
+    };
+    __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.c);
+    Ring<C::kPartials> t;
+    bool ok = aligned;
     // thread i: the scale of column i, times the block's of B, kLead blocks ahead
     constexpr int kLead = 4;
     const bool column = tid < NT && tok0 + tid < p.m;
@@ -366,10 +383,11 @@ __global__ void __launch_bounds__(kThreads, 2)
       na[i] = column && kb < kb1 ? ld_dep(sa + kb) : 0.f;
       nb[i] = column && kb < kb1 ? ld_dep(sb + kb) : 0.f;
     };
-    bool ok = aligned;
+    float acc[NT];
+#pragma unroll
+    for (int i = 0; i < NT; ++i) acc[i] = 0.f;
 #pragma unroll
     for (int i = 0; i < kLead; ++i) ahead(i, kb0 + i);
-    Ring<C::kPartials> t;
     for (int k4 = kb0; k4 < kb1; k4 += kLead) {
 #pragma unroll
       for (int i = 0; i < kLead; ++i) {
@@ -378,32 +396,68 @@ __global__ void __launch_bounds__(kThreads, 2)
         float* sc = scales + (i & 1) * NT;
         if (tid < NT) sc[tid] = na[i] * nb[i];
         ahead(i, kb + kLead);
-        asm volatile("bar.sync 1, 128;" ::: "memory");  // every warp comes here for every block, whatever its waits said
+        epi_sync();
         ok = ok && __all_sync(kFull, mbar_wait(pfull(t.s), t.phase, abort_flag));
         if (ok) {
           tc_fence_after();
+          constexpr int kCols = NT < 32 ? NT : 32;  // columns on their way at a time
 #pragma unroll
-          for (int c0 = 0; c0 < NT; c0 += 16) {
-            uint32_t v[16];
-            tmem_ld16(lanes + t.s * NT + c0, v);
+          for (int c0 = 0; c0 < NT; c0 += kCols) {
+            uint32_t v[kCols / 16][16];
+#pragma unroll
+            for (int c = 0; c < kCols / 16; ++c) tmem_ld16(lanes + t.s * NT + c0 + 16 * c, v[c]);
             tmem_ld_wait();
+            if (c0 + kCols == NT) {  // the partial is in registers
+              tc_fence_before();
+              __syncwarp();
+              if (lane == 0) mbar_arrive(pempty(t.s));
+            }
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const float4 f = *reinterpret_cast<const float4*>(sc + c0 + 4 * j);
-              acc[c0 + 4 * j] = fmaf(f.x, __uint_as_float(v[4 * j]), acc[c0 + 4 * j]);
-              acc[c0 + 4 * j + 1] = fmaf(f.y, __uint_as_float(v[4 * j + 1]), acc[c0 + 4 * j + 1]);
-              acc[c0 + 4 * j + 2] = fmaf(f.z, __uint_as_float(v[4 * j + 2]), acc[c0 + 4 * j + 2]);
-              acc[c0 + 4 * j + 3] = fmaf(f.w, __uint_as_float(v[4 * j + 3]), acc[c0 + 4 * j + 3]);
+            for (int c = 0; c < kCols; c += 4) {
+              const float4 f = *reinterpret_cast<const float4*>(sc + c0 + c);
+              const uint32_t* x = &v[c / 16][c % 16];
+              acc[c0 + c] = fmaf(f.x, __uint_as_float(x[0]), acc[c0 + c]);
+              acc[c0 + c + 1] = fmaf(f.y, __uint_as_float(x[1]), acc[c0 + c + 1]);
+              acc[c0 + c + 2] = fmaf(f.z, __uint_as_float(x[2]), acc[c0 + c + 2]);
+              acc[c0 + c + 3] = fmaf(f.w, __uint_as_float(x[3]), acc[c0 + c + 3]);
             }
           }
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(pempty(t.s));
         }
         t.advance();
       }
     }
+    if (S == 1) {
+      const int n = row0 + r;
+#pragma unroll
+      for (int c = 0; c < NT; ++c)
+        if (ok && n < p.n && tok0 + c < p.m)
+          out[static_cast<long long>(tok0 + c) * p.ldc + n] = __float2bfloat16_rn(acc[c]);
+    } else {
+      cluster_wait();
+      const uint32_t to = r / rows;
+      const uint32_t at = map_rank(smem_u32(sums + (rank * rows + (r - static_cast<int>(to) * rows)) * C::kPitch), to);
+      const uint32_t bar = map_rank(received, to);
+      if (ok)
+#pragma unroll
+        for (int c = 0; c < NT / 4; ++c)
+          if (c < cols4) send4(at + 16 * c, bar, acc[4 * c], acc[4 * c + 1], acc[4 * c + 2], acc[4 * c + 3]);
+      ok = ok && __all_sync(kFull, mbar_wait(received, 0, abort_flag));
+      const int total = rows * min(NT, p.m - tok0);
+      for (int i = tid; ok && i < total; i += kEpiThreads) {
+        const int rr = i & (rows - 1), c = i / rows, n = row0 + rank * rows + rr;  // (rows: a power of two)
+        if (n >= p.n) continue;
+        float v = sums[rr * C::kPitch + c];
+        for (int s = 1; s < S; ++s) v += sums[(s * rows + rr) * C::kPitch + c];
+        out[static_cast<long long>(tok0 + c) * p.ldc + n] = __float2bfloat16_rn(v);
+      }
+    }
     if (!ok && lane == 0 && aligned) give_up();
+  }
+  if (S > 1) {  // no CTA leaves while another may still send to it
+    if (warp < 2) cluster_wait();
+    __syncwarp();
+    cluster_arrive_release();
+    cluster_wait();
   }
   __syncwarp();
   tc_fence_before();
@@ -411,37 +465,6 @@ __global__ void __launch_bounds__(kThreads, 2)
   if (warp == 1) {
     tc_fence_after();
     tmem_dealloc(tmem_base, C::kTmem);
-  }
-
-  // ---- out
-  __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.c);
-  if (S == 1) {
-    if (warp >= 2) {
-      const int n = row0 + (warp & 3) * 32 + lane;
-#pragma unroll
-      for (int c = 0; c < NT; ++c)
-        if (n < p.n && tok0 + c < p.m) out[static_cast<long long>(tok0 + c) * p.ldc + n] = __float2bfloat16_rn(acc[c]);
-    }
-    return;
-  }
-  const int cols = NT / S;  // that this CTA adds
-  cluster_sync();           // the ring's place may be written (and every CTA of the cluster has started)
-  if (warp >= 2) {
-    const int r = (warp & 3) * 32 + lane;
-#pragma unroll
-    for (int c = 0; c < NT; ++c) {
-      const int to = c / cols;
-      const uint32_t at = map_rank(smem_u32(sums + (rank * cols + (c - to * cols)) * kRows + r), static_cast<uint32_t>(to));
-      if (tok0 + c < p.m) asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at), "f"(acc[c]) : "memory");
-    }
-  }
-  cluster_sync();
-  for (int i = threadIdx.x; i < cols * kRows; i += kThreads) {
-    const int c = i / kRows, t = tok0 + rank * cols + c, n = row0 + i % kRows;
-    if (t >= p.m || n >= p.n) continue;
-    float v = sums[i];
-    for (int s = 1; s < S; ++s) v += sums[s * cols * kRows + i];
-    out[static_cast<long long>(t) * p.ldc + n] = __float2bfloat16_rn(v);
   }
 }
 
@@ -461,38 +484,25 @@ constexpr int kWidePartials = 2;
 constexpr int kWideThreads = 32 * 12;
 constexpr int kCtrlRegs = 56, kEpiRegs = 224;
 static_assert(kCtrlRegs + 2 * kEpiRegs <= 3 * 168, "the register split stays within the launch's registers");
-constexpr int kWideBars = 2 * kWideStages + 2 * kWidePartials + 1;
+constexpr int kWideBars = 2 * kWideStages + 2 * kWidePartials + 3;
 constexpr int kStageWarp = 32 * 4 * 16;   // output staging of an epilogue warp
-constexpr int kSumPitch = kRows + 1;      // floats of a column of the slices' sums: rows and columns both meet every bank
+constexpr int kSumPitch = kWideN + 4;     // floats of a row of the slices' sums, which take the ring's place
 constexpr size_t kWideSmem = kWideStages * kWideStage + 8 * kStageWarp + 8 * kWideBars + 16;
 static_assert(kWideSmem <= 227 * 1024, "shared memory budget");
-static_assert(kWideN * kSumPitch * 4 <= kWideStages * kWideStage, "the sums fit the ring");
+static_assert(kRows * kSumPitch * 4 <= kWideStages * kWideStage, "the sums fit the ring");
 
 struct WideArgs {
   Fp8MatmulArgs p;
   int split, m_tiles, tiles;
-  int wide_c;  // rows of c start on 16-byte boundaries
+  int c_align;  // rows of c start on multiples of this many bytes (16, 4 or 2)
 };
-
-// Eight bf16 of row t from column n on, those of them that exist.
-__device__ __forceinline__ void store8(const Fp8MatmulArgs& p, int wide_c, int t, int n, const uint4& v) {
-  __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.c) + static_cast<long long>(t) * p.ldc + n;
-  if (t >= p.m) return;
-  if (wide_c && n + 8 <= p.n) {
-    *reinterpret_cast<uint4*>(out) = v;
-    return;
-  }
-  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-  for (int j = 0; j < 8; ++j)
-    if (n + j < p.n) reinterpret_cast<uint16_t*>(out)[j] = static_cast<uint16_t>(w[j >> 1] >> (16 * (j & 1)));
-}
 
 __device__ __forceinline__ void add16(float* acc, const uint32_t (&v)[16], float s) {
 #pragma unroll
   for (int j = 0; j < 16; ++j) acc[j] = fmaf(s, __uint_as_float(v[j]), acc[j]);
 }
 
+template <bool SPLIT>
 __global__ void __launch_bounds__(kWideThreads, 1)
     fp8_wide_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
                     const WideArgs args) {
@@ -500,7 +510,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
   const uint32_t base = smem_u32(smem_raw);
   const Fp8MatmulArgs& p = args.p;
   const bool aligned = (base & 1023u) == 0;  // the 128-byte swizzle needs it; the same in the cluster
-  const int S = args.split;
+  const int S = SPLIT ? args.split : 1;
   const int rank = blockIdx.x % S;
   const int blocks = (p.k + kFp8BK - 1) / kFp8BK;
   const int kb0 = static_cast<int>(static_cast<long long>(blocks) * rank / S);
@@ -513,7 +523,8 @@ __global__ void __launch_bounds__(kWideThreads, 1)
   auto empty = [&](int i) { return bar0 + 8u * (kWideStages + i); };
   auto pfull = [&](int i) { return bar0 + 8u * (2 * kWideStages + i); };
   auto pempty = [&](int i) { return bar0 + 8u * (2 * kWideStages + kWidePartials + i); };
-  const uint32_t drain = bar0 + 8u * (kWideBars - 1);
+  const uint32_t drain = bar0 + 8u * (kWideBars - 3), rings = drain + 8u, received = drain + 16u;
+  const int rows = kRows / S;  // whose sums this CTA adds
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + kWideBars);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -528,20 +539,26 @@ __global__ void __launch_bounds__(kWideThreads, 1)
       mbar_init(pempty(i), 8);
     }
     mbar_init(drain, 1);
+    mbar_init(rings, S);
+    mbar_init(received, 1);
     *abort_flag = aligned ? 0 : 1;
     fence_barrier_init();
+    if (SPLIT) mbar_arrive_expect_tx(received, static_cast<uint32_t>(kRows * kWideN * 4));
     tma_prefetch_desc(&tmA);
     tma_prefetch_desc(&tmB);
-    if (!aligned) record_status(p.status, ST_SMEM_ALIGN);
   } else if (warp == 1) {
     tmem_alloc(smem_u32(tmem_slot), 512);
     tmem_relinquish();
   }
+  __syncwarp();
+  if (SPLIT) cluster_arrive();  // this CTA's barriers stand
   pdl_wait();
+  if (!aligned && threadIdx.x == 0) record_status(p.status, ST_SMEM_ALIGN);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
+  bool waited = false;  // for the cluster's barriers to stand
   auto give_up = [&]() {
     *abort_flag = 1;
     record_status(p.status, ST_WAIT_TIMEOUT);
@@ -679,7 +696,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
       }
       if (!ok) break;
       add16(acc + 112, c1, s_prev);
-      if (S == 1) {
+      if constexpr (!SPLIT) {
         // four rounds of 32 columns: a row's 64 bytes cross the warp's staging (chunk j of row r at slot
         // j ^ ((r / 2) % 4): no bank conflicts) and leave as eight rows x 64 bytes per store instruction
 #pragma unroll
@@ -691,52 +708,90 @@ __global__ void __launch_bounds__(kWideThreads, 1)
                                                                    pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
           }
           __syncwarp();
-          const int cu = lane & 3;
+          const int t0 = tok0 + q * 32, n0 = row0 + 32 * rd;
+          __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.c) + static_cast<long long>(t0) * p.ldc + n0;
+          if (args.c_align == 16 && n0 + 32 <= p.n) {
+            const int cu = lane & 3;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int r = (lane >> 2) + 8 * i;
-            store8(p, args.wide_c, tok0 + q * 32 + r, row0 + 32 * rd + 8 * cu, stage[r * 4 + (cu ^ ((r >> 1) & 3))]);
+            for (int i = 0; i < 4; ++i) {
+              const int r = (lane >> 2) + 8 * i;
+              if (t0 + r < p.m)
+                *reinterpret_cast<uint4*>(out + r * p.ldc + 8 * cu) = stage[r * 4 + (cu ^ ((r >> 1) & 3))];
+            }
+          } else if (args.c_align >= 4 && (p.n & 1) == 0) {
+            // two columns a lane, two rows an instruction
+            const int c = 2 * (lane & 15);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const int r = (lane >> 4) + 2 * i;
+              const uint32_t v =
+                  reinterpret_cast<const uint32_t*>(&stage[r * 4 + ((c >> 3) ^ ((r >> 1) & 3))])[(c & 7) >> 1];
+              if (t0 + r < p.m && n0 + c < p.n) *reinterpret_cast<uint32_t*>(out + r * p.ldc + c) = v;
+            }
+          } else {
+#pragma unroll 8
+            for (int r = 0; r < 32; ++r) {
+              const uint16_t v =
+                  reinterpret_cast<const uint16_t*>(&stage[r * 4 + ((lane >> 3) ^ ((r >> 1) & 3))])[lane & 7];
+              if (t0 + r < p.m && n0 + lane < p.n) *reinterpret_cast<uint16_t*>(out + r * p.ldc + lane) = v;
+            }
           }
           __syncwarp();
         }
       } else {
-        cluster_sync();  // every CTA's ring is done with: the sums take its place
-        const int cols = kWideN / S;  // that a CTA adds
+        // every CTA's ring is done with (its last MMA has been seen to be): the sums take its place
+        cluster_wait();
+        waited = true;
+        if (warp == 4 && lane < S) mbar_arrive_remote(map_rank(rings, static_cast<uint32_t>(lane)));
+        ok = __all_sync(kFull, mbar_wait(rings, 0, abort_flag));
+        if (!ok) break;
         const int r = q * 32 + lane;
-        const float* sums = reinterpret_cast<const float*>(smem_raw);
+        const uint32_t to = r / rows;
+        const float* sums = reinterpret_cast<const float*>(smem_raw);  // [slice][row][column]
+        const uint32_t at = map_rank(
+            smem_u32(sums + (rank * rows + (r - static_cast<int>(to) * rows)) * kSumPitch + half * 128), to);
+        const uint32_t bar = map_rank(received, to);
 #pragma unroll
-        for (int j = 0; j < 128; ++j) {
-          const int c = half * 128 + j, to = c / cols;
-          const uint32_t at = map_rank(smem_u32(sums + (rank * cols + (c - to * cols)) * kSumPitch + r),
-                                       static_cast<uint32_t>(to));
-          asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at), "f"(acc[j]) : "memory");
+        for (int c = 0; c < 128; c += 4) send4(at + 4 * c, bar, acc[c], acc[c + 1], acc[c + 2], acc[c + 3]);
+        ok = __all_sync(kFull, mbar_wait(received, 0, abort_flag));
+        if (!ok) break;
+        const int n0 = tile / args.m_tiles * kWideN;
+        __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.c) + n0;
+        if (args.c_align >= 4 && (p.n & 1) == 0) {
+          for (int i = threadIdx.x - 128; i < rows * (kWideN / 2); i += 256) {
+            const int c = i % (kWideN / 2) * 2, rr = i / (kWideN / 2), t = tok0 + rank * rows + rr;
+            float2 v = make_float2(0.f, 0.f);
+            for (int s = 0; s < S; ++s) {
+              const float2 x = *reinterpret_cast<const float2*>(sums + (s * rows + rr) * kSumPitch + c);
+              v.x += x.x, v.y += x.y;
+            }
+            if (t < p.m && n0 + c < p.n)
+              *reinterpret_cast<uint32_t*>(out + static_cast<long long>(t) * p.ldc + c) = pack_bf16x2(v.x, v.y);
+          }
+        } else {
+          for (int i = threadIdx.x - 128; i < rows * kWideN; i += 256) {
+            const int c = i % kWideN, rr = i / kWideN, t = tok0 + rank * rows + rr;
+            float v = 0.f;
+            for (int s = 0; s < S; ++s) v += sums[(s * rows + rr) * kSumPitch + c];
+            if (t < p.m && n0 + c < p.n) out[static_cast<long long>(t) * p.ldc + c] = __float2bfloat16_rn(v);
+          }
         }
       }
     }
     if (!ok && aligned && lane == 0) give_up();
-    if (S > 1 && !ok) cluster_sync();  // (the barrier that the slices pass when all is well)
   }
-  if (S > 1 && warp < 4) cluster_sync();
+  if (SPLIT) {  // no CTA leaves while another may still send to it
+    if (!waited) cluster_wait();
+    __syncwarp();
+    cluster_arrive_release();
+    cluster_wait();
+  }
   __syncwarp();
   tc_fence_before();
   __syncthreads();
   if (warp == 1) {
     tc_fence_after();
     tmem_dealloc(tmem_base, 512);
-  }
-  if (S > 1) cluster_sync();
-  if (S > 1 && warp >= 4) {  // (the first warps' registers would not do)
-    const int tile = blockIdx.x / S, cols = kWideN / S;
-    const int tok0 = tile % args.m_tiles * kRows, n0 = tile / args.m_tiles * kWideN + rank * cols;
-    const float* sums = reinterpret_cast<const float*>(smem_raw);
-    __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.c);
-    for (int i = threadIdx.x - 128; i < cols * kRows; i += 256) {
-      const int c = i & (cols - 1), r = i / cols;
-      if (tok0 + r >= p.m || n0 + c >= p.n) continue;
-      float v = sums[c * kSumPitch + r];
-      for (int s = 1; s < S; ++s) v += sums[(s * cols + c) * kSumPitch + r];
-      out[static_cast<long long>(tok0 + r) * p.ldc + n0 + c] = __float2bfloat16_rn(v);
-    }
   }
 }
 
@@ -746,8 +801,10 @@ cudaError_t skinny(const CUtensorMap& tmA, const CUtensorMap& tmB, const Fp8Matm
   const int blocks = ceil_div(args.k, kFp8BK);
   SkinnyArgs a{args, 1, ceil_div(args.m, NT)};
   const long long tiles = static_cast<long long>(ceil_div(args.n, kRows)) * a.m_tiles;
-  // K slices until the tiles fill the GPU twice over, with at least four blocks each
-  while (a.split < kMaxSplit && tiles * a.split < 2 * num_sms && blocks / (2 * a.split) >= 4) a.split *= 2;
+  // K slices as long as all CTAs are resident at once (a second wave costs more than shorter slices save: 45 rows
+  // x 28672 x 4096 on 1, 2 and 4 slices 24, 38 and 46 us; 64 x 4096 x 14336 on 2, 4 and 8, all one wave, 31, 20
+  // and 18)
+  while (a.split < kMaxSplit && tiles * a.split * 2 <= 2 * num_sms && blocks >= 4 * a.split) a.split *= 2;
   return launch_pdl(fp8_skinny_kernel<NT>, dim3(static_cast<unsigned>(tiles * a.split)), dim3(kThreads),
                     Skinny<NT>::kSmem, s, a.split, tmA, tmB, a);
 }
@@ -758,10 +815,14 @@ cudaError_t wide(const CUtensorMap& tmA, const CUtensorMap& tmB, const Fp8Matmul
   WideArgs a{args, 1, ceil_div(args.m, kRows), 0, 0};
   const long long tiles = static_cast<long long>(ceil_div(args.n, kWideN)) * a.m_tiles;
   a.tiles = static_cast<int>(tiles);
-  a.wide_c = (reinterpret_cast<uintptr_t>(args.c) & 15u) == 0 && args.ldc % 8 == 0;
+  const uintptr_t at = reinterpret_cast<uintptr_t>(args.c) | static_cast<uintptr_t>(2 * args.ldc);
+  a.c_align = (at & 15u) == 0 ? 16 : (at & 3u) == 0 ? 4 : 2;
   while (a.split < kMaxSplit && tiles * a.split * 2 <= num_sms && blocks / (2 * a.split) >= 4) a.split *= 2;
   const long long grid = a.split > 1 ? tiles * a.split : std::min<long long>(tiles, num_sms);
-  return launch_pdl(fp8_wide_kernel, dim3(static_cast<unsigned>(grid)), dim3(kWideThreads), kWideSmem, s, a.split, tmA,
+  if (a.split > 1)
+    return launch_pdl(fp8_wide_kernel<true>, dim3(static_cast<unsigned>(grid)), dim3(kWideThreads), kWideSmem, s, a.split,
+                      tmA, tmB, a);
+  return launch_pdl(fp8_wide_kernel<false>, dim3(static_cast<unsigned>(grid)), dim3(kWideThreads), kWideSmem, s, 1, tmA,
                     tmB, a);
 }
 
@@ -776,7 +837,8 @@ cudaError_t fp8_matmul_set_attributes() {
   set(fp8_skinny_kernel<16>, Skinny<16>::kSmem);
   set(fp8_skinny_kernel<32>, Skinny<32>::kSmem);
   set(fp8_skinny_kernel<64>, Skinny<64>::kSmem);
-  set(fp8_wide_kernel, kWideSmem);
+  set(fp8_wide_kernel<false>, kWideSmem);
+  set(fp8_wide_kernel<true>, kWideSmem);
   return e;
 }
 
@@ -804,8 +866,8 @@ cudaError_t launch_fp8_quantize(const void* x, const void* u, int rows, int cols
                                 long long ldq, float* s, long long lds, cudaStream_t st) {
   const uintptr_t at = reinterpret_cast<uintptr_t>(x) | reinterpret_cast<uintptr_t>(u) | static_cast<uintptr_t>(2 * ld);
   const bool wide_q = ((reinterpret_cast<uintptr_t>(q) | static_cast<uintptr_t>(ldq)) & 15u) == 0;
-  const long long parts = static_cast<long long>(rows) * ceil_div(cols, kQuantCols);
-  const unsigned grid = static_cast<unsigned>(std::min<long long>((parts + 7) / 8, 152 * 8));
+  const long long groups = static_cast<long long>(rows) * ceil_div(cols, 128);
+  const unsigned grid = static_cast<unsigned>(std::min<long long>((groups + 31) / 32, 152 * 32));
   const uint16_t *xp = static_cast<const uint16_t*>(x), *up = static_cast<const uint16_t*>(u);
   uint8_t* qp = static_cast<uint8_t*>(q);
 #define ASAP_QUANT(SW, W)                                                                                            \

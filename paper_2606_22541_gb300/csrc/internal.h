@@ -177,7 +177,7 @@ struct Fp8MatmulArgs {
   long long ldc;
   uint32_t* status;  // nullable
 };
-cudaError_t fp8_matmul_set_attributes();
+cudaError_t fp8_matmul_set_attributes();  // once per device
 // The product; err names the operand that TMA cannot read.
 cudaError_t fp8_matmul_launch(const void* a, long long lda, const void* b, long long ldb, const Fp8MatmulArgs& args,
                               int num_sms, cudaStream_t s, std::string* err);
