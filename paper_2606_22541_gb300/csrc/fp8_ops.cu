@@ -169,9 +169,10 @@ __global__ void __launch_bounds__(kQuantThreads, 8) fp8_quantize_kernel(const ui
 // cluster of S CTAs shares a tile, each with a slice of K.  Every 128-wide K block
 // is multiplied into one of the TMEM partials, which the epilogue warps add, times
 // the block's scales, into registers; the slices' sums meet in distributed shared
-// memory, each CTA adding those of 128 / S rows in rank order.  They travel by
-// st.async, counted by the receiver's mbarrier (with plain stores between cluster
-// barriers one row x 4096 x 7168 took 10 us on eight slices, 8 so).  Two CTAs an
+// memory, each CTA adding those of 128 / S rows in rank order.  They travel as bulk
+// copies, counted by the receiver's mbarrier.  (Plain stores between cluster
+// barriers and 16-byte st.async move about 0.5 TB/s over the whole GPU: 64 rows x
+// 4096 x 14336 on eight slices, 8 MB of sums, took 22 and 17 us.)  Two CTAs an
 // SM, so that one's start and end pass beside the other's stream; persistent
 // CTAs, one an SM with a ring twice as deep and the sums of a tile exchanged while
 // the next one streams, took 8.9 us there and 30 instead of 24 for 45 rows x 28672
@@ -195,6 +196,7 @@ struct Skinny {
   static constexpr int kBars = 2 * kStages + 2 * kPartials + 2;
   static constexpr size_t kSmem = kStages * kStage + 4 * kSums + 2 * NT * 4 + 8 * kBars + 16;
   static_assert(2 * (kSmem + 1024) <= 228 * 1024, "two CTAs an SM");
+  static_assert(4 * kSums <= kStages * kStage, "the ring holds the sums to be sent");
 };
 
 struct SkinnyArgs {
@@ -219,10 +221,10 @@ __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.w
 __device__ __forceinline__ void mbar_arrive_remote(uint32_t addr) {
   asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(addr) : "memory");
 }
-// 16 bytes into a CTA of the cluster; its barrier counts them when they are visible there.
-__device__ __forceinline__ void send4(uint32_t addr, uint32_t bar, float a, float b, float c, float d) {
-  asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%2, %3, %4, %5}, [%1];" ::"r"(addr),
-               "r"(bar), "f"(a), "f"(b), "f"(c), "f"(d)
+// Shared memory of this CTA into one of the cluster, whose barrier counts the bytes.
+__device__ __forceinline__ void send(uint32_t to, uint32_t from, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.shared::cta.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(to),
+               "r"(from), "r"(bytes), "r"(bar)
                : "memory");
 }
 __device__ __forceinline__ void mma_e4m3(uint32_t d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t acc) {
@@ -260,8 +262,7 @@ __global__ void __launch_bounds__(kThreads, 2)
   auto pfull = [&](int i) { return bar0 + 8u * (2 * C::kStages + i); };
   auto pempty = [&](int i) { return bar0 + 8u * (2 * C::kStages + C::kPartials + i); };
   const uint32_t drain = bar0 + 8u * (C::kBars - 2), received = drain + 8u;
-  const int rows = kRows / S;                        // whose sums this CTA adds
-  const int cols4 = (min(NT, p.m - tok0) + 3) / 4;   // groups of columns that travel
+  const int rows = kRows / S;  // whose sums this CTA adds
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + C::kBars);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -279,7 +280,7 @@ __global__ void __launch_bounds__(kThreads, 2)
     mbar_init(received, 1);
     *abort_flag = aligned ? 0 : 1;
     fence_barrier_init();
-    if (S > 1) mbar_arrive_expect_tx(received, static_cast<uint32_t>(kRows * cols4 * 16));
+    if (S > 1) mbar_arrive_expect_tx(received, static_cast<uint32_t>(4 * C::kSums));
     tma_prefetch_desc(&tmA);
     tma_prefetch_desc(&tmB);
   } else if (warp == 1) {
@@ -433,14 +434,18 @@ __global__ void __launch_bounds__(kThreads, 2)
         if (ok && n < p.n && tok0 + c < p.m)
           out[static_cast<long long>(tok0 + c) * p.ldc + n] = __float2bfloat16_rn(acc[c]);
     } else {
-      cluster_wait();
-      const uint32_t to = r / rows;
-      const uint32_t at = map_rank(smem_u32(sums + (rank * rows + (r - static_cast<int>(to) * rows)) * C::kPitch), to);
-      const uint32_t bar = map_rank(received, to);
-      if (ok)
+      // the ring is done with (its last MMA has been seen to be): it holds the sums until they are sent
+      float4* row = reinterpret_cast<float4*>(smem_raw + r * C::kPitch * 4);
 #pragma unroll
-        for (int c = 0; c < NT / 4; ++c)
-          if (c < cols4) send4(at + 16 * c, bar, acc[4 * c], acc[4 * c + 1], acc[4 * c + 2], acc[4 * c + 3]);
+      for (int c = 0; c < NT / 4; ++c) row[c] = make_float4(acc[4 * c], acc[4 * c + 1], acc[4 * c + 2], acc[4 * c + 3]);
+      fence_proxy_async_smem();
+      epi_sync();
+      cluster_wait();
+      if (ok && tid < S) {
+        const uint32_t bytes = static_cast<uint32_t>(rows * C::kPitch * 4);
+        send(map_rank(smem_u32(sums) + rank * bytes, tid), base + tid * bytes, bytes, map_rank(received, tid));
+      }
+      __syncwarp();
       ok = ok && __all_sync(kFull, mbar_wait(received, 0, abort_flag));
       const int total = rows * min(NT, p.m - tok0);
       for (int i = tid; ok && i < total; i += kEpiThreads) {
@@ -484,12 +489,15 @@ constexpr int kWidePartials = 2;
 constexpr int kWideThreads = 32 * 12;
 constexpr int kCtrlRegs = 56, kEpiRegs = 224;
 static_assert(kCtrlRegs + 2 * kEpiRegs <= 3 * 168, "the register split stays within the launch's registers");
-constexpr int kWideBars = 2 * kWideStages + 2 * kWidePartials + 3;
+constexpr int kWideBars = 2 * kWideStages + 2 * kWidePartials + 6;
+constexpr int kWideSplit = 4;  // K slices at most
 constexpr int kStageWarp = 32 * 4 * 16;   // output staging of an epilogue warp
-constexpr int kSumPitch = kWideN + 4;     // floats of a row of the slices' sums, which take the ring's place
+// The slices' sums of a column half: those to be sent, then those that come, each at
+// most (S - 1) / S of 128 x 128 floats, in the ring's place.
+constexpr int kHalfSums = (kWideSplit - 1) * (kRows / kWideSplit) * 128 * 4;
 constexpr size_t kWideSmem = kWideStages * kWideStage + 8 * kStageWarp + 8 * kWideBars + 16;
 static_assert(kWideSmem <= 227 * 1024, "shared memory budget");
-static_assert(kRows * kSumPitch * 4 <= kWideStages * kWideStage, "the sums fit the ring");
+static_assert(4 * kHalfSums <= kWideStages * kWideStage, "the sums fit the ring");
 
 struct WideArgs {
   Fp8MatmulArgs p;
@@ -523,7 +531,8 @@ __global__ void __launch_bounds__(kWideThreads, 1)
   auto empty = [&](int i) { return bar0 + 8u * (kWideStages + i); };
   auto pfull = [&](int i) { return bar0 + 8u * (2 * kWideStages + i); };
   auto pempty = [&](int i) { return bar0 + 8u * (2 * kWideStages + kWidePartials + i); };
-  const uint32_t drain = bar0 + 8u * (kWideBars - 3), rings = drain + 8u, received = drain + 16u;
+  // all CTAs' rings are done with; per column half: the rows to be sent are written, the slices have come
+  const uint32_t drain = bar0 + 8u * (kWideBars - 6), rings = drain + 8u, written = drain + 16u, received = drain + 32u;
   const int rows = kRows / S;  // whose sums this CTA adds
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + kWideBars);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
@@ -540,10 +549,14 @@ __global__ void __launch_bounds__(kWideThreads, 1)
     }
     mbar_init(drain, 1);
     mbar_init(rings, S);
-    mbar_init(received, 1);
+    for (uint32_t i = 0; i < 2; ++i) {
+      mbar_init(written + 8u * i, 4);
+      mbar_init(received + 8u * i, 1);
+    }
     *abort_flag = aligned ? 0 : 1;
     fence_barrier_init();
-    if (SPLIT) mbar_arrive_expect_tx(received, static_cast<uint32_t>(kRows * kWideN * 4));
+    if (SPLIT)
+      for (int i = 0; i < 2; ++i) mbar_arrive_expect_tx(received + 8u * i, static_cast<uint32_t>((S - 1) * rows * 512));
     tma_prefetch_desc(&tmA);
     tma_prefetch_desc(&tmB);
   } else if (warp == 1) {
@@ -696,7 +709,50 @@ __global__ void __launch_bounds__(kWideThreads, 1)
       }
       if (!ok) break;
       add16(acc + 112, c1, s_prev);
-      if constexpr (!SPLIT) {
+      bool store = true;
+      if constexpr (SPLIT) {
+        // Every CTA sends the rows that others add (a warp's rows have one owner) and adds what comes for its own, in
+        // rank order behind its own sums.  A row's 16-byte chunk c lies at c ^ (row % 8): no bank conflicts.
+        const int owner = (q * 32) / rows, rr = q * 32 + lane - owner * rows;
+        store = owner == rank;
+        uint8_t* out_sums = smem_raw + half * 2 * kHalfSums;  // this CTA's ring is done with: its last MMA has been seen to be
+        const uint8_t* in_sums = out_sums + kHalfSums;
+        if (!store) {
+          uint8_t* row = out_sums + ((owner - (owner > rank ? 1 : 0)) * rows + rr) * 512;
+#pragma unroll
+          for (int c = 0; c < 32; ++c)
+            *reinterpret_cast<float4*>(row + ((c ^ (rr & 7)) << 4)) =
+                make_float4(acc[4 * c], acc[4 * c + 1], acc[4 * c + 2], acc[4 * c + 3]);
+          fence_proxy_async_smem();
+        }
+        cluster_wait();
+        waited = true;
+        if (warp == 4 && lane < S) mbar_arrive_remote(map_rank(rings, static_cast<uint32_t>(lane)));
+        __syncwarp();
+        if (lane == 0) mbar_arrive(written + 8u * half);
+        if (q == 0) ok = __all_sync(kFull, mbar_wait(rings, 0, abort_flag) && mbar_wait(written + 8u * half, 0, abort_flag));
+        if (!ok) break;
+        if (q == 0 && lane < S - 1) {
+          const int to = lane + (lane >= rank ? 1 : 0);
+          const uint32_t bytes = static_cast<uint32_t>(rows * 512);
+          send(map_rank(smem_u32(in_sums) + (rank - (rank > to ? 1 : 0)) * bytes, static_cast<uint32_t>(to)),
+               smem_u32(out_sums) + lane * bytes, bytes, map_rank(received + 8u * half, static_cast<uint32_t>(to)));
+        }
+        __syncwarp();
+        if (store) {
+          ok = __all_sync(kFull, mbar_wait(received + 8u * half, 0, abort_flag));
+          if (!ok) break;
+          for (int s = 0; s < S - 1; ++s) {
+            const uint8_t* row = in_sums + (s * rows + rr) * 512;
+#pragma unroll
+            for (int c = 0; c < 32; ++c) {
+              const float4 v = *reinterpret_cast<const float4*>(row + ((c ^ (rr & 7)) << 4));
+              acc[4 * c] += v.x, acc[4 * c + 1] += v.y, acc[4 * c + 2] += v.z, acc[4 * c + 3] += v.w;
+            }
+          }
+        }
+      }
+      if (store) {
         // four rounds of 32 columns: a row's 64 bytes cross the warp's staging (chunk j of row r at slot
         // j ^ ((r / 2) % 4): no bank conflicts) and leave as eight rows x 64 bytes per store instruction
 #pragma unroll
@@ -737,44 +793,6 @@ __global__ void __launch_bounds__(kWideThreads, 1)
             }
           }
           __syncwarp();
-        }
-      } else {
-        // every CTA's ring is done with (its last MMA has been seen to be): the sums take its place
-        cluster_wait();
-        waited = true;
-        if (warp == 4 && lane < S) mbar_arrive_remote(map_rank(rings, static_cast<uint32_t>(lane)));
-        ok = __all_sync(kFull, mbar_wait(rings, 0, abort_flag));
-        if (!ok) break;
-        const int r = q * 32 + lane;
-        const uint32_t to = r / rows;
-        const float* sums = reinterpret_cast<const float*>(smem_raw);  // [slice][row][column]
-        const uint32_t at = map_rank(
-            smem_u32(sums + (rank * rows + (r - static_cast<int>(to) * rows)) * kSumPitch + half * 128), to);
-        const uint32_t bar = map_rank(received, to);
-#pragma unroll
-        for (int c = 0; c < 128; c += 4) send4(at + 4 * c, bar, acc[c], acc[c + 1], acc[c + 2], acc[c + 3]);
-        ok = __all_sync(kFull, mbar_wait(received, 0, abort_flag));
-        if (!ok) break;
-        const int n0 = tile / args.m_tiles * kWideN;
-        __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.c) + n0;
-        if (args.c_align >= 4 && (p.n & 1) == 0) {
-          for (int i = threadIdx.x - 128; i < rows * (kWideN / 2); i += 256) {
-            const int c = i % (kWideN / 2) * 2, rr = i / (kWideN / 2), t = tok0 + rank * rows + rr;
-            float2 v = make_float2(0.f, 0.f);
-            for (int s = 0; s < S; ++s) {
-              const float2 x = *reinterpret_cast<const float2*>(sums + (s * rows + rr) * kSumPitch + c);
-              v.x += x.x, v.y += x.y;
-            }
-            if (t < p.m && n0 + c < p.n)
-              *reinterpret_cast<uint32_t*>(out + static_cast<long long>(t) * p.ldc + c) = pack_bf16x2(v.x, v.y);
-          }
-        } else {
-          for (int i = threadIdx.x - 128; i < rows * kWideN; i += 256) {
-            const int c = i % kWideN, rr = i / kWideN, t = tok0 + rank * rows + rr;
-            float v = 0.f;
-            for (int s = 0; s < S; ++s) v += sums[(s * rows + rr) * kSumPitch + c];
-            if (t < p.m && n0 + c < p.n) out[static_cast<long long>(t) * p.ldc + c] = __float2bfloat16_rn(v);
-          }
         }
       }
     }
@@ -817,7 +835,7 @@ cudaError_t wide(const CUtensorMap& tmA, const CUtensorMap& tmB, const Fp8Matmul
   a.tiles = static_cast<int>(tiles);
   const uintptr_t at = reinterpret_cast<uintptr_t>(args.c) | static_cast<uintptr_t>(2 * args.ldc);
   a.c_align = (at & 15u) == 0 ? 16 : (at & 3u) == 0 ? 4 : 2;
-  while (a.split < kMaxSplit && tiles * a.split * 2 <= num_sms && blocks / (2 * a.split) >= 4) a.split *= 2;
+  while (a.split < kWideSplit && tiles * a.split * 2 <= num_sms && blocks >= 8 * a.split) a.split *= 2;
   const long long grid = a.split > 1 ? tiles * a.split : std::min<long long>(tiles, num_sms);
   if (a.split > 1)
     return launch_pdl(fp8_wide_kernel<true>, dim3(static_cast<unsigned>(grid)), dim3(kWideThreads), kWideSmem, s, a.split,
