@@ -253,16 +253,17 @@ def asap_moe_route_noalloc(h, x, idx, w, counts, offsets, stream=None):
                                        _ptr(offsets), _stream(stream)))
 
 
-def _e4m3(t):
-    return t.dtype is torch.float8_e4m3fn or t.dtype is torch.uint8
+_BF16, _F32, _F8, _U8 = torch.bfloat16, torch.float32, torch.float8_e4m3fn, torch.uint8
 
 
 def _ld(t):
     """Row stride of a 2-D CUDA tensor whose columns are contiguous, else 0.  (A
     single row's stride says nothing: one that any row may have.)"""
+    if not t.is_cuda:
+        return 0
     s0, s1 = t.stride()
     rows, cols = t.shape
-    if not t.is_cuda or (s1 != 1 and cols > 1):
+    if s1 != 1 and cols > 1:
         return 0
     return s0 if rows > 1 else (cols + 15) // 16 * 16
 
@@ -275,33 +276,38 @@ def _refuse(what, **tensors):
 def asap_moe_fp8_quantize(x, q, scales, stream=None):
     """bf16 rows x [n, c] to e4m3 q [n, c] with scales [n, ceil(c / 128)]
     (fp32); any row strides."""
-    if x.dim() != 2 or x.dtype is not torch.bfloat16 or q.shape != x.shape or not _e4m3(q) or \
-            scales.dtype is not torch.float32 or scales.shape != (x.shape[0], (x.shape[1] + 127) // 128):
+    shape = x.shape
+    if len(shape) != 2 or x.dtype is not _BF16 or q.shape != shape or (q.dtype is not _F8 and q.dtype is not _U8) or \
+            scales.dtype is not _F32 or scales.shape != (shape[0], (shape[1] + 127) // 128):
         _refuse("x [n, c] bf16, q [n, c] e4m3, scales [n, ceil(c / 128)] fp32", x=x, q=q, scales=scales)
-    n, c = x.shape
+    n, c = shape
     ld, ldq, lds = _ld(x), _ld(q), _ld(scales)
     if not (ld and ldq and lds) and n and c:
         _refuse("CUDA tensors with contiguous columns", x=x, q=q, scales=scales)
-    check("asap_moe_fp8_quantize", lib().asap_moe_fp8_quantize(x.data_ptr(), ld, n, c, q.data_ptr(), ldq,
-                                                               scales.data_ptr(), lds, _stream(stream)))
+    code = lib().asap_moe_fp8_quantize(x.data_ptr(), ld, n, c, q.data_ptr(), ldq, scales.data_ptr(), lds,
+                                       _stream(stream))
+    if code:
+        check("asap_moe_fp8_quantize", code)
 
 
 def asap_moe_fp8_swiglu_quantize(gate, up, q, scales, stream=None):
     """silu(gate) * up of bf16 [n, c] tensors with one row stride (the halves of
     a product's rows) to e4m3 q [n, c] with scales [n, ceil(c / 128)]."""
-    if gate.dim() != 2 or gate.dtype is not torch.bfloat16 or up.shape != gate.shape or \
-            up.dtype is not torch.bfloat16 or q.shape != gate.shape or not _e4m3(q) or \
-            scales.dtype is not torch.float32 or scales.shape != (gate.shape[0], (gate.shape[1] + 127) // 128):
+    shape = gate.shape
+    if len(shape) != 2 or gate.dtype is not _BF16 or up.shape != shape or up.dtype is not _BF16 or \
+            q.shape != shape or (q.dtype is not _F8 and q.dtype is not _U8) or \
+            scales.dtype is not _F32 or scales.shape != (shape[0], (shape[1] + 127) // 128):
         _refuse("gate, up [n, c] bf16, q [n, c] e4m3, scales [n, ceil(c / 128)] fp32", gate=gate, up=up, q=q,
                 scales=scales)
-    n, c = gate.shape
-    ld, ldu, ldq, lds = _ld(gate), _ld(up), _ld(q), _ld(scales)
-    if not (ld and ldu == ld and ldq and lds) and n and c:
+    n, c = shape
+    ld, ldq, lds = _ld(gate), _ld(q), _ld(scales)
+    if not (ld and ldq and lds and _ld(up) == ld) and n and c:
         _refuse("CUDA tensors with contiguous columns, gate and up with one row stride", gate=gate, up=up, q=q,
                 scales=scales)
-    check("asap_moe_fp8_swiglu_quantize",
-          lib().asap_moe_fp8_swiglu_quantize(gate.data_ptr(), up.data_ptr(), ld, n, c, q.data_ptr(), ldq,
-                                             scales.data_ptr(), lds, _stream(stream)))
+    code = lib().asap_moe_fp8_swiglu_quantize(gate.data_ptr(), up.data_ptr(), ld, n, c, q.data_ptr(), ldq,
+                                              scales.data_ptr(), lds, _stream(stream))
+    if code:
+        check("asap_moe_fp8_swiglu_quantize", code)
 
 
 def asap_moe_fp8_matmul(a, a_scales, b, b_scales, out, stream=None, status=None):
@@ -309,22 +315,26 @@ def asap_moe_fp8_matmul(a, a_scales, b, b_scales, out, stream=None, status=None)
     boundaries) with fp32 scales [m, ceil(k / 128)] and [ceil(n / 128),
     ceil(k / 128)].  status: None or a one-element int32 CUDA tensor that gets
     error bits."""
-    if a.dim() != 2 or b.dim() != 2:
+    sa, sb = a.shape, b.shape
+    if len(sa) != 2 or len(sb) != 2:
         _refuse("a [m, k], b [n, k]", a=a, b=b)
-    (m, k), n = a.shape, b.shape[0]
+    m, k = sa
+    n = sb[0]
     blocks = (k + 127) // 128
-    if not _e4m3(a) or not _e4m3(b) or b.shape[1] != k or out.dtype is not torch.bfloat16 or out.shape != (m, n) or \
-            a_scales.dtype is not torch.float32 or a_scales.shape != (m, blocks) or \
-            b_scales.dtype is not torch.float32 or b_scales.shape != ((n + 127) // 128, blocks):
+    if (a.dtype is not _F8 and a.dtype is not _U8) or (b.dtype is not _F8 and b.dtype is not _U8) or sb[1] != k or \
+            out.dtype is not _BF16 or out.shape != (m, n) or \
+            a_scales.dtype is not _F32 or a_scales.shape != (m, blocks) or \
+            b_scales.dtype is not _F32 or b_scales.shape != ((n + 127) // 128, blocks):
         _refuse("a [m, k], b [n, k] e4m3, a_scales [m, ceil(k / 128)], b_scales [ceil(n / 128), ceil(k / 128)] fp32, "
                 "out [m, n] bf16", a=a, a_scales=a_scales, b=b, b_scales=b_scales, out=out)
     lda, lsa, ldb, lsb, ldc = _ld(a), _ld(a_scales), _ld(b), _ld(b_scales), _ld(out)
     if not (lda and lsa and ldb and lsb and ldc) and m and n and k:
         _refuse("CUDA tensors with contiguous columns", a=a, a_scales=a_scales, b=b, b_scales=b_scales, out=out)
-    check("asap_moe_fp8_matmul",
-          lib().asap_moe_fp8_matmul(a.data_ptr(), lda, a_scales.data_ptr(), lsa, b.data_ptr(), ldb,
-                                    b_scales.data_ptr(), lsb, out.data_ptr(), ldc, m, n, k,
-                                    None if status is None else status.data_ptr(), _stream(stream)))
+    code = lib().asap_moe_fp8_matmul(a.data_ptr(), lda, a_scales.data_ptr(), lsa, b.data_ptr(), ldb,
+                                     b_scales.data_ptr(), lsb, out.data_ptr(), ldc, m, n, k,
+                                     None if status is None else status.data_ptr(), _stream(stream))
+    if code:
+        check("asap_moe_fp8_matmul", code)
 
 
 class Mailbox:

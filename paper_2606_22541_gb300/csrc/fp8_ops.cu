@@ -221,6 +221,22 @@ __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.w
 __device__ __forceinline__ void mbar_arrive_remote(uint32_t addr) {
   asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(addr) : "memory");
 }
+// tma_load_2d into both CTAs of a pair, at the same offsets, completing on both barriers.
+__device__ __forceinline__ void tma_load_2d_both(uint32_t dst, const CUtensorMap* m, uint32_t bar, int x, int y,
+                                                 uint64_t policy) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes.multicast::cluster.L2::cache_hint"
+      " [%0], [%1, {%3, %4}], [%2], %5, %6;" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(m)), "r"(bar), "r"(x), "r"(y), "h"(static_cast<uint16_t>(3)), "l"(policy)
+      : "memory");
+}
+// tc_commit on the barrier at this offset in both CTAs of a pair.
+__device__ __forceinline__ void tc_commit_both(uint32_t bar) {
+  asm volatile(
+      "tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
+      "h"(static_cast<uint16_t>(3))
+      : "memory");
+}
 // Shared memory of this CTA into one of the cluster, whose barrier counts the bytes.
 __device__ __forceinline__ void send(uint32_t to, uint32_t from, uint32_t bytes, uint32_t bar) {
   asm volatile("cp.async.bulk.shared::cluster.shared::cta.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(to),
@@ -478,8 +494,10 @@ __global__ void __launch_bounds__(kThreads, 2)
 // two TMEM partials of 256 columns, which eight epilogue warps add, times row and
 // block scale, into registers (warp w: TMEM lanes 32 (w % 4) .., one half of the
 // columns, i.e. one row of scale blocks), two 16-column chunks in turn, so that one
-// is on its way while the other is added.  Without K slices the CTAs are
-// persistent; otherwise a cluster of S CTAs shares a tile as above.
+// is on its way while the other is added.  Three forms: a CTA takes a tile after
+// the other; CTA pairs do, on two tiles with the same rows of B, of which each loads
+// one half for both (a tile's operands through L2 would be 16 TB/s at 2.7 PFLOP/s);
+// or a cluster of S CTAs shares a tile as above.
 //   warp 0: TMA producer; warp 1: TMEM and MMA; warps 4-11: epilogue, which takes
 //   registers from the first four warps (56 + 2 x 224 a thread).
 constexpr int kWideN = 256;
@@ -492,6 +510,7 @@ static_assert(kCtrlRegs + 2 * kEpiRegs <= 3 * 168, "the register split stays wit
 constexpr int kWideBars = 2 * kWideStages + 2 * kWidePartials + 6;
 constexpr int kWideSplit = 4;  // K slices at most
 constexpr int kStageWarp = 32 * 4 * 16;   // output staging of an epilogue warp
+enum { WIDE_SINGLE = 0, WIDE_PAIR = 1, WIDE_SPLIT = 2 };
 // The slices' sums of a column half: those to be sent, then those that come, each at
 // most (S - 1) / S of 128 x 128 floats, in the ring's place.
 constexpr int kHalfSums = (kWideSplit - 1) * (kRows / kWideSplit) * 128 * 4;
@@ -501,7 +520,9 @@ static_assert(4 * kHalfSums <= kWideStages * kWideStage, "the sums fit the ring"
 
 struct WideArgs {
   Fp8MatmulArgs p;
-  int split, m_tiles, tiles;
+  int cluster;  // K slices of a tile, or 2 for pairs
+  int m_tiles;  // tiles, or pairs of tiles, along the rows of A
+  int tiles;    // (pairs of) tiles in all
   int c_align;  // rows of c start on multiples of this many bytes (16, 4 or 2)
 };
 
@@ -510,7 +531,7 @@ __device__ __forceinline__ void add16(float* acc, const uint32_t (&v)[16], float
   for (int j = 0; j < 16; ++j) acc[j] = fmaf(s, __uint_as_float(v[j]), acc[j]);
 }
 
-template <bool SPLIT>
+template <int FORM>
 __global__ void __launch_bounds__(kWideThreads, 1)
     fp8_wide_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
                     const WideArgs args) {
@@ -518,12 +539,14 @@ __global__ void __launch_bounds__(kWideThreads, 1)
   const uint32_t base = smem_u32(smem_raw);
   const Fp8MatmulArgs& p = args.p;
   const bool aligned = (base & 1023u) == 0;  // the 128-byte swizzle needs it; the same in the cluster
-  const int S = SPLIT ? args.split : 1;
-  const int rank = blockIdx.x % S;
+  constexpr bool SPLIT = FORM == WIDE_SPLIT, PAIR = FORM == WIDE_PAIR;
+  const int cluster = FORM == WIDE_SINGLE ? 1 : args.cluster;
+  const int in_cluster = blockIdx.x % cluster, first = blockIdx.x / cluster;
+  const int step = gridDim.x / cluster;  // (pairs of) tiles between a CTA's
+  const int S = SPLIT ? cluster : 1, rank = SPLIT ? in_cluster : 0;
   const int blocks = (p.k + kFp8BK - 1) / kFp8BK;
   const int kb0 = static_cast<int>(static_cast<long long>(blocks) * rank / S);
   const int kb1 = static_cast<int>(static_cast<long long>(blocks) * (rank + 1) / S);
-  const int step = gridDim.x / S;  // tiles between a CTA's
   uint4* stage_all = reinterpret_cast<uint4*>(smem_raw + kWideStages * kWideStage);
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem_raw + kWideStages * kWideStage + 8 * kStageWarp);
   const uint32_t bar0 = smem_u32(bars);
@@ -541,7 +564,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
   if (threadIdx.x == 0) {
     for (int i = 0; i < kWideStages; ++i) {
       mbar_init(full(i), 1);
-      mbar_init(empty(i), 1);
+      mbar_init(empty(i), PAIR ? 2 : 1);  // (pairs: both CTAs have read the stage)
     }
     for (int i = 0; i < kWidePartials; ++i) {
       mbar_init(pfull(i), 1);
@@ -564,13 +587,15 @@ __global__ void __launch_bounds__(kWideThreads, 1)
     tmem_relinquish();
   }
   __syncwarp();
-  if (SPLIT) cluster_arrive();  // this CTA's barriers stand
+  if (FORM != WIDE_SINGLE) cluster_arrive();  // this CTA's barriers stand
   pdl_wait();
   if (!aligned && threadIdx.x == 0) record_status(p.status, ST_SMEM_ALIGN);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
+  if (PAIR) cluster_wait();
+  auto tok_of = [&](int tile) { return (tile % args.m_tiles * (PAIR ? 2 : 1) + (PAIR ? in_cluster : 0)) * kRows; };
   bool waited = false;  // for the cluster's barriers to stand
   auto give_up = [&]() {
     *abort_flag = 1;
@@ -585,8 +610,8 @@ __global__ void __launch_bounds__(kWideThreads, 1)
       const uint64_t pol = l2_policy(2);
       int issued = 0;
       bool ok = aligned;
-      for (int tile = blockIdx.x / S; ok && tile < args.tiles; tile += step) {
-        const int tok0 = tile % args.m_tiles * kRows, row0 = tile / args.m_tiles * kWideN;
+      for (int tile = first; ok && tile < args.tiles; tile += step) {
+        const int tok0 = tok_of(tile), row0 = tile / args.m_tiles * kWideN;
         for (int kb = kb0; kb < kb1; ++kb) {
           ok = __all_sync(kFull, mbar_wait(empty(r.s), r.phase ^ 1u, abort_flag));
           if (!ok) break;
@@ -594,13 +619,22 @@ __global__ void __launch_bounds__(kWideThreads, 1)
             const uint32_t st = base + r.s * kWideStage;
             mbar_arrive_expect_tx(full(r.s), kWideStage);
             tma_load_2d(st, &tmA, full(r.s), kb * kFp8BK, tok0, pol);
-            tma_load_2d(st + kRows * kFp8BK, &tmB, full(r.s), kb * kFp8BK, row0, pol);
+            if (PAIR)  // this CTA's half of the rows of B, for both
+              tma_load_2d_both(st + kRows * kFp8BK + in_cluster * kBBytes, &tmB, full(r.s), kb * kFp8BK,
+                               row0 + in_cluster * kRows, pol);
+            else
+              tma_load_2d(st + kRows * kFp8BK, &tmB, full(r.s), kb * kFp8BK, row0, pol);
           }
           issued = min(issued + 1, kWideStages);
           r.advance();
         }
       }
       if (issuer) pdl_launch();  // nothing left to load
+      if (PAIR)  // both CTAs' commits on this ring have come before the CTA may leave
+        for (int i = 0; ok && i < kWideStages; ++i) {
+          ok = __all_sync(kFull, mbar_wait(empty(r.s), r.phase ^ 1u, abort_flag));
+          r.advance();
+        }
       if (!ok && aligned) {
         if (issuer) give_up();
         // the copies in flight land before the CTA's memory goes away
@@ -608,6 +642,11 @@ __global__ void __launch_bounds__(kWideThreads, 1)
         for (int i = issued; i > 0; --i) {
           const int b = r.s - i;
           mbar_wait(full(b < 0 ? b + kWideStages : b), b < 0 ? r.phase ^ 1u : r.phase, &dummy);
+        }
+        if (PAIR) {  // (and those into the other CTA, which only it can wait for: a TMA load takes microseconds)
+          const uint64_t t0 = globaltimer_ns();
+          while (globaltimer_ns() - t0 < 2000000ull) {
+          }
         }
       }
     } else if (warp == 1) {
@@ -617,7 +656,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
       Ring<kWideStages> r;
       Ring<kWidePartials> t;
       bool ok = aligned, issued = false;
-      for (int tile = blockIdx.x / S; ok && tile < args.tiles; tile += step) {
+      for (int tile = first; ok && tile < args.tiles; tile += step) {
         for (int kb = kb0; kb < kb1; ++kb) {
           ok = mbar_wait_all(lane < 16 ? full(r.s) : pempty(t.s), lane < 16 ? r.phase : t.phase ^ 1u, abort_flag);
           if (!ok) break;
@@ -629,7 +668,8 @@ __global__ void __launch_bounds__(kWideThreads, 1)
             for (int kk = 0; kk < kFp8BK / 32; ++kk)
               mma_e4m3(tmem_base + t.s * kWideN, ad + 2 * kk, bd + 2 * kk, id, kk > 0 ? 1u : 0u);
             tc_commit(pfull(t.s));
-            tc_commit(empty(r.s));
+            if (PAIR) tc_commit_both(empty(r.s));
+            else tc_commit(empty(r.s));
           }
           __syncwarp();
           issued = true;
@@ -654,8 +694,8 @@ __global__ void __launch_bounds__(kWideThreads, 1)
     uint4* stage = stage_all + (warp - 4) * (kStageWarp / 16);
     Ring<kWidePartials> t;
     bool ok = aligned;
-    for (int tile = blockIdx.x / S; tile < args.tiles; tile += step) {
-      const int tok0 = tile % args.m_tiles * kRows, row0 = tile / args.m_tiles * kWideN + half * 128;
+    for (int tile = first; tile < args.tiles; tile += step) {
+      const int tok0 = tok_of(tile), row0 = tile / args.m_tiles * kWideN + half * 128;
       float acc[128];
 #pragma unroll
       for (int j = 0; j < 128; ++j) acc[j] = 0.f;
@@ -798,8 +838,8 @@ __global__ void __launch_bounds__(kWideThreads, 1)
     }
     if (!ok && aligned && lane == 0) give_up();
   }
-  if (SPLIT) {  // no CTA leaves while another may still send to it
-    if (!waited) cluster_wait();
+  if (FORM != WIDE_SINGLE) {  // no CTA leaves while another may still write to it
+    if (SPLIT && !waited) cluster_wait();
     __syncwarp();
     cluster_arrive_release();
     cluster_wait();
@@ -827,21 +867,32 @@ cudaError_t skinny(const CUtensorMap& tmA, const CUtensorMap& tmB, const Fp8Matm
                     Skinny<NT>::kSmem, s, a.split, tmA, tmB, a);
 }
 
-cudaError_t wide(const CUtensorMap& tmA, const CUtensorMap& tmB, const Fp8MatmulArgs& args, int num_sms,
-                 cudaStream_t s) {
+cudaError_t wide(const void* a, long long lda, const void* b, long long ldb, const Fp8MatmulArgs& args, int num_sms,
+                 cudaStream_t s, std::string* err) {
   const int blocks = ceil_div(args.k, kFp8BK);
-  WideArgs a{args, 1, ceil_div(args.m, kRows), 0, 0};
-  const long long tiles = static_cast<long long>(ceil_div(args.n, kWideN)) * a.m_tiles;
-  a.tiles = static_cast<int>(tiles);
+  const int m_tiles = ceil_div(args.m, kRows);
+  const long long tiles = static_cast<long long>(ceil_div(args.n, kWideN)) * m_tiles;
+  int split = 1;
+  while (split < kWideSplit && tiles * split * 2 <= num_sms && blocks >= 8 * split) split *= 2;
+  // Pairs where operand traffic counts: long contractions in more than one wave of tiles (single / pairs, us: 8045 x
+  // 4096 x 7168 191 / 174, 16000 x 2048 x 7168 218 / 197, 1024 x 28672 x 4096 99 / 94; but 700 x 4096 x 7168, one
+  // wave, 28 / 34, and 4096 x 7168 x 2048 53 / 55 to 61: a pair's CTAs wait for one another at every tile's end).
+  const bool pairs = split == 1 && m_tiles >= 2 && tiles > num_sms && blocks >= 32;
+  CUtensorMap tmA, tmB;
+  if (!encode_tmap_u8(&tmA, a, args.m, args.k, kRows, err, lda) ||
+      !encode_tmap_u8(&tmB, b, args.n, args.k, pairs ? kWideN / 2 : kWideN, err, ldb))
+    return cudaErrorInvalidValue;
   const uintptr_t at = reinterpret_cast<uintptr_t>(args.c) | static_cast<uintptr_t>(2 * args.ldc);
-  a.c_align = (at & 15u) == 0 ? 16 : (at & 3u) == 0 ? 4 : 2;
-  while (a.split < kWideSplit && tiles * a.split * 2 <= num_sms && blocks >= 8 * a.split) a.split *= 2;
-  const long long grid = a.split > 1 ? tiles * a.split : std::min<long long>(tiles, num_sms);
-  if (a.split > 1)
-    return launch_pdl(fp8_wide_kernel<true>, dim3(static_cast<unsigned>(grid)), dim3(kWideThreads), kWideSmem, s, a.split,
-                      tmA, tmB, a);
-  return launch_pdl(fp8_wide_kernel<false>, dim3(static_cast<unsigned>(grid)), dim3(kWideThreads), kWideSmem, s, 1, tmA,
-                    tmB, a);
+  WideArgs w{args, pairs ? 2 : split, pairs ? ceil_div(m_tiles, 2) : m_tiles, 0,
+             (at & 15u) == 0 ? 16 : (at & 3u) == 0 ? 4 : 2};
+  w.tiles = ceil_div(args.n, kWideN) * w.m_tiles;
+  const dim3 block(kWideThreads);
+  if (split > 1)
+    return launch_pdl(fp8_wide_kernel<WIDE_SPLIT>, dim3(w.tiles * split), block, kWideSmem, s, split, tmA, tmB, w);
+  if (pairs)
+    return launch_pdl(fp8_wide_kernel<WIDE_PAIR>, dim3(2 * std::min(w.tiles, num_sms / 2)), block, kWideSmem, s, 2, tmA,
+                      tmB, w);
+  return launch_pdl(fp8_wide_kernel<WIDE_SINGLE>, dim3(std::min(w.tiles, num_sms)), block, kWideSmem, s, 1, tmA, tmB, w);
 }
 
 }  // namespace
@@ -855,28 +906,24 @@ cudaError_t fp8_matmul_set_attributes() {
   set(fp8_skinny_kernel<16>, Skinny<16>::kSmem);
   set(fp8_skinny_kernel<32>, Skinny<32>::kSmem);
   set(fp8_skinny_kernel<64>, Skinny<64>::kSmem);
-  set(fp8_wide_kernel<false>, kWideSmem);
-  set(fp8_wide_kernel<true>, kWideSmem);
+  set(fp8_wide_kernel<WIDE_SINGLE>, kWideSmem);
+  set(fp8_wide_kernel<WIDE_PAIR>, kWideSmem);
+  set(fp8_wide_kernel<WIDE_SPLIT>, kWideSmem);
   return e;
 }
 
 cudaError_t fp8_matmul_launch(const void* a, long long lda, const void* b, long long ldb, const Fp8MatmulArgs& args,
                               int num_sms, cudaStream_t s, std::string* err) {
+  if (args.m > 64) return wide(a, lda, b, ldb, args, num_sms, s, err);
   CUtensorMap tmA, tmB;
-  const int nt = args.m <= 16 ? 16 : args.m <= 32 ? 32 : args.m <= 64 ? 64 : kRows;
-  if (!encode_tmap_u8(&tmA, a, args.m, args.k, nt, err, lda)) {
-    *err = "a: " + *err;
+  const int nt = args.m <= 16 ? 16 : args.m <= 32 ? 32 : 64;
+  if (!encode_tmap_u8(&tmA, a, args.m, args.k, nt, err, lda) ||
+      !encode_tmap_u8(&tmB, b, args.n, args.k, kRows, err, ldb))
     return cudaErrorInvalidValue;
-  }
-  if (!encode_tmap_u8(&tmB, b, args.n, args.k, nt == kRows ? kWideN : kRows, err, ldb)) {
-    *err = "b: " + *err;
-    return cudaErrorInvalidValue;
-  }
   switch (nt) {
     case 16: return skinny<16>(tmA, tmB, args, num_sms, s);
     case 32: return skinny<32>(tmA, tmB, args, num_sms, s);
-    case 64: return skinny<64>(tmA, tmB, args, num_sms, s);
-    default: return wide(tmA, tmB, args, num_sms, s);
+    default: return skinny<64>(tmA, tmB, args, num_sms, s);
   }
 }
 

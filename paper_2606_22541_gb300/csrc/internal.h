@@ -178,7 +178,7 @@ struct Fp8MatmulArgs {
   uint32_t* status;  // nullable
 };
 cudaError_t fp8_matmul_set_attributes();  // once per device
-// The product; err names the operand that TMA cannot read.
+// The product; *err is set where TMA cannot read an operand.
 cudaError_t fp8_matmul_launch(const void* a, long long lda, const void* b, long long ldb, const Fp8MatmulArgs& args,
                               int num_sms, cudaStream_t s, std::string* err);
 // Rows of bf16 (u: nullptr), or silu(x) * u, to e4m3 with an fp32 scale per row
