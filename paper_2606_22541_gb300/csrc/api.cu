@@ -131,7 +131,7 @@ Layout layout(const asap_moe_config& c, long long n) {
 // K slices of a tile so that a launch of ``tiles`` tiles has at least
 // kFewItems work items (2.5 per SM of a GB300: the size of a workspace needs no
 // GPU), with at least kFewMinSteps k-steps each.
-constexpr int kFewItems = 380, kFewMinSteps = 4;
+constexpr int kFewItems = 380, kFewMinSteps = 8;
 int few_slices(long long tiles, int k_steps) {
   const long long want = (kFewItems + tiles - 1) / tiles;
   return static_cast<int>(std::max<long long>(1, std::min<long long>(want, k_steps / kFewMinSteps)));
@@ -170,10 +170,9 @@ FewLayout few_layout(const asap_moe_config& c, int n) {
   a.h_ready = a.down_tickets + tH;
   a.gate_claims = a.h_ready + 1 + a.max_active;
   a.n_counters = a.gate_claims + 2;
-  // rings: 32 KB of weights a stage; operand rows (e4m3: and their scales) of the widest k-step, BF16 h rows twice
-  const int m8 = asap::round_up_dev(n, 8);
-  const int rows = fp8 ? asap::round_up_dev(n, 16) : 2 * m8;
-  a.x_slot = asap::round_up_dev(std::max(rows * 128, fp8 ? m8 * 132 : 0), 1024);
+  // rings: 32 KB of weights a stage; the operand rows (and their scales) of the widest k-step, BF16 h rows twice
+  const int widest = fp8 ? asap::round_up_dev(n, 16) : 2 * asap::round_up_dev(n, 8);
+  a.x_slot = asap::round_up_dev(fp8 ? std::max(widest * 128, n * 128 + widest * 4) : widest * 128, 1024);
   const int room = static_cast<int>(asap::kFewSmem - asap::kFewSmemState);
   a.stages_w = 4;
   while ((room - a.stages_w * 32768) / a.x_slot < std::min(a.stages_w, 4)) --a.stages_w;
@@ -186,15 +185,15 @@ FewLayout few_layout(const asap_moe_config& c, int n) {
     return o;
   };
   const size_t nk = static_cast<size_t>(n) * k;
-  // groups of 8 rows of the active experts: at most one per row, and the rows over 8 plus one per expert
-  const size_t groups = std::min<size_t>(nk, nk / 8 + a.max_active);
-  const size_t row = fp8 ? 132 : 128, hrows = fp8 ? 8 : 16;
+  // rows of an operand image's k-step, and the groups of four scales of the active experts' (e4m3)
+  const size_t rows = fp8 ? 1 : 2, quads = fp8 ? std::min(nk, (nk + 3 * a.max_active) / 4) : 0;
+  auto step_bytes = [&](size_t r) { return r * 128 + (fp8 ? (r + 3) / 4 * 16 : 0); };
   L.logits = take(static_cast<size_t>(8) * n * c.n_experts * 4);
   L.counters = take(a.n_counters * sizeof(int));
   L.sel_e = take(static_cast<size_t>(n) * k * 4);
   L.sel_w = take(static_cast<size_t>(n) * k * 4);
-  L.ximg = take(a.H / step * m8 * row);
-  L.himg = take((a.Is / step * (m8 / 8) + a.I / step * groups) * hrows * row);
+  L.ximg = take(a.H / step * step_bytes(n));
+  L.himg = take(a.Is / step * step_bytes(rows * n) + a.I / step * (rows * nk * 128 + quads * 16));
   L.p1 = take(a.s1 * nk * 2 * a.I * 4);
   L.p1s = take(static_cast<size_t>(a.s1) * n * 2 * a.Is * 4);
   L.y = take(a.s2 * nk * a.H * 4);
@@ -203,10 +202,12 @@ FewLayout few_layout(const asap_moe_config& c, int n) {
   return L;
 }
 
-// Bytes of workspace that serve every enqueuing call of n tokens.
+// Bytes of workspace that serve every enqueuing call of up to n tokens (a few-token call of fewer tokens may
+// have more slices, and so need more).
 size_t workspace_bytes(const asap_moe_config& c, int n) {
-  const size_t b = layout(c, n).total;
-  return n <= asap::kFewTokens ? std::max(b, few_layout(c, n).total) : b;
+  size_t b = layout(c, n).total;
+  for (int m = 1; m <= std::min(n, asap::kFewTokens); ++m) b = std::max(b, few_layout(c, m).total);
+  return b;
 }
 
 template <typename T>

@@ -51,10 +51,10 @@ constexpr unsigned kFull = 0xffffffffu;
 // ------------------------------------------------------------ operand images
 // A k-step's rows: R rows of 128 bytes, 16-byte chunk c of row r at chunk
 // c ^ (r % 8) (the 128-byte swizzle of a tile that starts on a 1024-byte
-// boundary), then, for FP8, R fp32 scales.
+// boundary), then, for FP8, R fp32 scales, up to a multiple of 16 bytes.
 template <bool FP8>
 __host__ __device__ constexpr int step_bytes(int rows) {
-  return rows * (FP8 ? 132 : 128);
+  return rows * 128 + (FP8 ? (rows + 3) / 4 * 16 : 0);
 }
 __device__ __forceinline__ int swizzled(int row, int byte) {
   return row * 128 + ((((byte >> 4) ^ (row & 7)) << 4) | (byte & 15));
@@ -72,12 +72,12 @@ __device__ __forceinline__ uint32_t ordered(float f) {
 __device__ __forceinline__ float unordered(uint32_t o) { return __uint_as_float((o >> 31) ? o & 0x7fffffffu : ~o); }
 
 // ------------------------------------------------------------ logits
-// Hidden states as operand image: rows n .. are zero.
+// Hidden states as operand image.
 template <bool FP8>
-__device__ __forceinline__ void write_image(const FewArgs& a, int rows, int thread, int threads) {
+__device__ __forceinline__ void write_image(const FewArgs& a, int thread, int threads) {
   constexpr int kAhead = 4;
   const int V = a.H / 8;  // 16-byte vectors of a row
-  const int total = rows * V;
+  const int total = a.n * V;
   const uint4* x = static_cast<const uint4*>(a.x);
   // FP8: 16 threads a group of 128 channels (total and the stride are multiples of 32: a warp stays together)
   for (int i0 = thread; i0 < total; i0 += kAhead * threads) {
@@ -85,7 +85,7 @@ __device__ __forceinline__ void write_image(const FewArgs& a, int rows, int thre
 #pragma unroll
     for (int r = 0; r < kAhead; ++r) {
       const int i = i0 + r * threads;
-      d[r] = i < a.n * V ? ld_dep(x + i) : make_uint4(0, 0, 0, 0);  // (rows follow one another)
+      d[r] = i < total ? ld_dep(x + i) : make_uint4(0, 0, 0, 0);  // (rows follow one another)
     }
 #pragma unroll
     for (int r = 0; r < kAhead; ++r) {
@@ -93,7 +93,7 @@ __device__ __forceinline__ void write_image(const FewArgs& a, int rows, int thre
       if (i >= total) break;
       const int t = i / V, v = i - t * V;
       if constexpr (!FP8) {
-        *reinterpret_cast<uint4*>(a.ximg + static_cast<long long>(v >> 3) * step_bytes<false>(rows) +
+        *reinterpret_cast<uint4*>(a.ximg + static_cast<long long>(v >> 3) * step_bytes<false>(a.n) +
                                   swizzled(t, (v & 7) * 16)) = d[r];
       } else {
         const float f[8] = {bf16_lo(d[r].x), bf16_hi(d[r].x), bf16_lo(d[r].y), bf16_hi(d[r].y),
@@ -105,9 +105,9 @@ __device__ __forceinline__ void write_image(const FewArgs& a, int rows, int thre
         for (int o = 8; o > 0; o >>= 1) am = fmaxf(am, __shfl_xor_sync(kFull, am, o));
         const GroupScale gs(am);
         const uint2 q = make_uint2(e4m3x4(gs, f[0], f[1], f[2], f[3]), e4m3x4(gs, f[4], f[5], f[6], f[7]));
-        uint8_t* step = a.ximg + static_cast<long long>(v >> 4) * step_bytes<true>(rows);
+        uint8_t* step = a.ximg + static_cast<long long>(v >> 4) * step_bytes<true>(a.n);
         *reinterpret_cast<uint2*>(step + swizzled(t, (v & 15) * 8)) = q;
-        if ((v & 15) == 0) *reinterpret_cast<float*>(step + rows * 128 + t * 4) = gs.s;
+        if ((v & 15) == 0) *reinterpret_cast<float*>(step + a.n * 128 + t * 4) = gs.s;
       }
     }
   }
@@ -199,7 +199,7 @@ __global__ void __launch_bounds__(kLogitThreads) few_logits_kernel(const __grid_
   }
   const int thread = blockIdx.x * kLogitThreads + threadIdx.x, threads = gridDim.x * kLogitThreads;
   for (int i = thread; i < a.n_counters; i += threads) a.counters[i] = 0;
-  write_image<FP8>(a, round_up_dev(n, 8), thread, threads);
+  write_image<FP8>(a, thread, threads);
 }
 
 // ------------------------------------------------------------ expert FFN
@@ -248,7 +248,7 @@ struct FewSmem {  // behind the rings
   int active;
   int items;
   int warp_total[kEpiWarps];
-  int expert[kMaxExperts], start[kMaxExperts], row8[kMaxExperts];
+  int expert[kMaxExperts], start[kMaxExperts], quads[kMaxExperts];
   unsigned long long mask[kMaxExperts];
   int pos[kFewTokens * kMaxTopK];
   float w[kFewTokens * kMaxTopK];
@@ -312,19 +312,20 @@ __device__ __forceinline__ FewItem decode(const FewArgs& a, const FewSmem& s, in
   T.mask = T.shared ? (a.n == 64 ? ~0ull : (1ull << a.n) - 1) : s.mask[T.j];
   T.tokens = T.shared ? a.n : __popcll(T.mask);
   T.start = T.shared ? 0 : s.start[T.j];
-  const int m8 = round_up_dev(T.down ? T.tokens : a.n, 8);
-  T.rows = T.down && !FP8 ? 2 * m8 : m8;
-  T.n = round_up_dev(T.rows, 16);
+  T.rows = T.down ? T.tokens : a.n;
+  T.n = round_up_dev(T.down && !FP8 ? 2 * round_up_dev(T.rows, 8) : T.rows, 16);
   return T;
 }
 
-// The h image of an expert: its first byte (m8 row groups before it, the shared expert's rows first).
+// The h image of an expert: its first byte (the shared expert's rows first, then the active experts'; FP8:
+// quads[j] groups of four scales before expert j's).  A k-step of BF16 holds the values' rows, then the rows of
+// what their rounding left.
 template <bool FP8>
 __device__ __forceinline__ uint8_t* h_image(const FewArgs& a, const FewSmem& s, const FewItem& T) {
-  const int kit = a.I / (FP8 ? 128 : 64), kits = a.Is / (FP8 ? 128 : 64);
-  constexpr int group = FP8 ? 8 : 16;  // rows per group of 8 tokens
-  const long long shared = static_cast<long long>(kits) * step_bytes<FP8>(round_up_dev(a.n, 8) / 8 * group);
-  return a.himg + (T.shared ? 0 : shared + static_cast<long long>(kit) * step_bytes<FP8>(s.row8[T.j] * group));
+  if (T.shared) return a.himg;
+  const long long kit = a.I / (FP8 ? 128 : 64), kits = a.Is / (FP8 ? 128 : 64);
+  return a.himg + kits * step_bytes<FP8>(FP8 ? a.n : 2 * a.n) +
+         kit * (FP8 ? s.start[T.j] * 128 + s.quads[T.j] * 16 : s.start[T.j] * 256);
 }
 
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
@@ -490,7 +491,7 @@ __device__ __forceinline__ void gate_token(const FewArgs& a, FewSmem& s, int t, 
 }
 
 // The routing of the call in every CTA, by its epilogue warps: active experts in
-// increasing order, their tokens, first rows and row groups, the row and weight
+// increasing order, their tokens and first rows, the row and weight
 // of every slot, and the number of work items.  Up to kOwnGate tokens every CTA
 // gates for itself (a token takes about 1.5 us); more are gated once, claimed one
 // by one, and read by every CTA when all are done (about 4 us for the round trips).
@@ -524,7 +525,7 @@ __device__ __forceinline__ bool list_experts(const FewArgs& a, FewSmem& s, int w
   epi_sync();
   const unsigned long long mask = s.mask[tid];  // thread e: expert e
   const int m = __popcll(mask);
-  const int v = m ? 1 | (m << 10) | (((m + 7) / 8) << 20) : 0;  // at most 256, 512 and 512 in all
+  const int v = m ? 1 | (m << 10) | (((m + 3) / 4) << 20) : 0;  // at most 256, 512 and 512 in all
   int incl = v;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
@@ -542,7 +543,7 @@ __device__ __forceinline__ bool list_experts(const FewArgs& a, FewSmem& s, int w
     const int j = before & 1023;
     s.expert[j] = tid;
     s.start[j] = (before >> 10) & 1023;
-    s.row8[j] = before >> 20;
+    s.quads[j] = before >> 20;
     s.mask[j] = mask;
   }
   if (tid == kMaxExperts - 1) {
@@ -572,8 +573,8 @@ __device__ __forceinline__ void write_h(const FewArgs& a, const FewSmem& s, cons
   constexpr int up = FP8 ? 128 : 8;
   const float* src = (T.shared ? a.p1s : a.p1) + static_cast<long long>(T.start) * W + T.tile * 256 + grow;
   uint8_t* img = h_image<FP8>(a, s, T);
-  const int m8 = round_up_dev(T.tokens, 8);
-  for (int c0 = 0; c0 < T.tokens; c0 += kAhead) {
+  const int m = T.tokens;
+  for (int c0 = 0; c0 < m; c0 += kAhead) {
     float4 g[kAhead], u[kAhead];
 #pragma unroll
     for (int r = 0; r < kAhead; ++r) g[r] = u[r] = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -581,7 +582,7 @@ __device__ __forceinline__ void write_h(const FewArgs& a, const FewSmem& s, cons
       float4 gi[kAhead], ui[kAhead];
 #pragma unroll
       for (int r = 0; r < kAhead; ++r) {
-        const float* at = src + i * plane + static_cast<long long>(min(c0 + r, T.tokens - 1)) * W;
+        const float* at = src + i * plane + static_cast<long long>(min(c0 + r, m - 1)) * W;
         gi[r] = __ldcg(reinterpret_cast<const float4*>(at));
         ui[r] = __ldcg(reinterpret_cast<const float4*>(at + up));
       }
@@ -594,7 +595,7 @@ __device__ __forceinline__ void write_h(const FewArgs& a, const FewSmem& s, cons
 #pragma unroll
     for (int r = 0; r < kAhead; ++r) {
       const int c = c0 + r;
-      if (c >= T.tokens) break;
+      if (c >= m) break;
       const float h[4] = {g[r].x / (1.0f + expf(-g[r].x)) * u[r].x, g[r].y / (1.0f + expf(-g[r].y)) * u[r].y,
                           g[r].z / (1.0f + expf(-g[r].z)) * u[r].z, g[r].w / (1.0f + expf(-g[r].w)) * u[r].w};
       if constexpr (FP8) {
@@ -602,16 +603,16 @@ __device__ __forceinline__ void write_h(const FewArgs& a, const FewSmem& s, cons
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) am = fmaxf(am, __shfl_xor_sync(kFull, am, o));
         const GroupScale gs(am);
-        uint8_t* step = img + static_cast<long long>(T.tile) * step_bytes<true>(m8);
+        uint8_t* step = img + static_cast<long long>(T.tile) * step_bytes<true>(m);
         *reinterpret_cast<uint32_t*>(step + swizzled(c, 4 * lane)) = e4m3x4(gs, h[0], h[1], h[2], h[3]);
-        if (lane == 0) *reinterpret_cast<float*>(step + m8 * 128 + c * 4) = gs.s;
+        if (lane == 0) *reinterpret_cast<float*>(step + m * 128 + c * 4) = gs.s;
       } else {
-        uint8_t* step = img + static_cast<long long>(2 * T.tile + (lane >> 4)) * step_bytes<false>(2 * m8);
+        uint8_t* step = img + static_cast<long long>(2 * T.tile + (lane >> 4)) * step_bytes<false>(2 * m);
         const uint32_t a0 = pack_bf16x2(h[0], h[1]), a1 = pack_bf16x2(h[2], h[3]);
         const uint32_t b0 = pack_bf16x2(h[0] - bf16_lo(a0), h[1] - bf16_hi(a0));
         const uint32_t b1 = pack_bf16x2(h[2] - bf16_lo(a1), h[3] - bf16_hi(a1));
         *reinterpret_cast<uint2*>(step + swizzled(c, 8 * (lane & 15))) = make_uint2(a0, a1);
-        *reinterpret_cast<uint2*>(step + swizzled(m8 + c, 8 * (lane & 15))) = make_uint2(b0, b1);
+        *reinterpret_cast<uint2*>(step + m * 128 + swizzled(c, 8 * (lane & 15))) = make_uint2(b0, b1);
       }
     }
   }
@@ -846,7 +847,10 @@ __global__ void __launch_bounds__(FP8 && NT == 64 ? kThreads : 512, 1) few_ffn_k
       if (!ok || item < 0) break;
       if (lane == 0) {
         const FewItem T = decode<FP8>(a, s, item);
-        const uint32_t bytes = step_bytes<FP8>(T.rows);
+        // (BF16 h: the second rows go to the next multiple of 8, where their columns begin)
+        const bool two = T.down && !FP8;
+        const uint32_t bytes = step_bytes<FP8>(T.rows), step = two ? 2 * bytes : bytes;
+        const uint32_t second = round_up_dev(T.rows, 8) * 128;
         const uint8_t* img = T.down ? h_image<FP8>(a, s, T) : a.ximg;
         if (T.down && !T.combine) {
           const int* ready = a.counters + a.h_ready + (T.shared ? 0 : 1 + T.j);
@@ -857,8 +861,10 @@ __global__ void __launch_bounds__(FP8 && NT == 64 ? kThreads : 512, 1) few_ffn_k
         for (int kb = T.kb0; ok && kb < T.kb1; ++kb) {
           ok = mbar_wait(bar(B_EX + st), ph ^ 1u, abort_flag);
           if (!ok) break;
-          mbar_arrive_expect_tx(bar(B_FX + st), bytes);
-          bulk_load(sX + st * a.x_slot, img + static_cast<long long>(kb) * bytes, bytes, bar(B_FX + st));
+          mbar_arrive_expect_tx(bar(B_FX + st), step);
+          const uint8_t* from = img + static_cast<long long>(kb) * step;
+          bulk_load(sX + st * a.x_slot, from, bytes, bar(B_FX + st));
+          if (two) bulk_load(sX + st * a.x_slot + second, from + bytes, bytes, bar(B_FX + st));
           issued = min(issued + 1, SX);
           if (++st == SX) st = 0, ph ^= 1u;
         }
@@ -1067,7 +1073,7 @@ __global__ void __launch_bounds__(FP8 && NT == 64 ? kThreads : 512, 1) few_ffn_k
         if (ok) {
           tc_fence_after();
           const uint32_t t0 = lanes + p.s * 2 * kHalf;
-          const int cols = T.down ? T.rows / 2 : T.rows;  // down: the columns of the roundings follow
+          const int cols = round_up_dev(T.rows, 8);  // down: the columns of the roundings follow
           int c = 0;
           for (int c0 = 0; c0 < cols; c0 += 8) {
             const uint32_t some = T.down ? (c0 + 8 <= T.tokens ? 0xffu : (1u << (T.tokens - c0)) - 1u)
