@@ -169,7 +169,7 @@ __global__ void __launch_bounds__(kQuantThreads, 8) fp8_quantize_kernel(const ui
 // cluster of S CTAs shares a tile, each with a slice of K.  Every 128-wide K block
 // is multiplied into one of the TMEM partials, which the epilogue warps add, times
 // the block's scales, into registers; the slices' sums meet in distributed shared
-// memory, each CTA adding those of 128 / S rows in rank order.  They travel as bulk
+// memory, each CTA adding those of about 128 / S rows in rank order.  They travel as bulk
 // copies, counted by the receiver's mbarrier.  (Plain stores between cluster
 // barriers and 16-byte st.async move about 0.5 TB/s over the whole GPU: 64 rows x
 // 4096 x 14336 on eight slices, 8 MB of sums, took 22 and 17 us.)  Two CTAs an
@@ -188,15 +188,15 @@ constexpr int kMaxSplit = 8;
 template <int NT>
 struct Skinny {
   static constexpr int kStage = kBBytes + NT * kFp8BK;
-  static constexpr int kStages = NT == 16 ? 5 : NT == 32 ? 4 : 3;  // about 100 KB
+  static constexpr int kStages = NT == 16 ? 5 : NT == 32 ? 4 : 3;  // about 100 KB: two CTAs an SM
   static constexpr int kPartials = 4;
   static constexpr uint32_t kTmem = NT * kPartials;
   static constexpr int kPitch = NT + 4;  // floats of a row of the slices' sums
-  static constexpr int kSums = kRows * kPitch;
+  static constexpr int kSums = (kRows + kMaxSplit - 1) * kPitch;  // slices x the rows of a rank, rounded up
   static constexpr int kBars = 2 * kStages + 2 * kPartials + 2;
   static constexpr size_t kSmem = kStages * kStage + 4 * kSums + 2 * NT * 4 + 8 * kBars + 16;
   static_assert(2 * (kSmem + 1024) <= 228 * 1024, "two CTAs an SM");
-  static_assert(4 * kSums <= kStages * kStage, "the ring holds the sums to be sent");
+  static_assert(4 * kRows * kPitch <= kStages * kStage, "the ring holds the sums to be sent");
 };
 
 struct SkinnyArgs {
@@ -278,7 +278,8 @@ __global__ void __launch_bounds__(kThreads, 2)
   auto pfull = [&](int i) { return bar0 + 8u * (2 * C::kStages + i); };
   auto pempty = [&](int i) { return bar0 + 8u * (2 * C::kStages + C::kPartials + i); };
   const uint32_t drain = bar0 + 8u * (C::kBars - 2), received = drain + 8u;
-  const int rows = kRows / S;  // whose sums this CTA adds
+  auto first_row = [&](int to) { return kRows * to / S; };  // of the rows whose sums CTA ``to`` adds
+  const int rows = first_row(rank + 1) - first_row(rank);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + C::kBars);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -296,7 +297,7 @@ __global__ void __launch_bounds__(kThreads, 2)
     mbar_init(received, 1);
     *abort_flag = aligned ? 0 : 1;
     fence_barrier_init();
-    if (S > 1) mbar_arrive_expect_tx(received, static_cast<uint32_t>(4 * C::kSums));
+    if (S > 1) mbar_arrive_expect_tx(received, static_cast<uint32_t>(4 * S * rows * C::kPitch));
     tma_prefetch_desc(&tmA);
     tma_prefetch_desc(&tmB);
   } else if (warp == 1) {
@@ -458,18 +459,32 @@ __global__ void __launch_bounds__(kThreads, 2)
       epi_sync();
       cluster_wait();
       if (ok && tid < S) {
-        const uint32_t bytes = static_cast<uint32_t>(rows * C::kPitch * 4);
-        send(map_rank(smem_u32(sums) + rank * bytes, tid), base + tid * bytes, bytes, map_rank(received, tid));
+        const int at = first_row(tid);
+        const uint32_t bytes = static_cast<uint32_t>((first_row(tid + 1) - at) * C::kPitch * 4);
+        send(map_rank(smem_u32(sums) + rank * bytes, tid), base + at * C::kPitch * 4, bytes, map_rank(received, tid));
       }
       __syncwarp();
       ok = ok && __all_sync(kFull, mbar_wait(received, 0, abort_flag));
-      const int total = rows * min(NT, p.m - tok0);
-      for (int i = tid; ok && i < total; i += kEpiThreads) {
-        const int rr = i & (rows - 1), c = i / rows, n = row0 + rank * rows + rr;  // (rows: a power of two)
-        if (n >= p.n) continue;
-        float v = sums[rr * C::kPitch + c];
-        for (int s = 1; s < S; ++s) v += sums[(s * rows + rr) * C::kPitch + c];
-        out[static_cast<long long>(tok0 + c) * p.ldc + n] = __float2bfloat16_rn(v);
+      // four columns of a row at a time, rows along the lanes
+      const int cols = min(NT, p.m - tok0);
+      int c = tid / rows * 4, rr = tid % rows;
+      while (ok && c < cols) {
+        const float* at = sums + rr * C::kPitch + c;
+        float4 v = *reinterpret_cast<const float4*>(at);
+        for (int s = 1; s < S; ++s) {
+          at += rows * C::kPitch;
+          const float4 w = *reinterpret_cast<const float4*>(at);
+          v.x += w.x, v.y += w.y, v.z += w.z, v.w += w.w;
+        }
+        const int n = row0 + first_row(rank) + rr;
+        const float f[4] = {v.x, v.y, v.z, v.w};
+        __nv_bfloat16* o = out + static_cast<long long>(tok0 + c) * p.ldc + n;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (n < p.n && c + i < cols) o[i * p.ldc] = __float2bfloat16_rn(f[i]);
+        rr += kEpiThreads % rows;
+        c += kEpiThreads / rows * 4;
+        if (rr >= rows) rr -= rows, c += 4;
       }
     }
     if (!ok && lane == 0 && aligned) give_up();
@@ -859,10 +874,10 @@ cudaError_t skinny(const CUtensorMap& tmA, const CUtensorMap& tmB, const Fp8Matm
   const int blocks = ceil_div(args.k, kFp8BK);
   SkinnyArgs a{args, 1, ceil_div(args.m, NT)};
   const long long tiles = static_cast<long long>(ceil_div(args.n, kRows)) * a.m_tiles;
-  // K slices as long as all CTAs are resident at once (a second wave costs more than shorter slices save: 45 rows
-  // x 28672 x 4096 on 1, 2 and 4 slices 24, 38 and 46 us; 64 x 4096 x 14336 on 2, 4 and 8, all one wave, 31, 20
-  // and 18)
-  while (a.split < kMaxSplit && tiles * a.split * 2 <= 2 * num_sms && blocks >= 4 * a.split) a.split *= 2;
+  // K slices of two blocks and more as long as all CTAs are resident at once (a second wave costs more than shorter
+  // slices save: 45 rows x 28672 x 4096 on 1, 2 and 4 slices 24, 38 and 46 us; 64 x 4100 x 14300 on 4, 6 and 8, all
+  // one wave, 18.0, 16.9 and 15.4; 64 x 12288 x 6144 on 1 and 3 23.6 and 18.7)
+  a.split = static_cast<int>(std::max<long long>(1, std::min<long long>({kMaxSplit, 2 * num_sms / tiles, blocks / 2})));
   return launch_pdl(fp8_skinny_kernel<NT>, dim3(static_cast<unsigned>(tiles * a.split)), dim3(kThreads),
                     Skinny<NT>::kSmem, s, a.split, tmA, tmB, a);
 }
@@ -872,8 +887,10 @@ cudaError_t wide(const void* a, long long lda, const void* b, long long ldb, con
   const int blocks = ceil_div(args.k, kFp8BK);
   const int m_tiles = ceil_div(args.m, kRows);
   const long long tiles = static_cast<long long>(ceil_div(args.n, kWideN)) * m_tiles;
+  // (slices that meet cost 2.5 us on two CTAs and 5 on four: 400 x 2048 x 2048, 16 blocks, on 1, 2 and 4 slices 10.2,
+  // 10.0 and 12.2 us; 256 x 4096 x 4096, 32 blocks, 17.3, 14.4 and 15.5; 400 x 2048 x 7168, 56, 24.4, 19.0 and 17.8)
   int split = 1;
-  while (split < kWideSplit && tiles * split * 2 <= num_sms && blocks >= 8 * split) split *= 2;
+  while (split < kWideSplit && tiles * split * 2 <= num_sms && blocks >= 24 * split) split *= 2;
   // Pairs where operand traffic counts: long contractions in more than one wave of tiles (single / pairs, us: 8045 x
   // 4096 x 7168 191 / 174, 16000 x 2048 x 7168 218 / 197, 1024 x 28672 x 4096 99 / 94; but 700 x 4096 x 7168, one
   // wave, 28 / 34, and 4096 x 7168 x 2048 53 / 55 to 61: a pair's CTAs wait for one another at every tile's end).
@@ -914,7 +931,12 @@ cudaError_t fp8_matmul_set_attributes() {
 
 cudaError_t fp8_matmul_launch(const void* a, long long lda, const void* b, long long ldb, const Fp8MatmulArgs& args,
                               int num_sms, cudaStream_t s, std::string* err) {
-  if (args.m > 64) return wide(a, lda, b, ldb, args, num_sms, s, err);
+  // More than 64 rows go to the wide tiles, unless the product is so small that its narrow tiles, cut into slices,
+  // still are one wave and long enough to be worth cutting (wide / narrow: 65 x 512 x 2048 10.9 / 7.1 us, 128 x 2048 x
+  // 7168 17.9 / 14.2, 200 x 2048 x 7168 18.9 / 17.3, 1000 x 512 x 4096 18.0 / 15.5; but twice as many tiles, 256 x
+  // 4096 x 4096, 16.7 / 19.2, and half the blocks, 65 x 4096 x 1024, 8.0 / 10.7)
+  const long long narrow = static_cast<long long>(ceil_div(args.m, 64)) * ceil_div(args.n, kRows);
+  if (args.m > 64 && (narrow > num_sms / 2 || args.k <= 15 * kFp8BK)) return wide(a, lda, b, ldb, args, num_sms, s, err);
   CUtensorMap tmA, tmB;
   const int nt = args.m <= 16 ? 16 : args.m <= 32 ? 32 : 64;
   if (!encode_tmap_u8(&tmA, a, args.m, args.k, nt, err, lda) ||
