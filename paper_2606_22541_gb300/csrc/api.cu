@@ -1457,19 +1457,18 @@ ASAP_API int asap_moe_layer_batched_dyn(asap_moe_t h, const int32_t* layer_id, i
 namespace {
 
 // What the product needs to know of a device, found out once per device.
-struct MatmulDevice {
-  bool known = false;
-  int num_sms = 0;
-};
-
-int matmul_device(MatmulDevice* out) {
+int matmul_device(asap::Fp8MatmulDevice* out) {
+  struct Device {
+    bool known = false;
+    asap::Fp8MatmulDevice d;
+  };
   static std::mutex lock;
-  static std::vector<MatmulDevice> devices;
+  static std::vector<Device> devices;
   int dev = 0;
   CU_TRY(cudaGetDevice(&dev), "cudaGetDevice");
   std::lock_guard<std::mutex> g(lock);
   if (static_cast<size_t>(dev) >= devices.size()) devices.resize(dev + 1);
-  MatmulDevice& d = devices[dev];
+  Device& d = devices[dev];
   if (!d.known) {
     int major = 0, minor = 0;
     CU_TRY(cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev), "compute capability");
@@ -1477,11 +1476,11 @@ int matmul_device(MatmulDevice* out) {
     if (major != 10 || minor != 3)
       return fail(ASAP_ERR_UNSUPPORTED, "libasap_moe is built for sm_103a (GB300) only; device is sm_" +
                                             std::to_string(major) + std::to_string(minor));
-    CU_TRY(cudaDeviceGetAttribute(&d.num_sms, cudaDevAttrMultiProcessorCount, dev), "SM count");
-    CU_TRY(asap::fp8_matmul_set_attributes(), "product attributes");
+    CU_TRY(cudaDeviceGetAttribute(&d.d.num_sms, cudaDevAttrMultiProcessorCount, dev), "SM count");
+    CU_TRY(asap::fp8_matmul_device(&d.d), "product attributes");
     d.known = true;
   }
-  *out = d;
+  *out = d.d;
   return ASAP_OK;
 }
 
@@ -1530,7 +1529,7 @@ ASAP_API int asap_moe_fp8_matmul(const void* a, int64_t lda, const float* a_scal
   const int blocks = asap::ceil_div(k, 128);
   if (lda < k || ldb < k || ldc < n || lds_a < blocks || lds_b < blocks)
     return fail(ASAP_ERR_INVALID, "a row stride is shorter than its rows");
-  MatmulDevice dev;
+  asap::Fp8MatmulDevice dev;
   const int r = matmul_device(&dev);
   if (r != ASAP_OK) return r;
   asap::Fp8MatmulArgs args{};
@@ -1545,7 +1544,7 @@ ASAP_API int asap_moe_fp8_matmul(const void* a, int64_t lda, const float* a_scal
   args.ldc = ldc;
   args.status = status;
   std::string err;
-  const cudaError_t e = asap::fp8_matmul_launch(a, lda, b, ldb, args, dev.num_sms, S(stream), &err);
+  const cudaError_t e = asap::fp8_matmul_launch(a, lda, b, ldb, args, dev, S(stream), &err);
   if (!err.empty()) return fail(ASAP_ERR_INVALID, err);
   if (e != cudaSuccess) return cuda_fail(e, "product launch");
   return ASAP_OK;

@@ -3,6 +3,7 @@
 #include "common.cuh"
 #include "e4m3.cuh"
 #include "internal.h"
+#include "pair.cuh"
 
 #include <algorithm>
 
@@ -193,6 +194,10 @@ struct Skinny {
   static constexpr uint32_t kTmem = NT * kPartials;
   static constexpr int kPitch = NT + 4;  // floats of a row of the slices' sums
   static constexpr int kSums = (kRows + kMaxSplit - 1) * kPitch;  // slices x the rows of a rank, rounded up
+  // hundredths of a microsecond: a K block, the meeting of two slices, a second CTA on the SMs
+  static constexpr int kBlock = NT == 16 ? 23 : NT == 32 ? 29 : 31;
+  static constexpr int kMeet = NT == 16 ? 95 : NT == 32 ? 130 : 186;
+  static constexpr int kTwo = NT == 16 ? 100 : NT == 32 ? 150 : 250;
   static constexpr int kBars = 2 * kStages + 2 * kPartials + 2;
   static constexpr size_t kSmem = kStages * kStage + 4 * kSums + 2 * NT * 4 + 8 * kBars + 16;
   static_assert(2 * (kSmem + 1024) <= 228 * 1024, "two CTAs an SM");
@@ -204,39 +209,11 @@ struct SkinnyArgs {
   int split, m_tiles;
 };
 
-__device__ __forceinline__ uint32_t map_rank(uint32_t addr, uint32_t rank) {
-  uint32_t d;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(d) : "r"(addr), "r"(rank));
-  return d;
-}
 // Barrier of the cluster's threads; the first orders no memory (barriers are
 // initialised with a fence of their own).
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory"); }
 __device__ __forceinline__ void cluster_arrive_release() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait;" ::: "memory"); }
-// Arrive on a barrier of the cluster's CTA that addr names (map_rank).  Neither
-// this nor the waits take cluster scope, which stalls a thread for thousands of
-// cycles behind the loads in flight: what they order is counted in bytes or has
-// been seen to be done.
-__device__ __forceinline__ void mbar_arrive_remote(uint32_t addr) {
-  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(addr) : "memory");
-}
-// tma_load_2d into both CTAs of a pair, at the same offsets, completing on both barriers.
-__device__ __forceinline__ void tma_load_2d_both(uint32_t dst, const CUtensorMap* m, uint32_t bar, int x, int y,
-                                                 uint64_t policy) {
-  asm volatile(
-      "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes.multicast::cluster.L2::cache_hint"
-      " [%0], [%1, {%3, %4}], [%2], %5, %6;" ::"r"(dst),
-      "l"(reinterpret_cast<uint64_t>(m)), "r"(bar), "r"(x), "r"(y), "h"(static_cast<uint16_t>(3)), "l"(policy)
-      : "memory");
-}
-// tc_commit on the barrier at this offset in both CTAs of a pair.
-__device__ __forceinline__ void tc_commit_both(uint32_t bar) {
-  asm volatile(
-      "tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
-      "h"(static_cast<uint16_t>(3))
-      : "memory");
-}
 // Shared memory of this CTA into one of the cluster, whose barrier counts the bytes.
 __device__ __forceinline__ void send(uint32_t to, uint32_t from, uint32_t bytes, uint32_t bar) {
   asm volatile("cp.async.bulk.shared::cluster.shared::cta.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(to),
@@ -461,7 +438,7 @@ __global__ void __launch_bounds__(kThreads, 2)
       if (ok && tid < S) {
         const int at = first_row(tid);
         const uint32_t bytes = static_cast<uint32_t>((first_row(tid + 1) - at) * C::kPitch * 4);
-        send(map_rank(smem_u32(sums) + rank * bytes, tid), base + at * C::kPitch * 4, bytes, map_rank(received, tid));
+        send(pair_map(smem_u32(sums) + rank * bytes, tid), base + at * C::kPitch * 4, bytes, pair_map(received, tid));
       }
       __syncwarp();
       ok = ok && __all_sync(kFull, mbar_wait(received, 0, abort_flag));
@@ -505,85 +482,98 @@ __global__ void __launch_bounds__(kThreads, 2)
 }
 
 // ------------------------------------------------------------ product, rows of A as the M operand
-// A tile is 128 rows of A (M) and 256 of B (N).  Every 128-wide K block has one of
-// two TMEM partials of 256 columns, which eight epilogue warps add, times row and
-// block scale, into registers (warp w: TMEM lanes 32 (w % 4) .., one half of the
-// columns, i.e. one row of scale blocks), two 16-column chunks in turn, so that one
-// is on its way while the other is added.  Three forms: a CTA takes a tile after
-// the other; CTA pairs do, on two tiles with the same rows of B, of which each loads
-// one half for both (a tile's operands through L2 would be 16 TB/s at 2.7 PFLOP/s);
-// or a cluster of S CTAs shares a tile as above.
-//   warp 0: TMA producer; warp 1: TMEM and MMA; warps 4-11: epilogue, which takes
-//   registers from the first four warps (56 + 2 x 224 a thread).
-constexpr int kWideN = 256;
-constexpr int kWideStages = 4;
-constexpr int kWideStage = (kRows + kWideN) * kFp8BK;
-constexpr int kWidePartials = 2;
-constexpr int kWideThreads = 32 * 12;
-constexpr int kCtrlRegs = 56, kEpiRegs = 224;
-static_assert(kCtrlRegs + 2 * kEpiRegs <= 3 * 168, "the register split stays within the launch's registers");
-constexpr int kWideBars = 2 * kWideStages + 2 * kWidePartials + 6;
+// A tile is 128 rows of A (M) and TN = 256 or 128 of B (N).  Every 128-wide K block has one of two TMEM partials of TN
+// columns, which the epilogue warps add, times row and block scale, into registers (warp w: TMEM lanes 32 (w % 4) .., a
+// half of 128 columns, i.e. one row of scale blocks): two 16-column chunks in turn, so that one is on its way while the
+// other is added, in pairs (f32x2: 2 % of 8045 x 4096 x 7168, 4 % of 8045 x 28672 x 1024).  One CTA of 256 columns has
+// an SM, two of 128 do.  A CTA takes a tile after the other, or a cluster of S CTAs shares one as above.
+//   warp 0: TMA producer; warp 1: TMEM and MMA; from warp 4 on: epilogue, which takes
+//   registers from the first four warps.
+// What bounds it: the adding.  8045 x 4096 x 7168 takes 172 us (2.75 PFLOP/s at about 1.85 GHz), 154 with an epilogue
+// that only passes the partials on (3.07 PFLOP/s), 160 with one that reads them all and adds nothing.  On top of its K
+// loop a tile takes 1.5 us to round and store, while the next tile's first two blocks are multiplied: with short
+// contractions that shows (8045 x 28672 x 1024 229 us, 2.06 PFLOP/s).  Tried and no faster: 32-column chunks (the
+// control warps then have too few registers), pairs of CTAs that load each other's half of the rows of B by multicast,
+// and pairs that multiply 256 rows by 256 together (cta_group::2), both 180 us in single calls and 187 to 192 back to
+// back: what operands cost through L2 and shared memory is hidden behind the adding.
 constexpr int kWideSplit = 4;  // K slices at most
-constexpr int kStageWarp = 32 * 4 * 16;   // output staging of an epilogue warp
-enum { WIDE_SINGLE = 0, WIDE_PAIR = 1, WIDE_SPLIT = 2 };
-// The slices' sums of a column half: those to be sent, then those that come, each at
-// most (S - 1) / S of 128 x 128 floats, in the ring's place.
-constexpr int kHalfSums = (kWideSplit - 1) * (kRows / kWideSplit) * 128 * 4;
-constexpr size_t kWideSmem = kWideStages * kWideStage + 8 * kStageWarp + 8 * kWideBars + 16;
-static_assert(kWideSmem <= 227 * 1024, "shared memory budget");
-static_assert(4 * kHalfSums <= kWideStages * kWideStage, "the sums fit the ring");
+template <int TN>
+struct Wide {
+  static constexpr int kStages = TN == 256 ? 4 : 3;
+  static constexpr int kStage = (kRows + TN) * kFp8BK;
+  static constexpr int kPartials = 2;
+  static constexpr int kEpiWarps = TN / 32;
+  static constexpr int kThreads = 128 + 32 * kEpiWarps;
+  static constexpr int kCtas = 256 / TN;  // an SM
+  static constexpr int kCtrlRegs = TN == 256 ? 56 : 40, kEpiRegs = TN == 256 ? 224 : 216;
+  static constexpr int kLaunchRegs = 65536 / (kCtas * kThreads) / 8 * 8;
+  static_assert(4 * kCtrlRegs + kEpiWarps * kEpiRegs <= kThreads / 32 * kLaunchRegs,
+                "the register split stays within the launch's registers");
+  static constexpr int kBars = 2 * kStages + 2 * kPartials + 6;
+  static constexpr int kStageWarp = 2 * 32 * 64;  // an epilogue warp's output staging: two rounds of 32 columns
+  static constexpr size_t kSmem = kStages * kStage + kEpiWarps * kStageWarp + 8 * kBars + 16;
+  static_assert(kCtas * (kSmem + 1024) <= 228 * 1024, "shared memory budget");
+};
+// The slices' sums of 128 columns: those to be sent, then those that come, each at most (S - 1) / S of 128 x 128
+// floats, in the ring's place.
+constexpr int kSliceSums = (kWideSplit - 1) * (kRows / kWideSplit) * 128 * 4;
+static_assert(2 * kSliceSums <= Wide<128>::kStages * Wide<128>::kStage &&
+              4 * kSliceSums <= Wide<256>::kStages * Wide<256>::kStage, "the sums fit the ring");
 
 struct WideArgs {
   Fp8MatmulArgs p;
-  int cluster;  // K slices of a tile, or 2 for pairs
-  int m_tiles;  // tiles, or pairs of tiles, along the rows of A
-  int tiles;    // (pairs of) tiles in all
+  int split;    // K slices of a tile: the cluster
+  int m_tiles;  // tiles along the rows of A
+  int tiles;    // in all
   int c_align;  // rows of c start on multiples of this many bytes (16, 4 or 2)
 };
 
 __device__ __forceinline__ void add16(float* acc, const uint32_t (&v)[16], float s) {
+  const uint64_t ss = pair(s, s);
 #pragma unroll
-  for (int j = 0; j < 16; ++j) acc[j] = fmaf(s, __uint_as_float(v[j]), acc[j]);
+  for (int j = 0; j < 16; j += 2) {
+    const uint64_t r = fma2(pair(__uint_as_float(v[j]), __uint_as_float(v[j + 1])), ss, pair(acc[j], acc[j + 1]));
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(acc[j]), "=f"(acc[j + 1]) : "l"(r));
+  }
 }
 
-template <int FORM>
-__global__ void __launch_bounds__(kWideThreads, 1)
+template <bool SPLIT, int TN>
+__global__ void __launch_bounds__(Wide<TN>::kThreads, Wide<TN>::kCtas)
     fp8_wide_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
-                    const WideArgs args) {
+                    const __grid_constant__ CUtensorMap tmC, const WideArgs args) {
+  using C = Wide<TN>;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   const uint32_t base = smem_u32(smem_raw);
   const Fp8MatmulArgs& p = args.p;
   const bool aligned = (base & 1023u) == 0;  // the 128-byte swizzle needs it; the same in the cluster
-  constexpr bool SPLIT = FORM == WIDE_SPLIT, PAIR = FORM == WIDE_PAIR;
-  const int cluster = FORM == WIDE_SINGLE ? 1 : args.cluster;
-  const int in_cluster = blockIdx.x % cluster, first = blockIdx.x / cluster;
-  const int step = gridDim.x / cluster;  // (pairs of) tiles between a CTA's
-  const int S = SPLIT ? cluster : 1, rank = SPLIT ? in_cluster : 0;
+  const int S = SPLIT ? args.split : 1, rank = SPLIT ? blockIdx.x % S : 0;
+  const int first = blockIdx.x / S, step = gridDim.x / S;  // a CTA's tiles
   const int blocks = (p.k + kFp8BK - 1) / kFp8BK;
   const int kb0 = static_cast<int>(static_cast<long long>(blocks) * rank / S);
   const int kb1 = static_cast<int>(static_cast<long long>(blocks) * (rank + 1) / S);
-  uint4* stage_all = reinterpret_cast<uint4*>(smem_raw + kWideStages * kWideStage);
-  uint64_t* bars = reinterpret_cast<uint64_t*>(smem_raw + kWideStages * kWideStage + 8 * kStageWarp);
+  uint8_t* stage_all = smem_raw + C::kStages * C::kStage;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(stage_all + C::kEpiWarps * C::kStageWarp);
   const uint32_t bar0 = smem_u32(bars);
   auto full = [&](int i) { return bar0 + 8u * i; };
-  auto empty = [&](int i) { return bar0 + 8u * (kWideStages + i); };
-  auto pfull = [&](int i) { return bar0 + 8u * (2 * kWideStages + i); };
-  auto pempty = [&](int i) { return bar0 + 8u * (2 * kWideStages + kWidePartials + i); };
-  // all CTAs' rings are done with; per column half: the rows to be sent are written, the slices have come
-  const uint32_t drain = bar0 + 8u * (kWideBars - 6), rings = drain + 8u, written = drain + 16u, received = drain + 32u;
-  const int rows = kRows / S;  // whose sums this CTA adds
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + kWideBars);
+  auto empty = [&](int i) { return bar0 + 8u * (C::kStages + i); };
+  auto pfull = [&](int i) { return bar0 + 8u * (2 * C::kStages + i); };
+  auto pempty = [&](int i) { return bar0 + 8u * (2 * C::kStages + C::kPartials + i); };
+  // all CTAs' rings are done with; per 128 columns: the rows to be sent are written, the slices have come
+  const uint32_t drain = bar0 + 8u * (C::kBars - 6), rings = drain + 8u, written = drain + 16u, received = drain + 32u;
+  auto first_row = [&](int to) { return kRows * to / S; };  // of the rows whose sums CTA ``to`` adds
+  const int own0 = first_row(rank), own1 = first_row(rank + 1);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + C::kBars);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
-    for (int i = 0; i < kWideStages; ++i) {
+    for (int i = 0; i < C::kStages; ++i) {
       mbar_init(full(i), 1);
-      mbar_init(empty(i), PAIR ? 2 : 1);  // (pairs: both CTAs have read the stage)
+      mbar_init(empty(i), 1);
     }
-    for (int i = 0; i < kWidePartials; ++i) {
+    for (int i = 0; i < C::kPartials; ++i) {
       mbar_init(pfull(i), 1);
-      mbar_init(pempty(i), 8);
+      mbar_init(pempty(i), C::kEpiWarps);
     }
     mbar_init(drain, 1);
     mbar_init(rings, S);
@@ -594,23 +584,23 @@ __global__ void __launch_bounds__(kWideThreads, 1)
     *abort_flag = aligned ? 0 : 1;
     fence_barrier_init();
     if (SPLIT)
-      for (int i = 0; i < 2; ++i) mbar_arrive_expect_tx(received + 8u * i, static_cast<uint32_t>((S - 1) * rows * 512));
+      for (uint32_t i = 0; i < TN / 128; ++i)
+        mbar_arrive_expect_tx(received + 8u * i, static_cast<uint32_t>((S - 1) * (own1 - own0) * 512));
     tma_prefetch_desc(&tmA);
     tma_prefetch_desc(&tmB);
+    if (!SPLIT && args.c_align == 16) tma_prefetch_desc(&tmC);
   } else if (warp == 1) {
-    tmem_alloc(smem_u32(tmem_slot), 512);
+    tmem_alloc(smem_u32(tmem_slot), 2 * TN);
     tmem_relinquish();
   }
   __syncwarp();
-  if (FORM != WIDE_SINGLE) cluster_arrive();  // this CTA's barriers stand
+  if (SPLIT) cluster_arrive();  // this CTA's barriers stand
   pdl_wait();
   if (!aligned && threadIdx.x == 0) record_status(p.status, ST_SMEM_ALIGN);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
-  if (PAIR) cluster_wait();
-  auto tok_of = [&](int tile) { return (tile % args.m_tiles * (PAIR ? 2 : 1) + (PAIR ? in_cluster : 0)) * kRows; };
   bool waited = false;  // for the cluster's barriers to stand
   auto give_up = [&]() {
     *abort_flag = 1;
@@ -618,58 +608,44 @@ __global__ void __launch_bounds__(kWideThreads, 1)
   };
 
   if (warp < 4) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kCtrlRegs));
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kCtrlRegs));
     if (warp == 0) {
       const bool issuer = elect_one();
-      Ring<kWideStages> r;
+      Ring<C::kStages> r;
       const uint64_t pol = l2_policy(2);
       int issued = 0;
       bool ok = aligned;
       for (int tile = first; ok && tile < args.tiles; tile += step) {
-        const int tok0 = tok_of(tile), row0 = tile / args.m_tiles * kWideN;
+        const int tok0 = tile % args.m_tiles * kRows, row0 = tile / args.m_tiles * TN;
         for (int kb = kb0; kb < kb1; ++kb) {
           ok = __all_sync(kFull, mbar_wait(empty(r.s), r.phase ^ 1u, abort_flag));
           if (!ok) break;
           if (issuer) {
-            const uint32_t st = base + r.s * kWideStage;
-            mbar_arrive_expect_tx(full(r.s), kWideStage);
+            const uint32_t st = base + r.s * C::kStage;
+            mbar_arrive_expect_tx(full(r.s), C::kStage);
             tma_load_2d(st, &tmA, full(r.s), kb * kFp8BK, tok0, pol);
-            if (PAIR)  // this CTA's half of the rows of B, for both
-              tma_load_2d_both(st + kRows * kFp8BK + in_cluster * kBBytes, &tmB, full(r.s), kb * kFp8BK,
-                               row0 + in_cluster * kRows, pol);
-            else
-              tma_load_2d(st + kRows * kFp8BK, &tmB, full(r.s), kb * kFp8BK, row0, pol);
+            tma_load_2d(st + kRows * kFp8BK, &tmB, full(r.s), kb * kFp8BK, row0, pol);
           }
-          issued = min(issued + 1, kWideStages);
+          issued = min(issued + 1, C::kStages);
           r.advance();
         }
       }
       if (issuer) pdl_launch();  // nothing left to load
-      if (PAIR)  // both CTAs' commits on this ring have come before the CTA may leave
-        for (int i = 0; ok && i < kWideStages; ++i) {
-          ok = __all_sync(kFull, mbar_wait(empty(r.s), r.phase ^ 1u, abort_flag));
-          r.advance();
-        }
       if (!ok && aligned) {
         if (issuer) give_up();
         // the copies in flight land before the CTA's memory goes away
         int dummy = 0;
         for (int i = issued; i > 0; --i) {
           const int b = r.s - i;
-          mbar_wait(full(b < 0 ? b + kWideStages : b), b < 0 ? r.phase ^ 1u : r.phase, &dummy);
-        }
-        if (PAIR) {  // (and those into the other CTA, which only it can wait for: a TMA load takes microseconds)
-          const uint64_t t0 = globaltimer_ns();
-          while (globaltimer_ns() - t0 < 2000000ull) {
-          }
+          mbar_wait(full(b < 0 ? b + C::kStages : b), b < 0 ? r.phase ^ 1u : r.phase, &dummy);
         }
       }
     } else if (warp == 1) {
       const bool issuer = elect_one();
       constexpr uint32_t id =
-          (1u << 4) | (static_cast<uint32_t>(kWideN >> 3) << 17) | (static_cast<uint32_t>(kRows >> 4) << 24);
-      Ring<kWideStages> r;
-      Ring<kWidePartials> t;
+          (1u << 4) | (static_cast<uint32_t>(TN >> 3) << 17) | (static_cast<uint32_t>(kRows >> 4) << 24);
+      Ring<C::kStages> r;
+      Ring<C::kPartials> t;
       bool ok = aligned, issued = false;
       for (int tile = first; ok && tile < args.tiles; tile += step) {
         for (int kb = kb0; kb < kb1; ++kb) {
@@ -677,14 +653,13 @@ __global__ void __launch_bounds__(kWideThreads, 1)
           if (!ok) break;
           tc_fence_after();
           if (issuer) {
-            const uint64_t ad = smem_desc_sw128(base + r.s * kWideStage);
-            const uint64_t bd = smem_desc_sw128(base + r.s * kWideStage + kRows * kFp8BK);
+            const uint64_t ad = smem_desc_sw128(base + r.s * C::kStage);
+            const uint64_t bd = smem_desc_sw128(base + r.s * C::kStage + kRows * kFp8BK);
 #pragma unroll
             for (int kk = 0; kk < kFp8BK / 32; ++kk)
-              mma_e4m3(tmem_base + t.s * kWideN, ad + 2 * kk, bd + 2 * kk, id, kk > 0 ? 1u : 0u);
+              mma_e4m3(tmem_base + t.s * TN, ad + 2 * kk, bd + 2 * kk, id, kk > 0 ? 1u : 0u);
             tc_commit(pfull(t.s));
-            if (PAIR) tc_commit_both(empty(r.s));
-            else tc_commit(empty(r.s));
+            tc_commit(empty(r.s));
           }
           __syncwarp();
           issued = true;
@@ -703,14 +678,14 @@ __global__ void __launch_bounds__(kWideThreads, 1)
       }
     }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kEpiRegs));
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::kEpiRegs));
     const int q = warp & 3, half = (warp - 4) >> 2;
     const uint32_t col = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + half * 128;
-    uint4* stage = stage_all + (warp - 4) * (kStageWarp / 16);
-    Ring<kWidePartials> t;
+    uint8_t* stage_warp = stage_all + (warp - 4) * C::kStageWarp;
+    Ring<C::kPartials> t;
     bool ok = aligned;
     for (int tile = first; tile < args.tiles; tile += step) {
-      const int tok0 = tok_of(tile), row0 = tile / args.m_tiles * kWideN + half * 128;
+      const int tok0 = tile % args.m_tiles * kRows, row0 = tile / args.m_tiles * TN + half * 128;
       float acc[128];
 #pragma unroll
       for (int j = 0; j < 128; ++j) acc[j] = 0.f;
@@ -731,7 +706,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
         ok = ok && __all_sync(kFull, mbar_wait(pfull(t.s), t.phase, abort_flag));
         if (!ok) break;
         tc_fence_after();
-        const uint32_t ta = col + t.s * kWideN;
+        const uint32_t ta = col + t.s * TN;
         tmem_ld16(ta, c0);
         add16(acc + 112, c1, s_prev);
         tmem_ld_wait();
@@ -764,97 +739,112 @@ __global__ void __launch_bounds__(kWideThreads, 1)
       }
       if (!ok) break;
       add16(acc + 112, c1, s_prev);
-      bool store = true;
       if constexpr (SPLIT) {
-        // Every CTA sends the rows that others add (a warp's rows have one owner) and adds what comes for its own, in
-        // rank order behind its own sums.  A row's 16-byte chunk c lies at c ^ (row % 8): no bank conflicts.
-        const int owner = (q * 32) / rows, rr = q * 32 + lane - owner * rows;
-        store = owner == rank;
-        uint8_t* out_sums = smem_raw + half * 2 * kHalfSums;  // this CTA's ring is done with: its last MMA has been seen to be
-        const uint8_t* in_sums = out_sums + kHalfSums;
-        if (!store) {
-          uint8_t* row = out_sums + ((owner - (owner > rank ? 1 : 0)) * rows + rr) * 512;
+        // Every CTA sends the rows that others add and adds what comes for its own, in rank order behind its own sums.
+        // A row's 16-byte chunk c lies at c ^ (row % 8): no bank conflicts.
+        const int row = q * 32 + lane, owner = (row * S + S - 1) / kRows, rr = row - first_row(owner);
+        const int mine = own1 - own0;
+        uint8_t* out_sums = smem_raw + half * 2 * kSliceSums;  // this CTA's ring is done with: its last MMA has been seen to be
+        const uint8_t* in_sums = out_sums + kSliceSums;
+        const uint32_t sent = written + 8u * half, come = received + 8u * half;
+        if (owner != rank) {
+          uint8_t* to = out_sums + (row - (owner > rank ? mine : 0)) * 512;
 #pragma unroll
           for (int c = 0; c < 32; ++c)
-            *reinterpret_cast<float4*>(row + ((c ^ (rr & 7)) << 4)) =
+            *reinterpret_cast<float4*>(to + ((c ^ (rr & 7)) << 4)) =
                 make_float4(acc[4 * c], acc[4 * c + 1], acc[4 * c + 2], acc[4 * c + 3]);
           fence_proxy_async_smem();
         }
         cluster_wait();
         waited = true;
-        if (warp == 4 && lane < S) mbar_arrive_remote(map_rank(rings, static_cast<uint32_t>(lane)));
+        if (warp == 4 && lane < S) mbar_arrive_pair(pair_map(rings, static_cast<uint32_t>(lane)));
         __syncwarp();
-        if (lane == 0) mbar_arrive(written + 8u * half);
-        if (q == 0) ok = __all_sync(kFull, mbar_wait(rings, 0, abort_flag) && mbar_wait(written + 8u * half, 0, abort_flag));
+        if (lane == 0) mbar_arrive(sent);
+        if (q == 0) ok = __all_sync(kFull, mbar_wait(rings, 0, abort_flag) && mbar_wait(sent, 0, abort_flag));
         if (!ok) break;
         if (q == 0 && lane < S - 1) {
-          const int to = lane + (lane >= rank ? 1 : 0);
-          const uint32_t bytes = static_cast<uint32_t>(rows * 512);
-          send(map_rank(smem_u32(in_sums) + (rank - (rank > to ? 1 : 0)) * bytes, static_cast<uint32_t>(to)),
-               smem_u32(out_sums) + lane * bytes, bytes, map_rank(received + 8u * half, static_cast<uint32_t>(to)));
+          const int to = lane + (lane >= rank ? 1 : 0), r0 = first_row(to), theirs = first_row(to + 1) - r0;
+          send(pair_map(smem_u32(in_sums) + (rank - (rank > to ? 1 : 0)) * theirs * 512, static_cast<uint32_t>(to)),
+               smem_u32(out_sums) + (r0 - (to > rank ? mine : 0)) * 512, static_cast<uint32_t>(theirs * 512),
+               pair_map(come, static_cast<uint32_t>(to)));
         }
         __syncwarp();
-        if (store) {
-          ok = __all_sync(kFull, mbar_wait(received + 8u * half, 0, abort_flag));
-          if (!ok) break;
+        if (q * 32 >= own1 || q * 32 + 32 <= own0) break;  // (the only tile)
+        ok = __all_sync(kFull, mbar_wait(come, 0, abort_flag));
+        if (!ok) break;
+        if (owner == rank) {
           for (int s = 0; s < S - 1; ++s) {
-            const uint8_t* row = in_sums + (s * rows + rr) * 512;
+            const uint8_t* from = in_sums + (s * mine + rr) * 512;
 #pragma unroll
             for (int c = 0; c < 32; ++c) {
-              const float4 v = *reinterpret_cast<const float4*>(row + ((c ^ (rr & 7)) << 4));
+              const float4 v = *reinterpret_cast<const float4*>(from + ((c ^ (rr & 7)) << 4));
               acc[4 * c] += v.x, acc[4 * c + 1] += v.y, acc[4 * c + 2] += v.z, acc[4 * c + 3] += v.w;
             }
           }
         }
       }
-      if (store) {
-        // four rounds of 32 columns: a row's 64 bytes cross the warp's staging (chunk j of row r at slot
-        // j ^ ((r / 2) % 4): no bank conflicts) and leave as eight rows x 64 bytes per store instruction
+      // Four rounds of 32 columns, in two buffers: a row's 64 bytes cross the warp's staging, chunk j of row r at slot
+      // j ^ ((r / 2) % 4): no bank conflicts, and the 64-byte swizzle of a TMA box.
+      const int lo = own0 - q * 32, hi = min(own1 - q * 32, p.m - (tok0 + q * 32));  // the warp's rows to be stored
 #pragma unroll
-        for (int rd = 0; rd < 4; ++rd) {
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const float* v = acc + 32 * rd + 8 * j;
-            stage[lane * 4 + (j ^ ((lane >> 1) & 3))] = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]),
-                                                                   pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
-          }
-          __syncwarp();
-          const int t0 = tok0 + q * 32, n0 = row0 + 32 * rd;
-          __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.c) + static_cast<long long>(t0) * p.ldc + n0;
-          if (args.c_align == 16 && n0 + 32 <= p.n) {
-            const int cu = lane & 3;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const int r = (lane >> 2) + 8 * i;
-              if (t0 + r < p.m)
-                *reinterpret_cast<uint4*>(out + r * p.ldc + 8 * cu) = stage[r * 4 + (cu ^ ((r >> 1) & 3))];
-            }
-          } else if (args.c_align >= 4 && (p.n & 1) == 0) {
-            // two columns a lane, two rows an instruction
-            const int c = 2 * (lane & 15);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const int r = (lane >> 4) + 2 * i;
-              const uint32_t v =
-                  reinterpret_cast<const uint32_t*>(&stage[r * 4 + ((c >> 3) ^ ((r >> 1) & 3))])[(c & 7) >> 1];
-              if (t0 + r < p.m && n0 + c < p.n) *reinterpret_cast<uint32_t*>(out + r * p.ldc + c) = v;
-            }
-          } else {
-#pragma unroll 8
-            for (int r = 0; r < 32; ++r) {
-              const uint16_t v =
-                  reinterpret_cast<const uint16_t*>(&stage[r * 4 + ((lane >> 3) ^ ((r >> 1) & 3))])[lane & 7];
-              if (t0 + r < p.m && n0 + lane < p.n) *reinterpret_cast<uint16_t*>(out + r * p.ldc + lane) = v;
-            }
-          }
+      for (int rd = 0; rd < 4; ++rd) {
+        uint4* stage = reinterpret_cast<uint4*>(stage_warp + (rd & 1) * (C::kStageWarp / 2));
+        const int t0 = tok0 + q * 32, n0 = row0 + 32 * rd;
+        // (a box is cut at the tensor's edge in 16-byte pieces)
+        const bool bulk = !SPLIT && args.c_align == 16 && (n0 + 32 <= p.n || (p.n & 7) == 0);
+        if (!SPLIT) {  // the box of two rounds ago has been read
+          if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
           __syncwarp();
         }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float* v = acc + 32 * rd + 8 * j;
+          stage[lane * 4 + (j ^ ((lane >> 1) & 3))] = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]),
+                                                                 pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
+        }
+        if (bulk) {
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0 && t0 < p.m && n0 < p.n) tma_store_2d(&tmC, smem_u32(stage), n0, t0);
+          if (lane == 0) bulk_commit_group();
+          continue;
+        }
+        __syncwarp();
+        __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.c) + static_cast<long long>(t0) * p.ldc + n0;
+        if (SPLIT && args.c_align == 16 && n0 + 32 <= p.n) {  // eight rows x 64 bytes per store instruction
+          const int cu = lane & 3;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int r = (lane >> 2) + 8 * i;
+            if (r >= lo && r < hi)
+              *reinterpret_cast<uint4*>(out + r * p.ldc + 8 * cu) = stage[r * 4 + (cu ^ ((r >> 1) & 3))];
+          }
+        } else if (args.c_align >= 4 && (p.n & 1) == 0) {  // two columns a lane, two rows an instruction
+          const int c = 2 * (lane & 15);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int r = (lane >> 4) + 2 * i;
+            const uint32_t v =
+                reinterpret_cast<const uint32_t*>(&stage[r * 4 + ((c >> 3) ^ ((r >> 1) & 3))])[(c & 7) >> 1];
+            if (r >= lo && r < hi && n0 + c < p.n) *reinterpret_cast<uint32_t*>(out + r * p.ldc + c) = v;
+          }
+        } else {
+#pragma unroll 8
+          for (int r = 0; r < 32; ++r) {
+            const uint16_t v =
+                reinterpret_cast<const uint16_t*>(&stage[r * 4 + ((lane >> 3) ^ ((r >> 1) & 3))])[lane & 7];
+            if (r >= lo && r < hi && n0 + lane < p.n) *reinterpret_cast<uint16_t*>(out + r * p.ldc + lane) = v;
+          }
+        }
+        __syncwarp();
       }
     }
+    if (lane == 0) bulk_wait_group0();
+    __syncwarp();
     if (!ok && aligned && lane == 0) give_up();
   }
-  if (FORM != WIDE_SINGLE) {  // no CTA leaves while another may still write to it
-    if (SPLIT && !waited) cluster_wait();
+  if (SPLIT) {  // no CTA leaves while another may still write to it
+    if (!waited) cluster_wait();
     __syncwarp();
     cluster_arrive_release();
     cluster_wait();
@@ -864,57 +854,81 @@ __global__ void __launch_bounds__(kWideThreads, 1)
   __syncthreads();
   if (warp == 1) {
     tc_fence_after();
-    tmem_dealloc(tmem_base, 512);
+    tmem_dealloc(tmem_base, 2 * TN);
   }
 }
 
 template <int NT>
-cudaError_t skinny(const CUtensorMap& tmA, const CUtensorMap& tmB, const Fp8MatmulArgs& args, int num_sms,
+cudaError_t skinny(const CUtensorMap& tmA, const CUtensorMap& tmB, const Fp8MatmulArgs& args, const Fp8MatmulDevice& dev,
                    cudaStream_t s) {
+  using C = Skinny<NT>;
   const int blocks = ceil_div(args.k, kFp8BK);
   SkinnyArgs a{args, 1, ceil_div(args.m, NT)};
   const long long tiles = static_cast<long long>(ceil_div(args.n, kRows)) * a.m_tiles;
-  // K slices of two blocks and more as long as all CTAs are resident at once (a second wave costs more than shorter
-  // slices save: 45 rows x 28672 x 4096 on 1, 2 and 4 slices 24, 38 and 46 us; 64 x 4100 x 14300 on 4, 6 and 8, all
-  // one wave, 18.0, 16.9 and 15.4; 64 x 12288 x 6144 on 1 and 3 23.6 and 18.7)
-  a.split = static_cast<int>(std::max<long long>(1, std::min<long long>({kMaxSplit, 2 * num_sms / tiles, blocks / 2})));
-  return launch_pdl(fp8_skinny_kernel<NT>, dim3(static_cast<unsigned>(tiles * a.split)), dim3(kThreads),
-                    Skinny<NT>::kSmem, s, a.split, tmA, tmB, a);
+  // The number of slices by what they take: a slice's blocks, the meeting (the more slices, the fewer sums a CTA adds),
+  // and 1 to 2.5 us for the second CTAs of the SMs, which start a microsecond later and share the rest; no second wave
+  // (64 x 2048 x 2048 on 1, 2, 4, 6 and, more clusters than fit at once, 8 slices 8.9, 8.3, 6.6, 5.9 and 6.8 us; 64 x
+  // 4100 x 14300 on 4 and, two CTAs an SM, 6 and 8 18.0, 16.9 and 15.4; 45 rows x 28672 x 4096, two CTAs an SM, on 1, 2
+  // and, more waves, 4 24, 38 and 46).
+  constexpr int kShare[kMaxSplit] = {0, 100, 82, 73, 62, 51, 47, 42};  // hundredths of kMeet
+  long long best = -1;
+  for (int S = 1; S <= kMaxSplit && S <= blocks && (S == 1 || (tiles * S <= 2 * dev.num_sms && dev.clusters[S] > 0)); ++S) {
+    const long long cost = static_cast<long long>(ceil_div(blocks, S)) * C::kBlock + C::kMeet * kShare[S - 1] / 100 +
+                           (tiles > dev.clusters[S] ? C::kTwo : 0);
+    if (best < 0 || cost < best) best = cost, a.split = S;
+  }
+  return launch_pdl(fp8_skinny_kernel<NT>, dim3(static_cast<unsigned>(tiles * a.split)), dim3(kThreads), C::kSmem, s,
+                    a.split, tmA, tmB, a);
 }
 
-cudaError_t wide(const void* a, long long lda, const void* b, long long ldb, const Fp8MatmulArgs& args, int num_sms,
-                 cudaStream_t s, std::string* err) {
-  const int blocks = ceil_div(args.k, kFp8BK);
-  const int m_tiles = ceil_div(args.m, kRows);
-  const long long tiles = static_cast<long long>(ceil_div(args.n, kWideN)) * m_tiles;
-  // (slices that meet cost 2.5 us on two CTAs and 5 on four: 400 x 2048 x 2048, 16 blocks, on 1, 2 and 4 slices 10.2,
-  // 10.0 and 12.2 us; 256 x 4096 x 4096, 32 blocks, 17.3, 14.4 and 15.5; 400 x 2048 x 7168, 56, 24.4, 19.0 and 17.8)
-  int split = 1;
-  while (split < kWideSplit && tiles * split * 2 <= num_sms && blocks >= 24 * split) split *= 2;
-  // Pairs where operand traffic counts: long contractions in more than one wave of tiles (single / pairs, us: 8045 x
-  // 4096 x 7168 191 / 174, 16000 x 2048 x 7168 218 / 197, 1024 x 28672 x 4096 99 / 94; but 700 x 4096 x 7168, one
-  // wave, 28 / 34, and 4096 x 7168 x 2048 53 / 55 to 61: a pair's CTAs wait for one another at every tile's end).
-  const bool pairs = split == 1 && m_tiles >= 2 && tiles > num_sms && blocks >= 32;
-  CUtensorMap tmA, tmB;
-  if (!encode_tmap_u8(&tmA, a, args.m, args.k, kRows, err, lda) ||
-      !encode_tmap_u8(&tmB, b, args.n, args.k, pairs ? kWideN / 2 : kWideN, err, ldb))
-    return cudaErrorInvalidValue;
+template <bool SPLIT, int TN>
+cudaError_t wide(const void* a, long long lda, const void* b, long long ldb, const Fp8MatmulArgs& args, int split,
+                 int num_sms, cudaStream_t s, std::string* err) {
   const uintptr_t at = reinterpret_cast<uintptr_t>(args.c) | static_cast<uintptr_t>(2 * args.ldc);
-  WideArgs w{args, pairs ? 2 : split, pairs ? ceil_div(m_tiles, 2) : m_tiles, 0,
-             (at & 15u) == 0 ? 16 : (at & 3u) == 0 ? 4 : 2};
-  w.tiles = ceil_div(args.n, kWideN) * w.m_tiles;
-  const dim3 block(kWideThreads);
-  if (split > 1)
-    return launch_pdl(fp8_wide_kernel<WIDE_SPLIT>, dim3(w.tiles * split), block, kWideSmem, s, split, tmA, tmB, w);
-  if (pairs)
-    return launch_pdl(fp8_wide_kernel<WIDE_PAIR>, dim3(2 * std::min(w.tiles, num_sms / 2)), block, kWideSmem, s, 2, tmA,
-                      tmB, w);
-  return launch_pdl(fp8_wide_kernel<WIDE_SINGLE>, dim3(std::min(w.tiles, num_sms)), block, kWideSmem, s, 1, tmA, tmB, w);
+  WideArgs w{args, split, ceil_div(args.m, kRows), 0, (at & 15u) == 0 ? 16 : (at & 3u) == 0 ? 4 : 2};
+  w.tiles = ceil_div(args.n, TN) * w.m_tiles;
+  CUtensorMap tmA, tmB, tmC;
+  if (!encode_tmap_u8(&tmA, a, args.m, args.k, kRows, err, lda) || !encode_tmap_u8(&tmB, b, args.n, args.k, TN, err, ldb))
+    return cudaErrorInvalidValue;
+  if (SPLIT || w.c_align != 16) tmC = tmA;  // (not used)
+  else if (!encode_tmap_out(&tmC, args.c, args.m, args.n, args.ldc, err)) return cudaErrorInvalidValue;
+  const int grid = SPLIT ? w.tiles * split : std::min(w.tiles, Wide<TN>::kCtas * num_sms);
+  return launch_pdl(fp8_wide_kernel<SPLIT, TN>, dim3(grid), dim3(Wide<TN>::kThreads), Wide<TN>::kSmem, s, split, tmA,
+                    tmB, tmC, w);
+}
+
+// Width and slices of the wide tiles, by what they take in hundredths of a microsecond: a K block of a CTA, times the
+// blocks of its slice and the waves of CTAs, and the meeting of the slices.  A block takes 0.38 us in 256 columns, 0.36
+// in 128 and 0.47 in 128 with two CTAs on an SM (1000 x 4096 x 7168 25 and 30 us, 256 x 7168 x 2048 10.8 and 10.0);
+// slices are cut where every CTA has an SM to itself, at once (362 x 4100 x 14300 in 256 columns on 1 and 2 slices 48 and 33 us,
+// in 128 on 1, 2 and, two CTAs on an SM, 3 49, 39 and 47; 400 x 2048 x 7168 in 128 on 1, 2, 3 23.6, 16.2, 18.4).
+cudaError_t wide(const void* a, long long lda, const void* b, long long ldb, const Fp8MatmulArgs& args,
+                 const Fp8MatmulDevice& dev, cudaStream_t s, std::string* err) {
+  const int num_sms = dev.num_sms;
+  constexpr int kMeet[2][kWideSplit] = {{0, 460, 620, 660}, {0, 270, 350, 440}};
+  const long long blocks = ceil_div(args.k, kFp8BK), m_tiles = ceil_div(args.m, kRows);
+  bool narrow = false;
+  int split = 1;
+  long long best = -1;
+  for (int half = 0; half < 2; ++half) {
+    const long long tiles = m_tiles * ceil_div(args.n, half ? 128 : 256);
+    for (int S = 1; S <= kWideSplit && S <= blocks && (S == 1 || tiles <= dev.clusters[S]); ++S) {
+      const bool two = half && tiles > num_sms;
+      const long long wave = two ? 2 * num_sms : num_sms, block = !half ? 38 : two ? 47 : 36;
+      const long long cost = (tiles * S + wave - 1) / wave * ((blocks + S - 1) / S) * block + kMeet[half][S - 1];
+      if (best < 0 || cost < best) best = cost, narrow = half != 0, split = S;
+    }
+  }
+  if (narrow)
+    return split > 1 ? wide<true, 128>(a, lda, b, ldb, args, split, num_sms, s, err)
+                     : wide<false, 128>(a, lda, b, ldb, args, 1, num_sms, s, err);
+  return split > 1 ? wide<true, 256>(a, lda, b, ldb, args, split, num_sms, s, err)
+                   : wide<false, 256>(a, lda, b, ldb, args, 1, num_sms, s, err);
 }
 
 }  // namespace
 
-cudaError_t fp8_matmul_set_attributes() {
+cudaError_t fp8_matmul_device(Fp8MatmulDevice* dev) {
   cudaError_t e = cudaSuccess;
   auto set = [&](auto* f, size_t bytes) {
     if (e == cudaSuccess)
@@ -923,29 +937,56 @@ cudaError_t fp8_matmul_set_attributes() {
   set(fp8_skinny_kernel<16>, Skinny<16>::kSmem);
   set(fp8_skinny_kernel<32>, Skinny<32>::kSmem);
   set(fp8_skinny_kernel<64>, Skinny<64>::kSmem);
-  set(fp8_wide_kernel<WIDE_SINGLE>, kWideSmem);
-  set(fp8_wide_kernel<WIDE_PAIR>, kWideSmem);
-  set(fp8_wide_kernel<WIDE_SPLIT>, kWideSmem);
+  // (a register split that the launch's registers do not cover would wait for ever)
+  auto split = [&](auto* f, int regs) {
+    cudaFuncAttributes at{};
+    if (e == cudaSuccess) e = cudaFuncGetAttributes(&at, f);
+    if (e == cudaSuccess && at.numRegs < regs) e = cudaErrorInvalidConfiguration;
+  };
+  split(fp8_wide_kernel<false, 128>, Wide<128>::kLaunchRegs);
+  split(fp8_wide_kernel<true, 128>, Wide<128>::kLaunchRegs);
+  split(fp8_wide_kernel<false, 256>, Wide<256>::kLaunchRegs);
+  split(fp8_wide_kernel<true, 256>, Wide<256>::kLaunchRegs);
+  set(fp8_wide_kernel<false, 128>, Wide<128>::kSmem);
+  set(fp8_wide_kernel<true, 128>, Wide<128>::kSmem);
+  set(fp8_wide_kernel<false, 256>, Wide<256>::kSmem);
+  set(fp8_wide_kernel<true, 256>, Wide<256>::kSmem);
+  // clusters that are resident at once with one CTA an SM
+  dev->clusters[1] = dev->num_sms;
+  for (int S = 2; S <= kMaxSplit && e == cudaSuccess; ++S) {
+    cudaLaunchConfig_t c{};
+    c.gridDim = dim3(S * dev->num_sms);
+    c.blockDim = dim3(Wide<256>::kThreads);
+    c.dynamicSmemBytes = Wide<256>::kSmem;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = S;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    c.attrs = at;
+    c.numAttrs = 1;
+    e = cudaOccupancyMaxActiveClusters(&dev->clusters[S], fp8_wide_kernel<true, 256>, &c);
+  }
   return e;
 }
 
 cudaError_t fp8_matmul_launch(const void* a, long long lda, const void* b, long long ldb, const Fp8MatmulArgs& args,
-                              int num_sms, cudaStream_t s, std::string* err) {
-  // More than 64 rows go to the wide tiles, unless the product is so small that its narrow tiles, cut into slices,
-  // still are one wave and long enough to be worth cutting (wide / narrow: 65 x 512 x 2048 10.9 / 7.1 us, 128 x 2048 x
-  // 7168 17.9 / 14.2, 200 x 2048 x 7168 18.9 / 17.3, 1000 x 512 x 4096 18.0 / 15.5; but twice as many tiles, 256 x
-  // 4096 x 4096, 16.7 / 19.2, and half the blocks, 65 x 4096 x 1024, 8.0 / 10.7)
+                              const Fp8MatmulDevice& dev, cudaStream_t s, std::string* err) {
+  // More than 64 rows go to the wide tiles, unless there are so few narrow tiles that they can be cut into eight slices
+  // (64 rows of A at a time; wide / narrow, us: 65 x 512 x 2048 8.0 / 5.4, 128 x 2048 x 7168 12.9 / 10.4, 65 x 2048 x
+  // 14336 17.5 / 13.2; but with twice as many tiles 200 x 2048 x 7168 13.3 / 14.0, and 65 x 1024 x 1024, eight blocks,
+  // no faster)
   const long long narrow = static_cast<long long>(ceil_div(args.m, 64)) * ceil_div(args.n, kRows);
-  if (args.m > 64 && (narrow > num_sms / 2 || args.k <= 15 * kFp8BK)) return wide(a, lda, b, ldb, args, num_sms, s, err);
+  if (args.m > 64 && (narrow * kMaxSplit > 2 * dev.num_sms || args.k <= 15 * kFp8BK))
+    return wide(a, lda, b, ldb, args, dev, s, err);
   CUtensorMap tmA, tmB;
   const int nt = args.m <= 16 ? 16 : args.m <= 32 ? 32 : 64;
   if (!encode_tmap_u8(&tmA, a, args.m, args.k, nt, err, lda) ||
       !encode_tmap_u8(&tmB, b, args.n, args.k, kRows, err, ldb))
     return cudaErrorInvalidValue;
   switch (nt) {
-    case 16: return skinny<16>(tmA, tmB, args, num_sms, s);
-    case 32: return skinny<32>(tmA, tmB, args, num_sms, s);
-    default: return skinny<64>(tmA, tmB, args, num_sms, s);
+    case 16: return skinny<16>(tmA, tmB, args, dev, s);
+    case 32: return skinny<32>(tmA, tmB, args, dev, s);
+    default: return skinny<64>(tmA, tmB, args, dev, s);
   }
 }
 

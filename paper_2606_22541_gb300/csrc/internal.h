@@ -160,6 +160,9 @@ cudaError_t fp8_gemm_launch(int epi, const CUtensorMap* maps, const Fp8Args& arg
 // (0: cols).
 bool encode_tmap_u8(CUtensorMap* map, const void* ptr, uint64_t rows, uint64_t cols, uint32_t box_rows,
                     std::string* err, uint64_t ld = 0);
+// 2-D bf16 output [rows, cols], ld elements between rows (both 16-byte aligned), for 64-byte-swizzled boxes of
+// [32, 32].
+bool encode_tmap_out(CUtensorMap* map, void* ptr, uint64_t rows, uint64_t cols, uint64_t ld, std::string* err);
 
 // Rows of bf16 -> e4m3 with one fp32 scale per row per 128 channels
 // (s = amax / 448, q = round-to-nearest-even of v / s, saturated).
@@ -177,10 +180,14 @@ struct Fp8MatmulArgs {
   long long ldc;
   uint32_t* status;  // nullable
 };
-cudaError_t fp8_matmul_set_attributes();  // once per device
+struct Fp8MatmulDevice {
+  int num_sms = 0;
+  int clusters[9] = {};  // of so many CTAs, one to an SM, that are resident at once
+};
+cudaError_t fp8_matmul_device(Fp8MatmulDevice* dev);  // once per device; num_sms is given
 // The product; *err is set where TMA cannot read an operand.
 cudaError_t fp8_matmul_launch(const void* a, long long lda, const void* b, long long ldb, const Fp8MatmulArgs& args,
-                              int num_sms, cudaStream_t s, std::string* err);
+                              const Fp8MatmulDevice& dev, cudaStream_t s, std::string* err);
 // Rows of bf16 (u: nullptr), or silu(x) * u, to e4m3 with an fp32 scale per row
 // per 128 columns.  Any alignment and strides.
 cudaError_t launch_fp8_quantize(const void* x, const void* u, int rows, int cols, long long ld, void* q,
