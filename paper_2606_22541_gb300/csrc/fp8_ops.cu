@@ -509,23 +509,21 @@ struct Wide {
   static constexpr int kLaunchRegs = 65536 / (kCtas * kThreads) / 8 * 8;
   static_assert(4 * kCtrlRegs + kEpiWarps * kEpiRegs <= kThreads / 32 * kLaunchRegs,
                 "the register split stays within the launch's registers");
-  static constexpr int kBars = 2 * kStages + 2 * kPartials + 6;
+  static constexpr int kBars = 2 * kStages + 2 * kPartials + 4;
   static constexpr int kStageWarp = 2 * 32 * 64;  // an epilogue warp's output staging: two rounds of 32 columns
   static constexpr size_t kSmem = kStages * kStage + kEpiWarps * kStageWarp + 8 * kBars + 16;
   static_assert(kCtas * (kSmem + 1024) <= 228 * 1024, "shared memory budget");
+  // slices: a tile's sums, then those that come for a CTA's rows, in the place of the ring and the staging
+  static constexpr int kSums = kRows * TN * 4;
+  static_assert(kSums + (kWideSplit - 1) * (kRows / kWideSplit) * TN * 4 <= kStages * kStage + kEpiWarps * kStageWarp &&
+                kSums + 2 * ((kRows + 2) / 3) * TN * 4 <= kStages * kStage + kEpiWarps * kStageWarp, "the sums fit");
 };
-// The slices' sums of 128 columns: those to be sent, then those that come, each at most (S - 1) / S of 128 x 128
-// floats, in the ring's place.
-constexpr int kSliceSums = (kWideSplit - 1) * (kRows / kWideSplit) * 128 * 4;
-static_assert(2 * kSliceSums <= Wide<128>::kStages * Wide<128>::kStage &&
-              4 * kSliceSums <= Wide<256>::kStages * Wide<256>::kStage, "the sums fit the ring");
-
 struct WideArgs {
   Fp8MatmulArgs p;
   int split;    // K slices of a tile: the cluster
   int m_tiles;  // tiles along the rows of A
   int tiles;    // in all
-  int c_align;  // rows of c start on multiples of this many bytes (16, 4 or 2)
+  int c_align;  // rows of c start on multiples of this many bytes (16, 8, 4 or 2)
 };
 
 __device__ __forceinline__ void add16(float* acc, const uint32_t (&v)[16], float s) {
@@ -558,8 +556,8 @@ __global__ void __launch_bounds__(Wide<TN>::kThreads, Wide<TN>::kCtas)
   auto empty = [&](int i) { return bar0 + 8u * (C::kStages + i); };
   auto pfull = [&](int i) { return bar0 + 8u * (2 * C::kStages + i); };
   auto pempty = [&](int i) { return bar0 + 8u * (2 * C::kStages + C::kPartials + i); };
-  // all CTAs' rings are done with; per 128 columns: the rows to be sent are written, the slices have come
-  const uint32_t drain = bar0 + 8u * (C::kBars - 6), rings = drain + 8u, written = drain + 16u, received = drain + 32u;
+  // all CTAs' rings are done with, this one's sums are written, the slices have come
+  const uint32_t drain = bar0 + 8u * (C::kBars - 4), rings = drain + 8u, written = drain + 16u, received = drain + 24u;
   auto first_row = [&](int to) { return kRows * to / S; };  // of the rows whose sums CTA ``to`` adds
   const int own0 = first_row(rank), own1 = first_row(rank + 1);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + C::kBars);
@@ -577,15 +575,11 @@ __global__ void __launch_bounds__(Wide<TN>::kThreads, Wide<TN>::kCtas)
     }
     mbar_init(drain, 1);
     mbar_init(rings, S);
-    for (uint32_t i = 0; i < 2; ++i) {
-      mbar_init(written + 8u * i, 4);
-      mbar_init(received + 8u * i, 1);
-    }
+    mbar_init(written, C::kEpiWarps);
+    mbar_init(received, 1);
     *abort_flag = aligned ? 0 : 1;
     fence_barrier_init();
-    if (SPLIT)
-      for (uint32_t i = 0; i < TN / 128; ++i)
-        mbar_arrive_expect_tx(received + 8u * i, static_cast<uint32_t>((S - 1) * (own1 - own0) * 512));
+    if (SPLIT) mbar_arrive_expect_tx(received, static_cast<uint32_t>((S - 1) * (own1 - own0) * TN * 4));
     tma_prefetch_desc(&tmA);
     tma_prefetch_desc(&tmB);
     if (!SPLIT && args.c_align == 16) tma_prefetch_desc(&tmC);
@@ -740,103 +734,120 @@ __global__ void __launch_bounds__(Wide<TN>::kThreads, Wide<TN>::kCtas)
       if (!ok) break;
       add16(acc + 112, c1, s_prev);
       if constexpr (SPLIT) {
-        // Every CTA sends the rows that others add and adds what comes for its own, in rank order behind its own sums.
-        // A row's 16-byte chunk c lies at c ^ (row % 8): no bank conflicts.
-        const int row = q * 32 + lane, owner = (row * S + S - 1) / kRows, rr = row - first_row(owner);
-        const int mine = own1 - own0;
-        uint8_t* out_sums = smem_raw + half * 2 * kSliceSums;  // this CTA's ring is done with: its last MMA has been seen to be
-        const uint8_t* in_sums = out_sums + kSliceSums;
-        const uint32_t sent = written + 8u * half, come = received + 8u * half;
-        if (owner != rank) {
-          uint8_t* to = out_sums + (row - (owner > rank ? mine : 0)) * 512;
+        // Every CTA sends the rows that others add, and its warps add what has come for its own, in rank order, 128
+        // columns of a row at a time.  128 columns of a row are 512 bytes, 16-byte chunk c at c ^ (row % 8).  This CTA's
+        // ring is done with: its last MMA has been seen to be.
+        const int row = q * 32 + lane, mine = own1 - own0;
+        constexpr int kHalf = kRows * 512;  // bytes of 128 columns
+        uint8_t* to = smem_raw + half * kHalf + row * 512;
 #pragma unroll
-          for (int c = 0; c < 32; ++c)
-            *reinterpret_cast<float4*>(to + ((c ^ (rr & 7)) << 4)) =
-                make_float4(acc[4 * c], acc[4 * c + 1], acc[4 * c + 2], acc[4 * c + 3]);
-          fence_proxy_async_smem();
-        }
+        for (int c = 0; c < 32; ++c)
+          *reinterpret_cast<float4*>(to + ((c ^ (row & 7)) << 4)) =
+              make_float4(acc[4 * c], acc[4 * c + 1], acc[4 * c + 2], acc[4 * c + 3]);
+        fence_proxy_async_smem();
         cluster_wait();
         waited = true;
         if (warp == 4 && lane < S) mbar_arrive_pair(pair_map(rings, static_cast<uint32_t>(lane)));
         __syncwarp();
-        if (lane == 0) mbar_arrive(sent);
-        if (q == 0) ok = __all_sync(kFull, mbar_wait(rings, 0, abort_flag) && mbar_wait(sent, 0, abort_flag));
+        if (lane == 0) mbar_arrive(written);
+        ok = __all_sync(kFull, mbar_wait(written, 0, abort_flag) && (warp != 4 || mbar_wait(rings, 0, abort_flag)));
         if (!ok) break;
-        if (q == 0 && lane < S - 1) {
-          const int to = lane + (lane >= rank ? 1 : 0), r0 = first_row(to), theirs = first_row(to + 1) - r0;
-          send(pair_map(smem_u32(in_sums) + (rank - (rank > to ? 1 : 0)) * theirs * 512, static_cast<uint32_t>(to)),
-               smem_u32(out_sums) + (r0 - (to > rank ? mine : 0)) * 512, static_cast<uint32_t>(theirs * 512),
-               pair_map(come, static_cast<uint32_t>(to)));
+        if (warp == 4 && lane < (S - 1) * (TN / 128)) {
+          const int h = lane / (S - 1), i = lane - h * (S - 1), dst = i + (i >= rank ? 1 : 0);
+          const int r0 = first_row(dst), theirs = first_row(dst + 1) - r0;
+          send(pair_map(base + C::kSums + (h * (S - 1) + rank - (rank > dst ? 1 : 0)) * theirs * 512, static_cast<uint32_t>(dst)),
+               base + h * kHalf + r0 * 512, static_cast<uint32_t>(theirs * 512),
+               pair_map(received, static_cast<uint32_t>(dst)));
         }
         __syncwarp();
-        if (q * 32 >= own1 || q * 32 + 32 <= own0) break;  // (the only tile)
-        ok = __all_sync(kFull, mbar_wait(come, 0, abort_flag));
+        ok = __all_sync(kFull, mbar_wait(received, 0, abort_flag));
         if (!ok) break;
-        if (owner == rank) {
-          for (int s = 0; s < S - 1; ++s) {
-            const uint8_t* from = in_sums + (s * mine + rr) * 512;
+        // eight rows on their way at a time (rows that stay with the warp that has them in registers, whose lanes add and
+        // store them, take up to 1.2 us longer: the other warps wait)
+        constexpr int kAhead = 8;
+#pragma unroll 1
+        for (int h = 0; h < TN / 128; ++h) {
+          const int n0 = tile / args.m_tiles * TN + h * 128 + 4 * lane;
+          const uint8_t* own = smem_raw + h * kHalf + own0 * 512;
+          const uint8_t* come = smem_raw + C::kSums + h * (S - 1) * mine * 512;
+#pragma unroll 1
+          for (int r0 = warp - 4; r0 < mine; r0 += kAhead * C::kEpiWarps) {
+            float4 v[kAhead];
 #pragma unroll
-            for (int c = 0; c < 32; ++c) {
-              const float4 v = *reinterpret_cast<const float4*>(from + ((c ^ (rr & 7)) << 4));
-              acc[4 * c] += v.x, acc[4 * c + 1] += v.y, acc[4 * c + 2] += v.z, acc[4 * c + 3] += v.w;
+            for (int u = 0; u < kAhead; ++u) v[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+            for (int sl = 0; sl < S; ++sl) {
+              const uint8_t* from = sl == rank ? own : come + (sl - (sl > rank ? 1 : 0)) * mine * 512;
+#pragma unroll
+              for (int u = 0; u < kAhead; ++u) {
+                const int r = min(r0 + u * C::kEpiWarps, mine - 1);
+                const float4 w = *reinterpret_cast<const float4*>(from + r * 512 + ((lane ^ ((own0 + r) & 7)) << 4));
+                v[u].x += w.x, v[u].y += w.y, v[u].z += w.z, v[u].w += w.w;
+              }
+            }
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+              const int r = r0 + u * C::kEpiWarps, t = tok0 + own0 + r;
+              if (r >= mine || t >= p.m) break;
+              __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.c) + static_cast<long long>(t) * p.ldc + n0;
+              if (args.c_align >= 8 && n0 + 4 <= p.n) {
+                *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16x2(v[u].x, v[u].y), pack_bf16x2(v[u].z, v[u].w));
+              } else {
+                const float f[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                  if (n0 + e < p.n) out[e] = __float2bfloat16_rn(f[e]);
+              }
             }
           }
         }
-      }
-      // Four rounds of 32 columns, in two buffers: a row's 64 bytes cross the warp's staging, chunk j of row r at slot
-      // j ^ ((r / 2) % 4): no bank conflicts, and the 64-byte swizzle of a TMA box.
-      const int lo = own0 - q * 32, hi = min(own1 - q * 32, p.m - (tok0 + q * 32));  // the warp's rows to be stored
+        break;  // (the only tile)
+      } else {
+        // Four rounds of 32 columns, in two buffers: a row's 64 bytes cross the warp's staging, chunk j of row r at slot
+        // j ^ ((r / 2) % 4): no bank conflicts, and the 64-byte swizzle of a TMA box.
 #pragma unroll
-      for (int rd = 0; rd < 4; ++rd) {
-        uint4* stage = reinterpret_cast<uint4*>(stage_warp + (rd & 1) * (C::kStageWarp / 2));
-        const int t0 = tok0 + q * 32, n0 = row0 + 32 * rd;
-        // (a box is cut at the tensor's edge in 16-byte pieces)
-        const bool bulk = !SPLIT && args.c_align == 16 && (n0 + 32 <= p.n || (p.n & 7) == 0);
-        if (!SPLIT) {  // the box of two rounds ago has been read
+        for (int rd = 0; rd < 4; ++rd) {
+          uint4* stage = reinterpret_cast<uint4*>(stage_warp + (rd & 1) * (C::kStageWarp / 2));
+          const int t0 = tok0 + q * 32, n0 = row0 + 32 * rd;
+          // (a box is cut at the tensor's edge in 16-byte pieces)
+          const bool bulk = args.c_align == 16 && (n0 + 32 <= p.n || (p.n & 7) == 0);
+          // the box of two rounds ago has been read
           if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
           __syncwarp();
-        }
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float* v = acc + 32 * rd + 8 * j;
-          stage[lane * 4 + (j ^ ((lane >> 1) & 3))] = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]),
-                                                                 pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
-        }
-        if (bulk) {
-          fence_proxy_async_smem();
+          for (int j = 0; j < 4; ++j) {
+            const float* v = acc + 32 * rd + 8 * j;
+            stage[lane * 4 + (j ^ ((lane >> 1) & 3))] = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]),
+                                                                   pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
+          }
+          if (bulk) {
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0 && t0 < p.m && n0 < p.n) tma_store_2d(&tmC, smem_u32(stage), n0, t0);
+            if (lane == 0) bulk_commit_group();
+            continue;
+          }
           __syncwarp();
-          if (lane == 0 && t0 < p.m && n0 < p.n) tma_store_2d(&tmC, smem_u32(stage), n0, t0);
-          if (lane == 0) bulk_commit_group();
-          continue;
-        }
-        __syncwarp();
-        __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.c) + static_cast<long long>(t0) * p.ldc + n0;
-        if (SPLIT && args.c_align == 16 && n0 + 32 <= p.n) {  // eight rows x 64 bytes per store instruction
-          const int cu = lane & 3;
+          __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.c) + static_cast<long long>(t0) * p.ldc + n0;
+          if (args.c_align >= 4 && (p.n & 1) == 0) {  // two columns a lane, two rows an instruction
+            const int c = 2 * (lane & 15);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int r = (lane >> 2) + 8 * i;
-            if (r >= lo && r < hi)
-              *reinterpret_cast<uint4*>(out + r * p.ldc + 8 * cu) = stage[r * 4 + (cu ^ ((r >> 1) & 3))];
-          }
-        } else if (args.c_align >= 4 && (p.n & 1) == 0) {  // two columns a lane, two rows an instruction
-          const int c = 2 * (lane & 15);
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int r = (lane >> 4) + 2 * i;
-            const uint32_t v =
-                reinterpret_cast<const uint32_t*>(&stage[r * 4 + ((c >> 3) ^ ((r >> 1) & 3))])[(c & 7) >> 1];
-            if (r >= lo && r < hi && n0 + c < p.n) *reinterpret_cast<uint32_t*>(out + r * p.ldc + c) = v;
-          }
-        } else {
+            for (int i = 0; i < 16; ++i) {
+              const int r = (lane >> 4) + 2 * i;
+              const uint32_t v =
+                  reinterpret_cast<const uint32_t*>(&stage[r * 4 + ((c >> 3) ^ ((r >> 1) & 3))])[(c & 7) >> 1];
+              if (t0 + r < p.m && n0 + c < p.n) *reinterpret_cast<uint32_t*>(out + r * p.ldc + c) = v;
+            }
+          } else {
 #pragma unroll 8
-          for (int r = 0; r < 32; ++r) {
-            const uint16_t v =
-                reinterpret_cast<const uint16_t*>(&stage[r * 4 + ((lane >> 3) ^ ((r >> 1) & 3))])[lane & 7];
-            if (r >= lo && r < hi && n0 + lane < p.n) *reinterpret_cast<uint16_t*>(out + r * p.ldc + lane) = v;
+            for (int r = 0; r < 32; ++r) {
+              const uint16_t v =
+                  reinterpret_cast<const uint16_t*>(&stage[r * 4 + ((lane >> 3) ^ ((r >> 1) & 3))])[lane & 7];
+              if (t0 + r < p.m && n0 + lane < p.n) *reinterpret_cast<uint16_t*>(out + r * p.ldc + lane) = v;
+            }
           }
+          __syncwarp();
         }
-        __syncwarp();
       }
     }
     if (lane == 0) bulk_wait_group0();
@@ -885,7 +896,7 @@ template <bool SPLIT, int TN>
 cudaError_t wide(const void* a, long long lda, const void* b, long long ldb, const Fp8MatmulArgs& args, int split,
                  int num_sms, cudaStream_t s, std::string* err) {
   const uintptr_t at = reinterpret_cast<uintptr_t>(args.c) | static_cast<uintptr_t>(2 * args.ldc);
-  WideArgs w{args, split, ceil_div(args.m, kRows), 0, (at & 15u) == 0 ? 16 : (at & 3u) == 0 ? 4 : 2};
+  WideArgs w{args, split, ceil_div(args.m, kRows), 0, (at & 15u) == 0 ? 16 : (at & 7u) == 0 ? 8 : (at & 3u) == 0 ? 4 : 2};
   w.tiles = ceil_div(args.n, TN) * w.m_tiles;
   CUtensorMap tmA, tmB, tmC;
   if (!encode_tmap_u8(&tmA, a, args.m, args.k, kRows, err, lda) || !encode_tmap_u8(&tmB, b, args.n, args.k, TN, err, ldb))
@@ -900,12 +911,12 @@ cudaError_t wide(const void* a, long long lda, const void* b, long long ldb, con
 // Width and slices of the wide tiles, by what they take in hundredths of a microsecond: a K block of a CTA, times the
 // blocks of its slice and the waves of CTAs, and the meeting of the slices.  A block takes 0.38 us in 256 columns, 0.36
 // in 128 and 0.47 in 128 with two CTAs on an SM (1000 x 4096 x 7168 25 and 30 us, 256 x 7168 x 2048 10.8 and 10.0);
-// slices are cut where every CTA has an SM to itself, at once (362 x 4100 x 14300 in 256 columns on 1 and 2 slices 48 and 33 us,
-// in 128 on 1, 2 and, two CTAs on an SM, 3 49, 39 and 47; 400 x 2048 x 7168 in 128 on 1, 2, 3 23.6, 16.2, 18.4).
+// slices are cut where every CTA has an SM to itself, at once (362 x 4100 x 14300 in 256 columns on 1 and 2 slices 48 and 31 us,
+// in 128 on 1 and, two CTAs on an SM, 2 and 3 49, 41 and 46; 400 x 2048 x 7168 in 128 on 1, 2, 3 23.6, 16.2, 18.9).
 cudaError_t wide(const void* a, long long lda, const void* b, long long ldb, const Fp8MatmulArgs& args,
                  const Fp8MatmulDevice& dev, cudaStream_t s, std::string* err) {
   const int num_sms = dev.num_sms;
-  constexpr int kMeet[2][kWideSplit] = {{0, 460, 620, 660}, {0, 270, 350, 440}};
+  constexpr int kMeet[2][kWideSplit] = {{0, 390, 500, 580}, {0, 230, 300, 360}};
   const long long blocks = ceil_div(args.k, kFp8BK), m_tiles = ceil_div(args.m, kRows);
   bool narrow = false;
   int split = 1;
