@@ -190,6 +190,7 @@ template <int NT>
 struct Skinny {
   static constexpr int kStage = kBBytes + NT * kFp8BK;
   static constexpr int kStages = NT == 16 ? 5 : NT == 32 ? 4 : 3;  // about 100 KB: two CTAs an SM
+  static constexpr int kAlone = NT == 16 ? 8 : 7;  // of a CTA that has its SM to itself (0.1 to 0.5 us less)
   static constexpr int kPartials = 4;
   static constexpr uint32_t kTmem = NT * kPartials;
   static constexpr int kPitch = NT + 4;  // floats of a row of the slices' sums
@@ -198,15 +199,30 @@ struct Skinny {
   static constexpr int kBlock = NT == 16 ? 23 : NT == 32 ? 29 : 31;
   static constexpr int kMeet = NT == 16 ? 95 : NT == 32 ? 130 : 186;
   static constexpr int kTwo = NT == 16 ? 100 : NT == 32 ? 150 : 250;
-  static constexpr int kBars = 2 * kStages + 2 * kPartials + 2;
-  static constexpr size_t kSmem = kStages * kStage + 4 * kSums + 2 * NT * 4 + 8 * kBars + 16;
-  static_assert(2 * (kSmem + 1024) <= 228 * 1024, "two CTAs an SM");
+  static constexpr int kBars = 2 * kAlone + 2 * kPartials + 2;
+  static constexpr size_t kRest = 4 * kSums + 2 * NT * 4 + 8 * kBars + 16;
+  static_assert(2 * (kStages * kStage + kRest + 1024) <= 228 * 1024, "two CTAs an SM");
+  static_assert(kAlone * kStage + kRest <= 227 * 1024, "shared memory budget");
   static_assert(4 * kRows * kPitch <= kStages * kStage, "the ring holds the sums to be sent");
 };
 
 struct SkinnyArgs {
   Fp8MatmulArgs p;
   int split, m_tiles;
+  int stages;  // of the ring
+};
+
+// Ring of a number of stages that the launch chooses.
+struct RingOf {
+  int stages, s = 0;
+  uint32_t phase = 0;
+  __device__ __forceinline__ explicit RingOf(int n) : stages(n) {}
+  __device__ __forceinline__ void advance() {
+    if (++s == stages) {
+      s = 0;
+      phase ^= 1u;
+    }
+  }
 };
 
 // Barrier of the cluster's threads; the first orders no memory (barriers are
@@ -246,14 +262,14 @@ __global__ void __launch_bounds__(kThreads, 2)
   const int blocks = (p.k + kFp8BK - 1) / kFp8BK;
   const int kb0 = static_cast<int>(static_cast<long long>(blocks) * rank / S);
   const int kb1 = static_cast<int>(static_cast<long long>(blocks) * (rank + 1) / S);
-  float* sums = reinterpret_cast<float*>(smem_raw + C::kStages * C::kStage);  // [slice][row][column]
+  float* sums = reinterpret_cast<float*>(smem_raw + args.stages * C::kStage);  // [slice][row][column]
   float* scales = sums + C::kSums;                                            // [2][NT]
   uint64_t* bars = reinterpret_cast<uint64_t*>(scales + 2 * NT);
   const uint32_t bar0 = smem_u32(bars);
   auto full = [&](int i) { return bar0 + 8u * i; };
-  auto empty = [&](int i) { return bar0 + 8u * (C::kStages + i); };
-  auto pfull = [&](int i) { return bar0 + 8u * (2 * C::kStages + i); };
-  auto pempty = [&](int i) { return bar0 + 8u * (2 * C::kStages + C::kPartials + i); };
+  auto empty = [&](int i) { return bar0 + 8u * (C::kAlone + i); };
+  auto pfull = [&](int i) { return bar0 + 8u * (2 * C::kAlone + i); };
+  auto pempty = [&](int i) { return bar0 + 8u * (2 * C::kAlone + C::kPartials + i); };
   const uint32_t drain = bar0 + 8u * (C::kBars - 2), received = drain + 8u;
   auto first_row = [&](int to) { return kRows * to / S; };  // of the rows whose sums CTA ``to`` adds
   const int rows = first_row(rank + 1) - first_row(rank);
@@ -262,7 +278,7 @@ __global__ void __launch_bounds__(kThreads, 2)
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
-    for (int i = 0; i < C::kStages; ++i) {
+    for (int i = 0; i < args.stages; ++i) {
       mbar_init(full(i), 1);
       mbar_init(empty(i), 1);
     }
@@ -295,7 +311,7 @@ __global__ void __launch_bounds__(kThreads, 2)
   };
   if (warp == 0) {
     if (lane == 0 && aligned) {
-      Ring<C::kStages> r;
+      RingOf r(args.stages);
       const uint64_t pol_b = l2_policy(args.m_tiles == 1 ? 1 : 0), pol_a = l2_policy(2);
       int issued = 0;
       bool ok = true;
@@ -306,7 +322,7 @@ __global__ void __launch_bounds__(kThreads, 2)
         mbar_arrive_expect_tx(full(r.s), C::kStage);
         tma_load_2d(st, &tmB, full(r.s), kb * kFp8BK, row0, pol_b);
         tma_load_2d(st + kBBytes, &tmA, full(r.s), kb * kFp8BK, tok0, pol_a);
-        issued = min(issued + 1, C::kStages);
+        issued = min(issued + 1, args.stages);
         r.advance();
       }
       pdl_launch();  // nothing left to load
@@ -316,7 +332,7 @@ __global__ void __launch_bounds__(kThreads, 2)
         int dummy = 0;
         for (int i = issued; i > 0; --i) {
           const int b = r.s - i;
-          mbar_wait(full(b < 0 ? b + C::kStages : b), b < 0 ? r.phase ^ 1u : r.phase, &dummy);
+          mbar_wait(full(b < 0 ? b + args.stages : b), b < 0 ? r.phase ^ 1u : r.phase, &dummy);
         }
       }
     }
@@ -324,7 +340,7 @@ __global__ void __launch_bounds__(kThreads, 2)
     const bool issuer = elect_one();
     constexpr uint32_t id =
         (1u << 4) | (static_cast<uint32_t>(NT >> 3) << 17) | (static_cast<uint32_t>(kRows >> 4) << 24);
-    Ring<C::kStages> r;
+    RingOf r(args.stages);
     Ring<C::kPartials> t;
     bool ok = aligned, issued = false;
     for (int kb = kb0; ok && kb < kb1; ++kb) {
@@ -486,7 +502,7 @@ __global__ void __launch_bounds__(kThreads, 2)
 // columns, which the epilogue warps add, times row and block scale, into registers (warp w: TMEM lanes 32 (w % 4) .., a
 // half of 128 columns, i.e. one row of scale blocks): two 16-column chunks in turn, so that one is on its way while the
 // other is added, in pairs (f32x2: 2 % of 8045 x 4096 x 7168, 4 % of 8045 x 28672 x 1024).  One CTA of 256 columns has
-// an SM, two of 128 do.  A CTA takes a tile after the other, or a cluster of S CTAs shares one as above.
+// an SM, up to two of 128 do.  A CTA takes a tile after the other, or a cluster of S CTAs shares one as above.
 //   warp 0: TMA producer; warp 1: TMEM and MMA; from warp 4 on: epilogue, which takes
 //   registers from the first four warps.
 // What bounds it: the adding.  8045 x 4096 x 7168 takes 172 us (2.75 PFLOP/s at about 1.85 GHz), 154 with an epilogue
@@ -500,6 +516,9 @@ constexpr int kWideSplit = 4;  // K slices at most
 template <int TN>
 struct Wide {
   static constexpr int kStages = TN == 256 ? 4 : 3;
+  // of a CTA that has its SM to itself (6 instead of 3: 256 x 7168 x 2048 10.0 to 8.8 us, 65 x 2048 x 14336 on one
+  // slice 43 to 35: a load takes about a microsecond)
+  static constexpr int kAlone = TN == 256 ? 4 : 6;
   static constexpr int kStage = (kRows + TN) * kFp8BK;
   static constexpr int kPartials = 2;
   static constexpr int kEpiWarps = TN / 32;
@@ -509,10 +528,11 @@ struct Wide {
   static constexpr int kLaunchRegs = 65536 / (kCtas * kThreads) / 8 * 8;
   static_assert(4 * kCtrlRegs + kEpiWarps * kEpiRegs <= kThreads / 32 * kLaunchRegs,
                 "the register split stays within the launch's registers");
-  static constexpr int kBars = 2 * kStages + 2 * kPartials + 4;
+  static constexpr int kBars = 2 * kAlone + 2 * kPartials + 4;
   static constexpr int kStageWarp = 2 * 32 * 64;  // an epilogue warp's output staging: two rounds of 32 columns
-  static constexpr size_t kSmem = kStages * kStage + kEpiWarps * kStageWarp + 8 * kBars + 16;
-  static_assert(kCtas * (kSmem + 1024) <= 228 * 1024, "shared memory budget");
+  static constexpr size_t kRest = kEpiWarps * kStageWarp + 8 * kBars + 16;
+  static_assert(kCtas * (kStages * kStage + kRest + 1024) <= 228 * 1024 && kAlone * kStage + kRest <= 227 * 1024,
+                "shared memory budget");
   // slices: a tile's sums, then those that come for a CTA's rows, in the place of the ring and the staging
   static constexpr int kSums = kRows * TN * 4;
   static_assert(kSums + (kWideSplit - 1) * (kRows / kWideSplit) * TN * 4 <= kStages * kStage + kEpiWarps * kStageWarp &&
@@ -523,6 +543,7 @@ struct WideArgs {
   int split;    // K slices of a tile: the cluster
   int m_tiles;  // tiles along the rows of A
   int tiles;    // in all
+  int stages;   // of the ring
   int c_align;  // rows of c start on multiples of this many bytes (16, 8, 4 or 2)
 };
 
@@ -549,13 +570,13 @@ __global__ void __launch_bounds__(Wide<TN>::kThreads, Wide<TN>::kCtas)
   const int blocks = (p.k + kFp8BK - 1) / kFp8BK;
   const int kb0 = static_cast<int>(static_cast<long long>(blocks) * rank / S);
   const int kb1 = static_cast<int>(static_cast<long long>(blocks) * (rank + 1) / S);
-  uint8_t* stage_all = smem_raw + C::kStages * C::kStage;
+  uint8_t* stage_all = smem_raw + args.stages * C::kStage;
   uint64_t* bars = reinterpret_cast<uint64_t*>(stage_all + C::kEpiWarps * C::kStageWarp);
   const uint32_t bar0 = smem_u32(bars);
   auto full = [&](int i) { return bar0 + 8u * i; };
-  auto empty = [&](int i) { return bar0 + 8u * (C::kStages + i); };
-  auto pfull = [&](int i) { return bar0 + 8u * (2 * C::kStages + i); };
-  auto pempty = [&](int i) { return bar0 + 8u * (2 * C::kStages + C::kPartials + i); };
+  auto empty = [&](int i) { return bar0 + 8u * (C::kAlone + i); };
+  auto pfull = [&](int i) { return bar0 + 8u * (2 * C::kAlone + i); };
+  auto pempty = [&](int i) { return bar0 + 8u * (2 * C::kAlone + C::kPartials + i); };
   // all CTAs' rings are done with, this one's sums are written, the slices have come
   const uint32_t drain = bar0 + 8u * (C::kBars - 4), rings = drain + 8u, written = drain + 16u, received = drain + 24u;
   auto first_row = [&](int to) { return kRows * to / S; };  // of the rows whose sums CTA ``to`` adds
@@ -565,7 +586,7 @@ __global__ void __launch_bounds__(Wide<TN>::kThreads, Wide<TN>::kCtas)
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
-    for (int i = 0; i < C::kStages; ++i) {
+    for (int i = 0; i < args.stages; ++i) {
       mbar_init(full(i), 1);
       mbar_init(empty(i), 1);
     }
@@ -605,7 +626,7 @@ __global__ void __launch_bounds__(Wide<TN>::kThreads, Wide<TN>::kCtas)
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kCtrlRegs));
     if (warp == 0) {
       const bool issuer = elect_one();
-      Ring<C::kStages> r;
+      RingOf r(args.stages);
       const uint64_t pol = l2_policy(2);
       int issued = 0;
       bool ok = aligned;
@@ -620,7 +641,7 @@ __global__ void __launch_bounds__(Wide<TN>::kThreads, Wide<TN>::kCtas)
             tma_load_2d(st, &tmA, full(r.s), kb * kFp8BK, tok0, pol);
             tma_load_2d(st + kRows * kFp8BK, &tmB, full(r.s), kb * kFp8BK, row0, pol);
           }
-          issued = min(issued + 1, C::kStages);
+          issued = min(issued + 1, args.stages);
           r.advance();
         }
       }
@@ -631,14 +652,14 @@ __global__ void __launch_bounds__(Wide<TN>::kThreads, Wide<TN>::kCtas)
         int dummy = 0;
         for (int i = issued; i > 0; --i) {
           const int b = r.s - i;
-          mbar_wait(full(b < 0 ? b + C::kStages : b), b < 0 ? r.phase ^ 1u : r.phase, &dummy);
+          mbar_wait(full(b < 0 ? b + args.stages : b), b < 0 ? r.phase ^ 1u : r.phase, &dummy);
         }
       }
     } else if (warp == 1) {
       const bool issuer = elect_one();
       constexpr uint32_t id =
           (1u << 4) | (static_cast<uint32_t>(TN >> 3) << 17) | (static_cast<uint32_t>(kRows >> 4) << 24);
-      Ring<C::kStages> r;
+      RingOf r(args.stages);
       Ring<C::kPartials> t;
       bool ok = aligned, issued = false;
       for (int tile = first; ok && tile < args.tiles; tile += step) {
@@ -888,31 +909,34 @@ cudaError_t skinny(const CUtensorMap& tmA, const CUtensorMap& tmB, const Fp8Matm
                            (tiles > dev.clusters[S] ? C::kTwo : 0);
     if (best < 0 || cost < best) best = cost, a.split = S;
   }
-  return launch_pdl(fp8_skinny_kernel<NT>, dim3(static_cast<unsigned>(tiles * a.split)), dim3(kThreads), C::kSmem, s,
-                    a.split, tmA, tmB, a);
+  a.stages = tiles <= dev.clusters[a.split] ? C::kAlone : C::kStages;
+  return launch_pdl(fp8_skinny_kernel<NT>, dim3(static_cast<unsigned>(tiles * a.split)), dim3(kThreads),
+                    a.stages * C::kStage + C::kRest, s, a.split, tmA, tmB, a);
 }
 
 template <bool SPLIT, int TN>
 cudaError_t wide(const void* a, long long lda, const void* b, long long ldb, const Fp8MatmulArgs& args, int split,
-                 int num_sms, cudaStream_t s, std::string* err) {
+                 const Fp8MatmulDevice& dev, cudaStream_t s, std::string* err) {
   const uintptr_t at = reinterpret_cast<uintptr_t>(args.c) | static_cast<uintptr_t>(2 * args.ldc);
-  WideArgs w{args, split, ceil_div(args.m, kRows), 0, (at & 15u) == 0 ? 16 : (at & 7u) == 0 ? 8 : (at & 3u) == 0 ? 4 : 2};
+  WideArgs w{args, split, ceil_div(args.m, kRows), 0, 0, (at & 15u) == 0 ? 16 : (at & 7u) == 0 ? 8 : (at & 3u) == 0 ? 4 : 2};
   w.tiles = ceil_div(args.n, TN) * w.m_tiles;
+  w.stages = w.tiles <= dev.clusters[split] ? Wide<TN>::kAlone : Wide<TN>::kStages;
   CUtensorMap tmA, tmB, tmC;
   if (!encode_tmap_u8(&tmA, a, args.m, args.k, kRows, err, lda) || !encode_tmap_u8(&tmB, b, args.n, args.k, TN, err, ldb))
     return cudaErrorInvalidValue;
   if (SPLIT || w.c_align != 16) tmC = tmA;  // (not used)
   else if (!encode_tmap_out(&tmC, args.c, args.m, args.n, args.ldc, err)) return cudaErrorInvalidValue;
-  const int grid = SPLIT ? w.tiles * split : std::min(w.tiles, Wide<TN>::kCtas * num_sms);
-  return launch_pdl(fp8_wide_kernel<SPLIT, TN>, dim3(grid), dim3(Wide<TN>::kThreads), Wide<TN>::kSmem, s, split, tmA,
-                    tmB, tmC, w);
+  const int grid = SPLIT ? w.tiles * split : std::min(w.tiles, Wide<TN>::kCtas * dev.num_sms);
+  return launch_pdl(fp8_wide_kernel<SPLIT, TN>, dim3(grid), dim3(Wide<TN>::kThreads),
+                    w.stages * Wide<TN>::kStage + Wide<TN>::kRest, s, split, tmA, tmB, tmC, w);
 }
 
 // Width and slices of the wide tiles, by what they take in hundredths of a microsecond: a K block of a CTA, times the
-// blocks of its slice and the waves of CTAs, and the meeting of the slices.  A block takes 0.38 us in 256 columns, 0.36
-// in 128 and 0.47 in 128 with two CTAs on an SM (1000 x 4096 x 7168 25 and 30 us, 256 x 7168 x 2048 10.8 and 10.0);
-// slices are cut where every CTA has an SM to itself, at once (362 x 4100 x 14300 in 256 columns on 1 and 2 slices 48 and 31 us,
-// in 128 on 1 and, two CTAs on an SM, 2 and 3 49, 41 and 46; 400 x 2048 x 7168 in 128 on 1, 2, 3 23.6, 16.2, 18.9).
+// blocks of its slice and the waves of CTAs, and the meeting of the slices.  A block takes 0.38 us in 256 columns, 0.3
+// in 128 and 0.47 in 128 with two CTAs on an SM (1000 x 4096 x 7168 25 and 30 us, 256 x 7168 x 2048 10.8 and 8.8);
+// slices are cut where every CTA has an SM to itself, at once (362 x 4100 x 14300 in 256 columns on 1 and 2 slices 48
+// and 31 us, in 128 on 2 and 3 slices, two CTAs an SM, 41 and 46; 400 x 2048 x 7168 in 128 on 2 and, two CTAs an SM, 3
+// 14.8 and 18.9).
 cudaError_t wide(const void* a, long long lda, const void* b, long long ldb, const Fp8MatmulArgs& args,
                  const Fp8MatmulDevice& dev, cudaStream_t s, std::string* err) {
   const int num_sms = dev.num_sms;
@@ -925,16 +949,16 @@ cudaError_t wide(const void* a, long long lda, const void* b, long long ldb, con
     const long long tiles = m_tiles * ceil_div(args.n, half ? 128 : 256);
     for (int S = 1; S <= kWideSplit && S <= blocks && (S == 1 || tiles <= dev.clusters[S]); ++S) {
       const bool two = half && tiles > num_sms;
-      const long long wave = two ? 2 * num_sms : num_sms, block = !half ? 38 : two ? 47 : 36;
+      const long long wave = two ? 2 * num_sms : num_sms, block = !half ? 38 : two ? 47 : 30;
       const long long cost = (tiles * S + wave - 1) / wave * ((blocks + S - 1) / S) * block + kMeet[half][S - 1];
       if (best < 0 || cost < best) best = cost, narrow = half != 0, split = S;
     }
   }
   if (narrow)
-    return split > 1 ? wide<true, 128>(a, lda, b, ldb, args, split, num_sms, s, err)
-                     : wide<false, 128>(a, lda, b, ldb, args, 1, num_sms, s, err);
-  return split > 1 ? wide<true, 256>(a, lda, b, ldb, args, split, num_sms, s, err)
-                   : wide<false, 256>(a, lda, b, ldb, args, 1, num_sms, s, err);
+    return split > 1 ? wide<true, 128>(a, lda, b, ldb, args, split, dev, s, err)
+                     : wide<false, 128>(a, lda, b, ldb, args, 1, dev, s, err);
+  return split > 1 ? wide<true, 256>(a, lda, b, ldb, args, split, dev, s, err)
+                   : wide<false, 256>(a, lda, b, ldb, args, 1, dev, s, err);
 }
 
 }  // namespace
@@ -945,9 +969,9 @@ cudaError_t fp8_matmul_device(Fp8MatmulDevice* dev) {
     if (e == cudaSuccess)
       e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes));
   };
-  set(fp8_skinny_kernel<16>, Skinny<16>::kSmem);
-  set(fp8_skinny_kernel<32>, Skinny<32>::kSmem);
-  set(fp8_skinny_kernel<64>, Skinny<64>::kSmem);
+  set(fp8_skinny_kernel<16>, Skinny<16>::kAlone * Skinny<16>::kStage + Skinny<16>::kRest);
+  set(fp8_skinny_kernel<32>, Skinny<32>::kAlone * Skinny<32>::kStage + Skinny<32>::kRest);
+  set(fp8_skinny_kernel<64>, Skinny<64>::kAlone * Skinny<64>::kStage + Skinny<64>::kRest);
   // (a register split that the launch's registers do not cover would wait for ever)
   auto split = [&](auto* f, int regs) {
     cudaFuncAttributes at{};
@@ -958,17 +982,17 @@ cudaError_t fp8_matmul_device(Fp8MatmulDevice* dev) {
   split(fp8_wide_kernel<true, 128>, Wide<128>::kLaunchRegs);
   split(fp8_wide_kernel<false, 256>, Wide<256>::kLaunchRegs);
   split(fp8_wide_kernel<true, 256>, Wide<256>::kLaunchRegs);
-  set(fp8_wide_kernel<false, 128>, Wide<128>::kSmem);
-  set(fp8_wide_kernel<true, 128>, Wide<128>::kSmem);
-  set(fp8_wide_kernel<false, 256>, Wide<256>::kSmem);
-  set(fp8_wide_kernel<true, 256>, Wide<256>::kSmem);
+  set(fp8_wide_kernel<false, 128>, Wide<128>::kAlone * Wide<128>::kStage + Wide<128>::kRest);
+  set(fp8_wide_kernel<true, 128>, Wide<128>::kAlone * Wide<128>::kStage + Wide<128>::kRest);
+  set(fp8_wide_kernel<false, 256>, Wide<256>::kAlone * Wide<256>::kStage + Wide<256>::kRest);
+  set(fp8_wide_kernel<true, 256>, Wide<256>::kAlone * Wide<256>::kStage + Wide<256>::kRest);
   // clusters that are resident at once with one CTA an SM
   dev->clusters[1] = dev->num_sms;
   for (int S = 2; S <= kMaxSplit && e == cudaSuccess; ++S) {
     cudaLaunchConfig_t c{};
     c.gridDim = dim3(S * dev->num_sms);
     c.blockDim = dim3(Wide<256>::kThreads);
-    c.dynamicSmemBytes = Wide<256>::kSmem;
+    c.dynamicSmemBytes = Wide<256>::kStages * Wide<256>::kStage + Wide<256>::kRest;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeClusterDimension;
     at[0].val.clusterDim.x = S;
