@@ -344,8 +344,10 @@ int asap_moe_layer_dyn(asap_moe_t h, const int32_t* layer_id, const void* x, int
  *    two bf16 and expert outputs in fp32 until the final rounding; FP8 layers
  *    quantise x and h with correctly rounded quotients and keep expert outputs
  *    in fp32.  The same call gives the same bits each time.
- *  - The workspace is asap_moe_workspace_size for n tokens; its contents
- *    before the call do not matter. */
+ *  - The workspace is asap_moe_workspace_size for n tokens or more; its
+ *    contents before the call do not matter.
+ *  - Made for layers that are a stream of weights.  One whose weights are read
+ *    within about 10 us is served faster by asap_moe_layer from 17 tokens on. */
 #define ASAP_MOE_FEW_MAX_TOKENS 64
 int asap_moe_layer_few(asap_moe_t h, const int32_t* layer_id, const void* x, int32_t n, void* out,
                        void* ws, size_t ws_bytes, void* stream);

@@ -130,7 +130,9 @@ Layout layout(const asap_moe_config& c, long long n) {
 // ------------------------------------------------------------ few tokens
 // K slices of a tile so that a launch of ``tiles`` tiles has at least
 // kFewItems work items (2.5 per SM of a GB300: the size of a workspace needs no
-// GPU), with at least kFewMinSteps k-steps each.
+// GPU), with at least kFewMinSteps k-steps each.  One token on 152, 380 and 760
+// items, us: Mixtral 113, 108 and 107, DeepSeek-V3 121, 113 and 113, its e4m3
+// layer 72, 65 and 72; from 8 tokens on there are more tiles than that.
 constexpr int kFewItems = 380, kFewMinSteps = 8;
 int few_slices(long long tiles, int k_steps) {
   const long long want = (kFewItems + tiles - 1) / tiles;
@@ -174,6 +176,8 @@ FewLayout few_layout(const asap_moe_config& c, int n) {
   const int widest = fp8 ? asap::round_up_dev(n, 16) : 2 * asap::round_up_dev(n, 8);
   a.x_slot = asap::round_up_dev(fp8 ? std::max(widest * 128, n * 128 + widest * 4) : widest * 128, 1024);
   const int room = static_cast<int>(asap::kFewSmem - asap::kFewSmemState);
+  // (2, 3, 4 and 5 stages of weights, us: Mixtral, one token 120, 108, 108 and 109, DeepSeek-V3 e4m3, 8 tokens 396,
+  // 352, 348 and 350; longer rings leave less shared memory to the operand rows)
   a.stages_w = 4;
   while ((room - a.stages_w * 32768) / a.x_slot < std::min(a.stages_w, 4)) --a.stages_w;
   a.stages_x = std::min(asap::kFewMaxStages, (room - a.stages_w * 32768) / a.x_slot);

@@ -27,11 +27,20 @@
 //    h keeps 16 bits at no cost.
 //  - down: a tile waits until its expert's h is complete; its partial sums are
 //    fp32.
-//  - combine: 256 channels of one token, once the output tile's partial sums
-//    are complete: the experts' in slot order, then the shared expert's.
+//  - combine: 256 channels of one token, or from 8 tokens on of eight, once the
+//    output tile's partial sums are complete: the experts' in slot order, then
+//    the shared expert's.
 // Sums are taken in a fixed order, so a call gives the same bits each time.
 // An item waits only for items claimed before it, by CTAs that are running,
 // so the launch needs no co-residency to make progress.
+//
+// What bounds it: the weight stream, after 10 us of start (4 to 7 of them the
+// logits, up to 6 the gating from 4 tokens on) that the shared expert's weights
+// fill where there is one, and 2 to 4 us of last sums at the end.  One token:
+// Mixtral's shape (two experts of 176 M parameters) 108.6 us, 6.5 TB/s;
+// DeepSeek-V3's 113 us, 7.0 TB/s (the stream alone passes the rate of a plain
+// copy), in e4m3 64.8 us, 6.2 TB/s; 61 tokens of the latter, 210 experts, 1300 us,
+// 7.1 TB/s.
 #include "common.cuh"
 #include "e4m3.cuh"
 #include "few.h"

@@ -76,6 +76,9 @@ __device__ __forceinline__ uint32_t max_abs2(uint32_t a, uint32_t b) {
   return *reinterpret_cast<const uint32_t*>(&m);
 }
 
+// The approximate exponential and quotient, 2 to 4 units in the last place of fp32, before a rounding to 3 bits: of 98.6
+// million values 106 came out other than the exact value's, 79 with fp32 arithmetic elsewhere.  expf and a division gave
+// 83 and took 22 us instead of 15.4 (4014 x 4096), the products and the quotient with their remainders 91 and 19.2.
 __device__ __forceinline__ float swiglu(float g, float u) { return __fdividef(g, 1.0f + __expf(-g)) * u; }
 
 template <bool SWIGLU, int W>
@@ -508,10 +511,11 @@ __global__ void __launch_bounds__(kThreads, 2)
 // What bounds it: the adding.  8045 x 4096 x 7168 takes 172 us (2.75 PFLOP/s at about 1.85 GHz), 154 with an epilogue
 // that only passes the partials on (3.07 PFLOP/s), 160 with one that reads them all and adds nothing.  On top of its K
 // loop a tile takes 1.5 us to round and store, while the next tile's first two blocks are multiplied: with short
-// contractions that shows (8045 x 28672 x 1024 229 us, 2.06 PFLOP/s).  Tried and no faster: 32-column chunks (the
-// control warps then have too few registers), pairs of CTAs that load each other's half of the rows of B by multicast,
-// and pairs that multiply 256 rows by 256 together (cta_group::2), both 180 us in single calls and 187 to 192 back to
-// back: what operands cost through L2 and shared memory is hidden behind the adding.
+// contractions that shows (8045 x 28672 x 1024 232 us, 2.04 PFLOP/s).  Tried and no faster: chunks of 32 columns, four
+// partials of 128 columns, pairs of CTAs that load each other's half of the rows of B by multicast, and pairs that
+// multiply 256 rows by 256 together (cta_group::2; 180 us in single calls, where one CTA a tile takes 182): what
+// operands cost through L2 and shared memory is hidden behind the adding.  Back to back for milliseconds the clock
+// falls with the power, by up to a tenth.
 constexpr int kWideSplit = 4;  // K slices at most
 template <int TN>
 struct Wide {
@@ -776,15 +780,15 @@ __global__ void __launch_bounds__(Wide<TN>::kThreads, Wide<TN>::kCtas)
         if (warp == 4 && lane < (S - 1) * (TN / 128)) {
           const int h = lane / (S - 1), i = lane - h * (S - 1), dst = i + (i >= rank ? 1 : 0);
           const int r0 = first_row(dst), theirs = first_row(dst + 1) - r0;
-          send(pair_map(base + C::kSums + (h * (S - 1) + rank - (rank > dst ? 1 : 0)) * theirs * 512, static_cast<uint32_t>(dst)),
-               base + h * kHalf + r0 * 512, static_cast<uint32_t>(theirs * 512),
+          const uint32_t place = base + C::kSums + (h * (S - 1) + rank - (rank > dst ? 1 : 0)) * theirs * 512;
+          send(pair_map(place, static_cast<uint32_t>(dst)), base + h * kHalf + r0 * 512, static_cast<uint32_t>(theirs * 512),
                pair_map(received, static_cast<uint32_t>(dst)));
         }
         __syncwarp();
         ok = __all_sync(kFull, mbar_wait(received, 0, abort_flag));
         if (!ok) break;
-        // eight rows on their way at a time (rows that stay with the warp that has them in registers, whose lanes add and
-        // store them, take up to 1.2 us longer: the other warps wait)
+        // eight rows on their way at a time (where the warps that have the rows in registers added and stored them, the
+        // others waited: up to 1.2 us longer)
         constexpr int kAhead = 8;
 #pragma unroll 1
         for (int h = 0; h < TN / 128; ++h) {
@@ -904,7 +908,8 @@ cudaError_t skinny(const CUtensorMap& tmA, const CUtensorMap& tmB, const Fp8Matm
   // and, more waves, 4 24, 38 and 46).
   constexpr int kShare[kMaxSplit] = {0, 100, 82, 73, 62, 51, 47, 42};  // hundredths of kMeet
   long long best = -1;
-  for (int S = 1; S <= kMaxSplit && S <= blocks && (S == 1 || (tiles * S <= 2 * dev.num_sms && dev.clusters[S] > 0)); ++S) {
+  for (int S = 1; S <= std::min(kMaxSplit, blocks); ++S) {
+    if (S > 1 && (tiles * S > 2 * dev.num_sms || dev.clusters[S] == 0)) continue;
     const long long cost = static_cast<long long>(ceil_div(blocks, S)) * C::kBlock + C::kMeet * kShare[S - 1] / 100 +
                            (tiles > dev.clusters[S] ? C::kTwo : 0);
     if (best < 0 || cost < best) best = cost, a.split = S;
@@ -918,13 +923,15 @@ template <bool SPLIT, int TN>
 cudaError_t wide(const void* a, long long lda, const void* b, long long ldb, const Fp8MatmulArgs& args, int split,
                  const Fp8MatmulDevice& dev, cudaStream_t s, std::string* err) {
   const uintptr_t at = reinterpret_cast<uintptr_t>(args.c) | static_cast<uintptr_t>(2 * args.ldc);
-  WideArgs w{args, split, ceil_div(args.m, kRows), 0, 0, (at & 15u) == 0 ? 16 : (at & 7u) == 0 ? 8 : (at & 3u) == 0 ? 4 : 2};
+  const int c_align = (at & 15u) == 0 ? 16 : (at & 7u) == 0 ? 8 : (at & 3u) == 0 ? 4 : 2;
+  WideArgs w{args, split, ceil_div(args.m, kRows), 0, 0, c_align};
   w.tiles = ceil_div(args.n, TN) * w.m_tiles;
   w.stages = w.tiles <= dev.clusters[split] ? Wide<TN>::kAlone : Wide<TN>::kStages;
   CUtensorMap tmA, tmB, tmC;
-  if (!encode_tmap_u8(&tmA, a, args.m, args.k, kRows, err, lda) || !encode_tmap_u8(&tmB, b, args.n, args.k, TN, err, ldb))
+  if (!encode_tmap_u8(&tmA, a, args.m, args.k, kRows, err, lda) ||
+      !encode_tmap_u8(&tmB, b, args.n, args.k, TN, err, ldb))
     return cudaErrorInvalidValue;
-  if (SPLIT || w.c_align != 16) tmC = tmA;  // (not used)
+  if (SPLIT || c_align != 16) tmC = tmA;  // (not used)
   else if (!encode_tmap_out(&tmC, args.c, args.m, args.n, args.ldc, err)) return cudaErrorInvalidValue;
   const int grid = SPLIT ? w.tiles * split : std::min(w.tiles, Wide<TN>::kCtas * dev.num_sms);
   return launch_pdl(fp8_wide_kernel<SPLIT, TN>, dim3(grid), dim3(Wide<TN>::kThreads),
