@@ -99,6 +99,29 @@ def lib():
     return _lib
 
 
+_fast = None
+
+
+def fast():
+    """The compiled marshalling of the short calls, bound to the library, or
+    False where it has not been built."""
+    global _fast
+    if _fast is None:
+        try:
+            from . import _marshal
+        except ImportError:
+            _fast = False
+        else:
+            import torch
+            L = lib()
+            _marshal.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
+                L.asap_moe_fp8_quantize, L.asap_moe_fp8_swiglu_quantize, L.asap_moe_fp8_matmul)),
+                torch.bfloat16, torch.float32, torch.float8_e4m3fn, torch.uint8,
+                torch.cuda.current_device, torch._C._cuda_getCurrentRawStream)
+            _fast = _marshal
+    return _fast
+
+
 class AsapError(RuntimeError):
     def __init__(self, fn, code):
         msg = lib().asap_moe_last_error().decode(errors="replace")

@@ -10,7 +10,7 @@ import threading
 import torch
 
 from . import _native
-from ._native import AsapMoeConfig, AsapMoeWeights, check, lib
+from ._native import AsapMoeConfig, AsapMoeWeights, check, fast, lib
 from .configs import GATING, DTYPE
 
 
@@ -276,6 +276,15 @@ def _refuse(what, **tensors):
 def asap_moe_fp8_quantize(x, q, scales, stream=None):
     """bf16 rows x [n, c] to e4m3 q [n, c] with scales [n, ceil(c / 128)]
     (fp32); any row strides."""
+    f = fast()
+    code = f.quantize(x, q, scales, stream) if f else None
+    if code is None:
+        code = _quantize(x, q, scales, stream)
+    if code:
+        check("asap_moe_fp8_quantize", code)
+
+
+def _quantize(x, q, scales, stream):
     shape = x.shape
     if len(shape) != 2 or x.dtype is not _BF16 or q.shape != shape or (q.dtype is not _F8 and q.dtype is not _U8) or \
             scales.dtype is not _F32 or scales.shape != (shape[0], (shape[1] + 127) // 128):
@@ -286,13 +295,21 @@ def asap_moe_fp8_quantize(x, q, scales, stream=None):
         _refuse("CUDA tensors with contiguous columns", x=x, q=q, scales=scales)
     code = lib().asap_moe_fp8_quantize(x.data_ptr(), ld, n, c, q.data_ptr(), ldq, scales.data_ptr(), lds,
                                        _stream(stream))
-    if code:
-        check("asap_moe_fp8_quantize", code)
+    return code
 
 
 def asap_moe_fp8_swiglu_quantize(gate, up, q, scales, stream=None):
     """silu(gate) * up of bf16 [n, c] tensors with one row stride (the halves of
     a product's rows) to e4m3 q [n, c] with scales [n, ceil(c / 128)]."""
+    f = fast()
+    code = f.swiglu_quantize(gate, up, q, scales, stream) if f else None
+    if code is None:
+        code = _swiglu_quantize(gate, up, q, scales, stream)
+    if code:
+        check("asap_moe_fp8_swiglu_quantize", code)
+
+
+def _swiglu_quantize(gate, up, q, scales, stream):
     shape = gate.shape
     if len(shape) != 2 or gate.dtype is not _BF16 or up.shape != shape or up.dtype is not _BF16 or \
             q.shape != shape or (q.dtype is not _F8 and q.dtype is not _U8) or \
@@ -306,8 +323,7 @@ def asap_moe_fp8_swiglu_quantize(gate, up, q, scales, stream=None):
                 scales=scales)
     code = lib().asap_moe_fp8_swiglu_quantize(gate.data_ptr(), up.data_ptr(), ld, n, c, q.data_ptr(), ldq,
                                               scales.data_ptr(), lds, _stream(stream))
-    if code:
-        check("asap_moe_fp8_swiglu_quantize", code)
+    return code
 
 
 def asap_moe_fp8_matmul(a, a_scales, b, b_scales, out, stream=None, status=None):
@@ -315,6 +331,15 @@ def asap_moe_fp8_matmul(a, a_scales, b, b_scales, out, stream=None, status=None)
     boundaries) with fp32 scales [m, ceil(k / 128)] and [ceil(n / 128),
     ceil(k / 128)].  status: None or a one-element int32 CUDA tensor that gets
     error bits."""
+    f = fast()
+    code = f.matmul(a, a_scales, b, b_scales, out, stream, status) if f else None
+    if code is None:
+        code = _matmul(a, a_scales, b, b_scales, out, stream, status)
+    if code:
+        check("asap_moe_fp8_matmul", code)
+
+
+def _matmul(a, a_scales, b, b_scales, out, stream, status):
     sa, sb = a.shape, b.shape
     if len(sa) != 2 or len(sb) != 2:
         _refuse("a [m, k], b [n, k]", a=a, b=b)
@@ -333,8 +358,7 @@ def asap_moe_fp8_matmul(a, a_scales, b, b_scales, out, stream=None, status=None)
     code = lib().asap_moe_fp8_matmul(a.data_ptr(), lda, a_scales.data_ptr(), lsa, b.data_ptr(), ldb,
                                      b_scales.data_ptr(), lsb, out.data_ptr(), ldc, m, n, k,
                                      None if status is None else status.data_ptr(), _stream(stream))
-    if code:
-        check("asap_moe_fp8_matmul", code)
+    return code
 
 
 class Mailbox:
