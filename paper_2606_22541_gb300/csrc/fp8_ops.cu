@@ -18,9 +18,9 @@ constexpr unsigned kFull = 0xffffffffu;
 // take groups that follow one another.  W: columns per load (8, 4 or 1, by the
 // alignment of the rows).  The arithmetic per column would bound a scalar kernel
 // (45 us for 8045 rows of 7168), so quotients go in pairs (f32x2) and bf16
-// magnitudes two to a register.  Loads are hidden by eight CTAs an SM rather than
-// by several groups of a team on their way, whose registers cost more (1, 2 and 4
-// groups: 29.5, 33 and 35 us; SwiGLU of 4014 rows of 4096: 16, 18 and 23).
+// magnitudes two to a register.  Loads are hidden by eight CTAs an SM (six for
+// SwiGLU's registers) rather than by several groups of a team on their way, whose
+// registers cost more (1, 2 and 4 groups: 29.5, 33 and 35 us).
 constexpr int kQuantThreads = 256;
 constexpr int kTeam = 8;
 
@@ -76,15 +76,25 @@ __device__ __forceinline__ uint32_t max_abs2(uint32_t a, uint32_t b) {
   return *reinterpret_cast<const uint32_t*>(&m);
 }
 
-// The approximate exponential and quotient, 2 to 4 units in the last place of fp32, before a rounding to 3 bits: of 98.6
-// million values 106 came out other than the exact value's, 79 with fp32 arithmetic elsewhere.  expf and a division gave
-// 83 and took 22 us instead of 15.4 (4014 x 4096), the products and the quotient with their remainders 91 and 19.2.
-__device__ __forceinline__ float swiglu(float g, float u) { return __fdividef(g, 1.0f + __expf(-g)) * u; }
+// silu(g) * u of two columns: expf, and the quotient from the approximate reciprocal with one correction by its
+// remainder (Markstein), which leaves it right but for the last bit's ties.  Where e^-g overflows, or nearly, it is
+// divided.  Of 98.6 million values 83 came out other than the exact value's e4m3, as with a division, and 74 to 79 with
+// fp32 arithmetic elsewhere.  With __expf and __fdividef it was 106, and 15.4 us instead of 20 (4014 x 4096; a division
+// everywhere 22): not worth a third more values on the wrong side.
+__device__ __noinline__ float swiglu_far(float g, float u) { return g / (1.0f + expf(-g)) * u; }
+__device__ __forceinline__ float2 swiglu2(float2 g, float2 u) {
+  const float dx = 1.0f + expf(-g.x), dy = 1.0f + expf(-g.y);
+  float rx, ry;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(rx) : "f"(dx));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(ry) : "f"(dy));
+  const uint64_t x = pair(g.x, g.y), nd = pair(-dx, -dy), r = pair(rx, ry), q = mul2(x, r);
+  return unpair(mul2(fma2(fma2(q, nd, x), r, q), pair(u.x, u.y)));
+}
 
 template <bool SWIGLU, int W>
-__global__ void __launch_bounds__(kQuantThreads, 8) fp8_quantize_kernel(const uint16_t* x, const uint16_t* u, int rows,
-                                                                    int cols, long long ld, uint8_t* q, long long ldq,
-                                                                    float* s, long long lds, bool wide_q) {
+__global__ void __launch_bounds__(kQuantThreads, SWIGLU ? 6 : 8)
+    fp8_quantize_kernel(const uint16_t* x, const uint16_t* u, int rows, int cols, long long ld, uint8_t* q,
+                        long long ldq, float* s, long long lds, bool wide_q) {
   pdl_wait();
   pdl_launch();
   const int lane = threadIdx.x & (kTeam - 1);
@@ -118,11 +128,16 @@ __global__ void __launch_bounds__(kQuantThreads, 8) fp8_quantize_kernel(const ui
       f[2 * j + 1] = bf16_hi(g[j]);
     }
     if constexpr (SWIGLU) {
+      const uint32_t m = max_abs2(max_abs2(max_abs2(g[0], g[1]), max_abs2(g[2], g[3])),
+                                  max_abs2(max_abs2(g[4], g[5]), max_abs2(g[6], g[7])));
+      const bool far = fmaxf(bf16_lo(m), bf16_hi(m)) >= 80.f;
       am = 0.f;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        f[2 * j] = swiglu(f[2 * j], bf16_lo(up[j]));
-        f[2 * j + 1] = swiglu(f[2 * j + 1], bf16_hi(up[j]));
+        const float2 gj = make_float2(f[2 * j], f[2 * j + 1]), uj = make_float2(bf16_lo(up[j]), bf16_hi(up[j]));
+        const float2 v = far ? make_float2(swiglu_far(gj.x, uj.x), swiglu_far(gj.y, uj.y)) : swiglu2(gj, uj);
+        f[2 * j] = v.x;
+        f[2 * j + 1] = v.y;
         am = fmaxf(am, fmaxf(fabsf(f[2 * j]), fabsf(f[2 * j + 1])));
       }
 #pragma unroll
