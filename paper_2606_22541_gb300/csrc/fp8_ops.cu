@@ -523,14 +523,14 @@ __global__ void __launch_bounds__(kThreads, 2)
 // an SM, up to two of 128 do.  A CTA takes a tile after the other, or a cluster of S CTAs shares one as above.
 //   warp 0: TMA producer; warp 1: TMEM and MMA; from warp 4 on: epilogue, which takes
 //   registers from the first four warps.
-// What bounds it: the adding.  8045 x 4096 x 7168 takes 172 us (2.75 PFLOP/s at about 1.85 GHz), 154 with an epilogue
-// that only passes the partials on (3.07 PFLOP/s), 160 with one that reads them all and adds nothing.  On top of its K
-// loop a tile takes 1.5 us to round and store, while the next tile's first two blocks are multiplied: with short
-// contractions that shows (8045 x 28672 x 1024 232 us, 2.04 PFLOP/s).  Tried and no faster: chunks of 32 columns, four
-// partials of 128 columns, pairs of CTAs that load each other's half of the rows of B by multicast, and pairs that
-// multiply 256 rows by 256 together (cta_group::2; 180 us in single calls, where one CTA a tile takes 182): what
-// operands cost through L2 and shared memory is hidden behind the adding.  Back to back for milliseconds the clock
-// falls with the power, by up to a tenth.
+// What bounds it: the adding, and for long runs power.  8045 x 4096 x 7168 takes 172 us (2.75 PFLOP/s at about 1.85
+// GHz) after a pause and 198 in a steady state of power; 154 with an epilogue that only passes the partials on (3.07
+// PFLOP/s), 160 with one that reads them all and adds nothing.  On top of its K loop a tile takes 1.5 us to round and
+// store, while the next tile's first two blocks are multiplied: with short contractions that shows (8045 x 28672 x 1024
+// 232 us, 2.04 PFLOP/s).  Tried and no faster: chunks of 32 columns, four partials of 128 columns, pairs of CTAs that
+// load each other's half of the rows of B by multicast, and pairs that multiply 256 rows by 256 together (cta_group::2,
+// six stages: 198 us in the steady state too, 186 against 180 in single calls, 252 against 242 for 8045 x 28672 x 1024):
+// what operands cost through L2 and shared memory is hidden behind the adding.
 constexpr int kWideSplit = 4;  // K slices at most
 template <int TN>
 struct Wide {
