@@ -198,6 +198,8 @@ __global__ void __launch_bounds__(kQuantThreads, SWIGLU ? 6 : 8)
 // x 4096: their four epilogue warps are a CTA's only ones.
 //   warp 0: TMA producer; warp 1: TMEM and MMA; warps 2-5: epilogue, one TMEM
 //   lane quarter (32 rows of B) each.
+// Two CTAs of this file's kernels hold at most the 512 TMEM columns of an SM, and no other kernel that uses TMEM leaves
+// shared memory for one of them: an allocation never waits for a CTA whose cluster waits for this one.
 constexpr int kRows = 128;
 constexpr int kBBytes = kRows * kFp8BK;
 constexpr int kEpiThreads = 128;
