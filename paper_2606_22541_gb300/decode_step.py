@@ -115,10 +115,14 @@ def main(argv=None):
         ev[1].record()
         torch.cuda.synchronize()
         us = ev[0].elapsed_time(ev[1]) * 1e3 / a.steps
-        # the experts that the step's tokens chose, from the routing call of the prompt path
+        # the experts that the first MoE layer's tokens chose, from the routing call of the prompt path
+        z, y = x0.clone(), torch.empty_like(x0)
+        for layer in dense:
+            layer(z, y)
+            z += y
         i32 = dict(dtype=torch.int32, device="cuda")
         idx, counts = torch.empty((n, cfg.top_k), **i32), torch.empty(cfg.n_experts, **i32)
-        api.asap_moe_route(handle, x0, idx, torch.empty((n, cfg.top_k), device="cuda"), counts,
+        api.asap_moe_route(handle, z, idx, torch.empty((n, cfg.top_k), device="cuda"), counts,
                            torch.empty(cfg.n_experts + 1, **i32), step.ws)
         active = int((counts > 0).sum())
         expert = 3 * cfg.hidden * cfg.inter
