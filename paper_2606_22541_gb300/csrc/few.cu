@@ -974,6 +974,7 @@ __global__ void __launch_bounds__(FP8 && NT == 64 ? kThreads : 512, 1) few_ffn_k
       int last = 0;
       if (lane == 0) last = arrive_acq_rel(a.counters + T.ticket) == T.arrivals - 1;
       if (!__shfl_sync(kFull, last, 0)) continue;
+      __syncwarp();  // what lane 0 has acquired is every lane's to read
       write_h<FP8>(a, s, T, lane);
       fence_proxy_async_all();
       __syncwarp();
