@@ -192,9 +192,20 @@ FEW_MAX_TOKENS = 64
 def asap_moe_layer_few(h, x, out, ws, stream=None, layer_id=None):
     """The whole layer for 1 to FEW_MAX_TOKENS tokens in two kernels (the
     decode steps of a handle whose prompt batches go through asap_moe_layer).
+    x [n, hidden] and out (n rows or more) are bf16 and contiguous.
     layer_id: None (layer 0) or a one-element int32 CUDA tensor."""
+    rows = x.shape[0]
+    size = rows * h.cfg.hidden
+    if x.dtype is not _BF16 or out.dtype is not _BF16 or x.numel() != size or out.numel() < size or \
+            not (x.is_cuda and out.is_cuda and x.is_contiguous() and out.is_contiguous()):
+        _refuse(f"x [n, {h.cfg.hidden}] and out of as many rows or more, bf16 contiguous CUDA tensors", x=x, out=out)
+    if ws is not None and not (ws.is_cuda and ws.is_contiguous()):
+        _refuse("a contiguous CUDA tensor for the workspace", ws=ws)
+    if layer_id is not None and (not layer_id.is_cuda or layer_id.is_floating_point() or
+                                 layer_id.numel() * layer_id.element_size() < 4):
+        _refuse("layer_id: an int32 on the GPU", layer_id=layer_id)
     p, n = _ws(ws)
-    check("asap_moe_layer_few", lib().asap_moe_layer_few(h.ptr, _ptr(layer_id), _ptr(x), x.shape[0], _ptr(out), p, n,
+    check("asap_moe_layer_few", lib().asap_moe_layer_few(h.ptr, _ptr(layer_id), _ptr(x), rows, _ptr(out), p, n,
                                                          _stream(stream)))
 
 
