@@ -265,6 +265,7 @@ def asap_moe_route_noalloc(h, x, idx, w, counts, offsets, stream=None):
 
 
 _BF16, _F32, _F8, _U8 = torch.bfloat16, torch.float32, torch.float8_e4m3fn, torch.uint8
+_WORD = (torch.int32, torch.uint32)
 
 
 def _ld(t):
@@ -342,6 +343,8 @@ def asap_moe_fp8_matmul(a, a_scales, b, b_scales, out, stream=None, status=None)
     boundaries) with fp32 scales [m, ceil(k / 128)] and [ceil(n / 128),
     ceil(k / 128)].  status: None or a one-element int32 CUDA tensor that gets
     error bits."""
+    if status is not None and not (status.is_cuda and status.dtype in _WORD and status.numel()):
+        _refuse("status: an int32 on the GPU", status=status)
     f = fast()
     code = f.matmul(a, a_scales, b, b_scales, out, stream, status) if f else None
     if code is None:

@@ -128,7 +128,7 @@ static PyObject* swiglu_quantize(PyObject* self, PyObject* const* a, Py_ssize_t 
   return PyLong_FromLong(code);
 }
 
-/* matmul(a, a_scales, b, b_scales, out, stream, status) */
+/* matmul(a, a_scales, b, b_scales, out, stream, status); the caller has checked status */
 static PyObject* matmul(PyObject* self, PyObject* const* a, Py_ssize_t n) {
   Mat x, sx, w, sw, o;
   void *st, *status = NULL;
