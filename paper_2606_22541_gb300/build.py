@@ -6,7 +6,9 @@ The translation units compile in parallel; the library links the CUDA
 runtime statically and resolves the one driver entry point it needs
 (cuTensorMapEncodeTiled) at run time, so it loads on machines without a GPU.
 """
+import contextlib
 import os
+import shutil
 import subprocess
 import sys
 import sysconfig
@@ -23,7 +25,7 @@ SOURCES = ["api.cu", "gemm_tc.cu", "gemm_pair.cu", "gemm_fp8.cu", "route.cu", "r
 HEADERS = [os.path.join(CSRC, "common.cuh"), os.path.join(CSRC, "internal.h"), os.path.join(CSRC, "gemm_sched.cuh"), os.path.join(CSRC, "gemm_config.h"),
            os.path.join(CSRC, "pair.cuh"), os.path.join(CSRC, "few.h"), os.path.join(CSRC, "e4m3.cuh"),
            os.path.join(INCLUDE, "asap_moe.h")]
-MARSHAL = os.path.join(PKG, "_marshal.so")
+MARSHAL = os.path.join(PKG, "_marshal" + sysconfig.get_config_var("EXT_SUFFIX"))  # loaded by this Python version only
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC,-fvisibility=hidden",
          "-I", INCLUDE, "-I", CSRC]
@@ -79,12 +81,17 @@ def build(force=False, verbose=False, extra_flags=()):
 
 def build_marshal(force=False):
     """The Python binding's marshalling of the short calls, where Python's
-    headers are installed (without it they are marshalled in Python)."""
+    headers and a C compiler are installed (without it they are marshalled in
+    Python)."""
     src, include = os.path.join(CSRC, "marshal.c"), sysconfig.get_paths()["include"]
-    if not os.path.exists(os.path.join(include, "Python.h")) or not (force or _stale(MARSHAL, [src])):
+    untagged = os.path.join(PKG, "_marshal.so")  # any Python version would load it
+    with contextlib.suppress(FileNotFoundError):
+        os.remove(untagged)
+    gcc = shutil.which("gcc")
+    if gcc is None or not os.path.exists(os.path.join(include, "Python.h")) or not (force or _stale(MARSHAL, [src])):
         return
     tmp = MARSHAL + ".tmp"
-    cmd = ["gcc", "-O2", "-Wall", "-shared", "-fPIC", "-fvisibility=hidden", "-I", include, src, "-o", tmp]
+    cmd = [gcc, "-O2", "-Wall", "-shared", "-fPIC", "-fvisibility=hidden", "-I", include, src, "-o", tmp]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError("gcc failed:\n" + " ".join(cmd) + "\n" + r.stdout + r.stderr)
