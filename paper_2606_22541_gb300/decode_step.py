@@ -98,6 +98,7 @@ def main(argv=None):
         x0 = inputs.make_tokens(cfg, n, 0, "cuda")
         x = x0.clone()
         side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())  # which makes the weights, the ids and x
         with torch.cuda.stream(side):
             step(x)
         torch.cuda.synchronize()
@@ -129,6 +130,8 @@ def main(argv=None):
         moe = active * expert + 3 * cfg.hidden * cfg.shared_inter + 2 * cfg.n_experts * cfg.hidden
         read = sum(d.weight_bytes() for d in dense) + a.moe * moe
         code, word = api.asap_moe_status(handle)
+        if code:
+            raise RuntimeError(f"device status word {word:#x}")
         print(f"{n:3d} tokens: {us:8.1f} us per step, about {read / 1e6:.0f} MB of weights ({active} experts in the first "
               f"MoE layer), {read / us / 1e3 / a.gbs:.2f} of {a.gbs:.0f} GB/s, status {word}", flush=True)
     handle.close()
