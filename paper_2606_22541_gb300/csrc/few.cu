@@ -617,7 +617,11 @@ __device__ __forceinline__ void write_h(const FewArgs& a, const FewSmem& s, cons
         if (lane == 0) *reinterpret_cast<float*>(step + m * 128 + c * 4) = gs.s;
       } else {
         uint8_t* step = img + static_cast<long long>(2 * T.tile + (lane >> 4)) * step_bytes<false>(2 * m);
-        const uint32_t a0 = pack_bf16x2(h[0], h[1]), a1 = pack_bf16x2(h[2], h[3]);
+        // (the value stays below what bf16 rounds to infinity: the difference is then the rest of a finite h and,
+        // with the sign of h, infinite for an infinite one; a NaN is in the difference)
+        constexpr float kMost = 0x1.fep127f;  // the largest bf16
+        auto within = [](float v) { return fminf(fmaxf(v, -kMost), kMost); };
+        const uint32_t a0 = pack_bf16x2(within(h[0]), within(h[1])), a1 = pack_bf16x2(within(h[2]), within(h[3]));
         const uint32_t b0 = pack_bf16x2(h[0] - bf16_lo(a0), h[1] - bf16_hi(a0));
         const uint32_t b1 = pack_bf16x2(h[2] - bf16_lo(a1), h[3] - bf16_hi(a1));
         *reinterpret_cast<uint2*>(step + swizzled(c, 8 * (lane & 15))) = make_uint2(a0, a1);
