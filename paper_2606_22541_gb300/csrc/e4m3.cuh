@@ -23,11 +23,12 @@ struct GroupScale {
   // reciprocal is correctly rounded, by its residual): the quotient is the one a
   // division gives.  bf16 values over amax / 448 fall exactly between two e4m3
   // values for about one element in 500, and those must not depend on how the
-  // quotient was taken.  (An infinite s gives NaN.)
+  // quotient was taken.  (An infinite s gives NaN.  The residual is rounded
+  // down: that of an exact zero is -0, with which a quotient of -0 keeps its sign.)
   __device__ __forceinline__ float operator()(float v) const {
     v *= up;
     const float q = v * inv;
-    return fmaf(fmaf(-q, scaled, v), inv, q);
+    return fmaf(__fmaf_rd(-q, scaled, v), inv, q);
   }
 };
 

@@ -64,6 +64,13 @@ __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
   asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
   return r;
 }
+// a b + c rounded down, for the remainder of a quotient: that of an exact zero is -0, which leaves a quotient of -0 as it
+// is (+0 would not); other remainders are exact, or far below what they correct.
+__device__ __forceinline__ uint64_t remainder2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rm.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
 __device__ __forceinline__ float2 unpair(uint64_t p) {
   float2 r;
   asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(p));
@@ -88,7 +95,7 @@ __device__ __forceinline__ float2 swiglu2(float2 g, float2 u) {
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(rx) : "f"(dx));
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(ry) : "f"(dy));
   const uint64_t x = pair(g.x, g.y), nd = pair(-dx, -dy), r = pair(rx, ry), q = mul2(x, r);
-  return unpair(mul2(fma2(fma2(q, nd, x), r, q), pair(u.x, u.y)));
+  return unpair(mul2(fma2(remainder2(q, nd, x), r, q), pair(u.x, u.y)));
 }
 
 template <bool SWIGLU, int W>
@@ -162,8 +169,8 @@ __global__ void __launch_bounds__(kQuantThreads, SWIGLU ? 6 : 8)
           v1 = mul2(v1, by);
         }
         uint64_t q0 = mul2(v0, inv), q1 = mul2(v1, inv);  // GroupScale's quotient, two at a time
-        q0 = fma2(fma2(q0, neg, v0), inv, q0);
-        q1 = fma2(fma2(q1, neg, v1), inv, q1);
+        q0 = fma2(remainder2(q0, neg, v0), inv, q0);
+        q1 = fma2(remainder2(q1, neg, v1), inv, q1);
         const float2 a = unpair(q0), b = unpair(q1);
         w[j] = e4m3x4(a.x, a.y, b.x, b.y);
       }
