@@ -869,12 +869,16 @@ __global__ void __launch_bounds__(Wide<TN>::kThreads, Wide<TN>::kCtas)
             stage[lane * 4 + (j ^ ((lane >> 1) & 3))] = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]),
                                                                    pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
           }
-          if (bulk) fence_proxy_async_smem();
-          __syncwarp();
-          if (bulk && lane == 0 && t0 < p.m && n0 < p.n) tma_store_2d(&tmC, smem_u32(stage), n0, t0);
           // (a group a round, an empty one too: the one that may stay pending above is the round before)
+          if (bulk) {
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0 && t0 < p.m && n0 < p.n) tma_store_2d(&tmC, smem_u32(stage), n0, t0);
+            if (lane == 0) bulk_commit_group();
+            continue;
+          }
           if (lane == 0) bulk_commit_group();
-          if (bulk) continue;
+          __syncwarp();
           __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.c) + static_cast<long long>(t0) * p.ldc + n0;
           if (args.c_align >= 4 && (p.n & 1) == 0) {  // two columns a lane, two rows an instruction
             const int c = 2 * (lane & 15);

@@ -25,25 +25,28 @@ def _round():
 
 
 def _commits():
-    """(whether a round stored by a bulk store commits a group, whether a direct one does)."""
+    """(whether a round stored by a bulk store commits one group, whether a direct one does)."""
     body = _round()
-    assert body.count("bulk_commit_group()") == 1 and body.count("wait_group.read 1") == 1
-    assert body.index("wait_group.read 1") < body.index("uint4* stage") or \
-        body.index("wait_group.read 1") < body.index("stage[lane * 4")
-    # braces open at the commit: the conditions it stands under
-    at, stack = body.index("bulk_commit_group()"), []
-    for i, c in enumerate(body[:at]):
-        if c == "{":
-            stack.append(body[max(body.rfind(";", 0, i), body.rfind("}", 0, i), body.rfind("{", 0, i)) + 1:i].strip())
-        elif c == "}":
-            stack.pop()
-    line = body[body.rfind("\n", 0, at):at].strip()
-    assert line == "if (lane == 0)"
-    conditions = [s for s in stack if s.startswith("if")]
-    assert conditions in ([], ["if (bulk)"]), conditions
-    early = re.search(r"\b(continue|break|return)\b", body[:at])
-    assert early is None
-    return True, not conditions
+    assert body.count("wait_group.read 1") == 1 and body.index("wait_group.read 1") < body.index("stage[lane * 4")
+    # each commit's guard, the conditions it stands under and whether a round by a bulk store gets there
+    by_bulk = by_hand = 0
+    for m in re.finditer(r"bulk_commit_group\(\)", body):
+        at, stack = m.start(), []
+        for i, c in enumerate(body[:at]):
+            if c == "{":
+                stack.append(body[max(body.rfind(k, 0, i) for k in ";}{") + 1:i].strip())
+            elif c == "}":
+                stack.pop()
+        assert body[body.rfind("\n", 0, at):at].strip() == "if (lane == 0)"
+        conditions = [s for s in stack if s.startswith(("if", "else"))]
+        left = re.findall(r"\b(?:continue|break|return)\b", body[:at])  # a bulk round leaves at its end, if at all
+        assert conditions in ([], ["if (bulk)"]) and left in ([], ["continue"]), (conditions, left)
+        if left:
+            assert not conditions and re.search(r"if \(bulk\) \{[^{}]*continue;\s*\}|if \(bulk\) continue;", body[:at])
+        by_bulk += not left
+        by_hand += not conditions
+    assert by_bulk <= 1 and by_hand <= 1
+    return bool(by_bulk), bool(by_hand)
 
 
 def _rounds(n, aligned):
