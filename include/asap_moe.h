@@ -346,8 +346,12 @@ int asap_moe_layer_dyn(asap_moe_t h, const int32_t* layer_id, const void* x, int
  *    in fp32.  The same call gives the same bits each time.
  *  - The workspace is asap_moe_workspace_size for n tokens or more; its
  *    contents before the call do not matter.
- *  - Made for layers that are a stream of weights.  One whose weights are read
- *    within about 10 us is served faster by asap_moe_layer from 17 tokens on. */
+ *  - Made for layers that are a stream of weights.  The faster of the two calls
+ *    up to 8 tokens on every layer measured, and on wide layers up to 64.  From
+ *    17 tokens on asap_moe_layer is faster where few weights are read: 8 experts
+ *    of 1024 x 384 (29 us here and 26 there for 32 tokens), in e4m3 also 256
+ *    experts of 512 x 256 (49 and 43 for 20), and, from about 60 tokens on, 8
+ *    of 2048 x 4096 (94 and 92). */
 #define ASAP_MOE_FEW_MAX_TOKENS 64
 int asap_moe_layer_few(asap_moe_t h, const int32_t* layer_id, const void* x, int32_t n, void* out,
                        void* ws, size_t ws_bytes, void* stream);

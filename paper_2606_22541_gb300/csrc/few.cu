@@ -39,8 +39,8 @@
 // fill where there is one, and 2 to 4 us of last sums at the end.  One token:
 // Mixtral's shape (two experts of 176 M parameters) 108.6 us, 6.5 TB/s;
 // DeepSeek-V3's 113 us, 7.0 TB/s (the stream alone passes the rate of a plain
-// copy), in e4m3 64.8 us, 6.2 TB/s; 61 tokens of the latter, 210 experts, 1300 us,
-// 7.1 TB/s.
+// copy), in e4m3 64.8 us, 6.2 TB/s; 61 tokens of the latter, 209 experts, 1300 to
+// 1327 us, 7.0 to 7.1 TB/s.
 #include "common.cuh"
 #include "e4m3.cuh"
 #include "few.h"

@@ -532,8 +532,8 @@ __global__ void __launch_bounds__(kThreads, 2)
 // an SM, up to two of 128 do.  A CTA takes a tile after the other, or a cluster of S CTAs shares one as above.
 //   warp 0: TMA producer; warp 1: TMEM and MMA; from warp 4 on: epilogue, which takes
 //   registers from the first four warps.
-// What bounds it: the adding, and for long runs power.  8045 x 4096 x 7168 takes 172 us (2.75 PFLOP/s at about 1.85
-// GHz) after a pause and 198 in a steady state of power; 154 with an epilogue that only passes the partials on (3.07
+// What bounds it: the adding, and for long runs power.  8045 x 4096 x 7168 takes 198 to 204 us in a stream of calls (2.36
+// PFLOP/s, in a steady state of power) and 172 after a pause (2.75 PFLOP/s at about 1.85 GHz); 154 with an epilogue that only passes the partials on (3.07
 // PFLOP/s), 160 with one that reads them all and adds nothing.  On top of its K loop a tile takes 1.5 us to round and
 // store, while the next tile's first two blocks are multiplied: with short contractions that shows (8045 x 28672 x 1024
 // 232 us, 2.04 PFLOP/s).  Tried and no faster: chunks of 32 columns, four partials of 128 columns, pairs of CTAs that
