@@ -347,8 +347,9 @@ int asap_moe_layer_dyn(asap_moe_t h, const int32_t* layer_id, const void* x, int
  *  - The workspace is asap_moe_workspace_size for n tokens or more; its
  *    contents before the call do not matter.
  *  - Made for layers that are a stream of weights.  The faster of the two calls
- *    up to 8 tokens on every layer measured, and on wide layers up to 64.  From
- *    17 tokens on asap_moe_layer is faster where few weights are read: 8 experts
+ *    up to 8 tokens on every layer measured, and on wide layers up to 64 (in
+ *    e4m3 up to about 60, and within 2 % above).  From 17 tokens on
+ *    asap_moe_layer is faster where few weights are read: 8 experts
  *    of 1024 x 384 (29 us here and 26 there for 32 tokens), in e4m3 also 256
  *    experts of 512 x 256 (49 and 43 for 20), and, from about 60 tokens on, 8
  *    of 2048 x 4096 (94 and 92). */
