@@ -462,6 +462,100 @@ int asap_moe_fp8_matmul(const void* a, int64_t lda, const float* a_scales, int64
                         void* stream);
 
 /* ------------------------------------------------------------------------
+ * Around the expert products of a training step, on plain tensors: tokens
+ * sorted by expert and back with the gradients of both, and SwiGLU whose
+ * activations are kept for the backward pass in e4m3.  No handle; they launch
+ * on the caller's current device and only enqueue.  Strides (ld*) are in
+ * elements between rows and at least the rows' length; no extent may exceed
+ * 2^30, n * k stays below 2^31, k >= 1.  Any column count, stride and alignment
+ * (rows that start on 16-byte boundaries are the fast ones).  Outputs must not
+ * overlap inputs or each other.  The same call gives the same bits each time.
+ *
+ * perm_dst [n, k] int32: the row of (token t, slot j) among the rows of x_perm or
+ * y_perm, -1 where no expert takes the entry.  A row outside [0, rows) is treated
+ * like -1 and, other than -1, recorded as bit 2 of *status (NULL, or a device word
+ * that gets bits of asap_moe_status ORed in).  No row is named twice.
+ * ------------------------------------------------------------------------ */
+
+/* Element types of those tensors.  Sums and intermediate values are fp32;
+ * results are rounded once. */
+typedef enum {
+  ASAP_ELEM_BF16 = 0,
+  ASAP_ELEM_F16 = 1,
+  ASAP_ELEM_F32 = 2,
+  ASAP_ELEM_E4M3 = 3 /* asap_moe_permute alone (any bytes) */
+} asap_elem;
+
+/* Places of (token, slot) entries sorted by expert: experts idx [n, k] (int32;
+ * outside [0, n_experts): no expert takes the entry), offsets [n_experts + 1],
+ * perm_dst [n, k] (-1 for such an entry).  Inside an expert's segment places
+ * follow increasing (t, j), as asap_moe_dispatch has them; offsets[n_experts] is
+ * the number of entries taken.  perm_src: NULL, or [n * k], place -> token (only
+ * the places taken are written).  1 <= n_experts <= ASAP_MOE_SORT_MAX_EXPERTS.
+ * n == 0 writes the offsets (zeros).  ws: asap_moe_sort_workspace_size bytes,
+ * 4-byte aligned (NULL where that is 0); one of more entries serves fewer; two
+ * calls that run at the same time must not share one. */
+#define ASAP_MOE_SORT_MAX_EXPERTS 1024
+int asap_moe_sort_workspace_size(int32_t n, int32_t k, int32_t n_experts, size_t* bytes);
+int asap_moe_sort(const int32_t* idx, int32_t n, int32_t k, int32_t n_experts, int32_t* offsets,
+                  int32_t* perm_dst, int32_t* perm_src, void* ws, size_t ws_bytes, void* stream);
+
+/* x_perm[perm_dst[t, j]] = x[t] for x [n, cols], x_perm [rows, cols].  Rows that
+ * no entry names are left as they were. */
+int asap_moe_permute(int32_t type, const void* x, int64_t ldx, int32_t n, int32_t cols,
+                     const int32_t* perm_dst, int32_t k, void* x_perm, int64_t ldp, int32_t rows,
+                     uint32_t* status, void* stream);
+
+/* out[t] = sum_j w[t, j] y_perm[perm_dst[t, j]] in slot order, over the entries
+ * that have a row (none: zeros; their weights are not looked at).  w [n, k] fp32,
+ * or NULL for ones: then this is the gradient of asap_moe_permute. */
+int asap_moe_unpermute(int32_t type, const void* y_perm, int64_t ldy, int32_t rows, int32_t cols,
+                       const float* w, const int32_t* perm_dst, int32_t n, int32_t k, void* out,
+                       int64_t ldo, uint32_t* status, void* stream);
+
+/* The gradients of asap_moe_unpermute, from d_out [n, cols]:
+ *   d_y_perm[perm_dst[t, j]] = w[t, j] d_out[t]       (NULL: not wanted)
+ *   d_w[t, j] = <d_out[t], y_perm[perm_dst[t, j]]>, 0 for an entry without a row
+ *                                                     (NULL: not wanted)
+ * y_perm is read for d_w alone.  Rows of d_y_perm that no entry names are left
+ * as they were. */
+int asap_moe_unpermute_backward(int32_t type, const void* d_out, int64_t ldo, const void* y_perm,
+                                int64_t ldy, const float* w, const int32_t* perm_dst, int32_t n,
+                                int32_t k, int32_t cols, void* d_y_perm, int64_t ldd, int32_t rows,
+                                float* d_w, uint32_t* status, void* stream);
+
+/* h = silu(gate) * up (fp32, rounded to the type), and gate and up kept for
+ * asap_moe_swiglu_backward in e4m3 with a scale per row per 128 columns, as
+ * asap_moe_fp8_quantize would quantise them.  gate, up [rows, cols] with one
+ * stride (the halves of a product's rows, or two tensors), gate_q, up_q [rows,
+ * cols] and gate_s, up_s [rows, ceil(cols/128)] likewise.  n_rows: NULL, or a
+ * device int32 (offsets[n_experts] of the sort): only that many rows are read and
+ * written. */
+int asap_moe_swiglu_save(int32_t type, const void* gate, const void* up, int64_t ld, int32_t rows,
+                         int32_t cols, const int32_t* n_rows, void* h, int64_t ldh, void* gate_q,
+                         void* up_q, int64_t ldq, float* gate_s, float* up_s, int64_t lds,
+                         void* stream);
+
+/* The gradients of silu(gate) * up at what was kept (G, U: e4m3 times scale; S =
+ * 1 / (1 + exp(-G))):
+ *   d_gate = d_h U (S + G S (1 - S)),  d_up = d_h G S
+ * and h = G S U for the gradient of the next product's weight (NULL: not wanted).
+ * d_gate, d_up [rows, cols] with one stride; n_rows as above. */
+int asap_moe_swiglu_backward(int32_t type, const void* d_h, int64_t ldd, const void* gate_q,
+                             const void* up_q, int64_t ldq, const float* gate_s, const float* up_s,
+                             int64_t lds, int32_t rows, int32_t cols, const int32_t* n_rows,
+                             void* d_gate, void* d_up, int64_t ldg, void* h, int64_t ldh,
+                             void* stream);
+
+/* e4m3 rows with a scale per row per 128 columns (asap_moe_fp8_quantize's) back
+ * to x [rows, cols] of the type: row t times its scales to every row perm_dst[t,
+ * j] (tokens kept in e4m3, read back as the rows of their experts), or to row t
+ * with perm_dst NULL, k 1 and rows n. */
+int asap_moe_fp8_dequantize(int32_t type, const void* q, int64_t ldq, const float* scales,
+                            int64_t lds, int32_t n, int32_t cols, const int32_t* perm_dst, int32_t k,
+                            void* x, int64_t ldx, int32_t rows, uint32_t* status, void* stream);
+
+/* ------------------------------------------------------------------------
  * Mailbox: the device decides which micro-batches one grouped GEMM pass
  * serves.  The single-GPU form of the asynchronous primitives of Sections
  * 3.2.1 and 3.2.2 (Table 2: per DP group, regions for the token data and the

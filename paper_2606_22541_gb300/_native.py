@@ -62,6 +62,14 @@ SIGNATURES = {
     "asap_moe_fp8_quantize": [_P, _L, _I, _I, _P, _L, _P, _L, _P],
     "asap_moe_fp8_swiglu_quantize": [_P, _P, _L, _I, _I, _P, _L, _P, _L, _P],
     "asap_moe_fp8_matmul": [_P, _L, _P, _L, _P, _L, _P, _L, _P, _L, _I, _I, _I, _P, _P],
+    "asap_moe_sort_workspace_size": [_I, _I, _I, ctypes.POINTER(_SZ)],
+    "asap_moe_sort": [_P, _I, _I, _I, _P, _P, _P, _P, _SZ, _P],
+    "asap_moe_permute": [_I, _P, _L, _I, _I, _P, _I, _P, _L, _I, _P, _P],
+    "asap_moe_unpermute": [_I, _P, _L, _I, _I, _P, _P, _I, _I, _P, _L, _P, _P],
+    "asap_moe_unpermute_backward": [_I, _P, _L, _P, _L, _P, _P, _I, _I, _I, _P, _L, _I, _P, _P, _P],
+    "asap_moe_swiglu_save": [_I, _P, _P, _L, _I, _I, _P, _P, _L, _P, _P, _L, _P, _P, _L, _P],
+    "asap_moe_swiglu_backward": [_I, _P, _L, _P, _P, _L, _P, _P, _L, _I, _I, _P, _P, _P, _L, _P, _L, _P],
+    "asap_moe_fp8_dequantize": [_I, _P, _L, _P, _L, _I, _I, _P, _I, _P, _L, _I, _P, _P],
     "asap_moe_layer_batched": [_P, _I, ctypes.POINTER(_P), ctypes.POINTER(_I), ctypes.POINTER(_P), _P, _SZ, _P],
     "asap_moe_layer_dyn": [_P, _P, _P, _I, _P, _P, _SZ, _P],
     "asap_moe_layer_batched_dyn": [_P, _P, _I, ctypes.POINTER(_P), ctypes.POINTER(_I), ctypes.POINTER(_P), _P, _SZ,

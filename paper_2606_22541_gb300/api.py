@@ -375,6 +375,225 @@ def _matmul(a, a_scales, b, b_scales, out, stream, status):
     return code
 
 
+# ------------------------------------------------------------ around the expert products of a training step
+
+SORT_MAX_EXPERTS = 1024
+_ELEM = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
+_BYTES = {torch.float8_e4m3fn: 3, torch.uint8: 3, **_ELEM}   # what asap_moe_permute copies
+
+
+def asap_moe_sort_workspace_size(n, k, n_experts):
+    out = ctypes.c_size_t()
+    check("asap_moe_sort_workspace_size",
+          lib().asap_moe_sort_workspace_size(int(n), int(k), int(n_experts), ctypes.byref(out)))
+    return out.value
+
+
+def sort_workspace(n, k, n_experts, device="cuda"):
+    """A workspace tensor large enough for asap_moe_sort of n tokens or fewer."""
+    return torch.empty(max(asap_moe_sort_workspace_size(n, k, n_experts), 256), dtype=torch.uint8, device=device)
+
+
+def _data(t):
+    return None if t is None else t.data_ptr()
+
+
+def _here(*tensors):
+    """All on the current device, where the calls without a handle launch."""
+    index = None
+    for t in tensors:
+        if t is None:
+            continue
+        if not t.is_cuda:
+            return False
+        if index is None:
+            index = torch.cuda.current_device()
+        if t.get_device() != index:
+            return False
+    return True
+
+
+def _dense(t, dtype, shape):
+    return t.dtype is dtype and t.shape == shape and t.is_contiguous()
+
+
+def asap_moe_sort(idx, n_experts, offsets, perm_dst, ws=None, perm_src=None, stream=None):
+    """Entries sorted by expert: idx [n, k] int32 (outside [0, n_experts): no
+    expert takes it) to offsets [n_experts + 1], perm_dst [n, k] (the entry's
+    row, -1: none) and, if given, perm_src [n * k] (row -> token), all int32 and
+    contiguous.  ws: sort_workspace(n, k, n_experts), None where its size is 0."""
+    shape = idx.shape
+    if len(shape) != 2 or not _dense(idx, torch.int32, shape) or not _dense(perm_dst, torch.int32, shape) or \
+            not _dense(offsets, torch.int32, (n_experts + 1,)) or \
+            (perm_src is not None and not _dense(perm_src, torch.int32, (shape[0] * shape[1],))) or \
+            (ws is not None and not ws.is_contiguous()) or not _here(idx, offsets, perm_dst, perm_src, ws):
+        _refuse("contiguous int32 tensors on the current CUDA device, idx, perm_dst [n, k], offsets [n_experts + 1], perm_src [n * k] or None, "
+                "and a workspace", idx=idx, offsets=offsets, perm_dst=perm_dst,
+                **{k: t for k, t in (("perm_src", perm_src), ("ws", ws)) if t is not None})
+    p, nb = (None, 0) if ws is None else (ws.data_ptr(), ws.numel() * ws.element_size())
+    code = lib().asap_moe_sort(idx.data_ptr(), shape[0], shape[1], n_experts, offsets.data_ptr(), perm_dst.data_ptr(),
+                               _data(perm_src), p, nb, _stream(stream))
+    if code:
+        check("asap_moe_sort", code)
+
+
+def _check_status(status):
+    if status is not None and not (status.is_cuda and status.dtype in _WORD and status.numel()):
+        _refuse("status: an int32 on the GPU", status=status)
+
+
+def asap_moe_permute(x, perm_dst, x_perm, stream=None, status=None):
+    """x_perm[perm_dst[t, j]] = x[t]: x [n, c] and x_perm [rows, c] of one type
+    (bf16, fp16, fp32, e4m3 or uint8), perm_dst [n, k] int32 contiguous; any row
+    strides.  Rows of x_perm that nothing names stay as they were.  status: None
+    or a one-element int32 CUDA tensor that gets bit 2 for a row that does not
+    exist (other than -1)."""
+    _check_status(status)
+    if x.dim() != 2 or x_perm.dim() != 2 or perm_dst.dim() != 2 or x.dtype not in _BYTES or x_perm.dtype is not x.dtype or \
+            x_perm.shape[1] != x.shape[1] or not _dense(perm_dst, torch.int32, (x.shape[0], perm_dst.shape[1])) or \
+            not _here(x, x_perm, perm_dst, status):
+        _refuse("tensors on the current CUDA device, x [n, c], x_perm [rows, c] of one type, perm_dst [n, k] int32", x=x, perm_dst=perm_dst,
+                x_perm=x_perm)
+    n, c = x.shape
+    rows, ld, ldp = x_perm.shape[0], _ld(x), _ld(x_perm)
+    if not (ld and ldp) and n and c and rows:
+        _refuse("CUDA tensors with contiguous columns", x=x, x_perm=x_perm)
+    code = lib().asap_moe_permute(_BYTES[x.dtype], x.data_ptr(), ld, n, c, perm_dst.data_ptr(), perm_dst.shape[1],
+                                  x_perm.data_ptr(), ldp, rows, _data(status), _stream(stream))
+    if code:
+        check("asap_moe_permute", code)
+
+
+def asap_moe_unpermute(y_perm, w, perm_dst, out, stream=None, status=None):
+    """out[t] = sum_j w[t, j] y_perm[perm_dst[t, j]] over the entries that have a
+    row: y_perm [rows, c], out [n, c] of one type (bf16, fp16 or fp32), w [n, k]
+    fp32 or None (ones: the gradient of asap_moe_permute), perm_dst [n, k] int32,
+    both contiguous.  status as for asap_moe_permute."""
+    _check_status(status)
+    if y_perm.dim() != 2 or out.dim() != 2 or perm_dst.dim() != 2 or y_perm.dtype not in _ELEM or \
+            out.dtype is not y_perm.dtype or y_perm.shape[1] != out.shape[1] or \
+            not _dense(perm_dst, torch.int32, (out.shape[0], perm_dst.shape[1])) or \
+            (w is not None and not _dense(w, _F32, perm_dst.shape)) or not _here(y_perm, w, perm_dst, out, status):
+        _refuse("tensors on the current CUDA device, y_perm [rows, c], out [n, c] of one type, perm_dst [n, k] int32, w [n, k] fp32 or None",
+                y_perm=y_perm, perm_dst=perm_dst, out=out, **({} if w is None else {"w": w}))
+    n, c = out.shape
+    rows, ldy, ldo = y_perm.shape[0], _ld(y_perm), _ld(out)
+    if not (ldy and ldo) and n and c and rows:
+        _refuse("CUDA tensors with contiguous columns", y_perm=y_perm, out=out)
+    code = lib().asap_moe_unpermute(_ELEM[out.dtype], y_perm.data_ptr(), ldy, rows, c, _data(w), perm_dst.data_ptr(), n,
+                                    perm_dst.shape[1], out.data_ptr(), ldo, _data(status), _stream(stream))
+    if code:
+        check("asap_moe_unpermute", code)
+
+
+def asap_moe_unpermute_backward(d_out, y_perm, w, perm_dst, d_y_perm, d_w, stream=None, status=None):
+    """The gradients of asap_moe_unpermute: d_y_perm[perm_dst[t, j]] = w[t, j]
+    d_out[t] and d_w[t, j] = <d_out[t], y_perm[perm_dst[t, j]]> (0 where the entry
+    has no row).  d_out [n, c], y_perm and d_y_perm [rows, c] of one type, w and
+    d_w [n, k] fp32.  w None: ones; d_y_perm or d_w None: not wanted; y_perm may be
+    None where d_w is."""
+    _check_status(status)
+    y = {k: t for k, t in (("y_perm", y_perm), ("d_y_perm", d_y_perm)) if t is not None}
+    rows = next(iter(y.values())).shape[0] if y else 0
+    if d_out.dim() != 2 or perm_dst.dim() != 2 or d_out.dtype not in _ELEM or \
+            any(t.dtype is not d_out.dtype or t.shape != (rows, d_out.shape[1]) for t in y.values()) or \
+            not _dense(perm_dst, torch.int32, (d_out.shape[0], perm_dst.shape[1])) or \
+            any(t is not None and not _dense(t, _F32, perm_dst.shape) for t in (w, d_w)) or \
+            (d_w is not None and y_perm is None) or \
+            not _here(d_out, y_perm, w, perm_dst, d_y_perm, d_w, status):
+        _refuse("tensors on the current CUDA device, d_out [n, c], y_perm and d_y_perm [rows, c] of one type, perm_dst [n, k] int32, w and d_w "
+                "[n, k] fp32", d_out=d_out, perm_dst=perm_dst, **y,
+                **{k: t for k, t in (("w", w), ("d_w", d_w)) if t is not None})
+    n, c = d_out.shape
+    ldo, lds = _ld(d_out), {k: _ld(t) for k, t in y.items()}
+    if not (ldo and all(lds.values())) and n and c and rows:
+        _refuse("CUDA tensors with contiguous columns", d_out=d_out, **y)
+    code = lib().asap_moe_unpermute_backward(_ELEM[d_out.dtype], d_out.data_ptr(), ldo, _data(y_perm), lds.get("y_perm", 0),
+                                             _data(w), perm_dst.data_ptr(), n, perm_dst.shape[1], c, _data(d_y_perm),
+                                             lds.get("d_y_perm", 0), rows, _data(d_w), _data(status), _stream(stream))
+    if code:
+        check("asap_moe_unpermute_backward", code)
+
+
+def _swiglu_kept(rows, cols, gate_q, gate_s, up_q, up_s, n_rows, **others):
+    """Row strides of the kept tensors' values and scales; refuses what does not fit (others: [rows, cols] of one type)."""
+    shape, blocks = (rows, cols), (rows, (cols + 127) // 128)
+    first = next(iter(others.values()))
+    tensors = dict(others, gate_q=gate_q, gate_s=gate_s, up_q=up_q, up_s=up_s)
+    if first.dtype not in _ELEM or any(t.dtype is not first.dtype or t.shape != shape for t in others.values()) or \
+            any(t.dtype not in (_F8, _U8) or t.shape != shape for t in (gate_q, up_q)) or \
+            any(t.dtype is not _F32 or t.shape != blocks for t in (gate_s, up_s)) or \
+            (n_rows is not None and (n_rows.dtype is not torch.int32 or n_rows.numel() != 1)) or \
+            not _here(*tensors.values(), n_rows):
+        _refuse(f"tensors on the current CUDA device, {', '.join(others)} [n, c] of one type (bf16, fp16, fp32), gate_q, up_q [n, c] e4m3, gate_s, "
+                "up_s [n, ceil(c / 128)] fp32, n_rows None or one int32", **tensors,
+                **({} if n_rows is None else {"n_rows": n_rows}))
+    lds = {k: _ld(t) for k, t in tensors.items()}
+    pairs = [("gate_q", "up_q"), ("gate_s", "up_s"), ("gate", "up"), ("d_gate", "d_up")]
+    if rows and cols and (not all(lds.values()) or any(lds[a] != lds[b] for a, b in pairs if a in lds)):
+        _refuse("CUDA tensors with contiguous columns, gate and up (values, scales, gradients) with one row stride", **tensors)
+    return lds
+
+
+def asap_moe_swiglu_save(gate, up, h, gate_q, gate_s, up_q, up_s, stream=None, n_rows=None):
+    """h = silu(gate) * up, with gate and up kept for asap_moe_swiglu_backward as
+    asap_moe_fp8_quantize would quantise them.  gate, up, h [n, c] of one type
+    (bf16, fp16 or fp32), gate_q, up_q [n, c] e4m3, gate_s, up_s [n, ceil(c /
+    128)] fp32; gate and up have one row stride each time (the halves of a
+    product's rows).  n_rows: None or a one-element int32 CUDA tensor, the rows
+    that are read and written (offsets[-1:] of asap_moe_sort)."""
+    if gate.dim() != 2:
+        _refuse("gate [n, c]", gate=gate)
+    n, c = gate.shape
+    ld = _swiglu_kept(n, c, gate_q, gate_s, up_q, up_s, n_rows, gate=gate, up=up, h=h)
+    code = lib().asap_moe_swiglu_save(_ELEM[gate.dtype], gate.data_ptr(), up.data_ptr(), ld["gate"], n, c, _data(n_rows),
+                                      h.data_ptr(), ld["h"], gate_q.data_ptr(), up_q.data_ptr(), ld["gate_q"],
+                                      gate_s.data_ptr(), up_s.data_ptr(), ld["gate_s"], _stream(stream))
+    if code:
+        check("asap_moe_swiglu_save", code)
+
+
+def asap_moe_swiglu_backward(d_h, gate_q, gate_s, up_q, up_s, d_gate, d_up, h=None, stream=None, n_rows=None):
+    """The gradients of silu(gate) * up at the values kept by asap_moe_swiglu_save,
+    and (h not None) silu(gate) * up at them.  d_h, d_gate, d_up, h [n, c] of one
+    type, d_gate and d_up with one row stride; n_rows as there."""
+    if d_h.dim() != 2:
+        _refuse("d_h [n, c]", d_h=d_h)
+    n, c = d_h.shape
+    more = {} if h is None else {"h": h}
+    ld = _swiglu_kept(n, c, gate_q, gate_s, up_q, up_s, n_rows, d_h=d_h, d_gate=d_gate, d_up=d_up, **more)
+    code = lib().asap_moe_swiglu_backward(_ELEM[d_h.dtype], d_h.data_ptr(), ld["d_h"], gate_q.data_ptr(), up_q.data_ptr(),
+                                          ld["gate_q"], gate_s.data_ptr(), up_s.data_ptr(), ld["gate_s"], n, c,
+                                          _data(n_rows), d_gate.data_ptr(), d_up.data_ptr(), ld["d_gate"], _data(h),
+                                          ld.get("h", 0), _stream(stream))
+    if code:
+        check("asap_moe_swiglu_backward", code)
+
+
+def asap_moe_fp8_dequantize(q, scales, x, perm_dst=None, stream=None, status=None):
+    """e4m3 rows q [n, c] with scales [n, ceil(c / 128)] (asap_moe_fp8_quantize's)
+    back to x of bf16, fp16 or fp32: row t to every row perm_dst[t, j] of x [rows,
+    c], or, without perm_dst, to row t of x [n, c].  status as for
+    asap_moe_permute."""
+    _check_status(status)
+    if q.dim() != 2 or x.dim() != 2 or q.dtype not in (_F8, _U8) or x.dtype not in _ELEM or x.shape[1] != q.shape[1] or \
+            scales.dtype is not _F32 or scales.shape != (q.shape[0], (q.shape[1] + 127) // 128) or \
+            (x.shape[0] != q.shape[0] if perm_dst is None else
+             perm_dst.dim() != 2 or not _dense(perm_dst, torch.int32, (q.shape[0], perm_dst.shape[1]))) or \
+            not _here(q, scales, x, perm_dst, status):
+        _refuse("tensors on the current CUDA device, q [n, c] e4m3, scales [n, ceil(c / 128)] fp32, x [rows, c], perm_dst [n, k] int32 or None", q=q,
+                scales=scales, x=x, **({} if perm_dst is None else {"perm_dst": perm_dst}))
+    n, c = q.shape
+    ldq, lds, ldx = _ld(q), _ld(scales), _ld(x)
+    if not (ldq and lds and ldx) and n and c and x.shape[0]:
+        _refuse("CUDA tensors with contiguous columns", q=q, scales=scales, x=x)
+    k = 1 if perm_dst is None else perm_dst.shape[1]
+    code = lib().asap_moe_fp8_dequantize(_ELEM[x.dtype], q.data_ptr(), ldq, scales.data_ptr(), lds, n, c, _data(perm_dst), k,
+                                         x.data_ptr(), ldx, x.shape[0], _data(status), _stream(stream))
+    if code:
+        check("asap_moe_fp8_dequantize", code)
+
+
 class Mailbox:
     """Owns an asap_moe_mailbox_t (slots that DP-group streams post routed
     micro-batches into and that service rounds on the MoE stream claim on the

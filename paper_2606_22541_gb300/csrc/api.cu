@@ -4,6 +4,7 @@
 #include "../../include/asap_moe.h"
 #include "common.cuh"
 #include "few.h"
+#include "rows.h"
 #include "internal.h"
 #include "gemm_config.h"
 
@@ -1551,6 +1552,213 @@ ASAP_API int asap_moe_fp8_matmul(const void* a, int64_t lda, const float* a_scal
   const cudaError_t e = asap::fp8_matmul_launch(a, lda, b, ldb, args, dev, S(stream), &err);
   if (!err.empty()) return fail(ASAP_ERR_INVALID, err);
   if (e != cudaSuccess) return cuda_fail(e, "product launch");
+  return ASAP_OK;
+}
+
+// ------------------------------------------------------------ plain tensors in training
+namespace {
+
+int elem_bytes(int32_t type) {
+  switch (type) {
+    case ASAP_ELEM_BF16:
+    case ASAP_ELEM_F16: return 2;
+    case ASAP_ELEM_F32: return 4;
+    case ASAP_ELEM_E4M3: return 1;
+    default: return 0;
+  }
+}
+bool on(const void* p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & static_cast<uintptr_t>(bytes - 1)) == 0; }
+
+// Checks what every call on rows of tokens has in common.
+int check_rows(int32_t n, int32_t k, int32_t rows, int32_t cols, const int32_t* perm_dst, const float* w,
+               const uint32_t* status) {
+  if (n < 0 || rows < 0 || cols < 0 || n > kMaxExtent || rows > kMaxExtent || cols > kMaxExtent)
+    return fail(ASAP_ERR_INVALID, "n, rows and cols must be in [0, 2^30]");
+  if (k < 1 || static_cast<long long>(n) * k > INT32_MAX) return fail(ASAP_ERR_INVALID, "k must be at least 1, n * k below 2^31");
+  if (n > 0 && !perm_dst) return fail(ASAP_ERR_INVALID, "NULL tensor");
+  if (!on(perm_dst, 4) || !on(w, 4) || !on(status, 4))
+    return fail(ASAP_ERR_INVALID, "tensors must be aligned to their elements");
+  return ASAP_OK;
+}
+// One matrix of a call: there, aligned, rows not shorter than cols.
+int check_matrix(const void* p, int64_t ld, int32_t rows, int32_t cols, int bytes) {
+  if (rows == 0 || cols == 0) return ASAP_OK;
+  if (!p) return fail(ASAP_ERR_INVALID, "NULL tensor");
+  if (!on(p, bytes)) return fail(ASAP_ERR_INVALID, "tensors must be aligned to their elements");
+  if (ld < cols) return fail(ASAP_ERR_INVALID, "a row stride is shorter than its rows");
+  return ASAP_OK;
+}
+#define ASAP_CHECK(expr)               \
+  do {                                 \
+    const int _r = (expr);             \
+    if (_r != ASAP_OK) return _r;      \
+  } while (0)
+
+asap::RowsArgs rows_args(const int32_t* perm_dst, int32_t n, int32_t k, int32_t rows, int32_t cols, const float* w,
+                         uint32_t* status) {
+  asap::RowsArgs a{};
+  a.perm = perm_dst;
+  a.n = n;
+  a.k = k;
+  a.rows = rows;
+  a.cols = cols;
+  a.w = w;
+  a.status = status;
+  return a;
+}
+
+int check_sort(int32_t n, int32_t k, int32_t n_experts) {
+  if (n < 0 || k < 1 || n > kMaxExtent || static_cast<long long>(n) * k > INT32_MAX)
+    return fail(ASAP_ERR_INVALID, "n must be in [0, 2^30], k at least 1, n * k below 2^31");
+  if (n_experts < 1 || n_experts > asap::kSortMaxExperts)
+    return fail(ASAP_ERR_INVALID, "n_experts must be in [1, " + std::to_string(asap::kSortMaxExperts) + "]");
+  return ASAP_OK;
+}
+
+int check_swiglu(int32_t type, int32_t rows, int32_t cols, const int32_t* n_rows, const void* gate_q, const void* up_q,
+                 int64_t ldq, const float* gate_s, const float* up_s, int64_t lds) {
+  if (elem_bytes(type) < 2) return fail(ASAP_ERR_INVALID, "type must be bf16, fp16 or fp32");
+  if (rows < 0 || cols < 0 || rows > kMaxExtent || cols > kMaxExtent)
+    return fail(ASAP_ERR_INVALID, "rows and cols must be in [0, 2^30]");
+  if (!on(n_rows, 4)) return fail(ASAP_ERR_INVALID, "tensors must be aligned to their elements");
+  const int blocks = asap::ceil_div(cols, 128);
+  ASAP_CHECK(check_matrix(gate_q, ldq, rows, cols, 1));
+  ASAP_CHECK(check_matrix(up_q, ldq, rows, cols, 1));
+  ASAP_CHECK(check_matrix(gate_s, lds, rows, blocks, 4));
+  ASAP_CHECK(check_matrix(up_s, lds, rows, blocks, 4));
+  return ASAP_OK;
+}
+
+asap::SwigluArgs swiglu_args(int32_t rows, int32_t cols, const int32_t* n_rows, const void* gate_q, const void* up_q,
+                             int64_t ldq, const float* gate_s, const float* up_s, int64_t lds) {
+  asap::SwigluArgs a{};
+  a.rows = rows;
+  a.cols = cols;
+  a.n_rows = n_rows;
+  a.gate_q = static_cast<uint8_t*>(const_cast<void*>(gate_q));
+  a.up_q = static_cast<uint8_t*>(const_cast<void*>(up_q));
+  a.ldq = ldq;
+  a.gate_s = const_cast<float*>(gate_s);
+  a.up_s = const_cast<float*>(up_s);
+  a.lds = lds;
+  return a;
+}
+
+}  // namespace
+
+ASAP_API int asap_moe_sort_workspace_size(int32_t n, int32_t k, int32_t n_experts, size_t* bytes) {
+  if (!bytes) return fail(ASAP_ERR_INVALID, "NULL output");
+  ASAP_CHECK(check_sort(n, k, n_experts));
+  *bytes = asap::sort_workspace(static_cast<long long>(n) * k, n_experts);
+  return ASAP_OK;
+}
+
+ASAP_API int asap_moe_sort(const int32_t* idx, int32_t n, int32_t k, int32_t n_experts, int32_t* offsets,
+                           int32_t* perm_dst, int32_t* perm_src, void* ws, size_t ws_bytes, void* stream) {
+  ASAP_CHECK(check_sort(n, k, n_experts));
+  if (!offsets || (n > 0 && (!idx || !perm_dst))) return fail(ASAP_ERR_INVALID, "NULL tensor");
+  if (!on(idx, 4) || !on(offsets, 4) || !on(perm_dst, 4) || !on(perm_src, 4))
+    return fail(ASAP_ERR_INVALID, "tensors must be aligned to their elements");
+  const long long entries = static_cast<long long>(n) * k;
+  const size_t need = asap::sort_workspace(entries, n_experts);
+  if (need > 0 && (!ws || ws_bytes < need || !on(ws, 4)))
+    return fail(ASAP_ERR_WORKSPACE, "workspace of at least " + std::to_string(need) + " bytes, 4-byte aligned");
+  CU_TRY(asap::launch_sort(idx, entries, k, n_experts, offsets, perm_dst, perm_src, ws, S(stream)), "sort launch");
+  return ASAP_OK;
+}
+
+ASAP_API int asap_moe_permute(int32_t type, const void* x, int64_t ldx, int32_t n, int32_t cols, const int32_t* perm_dst,
+                              int32_t k, void* x_perm, int64_t ldp, int32_t rows, uint32_t* status, void* stream) {
+  const int bytes = elem_bytes(type);
+  if (!bytes) return fail(ASAP_ERR_INVALID, "unknown element type");
+  ASAP_CHECK(check_rows(n, k, rows, cols, perm_dst, nullptr, status));
+  ASAP_CHECK(check_matrix(x, ldx, n, cols, bytes));
+  ASAP_CHECK(check_matrix(x_perm, ldp, rows, cols, bytes));
+  if (n == 0 || cols == 0) return ASAP_OK;
+  CU_TRY(asap::launch_permute(bytes, x, ldx, x_perm, ldp, rows_args(perm_dst, n, k, rows, cols, nullptr, status), S(stream)),
+         "permute launch");
+  return ASAP_OK;
+}
+
+ASAP_API int asap_moe_unpermute(int32_t type, const void* y_perm, int64_t ldy, int32_t rows, int32_t cols, const float* w,
+                                const int32_t* perm_dst, int32_t n, int32_t k, void* out, int64_t ldo, uint32_t* status,
+                                void* stream) {
+  const int bytes = elem_bytes(type);
+  if (bytes < 2) return fail(ASAP_ERR_INVALID, "type must be bf16, fp16 or fp32");
+  ASAP_CHECK(check_rows(n, k, rows, cols, perm_dst, w, status));
+  ASAP_CHECK(check_matrix(y_perm, ldy, rows, cols, bytes));
+  ASAP_CHECK(check_matrix(out, ldo, n, cols, bytes));
+  if (n == 0 || cols == 0) return ASAP_OK;
+  CU_TRY(asap::launch_unpermute(type, y_perm, ldy, out, ldo, rows_args(perm_dst, n, k, rows, cols, w, status), S(stream)),
+         "unpermute launch");
+  return ASAP_OK;
+}
+
+ASAP_API int asap_moe_unpermute_backward(int32_t type, const void* d_out, int64_t ldo, const void* y_perm, int64_t ldy,
+                                         const float* w, const int32_t* perm_dst, int32_t n, int32_t k, int32_t cols,
+                                         void* d_y_perm, int64_t ldd, int32_t rows, float* d_w, uint32_t* status,
+                                         void* stream) {
+  const int bytes = elem_bytes(type);
+  if (bytes < 2) return fail(ASAP_ERR_INVALID, "type must be bf16, fp16 or fp32");
+  ASAP_CHECK(check_rows(n, k, rows, cols, perm_dst, w, status));
+  ASAP_CHECK(check_matrix(d_out, ldo, n, cols, bytes));
+  if (!on(d_w, 4)) return fail(ASAP_ERR_INVALID, "tensors must be aligned to their elements");
+  if (d_w) ASAP_CHECK(check_matrix(y_perm, ldy, rows, cols, bytes));
+  if (d_y_perm) ASAP_CHECK(check_matrix(d_y_perm, ldd, rows, cols, bytes));
+  if (n == 0 || (!d_w && (!d_y_perm || cols == 0))) return ASAP_OK;
+  CU_TRY(asap::launch_unpermute_backward(type, d_out, ldo, d_w ? y_perm : nullptr, ldy, d_y_perm, ldd, d_w,
+                                         rows_args(perm_dst, n, k, rows, cols, w, status), S(stream)),
+         "unpermute backward launch");
+  return ASAP_OK;
+}
+
+ASAP_API int asap_moe_fp8_dequantize(int32_t type, const void* q, int64_t ldq, const float* scales, int64_t lds, int32_t n,
+                                     int32_t cols, const int32_t* perm_dst, int32_t k, void* x, int64_t ldx, int32_t rows,
+                                     uint32_t* status, void* stream) {
+  const int bytes = elem_bytes(type);
+  if (bytes < 2) return fail(ASAP_ERR_INVALID, "type must be bf16, fp16 or fp32");
+  if (!perm_dst && (k != 1 || rows != n))
+    return fail(ASAP_ERR_INVALID, "without perm_dst k must be 1 and rows n");
+  ASAP_CHECK(check_rows(n, k, rows, cols, perm_dst ? perm_dst : reinterpret_cast<const int32_t*>(16), nullptr, status));
+  ASAP_CHECK(check_matrix(q, ldq, n, cols, 1));
+  ASAP_CHECK(check_matrix(scales, lds, n, asap::ceil_div(cols, 128), 4));
+  ASAP_CHECK(check_matrix(x, ldx, rows, cols, bytes));
+  if (n == 0 || cols == 0) return ASAP_OK;
+  CU_TRY(asap::launch_dequantize(type, q, ldq, scales, lds, x, ldx,
+                                 rows_args(perm_dst, n, k, rows, cols, nullptr, status), S(stream)),
+         "dequantise launch");
+  return ASAP_OK;
+}
+
+ASAP_API int asap_moe_swiglu_save(int32_t type, const void* gate, const void* up, int64_t ld, int32_t rows, int32_t cols,
+                                  const int32_t* n_rows, void* h, int64_t ldh, void* gate_q, void* up_q, int64_t ldq,
+                                  float* gate_s, float* up_s, int64_t lds, void* stream) {
+  ASAP_CHECK(check_swiglu(type, rows, cols, n_rows, gate_q, up_q, ldq, gate_s, up_s, lds));
+  const int bytes = elem_bytes(type);
+  ASAP_CHECK(check_matrix(gate, ld, rows, cols, bytes));
+  ASAP_CHECK(check_matrix(up, ld, rows, cols, bytes));
+  ASAP_CHECK(check_matrix(h, ldh, rows, cols, bytes));
+  if (rows == 0 || cols == 0) return ASAP_OK;
+  CU_TRY(asap::launch_swiglu_save(type, gate, up, ld, h, ldh,
+                                  swiglu_args(rows, cols, n_rows, gate_q, up_q, ldq, gate_s, up_s, lds), S(stream)),
+         "SwiGLU launch");
+  return ASAP_OK;
+}
+
+ASAP_API int asap_moe_swiglu_backward(int32_t type, const void* d_h, int64_t ldd, const void* gate_q, const void* up_q,
+                                      int64_t ldq, const float* gate_s, const float* up_s, int64_t lds, int32_t rows,
+                                      int32_t cols, const int32_t* n_rows, void* d_gate, void* d_up, int64_t ldg, void* h,
+                                      int64_t ldh, void* stream) {
+  ASAP_CHECK(check_swiglu(type, rows, cols, n_rows, gate_q, up_q, ldq, gate_s, up_s, lds));
+  const int bytes = elem_bytes(type);
+  ASAP_CHECK(check_matrix(d_h, ldd, rows, cols, bytes));
+  ASAP_CHECK(check_matrix(d_gate, ldg, rows, cols, bytes));
+  ASAP_CHECK(check_matrix(d_up, ldg, rows, cols, bytes));
+  if (h) ASAP_CHECK(check_matrix(h, ldh, rows, cols, bytes));
+  if (rows == 0 || cols == 0) return ASAP_OK;
+  CU_TRY(asap::launch_swiglu_backward(type, d_h, ldd, d_gate, d_up, ldg, h, ldh,
+                                      swiglu_args(rows, cols, n_rows, gate_q, up_q, ldq, gate_s, up_s, lds), S(stream)),
+         "SwiGLU backward launch");
   return ASAP_OK;
 }
 

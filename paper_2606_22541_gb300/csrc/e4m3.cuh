@@ -5,6 +5,8 @@
 #include <cuda_fp8.h>
 #include <stdint.h>
 
+#include "f32x2.cuh"
+
 namespace asap {
 
 // Scale of a group and what its quotients need: s = amax times the fp32
@@ -40,6 +42,25 @@ __device__ __forceinline__ uint32_t e4m3x4(float a, float b, float c, float d) {
 }
 __device__ __forceinline__ uint32_t e4m3x4(const GroupScale& g, float a, float b, float c, float d) {
   return e4m3x4(g(a), g(b), g(c), g(d));
+}
+
+// Sixteen values of a group: its quotients two at a time.
+__device__ __forceinline__ void e4m3x16(const GroupScale& gs, const float (&f)[16], uint32_t (&w)[4]) {
+  const uint64_t inv = pair(gs.inv, gs.inv), neg = pair(-gs.scaled, -gs.scaled);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    uint64_t v0 = pair(f[4 * j], f[4 * j + 1]), v1 = pair(f[4 * j + 2], f[4 * j + 3]);
+    if (gs.up != 1.0f) {
+      const uint64_t by = pair(gs.up, gs.up);
+      v0 = mul2(v0, by);
+      v1 = mul2(v1, by);
+    }
+    uint64_t q0 = mul2(v0, inv), q1 = mul2(v1, inv);
+    q0 = fma2(remainder2(q0, neg, v0), inv, q0);
+    q1 = fma2(remainder2(q1, neg, v1), inv, q1);
+    const float2 a = unpair(q0), b = unpair(q1);
+    w[j] = e4m3x4(a.x, a.y, b.x, b.y);
+  }
 }
 
 }  // namespace asap

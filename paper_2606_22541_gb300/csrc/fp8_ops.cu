@@ -2,6 +2,7 @@
 // matrix product with a scale per block of 128.
 #include "common.cuh"
 #include "e4m3.cuh"
+#include "f32x2.cuh"
 #include "internal.h"
 #include "pair.cuh"
 
@@ -49,33 +50,6 @@ __device__ __forceinline__ void load8(const uint16_t* p, int left, uint32_t* v) 
   }
 }
 
-__device__ __forceinline__ uint64_t pair(float lo, float hi) {
-  uint64_t r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
-  return r;
-}
-__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
-  uint64_t r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
-  uint64_t r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-  return r;
-}
-// a b + c rounded down, for the remainder of a quotient: that of an exact zero is -0, which leaves a quotient of -0 as it
-// is (+0 would not); other remainders are exact, or far below what they correct.
-__device__ __forceinline__ uint64_t remainder2(uint64_t a, uint64_t b, uint64_t c) {
-  uint64_t r;
-  asm("fma.rm.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-  return r;
-}
-__device__ __forceinline__ float2 unpair(uint64_t p) {
-  float2 r;
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(p));
-  return r;
-}
 // The larger magnitude of each half (a NaN loses).
 __device__ __forceinline__ uint32_t max_abs2(uint32_t a, uint32_t b) {
   const __nv_bfloat162 m = __hmax2(__habs2(*reinterpret_cast<const __nv_bfloat162*>(&a)),
@@ -158,22 +132,8 @@ __global__ void __launch_bounds__(kQuantThreads, SWIGLU ? 6 : 8)
     }
     const GroupScale gs(am);
     if (in) {
-      const uint64_t inv = pair(gs.inv, gs.inv), neg = pair(-gs.scaled, -gs.scaled);
       uint32_t w[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        uint64_t v0 = pair(f[4 * j], f[4 * j + 1]), v1 = pair(f[4 * j + 2], f[4 * j + 3]);
-        if (gs.up != 1.0f) {
-          const uint64_t by = pair(gs.up, gs.up);
-          v0 = mul2(v0, by);
-          v1 = mul2(v1, by);
-        }
-        uint64_t q0 = mul2(v0, inv), q1 = mul2(v1, inv);  // GroupScale's quotient, two at a time
-        q0 = fma2(remainder2(q0, neg, v0), inv, q0);
-        q1 = fma2(remainder2(q1, neg, v1), inv, q1);
-        const float2 a = unpair(q0), b = unpair(q1);
-        w[j] = e4m3x4(a.x, a.y, b.x, b.y);
-      }
+      e4m3x16(gs, f, w);
       uint8_t* out = q + row * ldq + c;
       if (wide_q && cols - c >= 16) {
         *reinterpret_cast<uint4*>(out) = make_uint4(w[0], w[1], w[2], w[3]);
