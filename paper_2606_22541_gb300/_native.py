@@ -126,6 +126,10 @@ def fast():
                 L.asap_moe_fp8_quantize, L.asap_moe_fp8_swiglu_quantize, L.asap_moe_fp8_matmul)),
                 torch.bfloat16, torch.float32, torch.float8_e4m3fn, torch.uint8,
                 torch.cuda.current_device, torch._C._cuda_getCurrentRawStream)
+            _marshal.bind_rows(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
+                L.asap_moe_sort, L.asap_moe_permute, L.asap_moe_unpermute, L.asap_moe_unpermute_backward,
+                L.asap_moe_swiglu_save, L.asap_moe_swiglu_backward, L.asap_moe_fp8_dequantize)),
+                torch.float16, torch.int32)
             _fast = _marshal
     return _fast
 

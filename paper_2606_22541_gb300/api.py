@@ -422,6 +422,15 @@ def asap_moe_sort(idx, n_experts, offsets, perm_dst, ws=None, perm_src=None, str
     expert takes it) to offsets [n_experts + 1], perm_dst [n, k] (the entry's
     row, -1: none) and, if given, perm_src [n * k] (row -> token), all int32 and
     contiguous.  ws: sort_workspace(n, k, n_experts), None where its size is 0."""
+    f = fast()
+    code = f.sort(idx, n_experts, offsets, perm_dst, ws, perm_src, stream) if f else None
+    if code is None:
+        code = _sort(idx, n_experts, offsets, perm_dst, ws, perm_src, stream)
+    if code:
+        check("asap_moe_sort", code)
+
+
+def _sort(idx, n_experts, offsets, perm_dst, ws, perm_src, stream):
     shape = idx.shape
     if len(shape) != 2 or not _dense(idx, torch.int32, shape) or not _dense(perm_dst, torch.int32, shape) or \
             not _dense(offsets, torch.int32, (n_experts + 1,)) or \
@@ -431,10 +440,8 @@ def asap_moe_sort(idx, n_experts, offsets, perm_dst, ws=None, perm_src=None, str
                 "and a workspace", idx=idx, offsets=offsets, perm_dst=perm_dst,
                 **{k: t for k, t in (("perm_src", perm_src), ("ws", ws)) if t is not None})
     p, nb = (None, 0) if ws is None else (ws.data_ptr(), ws.numel() * ws.element_size())
-    code = lib().asap_moe_sort(idx.data_ptr(), shape[0], shape[1], n_experts, offsets.data_ptr(), perm_dst.data_ptr(),
+    return lib().asap_moe_sort(idx.data_ptr(), shape[0], shape[1], n_experts, offsets.data_ptr(), perm_dst.data_ptr(),
                                _data(perm_src), p, nb, _stream(stream))
-    if code:
-        check("asap_moe_sort", code)
 
 
 def _check_status(status):
@@ -448,6 +455,15 @@ def asap_moe_permute(x, perm_dst, x_perm, stream=None, status=None):
     strides.  Rows of x_perm that nothing names stay as they were.  status: None
     or a one-element int32 CUDA tensor that gets bit 2 for a row that does not
     exist (other than -1)."""
+    f = fast()
+    code = f.permute(x, perm_dst, x_perm, stream, status) if f else None
+    if code is None:
+        code = _permute(x, perm_dst, x_perm, stream, status)
+    if code:
+        check("asap_moe_permute", code)
+
+
+def _permute(x, perm_dst, x_perm, stream, status):
     _check_status(status)
     if x.dim() != 2 or x_perm.dim() != 2 or perm_dst.dim() != 2 or x.dtype not in _BYTES or x_perm.dtype is not x.dtype or \
             x_perm.shape[1] != x.shape[1] or not _dense(perm_dst, torch.int32, (x.shape[0], perm_dst.shape[1])) or \
@@ -458,10 +474,8 @@ def asap_moe_permute(x, perm_dst, x_perm, stream=None, status=None):
     rows, ld, ldp = x_perm.shape[0], _ld(x), _ld(x_perm)
     if not (ld and ldp) and n and c and rows:
         _refuse("CUDA tensors with contiguous columns", x=x, x_perm=x_perm)
-    code = lib().asap_moe_permute(_BYTES[x.dtype], x.data_ptr(), ld, n, c, perm_dst.data_ptr(), perm_dst.shape[1],
+    return lib().asap_moe_permute(_BYTES[x.dtype], x.data_ptr(), ld, n, c, perm_dst.data_ptr(), perm_dst.shape[1],
                                   x_perm.data_ptr(), ldp, rows, _data(status), _stream(stream))
-    if code:
-        check("asap_moe_permute", code)
 
 
 def asap_moe_unpermute(y_perm, w, perm_dst, out, stream=None, status=None):
@@ -469,6 +483,15 @@ def asap_moe_unpermute(y_perm, w, perm_dst, out, stream=None, status=None):
     row: y_perm [rows, c], out [n, c] of one type (bf16, fp16 or fp32), w [n, k]
     fp32 or None (ones: the gradient of asap_moe_permute), perm_dst [n, k] int32,
     both contiguous.  status as for asap_moe_permute."""
+    f = fast()
+    code = f.unpermute(y_perm, w, perm_dst, out, stream, status) if f else None
+    if code is None:
+        code = _unpermute(y_perm, w, perm_dst, out, stream, status)
+    if code:
+        check("asap_moe_unpermute", code)
+
+
+def _unpermute(y_perm, w, perm_dst, out, stream, status):
     _check_status(status)
     if y_perm.dim() != 2 or out.dim() != 2 or perm_dst.dim() != 2 or y_perm.dtype not in _ELEM or \
             out.dtype is not y_perm.dtype or y_perm.shape[1] != out.shape[1] or \
@@ -480,10 +503,8 @@ def asap_moe_unpermute(y_perm, w, perm_dst, out, stream=None, status=None):
     rows, ldy, ldo = y_perm.shape[0], _ld(y_perm), _ld(out)
     if not (ldy and ldo) and n and c and rows:
         _refuse("CUDA tensors with contiguous columns", y_perm=y_perm, out=out)
-    code = lib().asap_moe_unpermute(_ELEM[out.dtype], y_perm.data_ptr(), ldy, rows, c, _data(w), perm_dst.data_ptr(), n,
+    return lib().asap_moe_unpermute(_ELEM[out.dtype], y_perm.data_ptr(), ldy, rows, c, _data(w), perm_dst.data_ptr(), n,
                                     perm_dst.shape[1], out.data_ptr(), ldo, _data(status), _stream(stream))
-    if code:
-        check("asap_moe_unpermute", code)
 
 
 def asap_moe_unpermute_backward(d_out, y_perm, w, perm_dst, d_y_perm, d_w, stream=None, status=None):
@@ -492,6 +513,15 @@ def asap_moe_unpermute_backward(d_out, y_perm, w, perm_dst, d_y_perm, d_w, strea
     has no row).  d_out [n, c], y_perm and d_y_perm [rows, c] of one type, w and
     d_w [n, k] fp32.  w None: ones; d_y_perm or d_w None: not wanted; y_perm may be
     None where d_w is."""
+    f = fast()
+    code = f.unpermute_backward(d_out, y_perm, w, perm_dst, d_y_perm, d_w, stream, status) if f else None
+    if code is None:
+        code = _unpermute_backward(d_out, y_perm, w, perm_dst, d_y_perm, d_w, stream, status)
+    if code:
+        check("asap_moe_unpermute_backward", code)
+
+
+def _unpermute_backward(d_out, y_perm, w, perm_dst, d_y_perm, d_w, stream, status):
     _check_status(status)
     y = {k: t for k, t in (("y_perm", y_perm), ("d_y_perm", d_y_perm)) if t is not None}
     rows = next(iter(y.values())).shape[0] if y else 0
@@ -508,11 +538,9 @@ def asap_moe_unpermute_backward(d_out, y_perm, w, perm_dst, d_y_perm, d_w, strea
     ldo, lds = _ld(d_out), {k: _ld(t) for k, t in y.items()}
     if not (ldo and all(lds.values())) and n and c and rows:
         _refuse("CUDA tensors with contiguous columns", d_out=d_out, **y)
-    code = lib().asap_moe_unpermute_backward(_ELEM[d_out.dtype], d_out.data_ptr(), ldo, _data(y_perm), lds.get("y_perm", 0),
+    return lib().asap_moe_unpermute_backward(_ELEM[d_out.dtype], d_out.data_ptr(), ldo, _data(y_perm), lds.get("y_perm", 0),
                                              _data(w), perm_dst.data_ptr(), n, perm_dst.shape[1], c, _data(d_y_perm),
                                              lds.get("d_y_perm", 0), rows, _data(d_w), _data(status), _stream(stream))
-    if code:
-        check("asap_moe_unpermute_backward", code)
 
 
 def _swiglu_kept(rows, cols, gate_q, gate_s, up_q, up_s, n_rows, **others):
@@ -542,32 +570,46 @@ def asap_moe_swiglu_save(gate, up, h, gate_q, gate_s, up_q, up_s, stream=None, n
     128)] fp32; gate and up have one row stride each time (the halves of a
     product's rows).  n_rows: None or a one-element int32 CUDA tensor, the rows
     that are read and written (offsets[-1:] of asap_moe_sort)."""
+    f = fast()
+    code = f.swiglu_save(gate, up, h, gate_q, gate_s, up_q, up_s, stream, n_rows) if f else None
+    if code is None:
+        code = _swiglu_save(gate, up, h, gate_q, gate_s, up_q, up_s, stream, n_rows)
+    if code:
+        check("asap_moe_swiglu_save", code)
+
+
+def _swiglu_save(gate, up, h, gate_q, gate_s, up_q, up_s, stream, n_rows):
     if gate.dim() != 2:
         _refuse("gate [n, c]", gate=gate)
     n, c = gate.shape
     ld = _swiglu_kept(n, c, gate_q, gate_s, up_q, up_s, n_rows, gate=gate, up=up, h=h)
-    code = lib().asap_moe_swiglu_save(_ELEM[gate.dtype], gate.data_ptr(), up.data_ptr(), ld["gate"], n, c, _data(n_rows),
+    return lib().asap_moe_swiglu_save(_ELEM[gate.dtype], gate.data_ptr(), up.data_ptr(), ld["gate"], n, c, _data(n_rows),
                                       h.data_ptr(), ld["h"], gate_q.data_ptr(), up_q.data_ptr(), ld["gate_q"],
                                       gate_s.data_ptr(), up_s.data_ptr(), ld["gate_s"], _stream(stream))
-    if code:
-        check("asap_moe_swiglu_save", code)
 
 
 def asap_moe_swiglu_backward(d_h, gate_q, gate_s, up_q, up_s, d_gate, d_up, h=None, stream=None, n_rows=None):
     """The gradients of silu(gate) * up at the values kept by asap_moe_swiglu_save,
     and (h not None) silu(gate) * up at them.  d_h, d_gate, d_up, h [n, c] of one
     type, d_gate and d_up with one row stride; n_rows as there."""
+    f = fast()
+    code = f.swiglu_backward(d_h, gate_q, gate_s, up_q, up_s, d_gate, d_up, h, stream, n_rows) if f else None
+    if code is None:
+        code = _swiglu_backward(d_h, gate_q, gate_s, up_q, up_s, d_gate, d_up, h, stream, n_rows)
+    if code:
+        check("asap_moe_swiglu_backward", code)
+
+
+def _swiglu_backward(d_h, gate_q, gate_s, up_q, up_s, d_gate, d_up, h, stream, n_rows):
     if d_h.dim() != 2:
         _refuse("d_h [n, c]", d_h=d_h)
     n, c = d_h.shape
     more = {} if h is None else {"h": h}
     ld = _swiglu_kept(n, c, gate_q, gate_s, up_q, up_s, n_rows, d_h=d_h, d_gate=d_gate, d_up=d_up, **more)
-    code = lib().asap_moe_swiglu_backward(_ELEM[d_h.dtype], d_h.data_ptr(), ld["d_h"], gate_q.data_ptr(), up_q.data_ptr(),
+    return lib().asap_moe_swiglu_backward(_ELEM[d_h.dtype], d_h.data_ptr(), ld["d_h"], gate_q.data_ptr(), up_q.data_ptr(),
                                           ld["gate_q"], gate_s.data_ptr(), up_s.data_ptr(), ld["gate_s"], n, c,
                                           _data(n_rows), d_gate.data_ptr(), d_up.data_ptr(), ld["d_gate"], _data(h),
                                           ld.get("h", 0), _stream(stream))
-    if code:
-        check("asap_moe_swiglu_backward", code)
 
 
 def asap_moe_fp8_dequantize(q, scales, x, perm_dst=None, stream=None, status=None):
@@ -575,6 +617,15 @@ def asap_moe_fp8_dequantize(q, scales, x, perm_dst=None, stream=None, status=Non
     back to x of bf16, fp16 or fp32: row t to every row perm_dst[t, j] of x [rows,
     c], or, without perm_dst, to row t of x [n, c].  status as for
     asap_moe_permute."""
+    f = fast()
+    code = f.dequantize(q, scales, x, perm_dst, stream, status) if f else None
+    if code is None:
+        code = _dequantize(q, scales, x, perm_dst, stream, status)
+    if code:
+        check("asap_moe_fp8_dequantize", code)
+
+
+def _dequantize(q, scales, x, perm_dst, stream, status):
     _check_status(status)
     if q.dim() != 2 or x.dim() != 2 or q.dtype not in (_F8, _U8) or x.dtype not in _ELEM or x.shape[1] != q.shape[1] or \
             scales.dtype is not _F32 or scales.shape != (q.shape[0], (q.shape[1] + 127) // 128) or \
@@ -588,10 +639,8 @@ def asap_moe_fp8_dequantize(q, scales, x, perm_dst=None, stream=None, status=Non
     if not (ldq and lds and ldx) and n and c and x.shape[0]:
         _refuse("CUDA tensors with contiguous columns", q=q, scales=scales, x=x)
     k = 1 if perm_dst is None else perm_dst.shape[1]
-    code = lib().asap_moe_fp8_dequantize(_ELEM[x.dtype], q.data_ptr(), ldq, scales.data_ptr(), lds, n, c, _data(perm_dst), k,
+    return lib().asap_moe_fp8_dequantize(_ELEM[x.dtype], q.data_ptr(), ldq, scales.data_ptr(), lds, n, c, _data(perm_dst), k,
                                          x.data_ptr(), ldx, x.shape[0], _data(status), _stream(stream))
-    if code:
-        check("asap_moe_fp8_dequantize", code)
 
 
 class Mailbox:

@@ -129,3 +129,105 @@ def test_the_binding_refuses_host_tensors_and_misfits():
                  lambda: api.asap_moe_permute(x, perm, y, status=torch.zeros(1, **i32))):
         with pytest.raises(ValueError):
             call()
+
+
+# ------------------------------------------------------------------ the compiled marshalling
+
+class T:
+    """What the compiled marshalling looks at of a tensor."""
+
+    def __init__(self, shape, dtype, ptr, strides=None, device=3):
+        self.shape, self.dtype, self._ptr, self._device = tuple(shape), dtype, ptr, device
+        self._strides = strides or tuple([shape[1], 1] if len(shape) == 2 else [1])
+
+    def get_device(self):
+        return self._device
+
+    def stride(self):
+        return self._strides
+
+    def data_ptr(self):
+        return self._ptr
+
+
+BF16, F16, F32, F8, U8, I32 = (object() for _ in range(6))
+NAMES = ["sort", "permute", "unpermute", "unpermute_backward", "swiglu_save", "swiglu_backward", "dequantize"]
+
+
+@pytest.fixture
+def calls():
+    import ctypes
+    build_mod.build()
+    marshal = pytest.importorskip("paper_2606_22541_gb300._marshal")
+    seen = []
+    none = [ctypes.CFUNCTYPE(ctypes.c_int32)(lambda: 0) for _ in range(3)]
+    entry = ["asap_moe_fp8_dequantize" if n == "dequantize" else "asap_moe_" + n for n in NAMES]
+    fns = [ctypes.CFUNCTYPE(ctypes.c_int32, *_native.SIGNATURES[e])(lambda *a, n=n: seen.append((n,) + a) or 7)
+           for n, e in zip(NAMES, entry)]
+    address = lambda f: ctypes.cast(f, ctypes.c_void_p).value
+    marshal.bind(*map(address, none), BF16, F32, F8, U8, lambda: 3, lambda d: 0x90 + d)
+    marshal.bind_rows(*map(address, fns), F16, I32)
+    yield marshal, seen
+    _native._fast = None  # bound to the library again by its next user
+
+
+def arguments():
+    perm, w = T((6, 2), I32, 0x10), T((6, 2), F32, 0x20)
+    x, y = T((6, 100), F16, 0x30, (104, 1)), T((12, 100), F16, 0x40, (112, 1))
+    q, s = T((12, 300), F8, 0x50, (304, 1)), T((12, 3), F32, 0x60, (4, 1))
+    q2, s2 = T((12, 300), U8, 0x51, (304, 1)), T((12, 3), F32, 0x61, (4, 1))
+    g, u, h = T((12, 300), BF16, 0x70, (600, 1)), T((12, 300), BF16, 0x71, (600, 1)), T((12, 300), BF16, 0x72)
+    count = T((1,), I32, 0x80)
+    return dict(
+        sort=[perm, 8, T((9,), I32, 0xA0), T((6, 2), I32, 0xB0), T((512,), U8, 0xC0), T((12,), I32, 0xD0), None],
+        permute=[x, perm, y, None, None], unpermute=[y, w, perm, x, None, None],
+        unpermute_backward=[x, y, w, perm, T((12, 100), F16, 0x41), T((6, 2), F32, 0x21), None, None],
+        swiglu_save=[g, u, h, q, s, q2, s2, None, count], swiglu_backward=[h, q, s, q2, s2, g, u, None, None, None],
+        dequantize=[T((6, 300), F8, 0x52), T((6, 3), F32, 0x62), T((12, 300), F32, 0x73), perm, None, None])
+
+
+def test_marshalled(calls):
+    marshal, seen = calls
+    want = dict(
+        sort=(0x10, 6, 2, 8, 0xA0, 0xB0, 0xD0, 0xC0, 512, 0x93),
+        permute=(1, 0x30, 104, 6, 100, 0x10, 2, 0x40, 112, 12, None, 0x93),
+        unpermute=(1, 0x40, 112, 12, 100, 0x20, 0x10, 6, 2, 0x30, 104, None, 0x93),
+        unpermute_backward=(1, 0x30, 104, 0x40, 112, 0x20, 0x10, 6, 2, 100, 0x41, 100, 12, 0x21, None, 0x93),
+        swiglu_save=(0, 0x70, 0x71, 600, 12, 300, 0x80, 0x72, 300, 0x50, 0x51, 304, 0x60, 0x61, 4, 0x93),
+        swiglu_backward=(0, 0x72, 300, 0x50, 0x51, 304, 0x60, 0x61, 4, 12, 300, None, 0x70, 0x71, 600, None, 0, 0x93),
+        dequantize=(2, 0x52, 300, 0x62, 3, 6, 300, 0x10, 2, 0x73, 300, 12, None, 0x93))
+    for name in NAMES:
+        assert getattr(marshal, name)(*arguments()[name]) == 7
+        assert seen.pop() == (name,) + want[name]
+    a = arguments()
+    a["sort"][4] = a["sort"][5] = None
+    assert marshal.sort(*a["sort"]) == 7 and seen.pop()[7:10] == (None, None, 0)
+    a["unpermute"][1] = None
+    assert marshal.unpermute(*a["unpermute"]) == 7 and seen.pop()[6] is None
+    a["dequantize"][3], a["dequantize"][2] = None, T((6, 300), BF16, 1)
+    assert marshal.dequantize(*a["dequantize"]) == 7 and seen.pop()[8:10] == (None, 1)
+    a["permute"][0], a["permute"][2] = T((6, 100), U8, 1), T((12, 100), U8, 1)
+    assert marshal.permute(*a["permute"]) == 7 and seen.pop()[1] == 3
+
+
+@pytest.mark.parametrize("name", NAMES)
+def test_what_does_not_fit_is_left_to_the_checks(calls, name):
+    """Every tensor in turn on another device, of another type, shape or stride, or no tensor at all."""
+    marshal, seen = calls
+    good = arguments()[name]
+    for i, t in enumerate(good):
+        if not isinstance(t, T):
+            continue
+        two = len(t.shape) == 2
+        others = [T(t.shape, t.dtype, 1, t._strides, device=2), T(t.shape, t.dtype, 1, t._strides, device=-1),
+                  T(t.shape, object(), 1, t._strides), T(t.shape + (1,), t.dtype, 1, t._strides + (1,)), 5]
+        if two:
+            if not (t.dtype is I32 and name in ("permute", "dequantize")):   # (any number of places a token)
+                others.append(T((t.shape[0], t.shape[1] + 129), t.dtype, 1))
+            others += [T((0, t.shape[1]), t.dtype, 1), T(t.shape, t.dtype, 1, (t._strides[0], 2))]
+        if not (name == "sort" and i == 4):   # (a workspace of any length)
+            others += [T((t.shape[0] + 1,) + t.shape[1:], t.dtype, 1)] if not two or t.dtype is I32 else []
+        for o in others:
+            assert getattr(marshal, name)(*good[:i], o, *good[i + 1:]) is None, (i, vars(o) if isinstance(o, T) else o)
+    assert getattr(marshal, name)(*good[:-1]) is None and getattr(marshal, name)() is None
+    assert not seen
