@@ -44,11 +44,12 @@ __device__ __forceinline__ uint32_t e4m3x4(const GroupScale& g, float a, float b
   return e4m3x4(g(a), g(b), g(c), g(d));
 }
 
-// Sixteen values of a group: its quotients two at a time.
-__device__ __forceinline__ void e4m3x16(const GroupScale& gs, const float (&f)[16], uint32_t (&w)[4]) {
+// Eight (or sixteen) values of a group: its quotients two at a time.
+template <int N>
+__device__ __forceinline__ void e4m3_pairs(const GroupScale& gs, const float (&f)[N], uint32_t (&w)[N / 4]) {
   const uint64_t inv = pair(gs.inv, gs.inv), neg = pair(-gs.scaled, -gs.scaled);
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
+  for (int j = 0; j < N / 4; ++j) {
     uint64_t v0 = pair(f[4 * j], f[4 * j + 1]), v1 = pair(f[4 * j + 2], f[4 * j + 3]);
     if (gs.up != 1.0f) {
       const uint64_t by = pair(gs.up, gs.up);

@@ -133,7 +133,7 @@ __global__ void __launch_bounds__(kQuantThreads, SWIGLU ? 6 : 8)
     const GroupScale gs(am);
     if (in) {
       uint32_t w[4];
-      e4m3x16(gs, f, w);
+      e4m3_pairs(gs, f, w);
       uint8_t* out = q + row * ldq + c;
       if (wide_q && cols - c >= 16) {
         *reinterpret_cast<uint4*>(out) = make_uint4(w[0], w[1], w[2], w[3]);

@@ -17,69 +17,122 @@ namespace {
 
 constexpr unsigned kFull = 0xffffffffu;
 constexpr int kThreads = 256;
-constexpr int kTeam = 8;  // lanes of a group of 128 columns, 16 columns each
-constexpr int kTeams = kThreads / kTeam;
+// Both kernels stream: 8 bytes a column forward (bf16), 10 backward, which the copy rate would move in 79.6 and 99.4 us for
+// 32768 x 2048; they take 84 and 100.
+// The forward pass has the arithmetic to hide as well (two scales, two quotients, a sigmoid), so a lane has 16 columns, over
+// which the maximum's exchange and the scales are spread, and four CTAs an SM (3: 93 us); with 8 columns a lane it took 103
+// to 113, and 95 with lanes of 16 neighbouring columns, whose accesses are half as wide as they look.  Backward there is little,
+// so a lane has one 16-byte chunk and its next group's loads on their way (118 us with 16 columns and no loads ahead; 106
+// with the e4m3 values decoded before the next loads are out, which takes the registers).
+// Grids of a few waves' CTAs, so that the SMs' ends are level: forward 4 to 50 CTAs for each SM make no difference, backward 10,
+// 20, 40 and all: 112, 104, 100, 110 us.
+constexpr int kSaveTeam = 8, kSaveCtas = 4, kSaveGrid = 16;  // lanes of a group, CTAs an SM, CTAs of the grid for each SM
+constexpr int kGradCtas = 5, kGradGrid = 40;
 
-// 1 / (1 + e^-g).  fp32 results take expf and a division; 16-bit ones, whose
-// rounding is 2^14 times coarser, the fast exponential and reciprocal (within
-// 2 + 1.16 |g| and 2 units of 2^-23 by CUDA's documentation; 0 where e^-g passes
-// 2^126, as it is there to 38 digits).
+// 1 / (1 + e^-g) of two columns.  fp32 results take expf and a division; 16-bit ones, whose rounding is 2^14 times
+// coarser, the fast exponential and reciprocal (relative 2^-22 and 2^-23 by their documentation, and |g| 2^-23 from the
+// exponent's own rounding; 0 where e^-g passes 2^126, as it is there to 37 digits).
 template <typename T>
-__device__ __forceinline__ float sigmoid(float g) {
-  if constexpr (sizeof(T) == 4)
-    return 1.0f / (1.0f + expf(-g));
-  else
-    return __fdividef(1.0f, 1.0f + __expf(-g));
+__device__ __forceinline__ uint64_t sigmoid2(uint64_t g) {
+  if constexpr (sizeof(T) == 4) {
+    const float2 v = unpair(g);
+    return pair(1.0f / (1.0f + expf(-v.x)), 1.0f / (1.0f + expf(-v.y)));
+  } else {
+    constexpr float kLog2E = 1.4426950408889634f;
+    float2 e = unpair(mul2(g, pair(-kLog2E, -kLog2E)));
+    asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(e.x));
+    asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(e.y));
+    e.x += 1.0f;
+    e.y += 1.0f;
+    asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(e.x));
+    asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(e.y));
+    return pair(e.x, e.y);
+  }
 }
 
-// 16 columns of a lane, W per access.
-template <typename T, int W>
-__device__ __forceinline__ void load16(const T* p, int left, float (&f)[16]) {
+// A lane's kCols columns of a group, as kChunks chunks of V = 16 bytes (or what W columns an access make of it): chunk i
+// of lane l starts at column i kTeam V + l V, so that a team's accesses are contiguous.
+template <typename T, int W, int kTeam>
+struct Lane {
+  static constexpr int kCols = 128 / kTeam, V = 16 / static_cast<int>(sizeof(T)), kChunks = kCols / V;
+  static constexpr int A = W < V ? W : V, kParts = V / A;
+  Cols<T, A> c[kChunks][kParts];
+  __device__ static __forceinline__ int column(int lane, int i) { return (i * kTeam + lane) * V; }
+  // p: the group's first column, left: columns from there
+  __device__ __forceinline__ void load(const T* p, int left, int lane) {
 #pragma unroll
-  for (int i = 0; i < 16; i += W) {
-    Cols<T, W> c;
-    c.load(p + i, left - i);
-    float v[W];
-    c.to(v);
+    for (int i = 0; i < kChunks; ++i)
 #pragma unroll
-    for (int j = 0; j < W; ++j) f[i + j] = v[j];
+      for (int j = 0; j < kParts; ++j) c[i][j].load(p + column(lane, i) + j * A, left - column(lane, i) - j * A);
   }
-}
-template <typename T, int W>
-__device__ __forceinline__ void store16(T* p, int left, const float (&f)[16]) {
+  __device__ __forceinline__ void to(float (&f)[kCols]) const {
 #pragma unroll
-  for (int i = 0; i < 16; i += W) {
-    float v[W];
+    for (int i = 0; i < kChunks; ++i)
 #pragma unroll
-    for (int j = 0; j < W; ++j) v[j] = f[i + j];
-    Cols<T, W> c;
-    c.from(v);
-    if (left > i) c.store(p + i, left - i);
+      for (int j = 0; j < kParts; ++j) {
+        float v[A];
+        c[i][j].to(v);
+#pragma unroll
+        for (int k = 0; k < A; ++k) f[i * V + j * A + k] = v[k];
+      }
   }
-}
-__device__ __forceinline__ void store_q(uint8_t* p, bool wide, int left, const uint32_t (&w)[4]) {
-  if (wide && left >= 16) {
-    *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
-    return;
+  __device__ static __forceinline__ void store(T* p, int left, int lane, const float (&f)[kCols]) {
+#pragma unroll
+    for (int i = 0; i < kChunks; ++i)
+#pragma unroll
+      for (int j = 0; j < kParts; ++j) {
+        float v[A];
+#pragma unroll
+        for (int k = 0; k < A; ++k) v[k] = f[i * V + j * A + k];
+        Cols<T, A> o;
+        o.from(v);
+        const int at = column(lane, i) + j * A;
+        if (left > at) o.store(p + at, left - at);
+      }
   }
+  // The same columns in e4m3.
+  __device__ static __forceinline__ void store_q(uint8_t* p, bool wide, int left, int lane, const uint32_t (&w)[kCols / 4]) {
 #pragma unroll
-  for (int j = 0; j < 16; ++j)
-    if (j < left) p[j] = static_cast<uint8_t>(w[j >> 2] >> (8 * (j & 3)));
-}
-__device__ __forceinline__ void load_q(const uint8_t* p, bool wide, int left, float s, float (&f)[16]) {
-  uint32_t w[4] = {0, 0, 0, 0};
-  if (wide && left >= 16) {
-    const uint4 v = ld_dep(reinterpret_cast<const uint4*>(p));
-    w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
-  } else {
+    for (int i = 0; i < kChunks; ++i) {
+      const int at = column(lane, i);
+      if (wide && left - at >= V) {
+        if constexpr (V == 8)
+          *reinterpret_cast<uint2*>(p + at) = make_uint2(w[2 * i], w[2 * i + 1]);
+        else
+          *reinterpret_cast<uint32_t*>(p + at) = w[i];
+      } else {
 #pragma unroll
-    for (int j = 0; j < 16; ++j)
-      if (j < left) w[j >> 2] |= static_cast<uint32_t>(*const_cast<const volatile uint8_t*>(p + j)) << (8 * (j & 3));
+        for (int j = 0; j < V; ++j)
+          if (at + j < left) p[at + j] = static_cast<uint8_t>(w[(i * V + j) >> 2] >> (8 * (j & 3)));
+      }
+    }
   }
+  __device__ static __forceinline__ void load_q(const uint8_t* p, bool wide, int left, int lane, uint32_t (&w)[kCols / 4]) {
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const __half2 h = __half2(__nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(w[j >> 1] >> (16 * (j & 1))),
-                                                         __NV_E4M3));
+    for (int i = 0; i < kChunks; ++i) {
+      const int at = column(lane, i);
+      if (wide && left - at >= V) {
+        if constexpr (V == 8)
+          asm volatile("ld.global.v2.b32 {%0, %1}, [%2];" : "=r"(w[2 * i]), "=r"(w[2 * i + 1]) : "l"(p + at));
+        else
+          asm volatile("ld.global.b32 %0, [%1];" : "=r"(w[i]) : "l"(p + at));
+      } else {
+#pragma unroll
+        for (int j = 0; j < V / 4; ++j) w[i * (V / 4) + j] = 0;
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+          if (at + j < left)
+            w[(i * V + j) >> 2] |= static_cast<uint32_t>(*const_cast<const volatile uint8_t*>(p + at + j)) << (8 * (j & 3));
+      }
+    }
+  }
+};
+template <int N>
+__device__ __forceinline__ void decode(const uint32_t (&q)[N / 4], float s, float (&f)[N]) {
+#pragma unroll
+  for (int j = 0; j < N / 2; ++j) {
+    const __half2 h = __half2(
+        __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(q[j >> 1] >> (16 * (j & 1))), __NV_E4M3));
     const float2 v = __half22float2(h);
     f[2 * j] = s * v.x;
     f[2 * j + 1] = s * v.y;
@@ -89,10 +142,11 @@ __device__ __forceinline__ void load_q(const uint8_t* p, bool wide, int left, fl
 // Rows and groups of a team: the groups first, first + teams, ... of rows x groups.
 struct Walk {
   int row, grp, dr, dg, groups;
-  __device__ __forceinline__ Walk(int cols) {
+  __device__ __forceinline__ Walk(int cols, int team) {
+    const int per = kThreads / team;
     groups = (cols + 127) / 128;
-    const int teams = gridDim.x * kTeams;
-    const int first = blockIdx.x * kTeams + threadIdx.x / kTeam;
+    const int teams = gridDim.x * per;
+    const int first = blockIdx.x * per + threadIdx.x / team;
     dr = teams / groups, dg = teams % groups;
     row = first / groups, grp = first % groups;
   }
@@ -105,73 +159,141 @@ struct Walk {
 __device__ __forceinline__ int filled(const SwigluArgs& a) {
   return a.n_rows ? min(max(ld_dep(a.n_rows), 0), a.rows) : a.rows;
 }
-__device__ __forceinline__ float amax16(const float (&f)[16]) {
-  float m = 0.f;  // (a NaN loses)
+// Largest magnitudes of a group of gate's and of up's columns (a NaN loses).
+// 16-bit values: gate's in the lower half of a register, up's in the upper, so that one exchange serves both.
+template <typename T, int W, int kTeam>
+__device__ __forceinline__ float2 amax(const Lane<T, W, kTeam>& gate, const Lane<T, W, kTeam>& up) {
+  using L = Lane<T, W, kTeam>;
+  if constexpr (sizeof(T) == 4) {
+    float g[L::kCols], u[L::kCols];
+    gate.to(g);
+    up.to(u);
+    float2 m = make_float2(0.f, 0.f);
 #pragma unroll
-  for (int i = 0; i < 16; ++i) m = fmaxf(m, fabsf(f[i]));
+    for (int i = 0; i < L::kCols; ++i) m.x = fmaxf(m.x, fabsf(g[i])), m.y = fmaxf(m.y, fabsf(u[i]));
 #pragma unroll
-  for (int o = kTeam / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(kFull, m, o));
-  return m;
+    for (int o = kTeam / 2; o > 0; o >>= 1) {
+      m.x = fmaxf(m.x, __shfl_xor_sync(kFull, m.x, o));
+      m.y = fmaxf(m.y, __shfl_xor_sync(kFull, m.y, o));
+    }
+    return m;
+  } else {
+    using T2 = std::conditional_t<std::is_same_v<T, __half>, __half2, __nv_bfloat162>;
+    auto larger = [](uint32_t a, uint32_t b) {
+      const T2 m = __hmax2(*reinterpret_cast<const T2*>(&a), *reinterpret_cast<const T2*>(&b));
+      return *reinterpret_cast<const uint32_t*>(&m);
+    };
+    constexpr uint32_t kAbs = 0x7FFF7FFFu;
+    uint32_t mg = 0, mu = 0;
+#pragma unroll
+    for (int i = 0; i < L::kChunks; ++i)
+#pragma unroll
+      for (int j = 0; j < L::kParts; ++j)
+#pragma unroll
+        for (int k = 0; k < Cols<T, L::A>::kWords; ++k)
+          mg = larger(mg, gate.c[i][j].w[k] & kAbs), mu = larger(mu, up.c[i][j].w[k] & kAbs);
+    uint32_t m = larger(__byte_perm(mg, mu, 0x5410), __byte_perm(mg, mu, 0x7632));
+#pragma unroll
+    for (int o = kTeam / 2; o > 0; o >>= 1) m = larger(m, __shfl_xor_sync(kFull, m, o));
+    return unpack2<T>(m);  // (zeros and NaNs alone: 0)
+  }
 }
 
 template <typename T, int W>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, kSaveCtas)
     swiglu_save_kernel(const T* gate, const T* up, long long ld, T* __restrict__ h, long long ldh, const SwigluArgs a,
                        bool wide_q) {
+  using L = Lane<T, W, kSaveTeam>;
   pdl_wait();
   pdl_launch();
-  const int lane = threadIdx.x & (kTeam - 1), rows = filled(a);
+  const int lane = threadIdx.x & (kSaveTeam - 1), rows = filled(a);
   // (a warp's teams leave together: their shuffles name the whole warp)
-  for (Walk at(a.cols); __any_sync(kFull, at.row < rows); at.next()) {
-    const int c = at.grp * 128 + lane * 16;
-    const bool in = at.row < rows && c < a.cols;
-    const int left = in ? a.cols - c : 0;
-    float g[16], u[16];
-    load16<T, W>(gate + at.row * ld + c, left, g);
-    load16<T, W>(up + at.row * ld + c, left, u);
-    const GroupScale gs(amax16(g)), us(amax16(u));
-    if (!in) continue;
-    uint32_t q[4];
-    e4m3x16(gs, g, q);
-    store_q(a.gate_q + at.row * a.ldq + c, wide_q, left, q);
-    e4m3x16(us, u, q);
-    store_q(a.up_q + at.row * a.ldq + c, wide_q, left, q);
+  for (Walk at(a.cols, kSaveTeam); __any_sync(kFull, at.row < rows); at.next()) {
+    const int c = at.grp * 128, left = at.row < rows ? a.cols - c : 0;
+    L gl, ul;
+    gl.load(gate + at.row * ld + c, left, lane);
+    ul.load(up + at.row * ld + c, left, lane);
+    const float2 m = amax<T, W, kSaveTeam>(gl, ul);
+    const GroupScale gs(m.x), us(m.y);
+    if (left <= 0) continue;
+    float g[L::kCols], u[L::kCols];
+    gl.to(g);
+    ul.to(u);
+    uint32_t q[L::kCols / 4];
+    const long long to = at.row * a.ldq + c;
+    e4m3_pairs(gs, g, q);
+    L::store_q(a.gate_q + to, wide_q, left, lane, q);
+    e4m3_pairs(us, u, q);
+    L::store_q(a.up_q + to, wide_q, left, lane, q);
     if (lane == 0) {
       a.gate_s[at.row * a.lds + at.grp] = gs.s;
       a.up_s[at.row * a.lds + at.grp] = us.s;
     }
 #pragma unroll
-    for (int i = 0; i < 16; ++i) g[i] = g[i] * sigmoid<T>(g[i]) * u[i];
-    store16<T, W>(h + at.row * ldh + c, left, g);
+    for (int i = 0; i < L::kCols; i += 2) {
+      const uint64_t g2 = pair(g[i], g[i + 1]);
+      const float2 v = unpair(mul2(mul2(g2, sigmoid2<T>(g2)), pair(u[i], u[i + 1])));
+      g[i] = v.x;
+      g[i + 1] = v.y;
+    }
+    L::store(h + at.row * ldh + c, left, lane, g);
   }
 }
 
 template <typename T, int W>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, kGradCtas)
     swiglu_backward_kernel(const T* d_h, long long ldd, T* __restrict__ d_gate, T* __restrict__ d_up, long long ldg,
                            T* __restrict__ h, long long ldh, const SwigluArgs a, bool wide_q) {
+  constexpr int kTeam = 8 * sizeof(T);  // one chunk a lane
+  using L = Lane<T, W, kTeam>;
+  constexpr int N = L::kCols;
   pdl_wait();
   pdl_launch();
   const int lane = threadIdx.x & (kTeam - 1), rows = filled(a);
-  for (Walk at(a.cols); at.row < rows; at.next()) {
-    const int c = at.grp * 128 + lane * 16;
-    if (c >= a.cols) continue;
-    const int left = a.cols - c;
-    float d[16], g[16], u[16];
-    load16<T, W>(d_h + at.row * ldd + c, left, d);
-    load_q(a.gate_q + at.row * a.ldq + c, wide_q, left, ld_dep(a.gate_s + at.row * a.lds + at.grp), g);
-    load_q(a.up_q + at.row * a.ldq + c, wide_q, left, ld_dep(a.up_s + at.row * a.lds + at.grp), u);
-    float dg[16], du[16];
+  L dn;  // the next group's
+  uint32_t gn[N / 4], un[N / 4];
+  float gsn, usn;
+  Walk at(a.cols, kTeam);
+  auto fetch = [&]() {
+    const int c = at.grp * 128;
+    const int left = at.row < rows ? a.cols - c : 0;
+    if (left <= L::column(lane, 0)) return;
+    dn.load(d_h + at.row * ldd + c, left, lane);
+    const long long from = at.row * a.ldq + c, scale = at.row * a.lds + at.grp;
+    L::load_q(a.gate_q + from, wide_q, left, lane, gn);
+    L::load_q(a.up_q + from, wide_q, left, lane, un);
+    gsn = ld_dep(a.gate_s + scale);
+    usn = ld_dep(a.up_s + scale);
+  };
+  fetch();
+  while (at.row < rows) {
+    const L dc = dn;
+    uint32_t gq[N / 4], uq[N / 4];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const float s = sigmoid<T>(g[i]), t = g[i] * s;
-      dg[i] = d[i] * u[i] * fmaf(t, 1.0f - s, s);
-      du[i] = d[i] * t;
-      u[i] *= t;
+    for (int i = 0; i < N / 4; ++i) gq[i] = gn[i], uq[i] = un[i];
+    const float gs = gsn, us = usn;
+    const int row = at.row, c = at.grp * 128, left = a.cols - c;
+    at.next();
+    fetch();
+    if (left <= L::column(lane, 0)) continue;
+    float d[N], g[N], u[N], dg[N], du[N];
+    dc.to(d);
+    decode(gq, gs, g);
+    decode(uq, us, u);
+#pragma unroll
+    for (int i = 0; i < N; i += 2) {
+      const float2 s2 = unpair(sigmoid2<T>(pair(g[i], g[i + 1])));
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const float s = j ? s2.y : s2.x, t = g[i + j] * s;
+        dg[i + j] = d[i + j] * u[i + j] * fmaf(t, 1.0f - s, s);
+        du[i + j] = d[i + j] * t;
+        u[i + j] *= t;
+      }
     }
-    store16<T, W>(d_gate + at.row * ldg + c, left, dg);
-    store16<T, W>(d_up + at.row * ldg + c, left, du);
-    if (h) store16<T, W>(h + at.row * ldh + c, left, u);
+    L::store(d_gate + row * ldg + c, left, lane, dg);
+    L::store(d_up + row * ldg + c, left, lane, du);
+    if (h) L::store(h + row * ldh + c, left, lane, u);
   }
 }
 
@@ -193,11 +315,12 @@ cudaError_t by_alignment(uintptr_t at, int elem, F f) {
   if (at % (4 * elem) == 0) return f(std::integral_constant<int, 4>{});
   return f(std::integral_constant<int, 1>{});
 }
-unsigned grid_of(const SwigluArgs& a) {
+unsigned grid_of(const SwigluArgs& a, int team, int most) {
   const long long groups = static_cast<long long>(a.rows) * ceil_div(a.cols, 128);
-  return static_cast<unsigned>(std::min<long long>((groups + kTeams - 1) / kTeams, 152 * 32));
+  const int teams = kThreads / team;
+  return static_cast<unsigned>(std::min<long long>((groups + teams - 1) / teams, 152 * most));
 }
-bool wide(const SwigluArgs& a) { return ((bits(a.gate_q) | bits(a.up_q) | static_cast<uintptr_t>(a.ldq)) & 15u) == 0; }
+bool wide(const SwigluArgs& a) { return ((bits(a.gate_q) | bits(a.up_q) | static_cast<uintptr_t>(a.ldq)) & 7u) == 0; }
 
 }  // namespace
 
@@ -207,7 +330,7 @@ cudaError_t launch_swiglu_save(int type, const void* gate, const void* up, long 
     using T = decltype(t);
     const uintptr_t at = bits(gate) | bits(up) | bits(h) | static_cast<uintptr_t>((ld | ldh) * sizeof(T));
     return by_alignment(at, sizeof(T), [&](auto w) {
-      return launch_pdl(swiglu_save_kernel<T, decltype(w)::value>, grid_of(a), kThreads, 0, s, 1,
+      return launch_pdl(swiglu_save_kernel<T, decltype(w)::value>, grid_of(a, kSaveTeam, kSaveGrid), kThreads, 0, s, 1,
                         static_cast<const T*>(gate), static_cast<const T*>(up), ld, static_cast<T*>(h), ldh, a, wide(a));
     });
   });
@@ -220,7 +343,7 @@ cudaError_t launch_swiglu_backward(int type, const void* d_h, long long ldd, voi
     uintptr_t at = bits(d_h) | bits(d_gate) | bits(d_up) | bits(h) | static_cast<uintptr_t>((ldd | ldg) * sizeof(T));
     if (h) at |= static_cast<uintptr_t>(ldh * sizeof(T));
     return by_alignment(at, sizeof(T), [&](auto w) {
-      return launch_pdl(swiglu_backward_kernel<T, decltype(w)::value>, grid_of(a), kThreads, 0, s, 1,
+      return launch_pdl(swiglu_backward_kernel<T, decltype(w)::value>, grid_of(a, 8 * sizeof(T), kGradGrid), kThreads, 0, s, 1,
                         static_cast<const T*>(d_h), ldd, static_cast<T*>(d_gate), static_cast<T*>(d_up), ldg,
                         static_cast<T*>(h), ldh, a, wide(a));
     });
