@@ -16,52 +16,75 @@ namespace {
 constexpr unsigned kFull = 0xffffffffu;
 
 // ------------------------------------------------------------ sort
-// place(i) = offsets[e_i] + #{i' < i : e_i' = e_i}.  A CTA ranks a chunk of
-// kSortChunk entries: a warp takes 256 that follow one another, 32 at a time; the
-// lanes with one expert find each other (match), the lowest of them adds their
-// number to the warp's counter, and the counter before it plus the lanes below is
-// an entry's rank in its warp.  Counters are then summed over the warps.  No
-// atomics, so a rank does not depend on any order of execution.
-constexpr int kSortWarps = kSortThreads / 32;
-constexpr int kSortRounds = kSortChunk / kSortThreads;
-constexpr int kWarpEntries = kSortChunk / kSortWarps;
+// place(i) = offsets[e_i] + #{i' < i : e_i' = e_i}.  A CTA ranks a chunk of up to 8
+// entries a thread: a warp takes up to 256 that follow one another, 32 at a time; the
+// lanes with one expert find each other (a vote per bit of its number: a match
+// instruction takes about 40 clocks of the SM, nine votes 12), the lowest of them
+// adds their number to the warp's counter, and the counter before it plus the
+// lanes below is an entry's rank in its warp.  Counters are then summed over the
+// warps.  No atomics, so a rank does not depend on any order of execution.
+constexpr int kSortRounds = 8;  // at most
 
+template <int THREADS>
 struct SortShared {
-  uint16_t before[kSortWarps][kSortMaxExperts];  // entries of an expert in the chunk's earlier warps
-  int total[kSortMaxExperts];                    // of an expert in the chunk; then its first place
-  int warp_sum[kSortWarps];
+  static constexpr int kWarps = THREADS / 32;
+  uint16_t* before;  // [kWarps][pitch]: entries of an expert in the chunk's earlier warps
+  int* total;        // [E] of an expert in the chunk
+  int* first;        // [E] first place of the chunk's entries of an expert
+  int* warp_sum;     // [kWarps]
+  int pitch;
+  static size_t bytes(int E) { return kWarps * 2 * ((E + 1) & ~1) + 8 * E + 4 * kWarps; }
+  __device__ __forceinline__ SortShared(void* smem, int E) {
+    pitch = (E + 1) & ~1;
+    before = static_cast<uint16_t*>(smem);
+    total = reinterpret_cast<int*>(before + kWarps * pitch);
+    first = total + E;
+    warp_sum = first + E;
+  }
 };
 
-__device__ __forceinline__ void rank_chunk(SortShared& s, const int32_t* idx, long long first, long long entries, int E,
-                                           int (&e)[kSortRounds], int (&rank)[kSortRounds]) {
+template <int THREADS>
+__device__ __forceinline__ void rank_chunk(SortShared<THREADS>& s, const int32_t* idx, long long from, long long entries,
+                                           int rounds, int E, int (&e)[kSortRounds], int (&rank)[kSortRounds]) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const long long at = first + warp * kWarpEntries + lane;
+  const long long at = from + warp * 32 * rounds + lane;
 #pragma unroll
   for (int r = 0; r < kSortRounds; ++r) {
-    e[r] = at + 32 * r < entries ? ld_dep(idx + at + 32 * r) : -1;
-    if (e[r] >= E) e[r] = -1;
-    if (e[r] < 0) e[r] = -1;
+    e[r] = r < rounds && at + 32 * r < entries ? ld_dep(idx + at + 32 * r) : -1;
+    if (e[r] >= E || e[r] < 0) e[r] = -1;
   }
-  for (int i = lane; i < E; i += 32) s.before[warp][i] = 0;
+  uint16_t* mine = s.before + warp * s.pitch;
+  for (int i = lane; i < s.pitch / 2; i += 32) reinterpret_cast<uint32_t*>(mine)[i] = 0;
+  unsigned same[kSortRounds];  // lanes with this one's expert
+#pragma unroll
+  for (int r = 0; r < kSortRounds; ++r) same[r] = __ballot_sync(kFull, e[r] >= 0);
+  for (int b = 1; b < E; b <<= 1) {
+#pragma unroll
+    for (int r = 0; r < kSortRounds; ++r) {
+      if (r >= rounds) break;
+      const unsigned set = __ballot_sync(kFull, e[r] & b);
+      same[r] &= e[r] & b ? set : ~set;
+    }
+  }
   __syncwarp();
 #pragma unroll
   for (int r = 0; r < kSortRounds; ++r) {
-    const unsigned same = __match_any_sync(kFull, e[r]);
-    const int below = __popc(same & ((1u << lane) - 1));
+    if (r >= rounds) break;
+    const int below = __popc(same[r] & ((1u << lane) - 1));
     int had = 0;
-    if (e[r] >= 0) had = s.before[warp][e[r]];
+    if (e[r] >= 0) had = mine[e[r]];
     __syncwarp();
-    if (e[r] >= 0 && below == 0) s.before[warp][e[r]] = static_cast<uint16_t>(had + __popc(same));
+    if (e[r] >= 0 && below == 0) mine[e[r]] = static_cast<uint16_t>(had + __popc(same[r]));
     __syncwarp();
     rank[r] = had + below;
   }
   __syncthreads();
-  for (int x = threadIdx.x; x < E; x += kSortThreads) {
+  for (int x = threadIdx.x; x < E; x += THREADS) {
     int sum = 0;
 #pragma unroll
-    for (int w = 0; w < kSortWarps; ++w) {
-      const int c = s.before[w][x];
-      s.before[w][x] = static_cast<uint16_t>(sum);
+    for (int w = 0; w < SortShared<THREADS>::kWarps; ++w) {
+      const int c = s.before[w * s.pitch + x];
+      s.before[w * s.pitch + x] = static_cast<uint16_t>(sum);
       sum += c;
     }
     s.total[x] = sum;
@@ -69,15 +92,16 @@ __device__ __forceinline__ void rank_chunk(SortShared& s, const int32_t* idx, lo
   __syncthreads();
 }
 
-// first[x] = sum of count(x') over x' < x, for x < E; returns the sum over all.
-template <typename F>
-__device__ __forceinline__ int scan_experts(SortShared& s, int E, int* first, F count) {
+// s.first[x] = sum of all(x') over x' < x, plus lower(x), for x < E; offsets (nullable): the sums without lower, and the
+// sum over all experts behind them.
+template <int THREADS, typename F>
+__device__ __forceinline__ void scan_experts(SortShared<THREADS>& s, int E, int32_t* offsets, F counts) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   int carry = 0;
-  for (int x0 = 0; x0 < E; x0 += kSortThreads) {
+  for (int x0 = 0; x0 < E; x0 += THREADS) {
     const int x = x0 + threadIdx.x;
-    const int c = x < E ? count(x) : 0;
-    int sum = c;
+    const int2 c = x < E ? counts(x) : make_int2(0, 0);  // of all chunks, of lower ones
+    int sum = c.x;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const int v = __shfl_up_sync(kFull, sum, o);
@@ -85,67 +109,103 @@ __device__ __forceinline__ int scan_experts(SortShared& s, int E, int* first, F 
     }
     if (lane == 31) s.warp_sum[warp] = sum;
     __syncthreads();
-    int lower = 0, all = 0;
+    int lower = carry, all = carry;
 #pragma unroll
-    for (int w = 0; w < kSortWarps; ++w) {
+    for (int w = 0; w < THREADS / 32; ++w) {
       const int v = s.warp_sum[w];
       if (w < warp) lower += v;
       all += v;
     }
-    if (x < E) first[x] = carry + lower + sum - c;
-    carry += all;
+    if (x < E) {
+      s.first[x] = lower + sum - c.x + c.y;
+      if (offsets) offsets[x] = lower + sum - c.x;
+    }
+    carry = all;
     __syncthreads();
   }
-  return carry;
+  if (offsets && threadIdx.x == 0) offsets[E] = carry;
 }
 
-__device__ __forceinline__ void write_places(const SortShared& s, long long first, long long entries, int k,
-                                             const int (&e)[kSortRounds], const int (&rank)[kSortRounds],
-                                             int32_t* perm_dst, int32_t* perm_src) {
+template <int THREADS>
+__device__ __forceinline__ void write_places(const SortShared<THREADS>& s, long long from, long long entries,
+                                             int rounds, int k, const int (&e)[kSortRounds],
+                                             const int (&rank)[kSortRounds], int32_t* perm_dst, int32_t* perm_src) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 #pragma unroll
   for (int r = 0; r < kSortRounds; ++r) {
-    const long long i = first + warp * kWarpEntries + 32 * r + lane;
-    if (i >= entries) continue;
-    const int place = e[r] < 0 ? -1 : s.total[e[r]] + s.before[warp][e[r]] + rank[r];
+    const long long i = from + (warp * rounds + r) * 32 + lane;
+    if (r >= rounds || i >= entries) continue;
+    const int place = e[r] < 0 ? -1 : s.first[e[r]] + s.before[warp * s.pitch + e[r]] + rank[r];
     perm_dst[i] = place;
     if (perm_src && place >= 0) perm_src[place] = static_cast<int32_t>(i / k);
   }
 }
 
-// One chunk: the whole sort.
-__global__ void __launch_bounds__(kSortThreads)
-    sort_small_kernel(const int32_t* idx, int entries, int k, int E, int32_t* offsets, int32_t* perm_dst,
-                      int32_t* perm_src) {
-  __shared__ SortShared s;
+// The whole sort in one cluster, a chunk a CTA; the chunks' counts are read from the CTAs' shared memory.
+template <int THREADS>
+__global__ void __launch_bounds__(THREADS)
+    sort_cluster_kernel(const int32_t* idx, int entries, int rounds, int k, int E, int32_t* offsets, int32_t* perm_dst,
+                        int32_t* perm_src) {
+  extern __shared__ __align__(16) uint8_t smem[];
+  SortShared<THREADS> s(smem, E);
   pdl_wait();
   pdl_launch();
+  const int ranks = gridDim.x, rank_of = blockIdx.x;  // (one cluster)
+  const long long from = static_cast<long long>(rank_of) * THREADS * rounds;
   int e[kSortRounds], rank[kSortRounds];
-  rank_chunk(s, idx, 0, entries, E, e, rank);
-  const int all = scan_experts(s, E, s.total, [&](int x) { return s.total[x]; });
-  for (int x = threadIdx.x; x < E; x += kSortThreads) offsets[x] = s.total[x];
-  if (threadIdx.x == 0) offsets[E] = all;
-  write_places(s, 0, entries, k, e, rank, perm_dst, perm_src);
+  rank_chunk(s, idx, from, entries, rounds, E, e, rank);
+  if (ranks > 1) {
+    asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+  }
+  scan_experts(s, E, rank_of == 0 ? offsets : nullptr, [&](int x) {
+    if (ranks == 1) return make_int2(s.total[x], 0);
+    int v[8];
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+      v[r] = 0;
+      if (r < ranks) {
+        uint32_t peer;
+        asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(peer) : "r"(smem_u32(s.total + x)), "r"(r));
+        asm volatile("ld.shared::cluster.b32 %0, [%1];" : "=r"(v[r]) : "r"(peer) : "memory");
+      }
+    }
+    int2 c = make_int2(0, 0);
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+      c.x += v[r];
+      if (r < rank_of) c.y += v[r];
+    }
+    return c;
+  });
+  if (ranks > 1) asm volatile("barrier.cluster.arrive.release;" ::: "memory");  // this CTA has read the others' counts
+  write_places(s, from, entries, rounds, k, e, rank, perm_dst, perm_src);
+  if (ranks > 1) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
 }
 
 // Many chunks: each one's counts (hist [chunk][E]); per expert, sums over the
 // earlier chunks (in place) and over all (total [E]); places.
-__global__ void __launch_bounds__(kSortThreads)
+constexpr int kManyThreads = 256, kManyChunk = kManyThreads * kSortRounds;
+
+__global__ void __launch_bounds__(kManyThreads)
     sort_count_kernel(const int32_t* idx, long long entries, int E, int32_t* hist) {
   __shared__ int count[kSortMaxExperts];
   pdl_wait();
   pdl_launch();
-  for (int x = threadIdx.x; x < E; x += kSortThreads) count[x] = 0;
+  for (int x = threadIdx.x; x < E; x += kManyThreads) count[x] = 0;
   __syncthreads();
-  const long long first = static_cast<long long>(blockIdx.x) * kSortChunk;
+  const long long from = static_cast<long long>(blockIdx.x) * kManyChunk;
+  int e[kSortRounds];
 #pragma unroll
   for (int r = 0; r < kSortRounds; ++r) {
-    const long long i = first + r * kSortThreads + threadIdx.x;
-    const int e = i < entries ? ld_dep(idx + i) : -1;
-    if (e >= 0 && e < E) atomicAdd(&count[e], 1);  // (a count: any order gives it)
+    const long long i = from + r * kManyThreads + threadIdx.x;
+    e[r] = i < entries ? ld_dep(idx + i) : -1;
   }
+#pragma unroll
+  for (int r = 0; r < kSortRounds; ++r)
+    if (e[r] >= 0 && e[r] < E) atomicAdd(&count[e[r]], 1);  // (a count: any order gives it)
   __syncthreads();
-  for (int x = threadIdx.x; x < E; x += kSortThreads) hist[static_cast<long long>(blockIdx.x) * E + x] = count[x];
+  for (int x = threadIdx.x; x < E; x += kManyThreads) hist[static_cast<long long>(blockIdx.x) * E + x] = count[x];
 }
 
 __global__ void __launch_bounds__(1024) sort_scan_kernel(int32_t* hist, int chunks, int E, int32_t* total) {
@@ -172,263 +232,558 @@ __global__ void __launch_bounds__(1024) sort_scan_kernel(int32_t* hist, int chun
   }
 }
 
-__global__ void __launch_bounds__(kSortThreads)
+__global__ void __launch_bounds__(kManyThreads)
     sort_place_kernel(const int32_t* idx, long long entries, int k, int E, const int32_t* hist, const int32_t* total,
                       int32_t* offsets, int32_t* perm_dst, int32_t* perm_src) {
-  __shared__ SortShared s;
+  extern __shared__ __align__(16) uint8_t smem[];
+  SortShared<kManyThreads> s(smem, E);
   pdl_wait();
   pdl_launch();
-  const long long first = static_cast<long long>(blockIdx.x) * kSortChunk;
+  const long long from = static_cast<long long>(blockIdx.x) * kManyChunk;
   int e[kSortRounds], rank[kSortRounds];
-  rank_chunk(s, idx, first, entries, E, e, rank);
-  const int all = scan_experts(s, E, s.total, [&](int x) { return ld_dep(total + x); });
-  if (blockIdx.x == 0) {
-    for (int x = threadIdx.x; x < E; x += kSortThreads) offsets[x] = s.total[x];
-    if (threadIdx.x == 0) offsets[E] = all;
-    __syncthreads();
-  }
-  for (int x = threadIdx.x; x < E; x += kSortThreads)
-    s.total[x] += ld_dep(hist + static_cast<long long>(blockIdx.x) * E + x);
-  __syncthreads();
-  write_places(s, first, entries, k, e, rank, perm_dst, perm_src);
+  rank_chunk(s, idx, from, entries, kSortRounds, E, e, rank);
+  const int32_t* lower = hist + static_cast<long long>(blockIdx.x) * E;
+  scan_experts(s, E, blockIdx.x == 0 ? offsets : nullptr,
+               [&](int x) { return make_int2(ld_dep(total + x), ld_dep(lower + x)); });
+  write_places(s, from, entries, kSortRounds, k, e, rank, perm_dst, perm_src);
 }
 
-// ------------------------------------------------------------ rows
-// Threads per token: a CTA takes 256 / PER tokens.
-constexpr int kRowThreads = 256;
-constexpr int kGroup = 8;  // places of a token handled together
+// Entries of one cluster at most; below which one small CTA ranks them all; entries for each CTA of a cluster.
+constexpr long long kClusterEntries = 32768, kSmallEntries = 4096, kCtaEntries = 1024;
+static_assert(kClusterEntries <= 8 * 1024 * kSortRounds && kSmallEntries <= 512 * kSortRounds, "entries of the launches");
 
-// The j0-th to j0 + 7-th places of token t, -1 where there is none.
-__device__ __forceinline__ void load_places(const RowsArgs& a, long long t, int j0, bool report, int (&p)[kGroup]) {
-#pragma unroll
-  for (int j = 0; j < kGroup; ++j) {
-    p[j] = -1;
-    if (j0 + j < a.k) {
-      p[j] = ld_dep(a.perm + t * a.k + j0 + j);
-      if (p[j] < 0 || p[j] >= a.rows) {
-        if (report && p[j] != -1) record_status(a.status, ST_BAD_POSITION);
-        p[j] = -1;
-      }
-    }
+// ------------------------------------------------------------ rows
+// A row is taken by blockDim.x threads (8, 16 or whole warps), blockDim.y rows by a
+// CTA; a thread has every blockDim.x-th unit of its row.  With few rows the
+// columns are spread over gridDim.y CTAs as well.
+constexpr int kRowThreads = 256;
+constexpr int kGridCtas = 32, kSumGrid = 8, kGradGrid = 16;  // CTAs of a grid for each SM at most; they take more rows in turn
+constexpr int kFewCtas = 152 * 4;  // below this many CTAs a call is short of work
+
+// Rows of a CTA: first_row() + threadIdx.y, and gridDim.x blockDim.y further on.
+__device__ __forceinline__ long long first_row() { return static_cast<long long>(blockIdx.x) * blockDim.y; }
+// Lanes of a warp that share a row.
+__device__ __forceinline__ int team_width() { return min(32, static_cast<int>(blockDim.x)); }
+
+// The place of entry (t, j) for the team's lane j, -1 where there is none (a place
+// that is no row of y is recorded).  All lanes of a warp call it.
+__device__ __forceinline__ int place_of(const RowsArgs& a, long long t, int j, bool wanted) {
+  if (!wanted || t >= a.n || j >= a.k) return -1;
+  int p = ld_dep(a.perm + t * a.k + j);
+  if (p < 0 || p >= a.rows) {
+    if (p != -1 && threadIdx.x < 32 && blockIdx.y == 0) record_status(a.status, ST_BAD_POSITION);
+    p = -1;
   }
+  return p;
 }
 
 __device__ __forceinline__ uint4 load_unit(const uint4* p) { return ld_dep(p); }
-__device__ __forceinline__ uint2 load_unit(const uint2* p) {
-  uint2 v;
-  asm volatile("ld.global.v2.b32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p));
-  return v;
-}
 template <typename U>
 __device__ __forceinline__ U load_unit(const U* p) {
   return *const_cast<const volatile U*>(p);
 }
 
-// x_perm[place] = x[t]: bytes in units of U, the last few of a row one by one.
-template <typename U, int PER>
+// x_perm[place] = x[t]: rows that start on 16 bytes, in units of 16, the last few bytes of a row one by one.
+// A thread has its next units (and the next row's places) on their way while it stores those it has.
+constexpr int kCopyUnits = 4;
 __global__ void __launch_bounds__(kRowThreads)
     permute_kernel(const char* x, long long ldx, char* __restrict__ y, long long ldy, long long row_bytes,
                    const RowsArgs a) {
   pdl_wait();
   pdl_launch();
-  const long long t = static_cast<long long>(blockIdx.x) * (kRowThreads / PER) + threadIdx.x / PER;
-  if (t >= a.n) return;
-  const int vt = threadIdx.x % PER;
-  const long long units = row_bytes / static_cast<int>(sizeof(U));
-  const char* row = x + t * ldx;
-  for (int j0 = 0; j0 < a.k; j0 += kGroup) {
-    int p[kGroup];
-    load_places(a, t, j0, vt == 0, p);
-    for (long long v = vt; v < units; v += PER) {
-      const U u = load_unit(reinterpret_cast<const U*>(row + v * sizeof(U)));
+  const int width = team_width(), lane = threadIdx.x & (width - 1);
+  using U = uint4;
+  const int units = static_cast<int>(row_bytes / static_cast<int>(sizeof(U)));
+  const int rest = static_cast<int>(row_bytes - static_cast<long long>(units) * sizeof(U));
+  const int start = blockIdx.y * blockDim.x * kCopyUnits;
+  const int step = gridDim.y * blockDim.x * kCopyUnits, rows = gridDim.x * blockDim.y;
+  long long base = first_row();
+  int v0 = start;  // (both the same in the CTA)
+  U next[kCopyUnits];
+  int next_place;
+  auto fetch = [&]() {
+    const long long t = base + threadIdx.y;
+    if (v0 == start) next_place = place_of(a, t, lane, true);
+    const U* row = reinterpret_cast<const U*>(x + t * ldx);
 #pragma unroll
-      for (int j = 0; j < kGroup; ++j)
-        if (p[j] >= 0) *reinterpret_cast<U*>(y + p[j] * ldy + v * sizeof(U)) = u;
+    for (int i = 0; i < kCopyUnits; ++i) {
+      const int v = v0 + static_cast<int>(i * blockDim.x + threadIdx.x);
+      if (t < a.n && v < units) next[i] = load_unit(row + v);
     }
-    for (long long b = units * sizeof(U) + vt; b < row_bytes; b += PER) {
-      const char u = load_unit(row + b);
+  };
+  auto put = [&](int mine, int places, int at, const U (&u)[kCopyUnits]) {
+    for (int j = 0; j < places; ++j) {
+      const int p = __shfl_sync(kFull, mine, j, width);
+      if (p < 0) continue;
+      U* to = reinterpret_cast<U*>(y + p * ldy);
 #pragma unroll
-      for (int j = 0; j < kGroup; ++j)
-        if (p[j] >= 0) y[p[j] * ldy + b] = u;
+      for (int i = 0; i < kCopyUnits; ++i) {
+        const int v = at + static_cast<int>(i * blockDim.x + threadIdx.x);
+        if (v < units) to[v] = u[i];
+      }
+    }
+  };
+  auto put_rest = [&](long long t, int mine, int places) {
+    for (int j = 0; j < places; ++j) {
+      const int p = __shfl_sync(kFull, mine, j, width);
+      if (p < 0) continue;
+      for (int b = threadIdx.x; b < rest; b += blockDim.x) {
+        const long long at = static_cast<long long>(units) * sizeof(U) + b;
+        y[p * ldy + at] = load_unit(x + t * ldx + at);
+      }
+    }
+  };
+  int mine = -1;
+  if (base < a.n) fetch();
+  while (base < a.n) {
+    U u[kCopyUnits];
+#pragma unroll
+    for (int i = 0; i < kCopyUnits; ++i) u[i] = next[i];
+    const long long t = base + threadIdx.y;
+    const int at = v0;
+    if (at == start) mine = next_place;
+    v0 += step;
+    if (v0 >= units) v0 = start, base += rows;
+    if (base < a.n) fetch();
+    put(mine, min(width, a.k), at, u);
+    const bool last = rest > 0 && at == start && blockIdx.y == 0;
+    if (last) put_rest(t, mine, min(width, a.k));
+    for (int j0 = width; j0 < a.k; j0 += width) {  // more places than lanes
+      const int more = place_of(a, t, j0 + lane, true), places = min(width, a.k - j0);
+      put(more, places, at, u);
+      if (last) put_rest(t, more, places);
     }
   }
 }
 
-// out[t] = sum_j w[t][j] y[place], fp32 in slot order.
-template <typename T, int N, int PER>
+// The same for rows at any address.  T: an element.  A thread has the aligned 16 bytes of x and those before them; a
+// place's row takes 16 of these 32 for an aligned store.
+constexpr int kAnyUnits = 2;  // of a thread on their way
+template <typename T>
 __global__ void __launch_bounds__(kRowThreads)
+    permute_any_kernel(const T* x, long long ldx, T* __restrict__ y, long long ldy, const RowsArgs a) {
+  using A = Any<T>;
+  constexpr int C = kAnyUnits;
+  pdl_wait();
+  pdl_launch();
+  const int width = team_width(), lane = threadIdx.x & (width - 1);
+  const int start = blockIdx.y * blockDim.x * C * A::N;
+  const int step = gridDim.y * blockDim.x * C * A::N, rows = gridDim.x * blockDim.y;
+  for (long long base = first_row(); base < a.n; base += rows) {
+    const long long t = base + threadIdx.y;
+    const T* row = x + t * ldx;
+    const int from = A::past(row);
+    for (int j0 = 0; j0 < a.k; j0 += width) {
+      const int mine = place_of(a, t, j0 + lane, true), places = min(width, a.k - j0);
+      for (int c0 = start; c0 < a.cols + 2 * A::N; c0 += step) {
+        typename A::V lo[C], hi[C];
+#pragma unroll
+        for (int i = 0; i < C; ++i) {
+          if (t >= a.n) continue;
+          const typename A::Raw r = A::fetch(row, c0 + static_cast<int>((i * blockDim.x + threadIdx.x) * A::N) - from - A::N, a.cols);
+          lo[i] = r.lo, hi[i] = r.hi;
+        }
+        for (int j = 0; j < places; ++j) {
+          const int p = __shfl_sync(kFull, mine, j, width);
+          if (p < 0) continue;
+          T* to = y + p * ldy;
+          // the byte of the 32 that comes to a boundary: 1 .. 16
+          const int o = (((from - A::past(to)) * A::kSize - 1) & 15) + 1;
+#pragma unroll
+          for (int i = 0; i < C; ++i) {
+            const int c = c0 + static_cast<int>((i * blockDim.x + threadIdx.x) * A::N) - from - A::N + o / A::kSize;
+            if (c + A::N > 0 && c < a.cols) A::store(to, c, a.cols, A::shifted(lo[i], hi[i], o));
+          }
+        }
+      }
+    }
+  }
+}
+
+constexpr int kSumCtas = 4;
+// out[t] = sum_j w[t][j] y[place], fp32 in slot order; J places and C units of N
+// columns at a time.
+// ANY: rows at any address, N columns as out's row has them on 16 bytes.
+template <typename T, int N, int J, int C, bool ANY>
+__global__ void __launch_bounds__(kRowThreads, ANY ? 3 : kSumCtas)
     unpermute_kernel(const T* y, long long ldy, T* __restrict__ out, long long ldo, const RowsArgs a) {
   pdl_wait();
   pdl_launch();
-  const long long t = static_cast<long long>(blockIdx.x) * (kRowThreads / PER) + threadIdx.x / PER;
-  if (t >= a.n) return;
-  const int vt = threadIdx.x % PER;
-  int p[kGroup];
-  load_places(a, t, 0, vt == 0, p);
-  for (long long c = static_cast<long long>(vt) * N; c < a.cols; c += PER * N) {
-    const int left = static_cast<int>(a.cols - c);
-    float acc[N];
+  const int width = team_width(), lane = threadIdx.x & (width - 1);
+  const int start = blockIdx.y * blockDim.x * C * N;
+  const int step = gridDim.y * blockDim.x * C * N, rows = gridDim.x * blockDim.y;
+  int next_place;
+  float next_w;
+  auto fetch = [&](long long t, int j0) {  // places and weights, by lane
+    next_place = place_of(a, t, j0 + lane, lane < J);
+    next_w = a.w && next_place >= 0 ? ld_dep(a.w + t * a.k + j0 + lane) : 1.f;
+  };
+  long long base = first_row();
+  if (base < a.n) fetch(base + threadIdx.y, 0);
+  for (; base < a.n; base += rows) {
+    const long long t = base + threadIdx.y;
+    int mine = next_place;
+    float wt = next_w;
+    if (base + rows < a.n) fetch(t + rows, 0);
+    const int pre = ANY ? Any<T>::past(out + t * ldo) : 0;
+    for (int c0 = start; c0 < a.cols + (ANY ? N : 0); c0 += step) {
+      float acc[C][N];
 #pragma unroll
-    for (int i = 0; i < N; ++i) acc[i] = 0.f;
-    for (int j0 = 0; j0 < a.k; j0 += kGroup) {
-      if (a.k > kGroup) load_places(a, t, j0, c == 0, p);
-      Cols<T, N> v[kGroup];
+      for (int i = 0; i < C; ++i)
 #pragma unroll
-      for (int j = 0; j < kGroup; ++j)
-        if (p[j] >= 0) v[j].load(y + p[j] * ldy + c, left);
-#pragma unroll
-      for (int j = 0; j < kGroup; ++j)
-        if (p[j] >= 0) {
-          const float w = a.w ? ld_dep(a.w + t * a.k + j0 + j) : 1.f;
-          float f[N];
-          v[j].to(f);
-#pragma unroll
-          for (int i = 0; i < N; ++i) acc[i] = fmaf(w, f[i], acc[i]);
+        for (int q = 0; q < N; ++q) acc[i][q] = 0.f;
+      for (int j0 = 0; j0 < a.k; j0 += J) {
+        if (a.k > J) {  // more places than are handled together
+          const int keep_place = next_place;
+          const float keep_w = next_w;
+          fetch(t, j0);
+          mine = next_place, wt = next_w;
+          next_place = keep_place, next_w = keep_w;
         }
+        std::conditional_t<ANY, typename Any<T>::Raw, Cols<T, N>> v[J][C];
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+          const int p = __shfl_sync(kFull, mine, j, width);
+          const T* from = y + p * ldy;
+#pragma unroll
+          for (int i = 0; i < C; ++i) {
+            const int c = c0 + static_cast<int>((i * blockDim.x + threadIdx.x) * N) - pre;
+            if (p < 0 || c >= a.cols) continue;
+            if constexpr (ANY)
+              v[j][i] = Any<T>::fetch(from, c, a.cols);
+            else
+              v[j][i].load(from + c, a.cols - c);
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+          const int p = __shfl_sync(kFull, mine, j, width);
+          const float w = __shfl_sync(kFull, wt, j, width);
+          if (p >= 0) {
+#pragma unroll
+            for (int i = 0; i < C; ++i) {
+              float f[N];
+              if constexpr (ANY)
+                Any<T>::columns(v[j][i], y + p * ldy, c0 + static_cast<int>((i * blockDim.x + threadIdx.x) * N) - pre).to(f);
+              else
+                v[j][i].to(f);
+#pragma unroll
+              for (int q = 0; q < N; ++q) acc[i][q] = fmaf(w, f[q], acc[i][q]);
+            }
+          }
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < C; ++i) {
+        const int c = c0 + static_cast<int>((i * blockDim.x + threadIdx.x) * N) - pre;
+        if (t >= a.n || c >= a.cols) continue;
+        Cols<T, N> o;
+        o.from(acc[i]);
+        if constexpr (ANY)
+          Any<T>::store(out + t * ldo, c, a.cols, o);
+        else
+          o.store(out + t * ldo + c, a.cols - c);
+      }
     }
-    Cols<T, N> o;
-    o.from(acc);
-    o.store(out + t * ldo + c, left);
   }
 }
 
-// d_y[place] = w d_out[t], d_w[t][j] = <d_out[t], y[place]> (fp32: per thread, then over the threads in a fixed tree).
-template <typename T, int N, int PER>
-__global__ void __launch_bounds__(kRowThreads)
+// d_y[place] = w d_out[t], d_w[t][j] = <d_out[t], y[place]> (fp32: per thread, then
+// over the lanes and the row's warps in a fixed tree).
+constexpr int kGradCtas = 4;
+// ANY: rows at any address, N columns as each row of d_y (of y without it) has them on 16 bytes.
+template <typename T, int N, int J, bool ANY>
+__global__ void __launch_bounds__(kRowThreads, ANY || (J == 8 && std::is_same_v<T, __half>) ? 3 : kGradCtas)
     unpermute_backward_kernel(const T* d_out, long long ldo, const T* y, long long ldy, T* __restrict__ d_y, long long ldd,
                               float* __restrict__ d_w, const RowsArgs a) {
-  __shared__ float part[kRowThreads / 32][kGroup];
+  __shared__ float part[2][kRowThreads / 32][J];
   pdl_wait();
   pdl_launch();
-  const long long t = static_cast<long long>(blockIdx.x) * (kRowThreads / PER) + threadIdx.x / PER;
-  const int vt = threadIdx.x % PER, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const bool live = t < a.n;
-  for (int j0 = 0; j0 < a.k; j0 += kGroup) {
-    int p[kGroup];
-    float w[kGroup], s[kGroup];
+  const int width = team_width(), lane = threadIdx.x & (width - 1);
+  const int warps = blockDim.x / 32, warp = (threadIdx.y * blockDim.x + threadIdx.x) / 32;
+  const unsigned rows = gridDim.x * blockDim.y;
+  int next_place, turn = 0;
+  float next_w;
+  long long base = first_row();
+  int j0 = 0;
+  auto fetch = [&](long long t) {
+    next_place = place_of(a, t, j0 + lane, lane < J);
+    next_w = a.w && next_place >= 0 ? ld_dep(a.w + t * a.k + j0 + lane) : 1.f;
+  };
+  if (base < a.n) fetch(base + threadIdx.y);
+  while (base < a.n) {
+    const long long t = base + threadIdx.y;
+    const bool live = t < a.n;
+    const int mine = next_place, jt = j0;
+    const float wt = next_w;
+    j0 += J;
+    if (j0 >= a.k) j0 = 0, base += rows;
+    if (base < a.n) fetch(base + threadIdx.y);
+    float s[J];
 #pragma unroll
-    for (int j = 0; j < kGroup; ++j) {
-      p[j] = -1;
-      s[j] = 0.f;
-      w[j] = 1.f;
-    }
-    if (live) {
-      load_places(a, t, j0, vt == 0, p);
-#pragma unroll
-      for (int j = 0; j < kGroup; ++j)
-        if (a.w && p[j] >= 0) w[j] = ld_dep(a.w + t * a.k + j0 + j);
-      for (long long c = static_cast<long long>(vt) * N; c < a.cols; c += PER * N) {
-        const int left = static_cast<int>(a.cols - c);
-        Cols<T, N> v[kGroup], d;
-        d.load(d_out + t * ldo + c, left);
-        if (d_w) {
-#pragma unroll
-          for (int j = 0; j < kGroup; ++j)
-            if (p[j] >= 0) v[j].load(y + p[j] * ldy + c, left);
+    for (int j = 0; j < J; ++j) s[j] = 0.f;
+    const T* d_row = d_out + t * ldo;
+    // (whole warps: they exchange places in the loop)
+    for (int c0 = 0; c0 < a.cols + (ANY ? N : 0); c0 += blockDim.x * N) {
+      const int ct = c0 + static_cast<int>(threadIdx.x) * N;
+      std::conditional_t<ANY, typename Any<T>::Raw, Cols<T, N>> v[J];
+      Cols<T, N> d, d_lo;  // (d_lo: the N columns before d's)
+      if constexpr (ANY) {
+        if (live) {
+          const auto hi = Any<T>::fetch(d_row, ct, a.cols), lo = Any<T>::fetch(d_row, ct - N, a.cols);
+          d = Any<T>::columns(hi, d_row, ct);
+          d_lo = Any<T>::columns(lo, d_row, ct - N);
         }
-        float g[N];
-        d.to(g);
+      } else if (live && ct < a.cols) {
+        d.load(d_row + ct, a.cols - ct);
+      }
 #pragma unroll
-        for (int j = 0; j < kGroup; ++j)
-          if (p[j] >= 0) {
-            float f[N];
-            if (d_w) {
-              v[j].to(f);
+      for (int j = 0; j < J; ++j) {
+        const int p = __shfl_sync(kFull, mine, j, width);
+        if (!d_w || p < 0) continue;
+        const T* from = y + p * ldy;
+        if constexpr (ANY)
+          v[j] = Any<T>::fetch(from, ct - Any<T>::past(d_y ? d_y + p * ldd : from), a.cols);
+        else if (ct < a.cols)
+          v[j].load(from + ct, a.cols - ct);
+      }
+      float g[N];
+      if (!ANY) d.to(g);
 #pragma unroll
-              for (int i = 0; i < N; ++i) s[j] = fmaf(g[i], f[i], s[j]);
-            }
-            if (d_y) {
+      for (int j = 0; j < J; ++j) {
+        const int p = __shfl_sync(kFull, mine, j, width);
+        const float w = __shfl_sync(kFull, wt, j, width);
+        if (p < 0) continue;  // (as are all of a row that is not there)
+        T* to = d_y + p * ldd;
+        int pre = 0;
+        if constexpr (ANY) {
+          pre = Any<T>::past(d_y ? to : y + p * ldy);
+          Any<T>::before(d_lo, d, pre).to(g);
+        }
+        const int c = ct - pre;
+        if (c >= a.cols) continue;
+        float f[N];
+        if (d_y) {
 #pragma unroll
-              for (int i = 0; i < N; ++i) f[i] = w[j] * g[i];
-              Cols<T, N> o;
-              o.from(f);
-              o.store(d_y + p[j] * ldd + c, left);
-            }
+          for (int i = 0; i < N; ++i) f[i] = w * g[i];
+          Cols<T, N> o;
+          o.from(f);
+          if constexpr (ANY)
+            Any<T>::store(to, c, a.cols, o);
+          else
+            o.store(to + c, a.cols - c);
+        }
+        if (d_w) {
+          if constexpr (ANY)
+            Any<T>::columns(v[j], y + p * ldy, c).to(f);
+          else
+            v[j].to(f);
+          if (ANY && (c < 0 || c + N > a.cols)) {  // (beside the row there may be anything)
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+              if (c + i < 0 || c + i >= a.cols) f[i] = 0.f, g[i] = 0.f;
           }
+#pragma unroll
+          for (int i = 0; i < N; ++i) s[j] = fmaf(g[i], f[i], s[j]);
+        }
       }
     }
     if (!d_w) continue;
 #pragma unroll
-    for (int j = 0; j < kGroup; ++j)
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) s[j] += __shfl_xor_sync(kFull, s[j], o);
-    if constexpr (PER > 32) {
+    for (int j = 0; j < J; ++j)
+      for (int o = width / 2; o > 0; o >>= 1) s[j] += __shfl_xor_sync(kFull, s[j], o);
+    if (warps > 1) {
+      // (two copies in turn: a warp that writes one again has passed the barrier after which the other was read)
       if (lane == 0) {
 #pragma unroll
-        for (int j = 0; j < kGroup; ++j) part[warp][j] = s[j];
+        for (int j = 0; j < J; ++j) part[turn][warp][j] = s[j];
       }
       __syncthreads();
-      if (live && vt < kGroup && j0 + vt < a.k) {
+      if (live && threadIdx.x < J && jt + static_cast<int>(threadIdx.x) < a.k) {
         float sum = 0.f;
-#pragma unroll
-        for (int v = 0; v < PER / 32; ++v) sum += part[warp + v][vt];
-        d_w[t * a.k + j0 + vt] = sum;
+        for (int v = 0; v < warps; ++v) sum += part[turn][warp + v][threadIdx.x];
+        d_w[t * a.k + jt + threadIdx.x] = sum;
       }
-      __syncthreads();
+      turn ^= 1;
     } else if (live) {
 #pragma unroll
-      for (int j = 0; j < kGroup; ++j)
-        if (lane == j && j0 + j < a.k) d_w[t * a.k + j0 + j] = s[j];
+      for (int j = 0; j < J; ++j)
+        if (lane == j && jt + j < a.k) d_w[t * a.k + jt + j] = s[j];
     }
   }
 }
 
 // y[place] = scale q[t], N columns at a time (a scale per 128).
-template <typename T, int N, int PER>
+constexpr int kDecodeUnits = 2;  // of a thread
+template <typename T, int N>
 __global__ void __launch_bounds__(kRowThreads)
     dequantize_kernel(const uint8_t* q, long long ldq, const float* scales, long long lds, T* __restrict__ y, long long ldy,
                       const RowsArgs a) {
   pdl_wait();
   pdl_launch();
-  const long long t = static_cast<long long>(blockIdx.x) * (kRowThreads / PER) + threadIdx.x / PER;
-  if (t >= a.n) return;
-  const int vt = threadIdx.x % PER;
-  for (int j0 = 0; j0 < a.k; j0 += kGroup) {
-    int p[kGroup];
-    if (a.perm) {
-      load_places(a, t, j0, vt == 0, p);
-    } else {
+  const int width = team_width(), lane = threadIdx.x & (width - 1);
+  const int start = blockIdx.y * blockDim.x * kDecodeUnits * N;
+  const int step = gridDim.y * blockDim.x * kDecodeUnits * N, rows = gridDim.x * blockDim.y;
+  long long base = first_row();
+  int c0 = start;  // (both the same in the CTA)
+  // the next units and their scales, the next row's places
+  uint32_t b[kDecodeUnits][(N + 3) / 4];
+  float s[kDecodeUnits];
+  int next_place;
+  auto fetch = [&]() {
+    const long long t = base + threadIdx.y;
+    if (c0 == start)
+      next_place = a.perm ? place_of(a, t, lane, true) : lane == 0 && t < a.n ? static_cast<int>(t) : -1;
 #pragma unroll
-      for (int j = 0; j < kGroup; ++j) p[j] = j == 0 && t < a.rows ? static_cast<int>(t) : -1;
-    }
-    for (long long c = static_cast<long long>(vt) * N; c < a.cols; c += PER * N) {
-      const int left = static_cast<int>(a.cols - c);
+    for (int i = 0; i < kDecodeUnits; ++i) {
+      const int c = c0 + static_cast<int>((i * blockDim.x + threadIdx.x) * N);
+      s[i] = 0.f;
+#pragma unroll
+      for (int k = 0; k < (N + 3) / 4; ++k) b[i][k] = 0;
+      if (t >= a.n || c >= a.cols) continue;
+      const int left = a.cols - c;
       const uint8_t* from = q + t * ldq + c;
-      uint8_t b[N];
-      if (N == 8 && left >= 8) {
-        uint32_t v[2];
-        asm volatile("ld.global.v2.b32 {%0, %1}, [%2];" : "=r"(v[0]), "=r"(v[1]) : "l"(from));
-#pragma unroll
-        for (int i = 0; i < N; ++i) b[i] = static_cast<uint8_t>(v[(i >> 2) & 1] >> (8 * (i & 3)));
+      s[i] = ld_dep(scales + t * lds + (c >> 7));
+      if (N >= 4 && left >= N) {
+        if constexpr (N == 8)
+          asm volatile("ld.global.v2.b32 {%0, %1}, [%2];" : "=r"(b[i][0]), "=r"(b[i][1]) : "l"(from));
+        else
+          asm volatile("ld.global.b32 %0, [%1];" : "=r"(b[i][0]) : "l"(from));
       } else {
 #pragma unroll
-        for (int i = 0; i < N; ++i) b[i] = i < left ? *reinterpret_cast<const volatile uint8_t*>(from + i) : 0;
+        for (int k = 0; k < N; ++k)
+          if (k < left) b[i][k / 4] |= static_cast<uint32_t>(load_unit(from + k)) << (8 * (k & 3));
       }
-      const float s = ld_dep(scales + t * lds + (c >> 7));
+    }
+  };
+  auto put = [&](int mine, int places, int at, const Cols<T, N> (&o)[kDecodeUnits]) {
+    for (int j = 0; j < places; ++j) {
+      const int p = __shfl_sync(kFull, mine, j, width);
+      if (p < 0) continue;
+#pragma unroll
+      for (int i = 0; i < kDecodeUnits; ++i) {
+        const int c = at + static_cast<int>((i * blockDim.x + threadIdx.x) * N);
+        if (c < a.cols) o[i].store(y + p * ldy + c, a.cols - c);
+      }
+    }
+  };
+  int mine = -1;
+  if (base < a.n) fetch();
+  while (base < a.n) {
+    Cols<T, N> o[kDecodeUnits];
+#pragma unroll
+    for (int i = 0; i < kDecodeUnits; ++i) {
       float f[N];
 #pragma unroll
-      for (int i = 0; i < N; ++i)
-        f[i] = s * __half2float(__half(__nv_cvt_fp8_to_halfraw(b[i], __NV_E4M3)));
-      Cols<T, N> o;
-      o.from(f);
+      for (int k = 0; k < N; ++k)
+        f[k] = s[i] * __half2float(__half(__nv_cvt_fp8_to_halfraw(static_cast<uint8_t>(b[i][k / 4] >> (8 * (k & 3))),
+                                                                 __NV_E4M3)));
+      o[i].from(f);
+    }
+    const long long t = base + threadIdx.y;
+    const int at = c0;
+    if (at == start) mine = next_place;
+    c0 += step;
+    if (c0 >= a.cols) c0 = start, base += rows;
+    if (base < a.n) fetch();
+    put(mine, min(width, a.k), at, o);
+    for (int j0 = width; j0 < a.k; j0 += width)  // more places than lanes
+      put(place_of(a, t, j0 + lane, true), min(width, a.k - j0), at, o);
+  }
+}
+
+// N e4m3 values and their scales as columns c .. c + N - 1 of y's type, zeros outside the row.
+template <typename T>
+__device__ __forceinline__ Cols<T, Any<T>::N> decode_any(const uint8_t* q, const float* scales, int c, int cols) {
+  constexpr int N = Any<T>::N;
+  float f[N];
+  if (c >= 0 && c + N <= cols) {
+    const uintptr_t at = reinterpret_cast<uintptr_t>(q + c), first = at & ~static_cast<uintptr_t>(7);
+    const int o = static_cast<int>(at & 7);
+    uint64_t b, next = 0;
+    asm volatile("ld.global.b64 %0, [%1];" : "=l"(b) : "l"(first));
+    if (o + N > 8) asm volatile("ld.global.b64 %0, [%1];" : "=l"(next) : "l"(first + 8));
+    if (o) b = b >> (8 * o) | next << (64 - 8 * o);
+    const float s = ld_dep(scales + (c >> 7));  // (c is a multiple of N: one scale)
 #pragma unroll
-      for (int j = 0; j < kGroup; ++j)
-        if (p[j] >= 0) o.store(y + p[j] * ldy + c, left);
+    for (int i = 0; i < N; ++i)
+      f[i] = s * __half2float(__half(__nv_cvt_fp8_to_halfraw(static_cast<uint8_t>(b >> (8 * i)), __NV_E4M3)));
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      f[i] = 0.f;
+      if (c + i >= 0 && c + i < cols)
+        f[i] = ld_dep(scales + ((c + i) >> 7)) * __half2float(__half(__nv_cvt_fp8_to_halfraw(load_unit(q + c + i), __NV_E4M3)));
+    }
+  }
+  Cols<T, N> v;
+  v.from(f);
+  return v;
+}
+
+// The same for rows at any address: a thread has N columns and the N before them; a place's row takes N of these for an
+// aligned store.
+template <typename T>
+__global__ void __launch_bounds__(kRowThreads)
+    dequantize_any_kernel(const uint8_t* q, long long ldq, const float* scales, long long lds, T* __restrict__ y,
+                          long long ldy, const RowsArgs a) {
+  using A = Any<T>;
+  constexpr int C = kAnyUnits;
+  pdl_wait();
+  pdl_launch();
+  const int width = team_width(), lane = threadIdx.x & (width - 1);
+  const int start = blockIdx.y * blockDim.x * C * A::N;
+  const int step = gridDim.y * blockDim.x * C * A::N, rows = gridDim.x * blockDim.y;
+  for (long long base = first_row(); base < a.n; base += rows) {
+    const long long t = base + threadIdx.y;
+    for (int j0 = 0; j0 < a.k; j0 += width) {
+      const int mine = a.perm ? place_of(a, t, j0 + lane, true) : lane == 0 && t < a.n ? static_cast<int>(t) : -1;
+      const int places = min(width, a.k - j0);
+      for (int c0 = start; c0 < a.cols + A::N; c0 += step) {
+        typename A::V lo[C], hi[C];
+#pragma unroll
+        for (int i = 0; i < C; ++i) {
+          const int c = c0 + static_cast<int>((i * blockDim.x + threadIdx.x) * A::N), cols = t < a.n ? a.cols : 0;
+          hi[i] = decode_any<T>(q + t * ldq, scales + t * lds, c, cols);
+          lo[i] = decode_any<T>(q + t * ldq, scales + t * lds, c - A::N, cols);
+        }
+        for (int j = 0; j < places; ++j) {
+          const int p = __shfl_sync(kFull, mine, j, width);
+          if (p < 0) continue;
+          T* to = y + p * ldy;
+          const int pre = A::past(to);
+#pragma unroll
+          for (int i = 0; i < C; ++i) {
+            const int c = c0 + static_cast<int>((i * blockDim.x + threadIdx.x) * A::N) - pre;
+            if (c < a.cols) A::store(to, c, a.cols, A::before(lo[i], hi[i], pre));
+          }
+        }
+      }
     }
   }
 }
 
-// Threads per token for rows of this many units.
-int threads_per_row(long long units) { return units <= 32 ? 32 : units <= 128 ? 64 : 256; }
-
-template <typename F>
-cudaError_t by_threads(long long units, F f) {
-  switch (threads_per_row(units)) {
-    case 32: return f(std::integral_constant<int, 32>{});
-    case 64: return f(std::integral_constant<int, 64>{});
-    default: return f(std::integral_constant<int, 256>{});
-  }
+// Threads and CTAs for n rows of ``units`` units, C of them a thread at a time: as
+// few threads as a row needs, in equal laps where it needs more than a CTA has;
+// laps side by side while the rows alone would leave SMs without work.
+struct RowLaunch {
+  dim3 grid, block;
+};
+RowLaunch row_launch(long long n, long long units, int C, bool split, int grid) {
+  constexpr int most = kRowThreads;
+  const long long need = std::max<long long>(1, (units + C - 1) / C);
+  const long long laps = (need + most - 1) / most;
+  const long long per = (need + laps - 1) / laps;
+  const unsigned x = per <= 8 ? 8 : per <= 16 ? 16 : static_cast<unsigned>((per + 31) / 32 * 32);
+  const unsigned y = std::max(1u, static_cast<unsigned>(kRowThreads) / x);
+  RowLaunch r;
+  r.block = dim3(x, y);
+  const long long ctas = (n + y - 1) / y;
+  r.grid = dim3(static_cast<unsigned>(std::min<long long>(ctas, 152 * grid)), 1);
+  if (split && ctas < kFewCtas) r.grid.y = static_cast<unsigned>(std::min<long long>(laps, 64));
+  return r;
 }
+
 template <typename F>
 cudaError_t by_type(int type, F f) {
   switch (type) {
@@ -438,75 +793,101 @@ cudaError_t by_type(int type, F f) {
     default: return cudaErrorInvalidValue;
   }
 }
-// Columns per access: 8 where every row starts on 16 bytes, 4 on 8, 2 on 4, else one.  at: addresses and strides in bytes.
+// Bytes an access where every row of T starts on as many (at: addresses and strides in bytes): 16, 8, or those of a word;
+// else 0.
+template <typename T, typename F>
+cudaError_t by_alignment(uintptr_t at, F f) {
+  if (at % 16 == 0) return f(std::integral_constant<int, 16>{});
+  if (at % 8 == 0) return f(std::integral_constant<int, 8>{});
+  return f(std::integral_constant<int, sizeof(T) == 4 ? 4 : 0>{});
+}
+// Units of a thread for accesses of this many bytes and J places: as many bytes on their way.
+constexpr int units_of(int access, int J) { return access == 0 ? 1 : access == 16 ? (J >= 4 ? 1 : 2) : access == 8 ? (J >= 8 ? 1 : 2) : (J >= 8 ? 2 : 4); }
+
+// Places handled together.
 template <typename F>
-cudaError_t by_alignment(uintptr_t at, int elem, F f) {
-  if (at % 16 == 0) return f(std::integral_constant<int, 8>{});
-  if (at % (4 * elem) == 0) return f(std::integral_constant<int, 4>{});
-  if (at % (2 * elem) == 0) return f(std::integral_constant<int, 2>{});
-  return f(std::integral_constant<int, 1>{});
+cudaError_t by_places(int k, F f) {
+  if (k == 1) return f(std::integral_constant<int, 1>{});
+  if (k == 2) return f(std::integral_constant<int, 2>{});
+  if (k <= 4) return f(std::integral_constant<int, 4>{});
+  return f(std::integral_constant<int, 8>{});
 }
 
 uintptr_t bits(const void* p) { return reinterpret_cast<uintptr_t>(p); }
-unsigned row_grid(const RowsArgs& a, int per) { return static_cast<unsigned>(ceil_div(a.n, kRowThreads / per)); }
 
 }  // namespace
 
 size_t sort_workspace(long long entries, int experts) {
-  const long long chunks = ceil_div(entries, kSortChunk);
-  return chunks <= 1 ? 0 : static_cast<size_t>(chunks + 1) * experts * 4;
+  if (entries <= kClusterEntries) return 0;
+  return static_cast<size_t>(ceil_div(entries, kManyChunk) + 1) * experts * 4;
 }
+
+namespace {
+template <int THREADS>
+cudaError_t sort_cluster(int ctas, const int32_t* idx, int entries, int k, int E, int32_t* offsets, int32_t* perm_dst,
+                         int32_t* perm_src, cudaStream_t s) {
+  const size_t smem = SortShared<THREADS>::bytes(E);
+  if (smem > 48 * 1024) {
+    const cudaError_t e = cudaFuncSetAttribute(sort_cluster_kernel<THREADS>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                               static_cast<int>(smem));
+    if (e != cudaSuccess) return e;
+  }
+  const int rounds = std::max(1, ceil_div(entries, ctas * THREADS));
+  return launch_pdl(sort_cluster_kernel<THREADS>, ctas, THREADS, smem, s, ctas, idx, entries, rounds, k, E, offsets, perm_dst,
+                    perm_src);
+}
+}  // namespace
 
 cudaError_t launch_sort(const int32_t* idx, long long entries, int k, int E, int32_t* offsets, int32_t* perm_dst,
                         int32_t* perm_src, void* ws, cudaStream_t s) {
-  const long long chunks = ceil_div(entries, kSortChunk);
-  if (chunks <= 1)
-    return launch_pdl(sort_small_kernel, 1, kSortThreads, 0, s, 1, idx, static_cast<int>(entries), k, E, offsets, perm_dst,
-                      perm_src);
+  if (entries <= kSmallEntries)
+    return sort_cluster<512>(1, idx, static_cast<int>(entries), k, E, offsets, perm_dst, perm_src, s);
+  if (entries <= kClusterEntries) {
+    const int ctas = std::min(8, ceil_div(entries, kCtaEntries));
+    return sort_cluster<1024>(ctas, idx, static_cast<int>(entries), k, E, offsets, perm_dst, perm_src, s);
+  }
+  const int chunks = ceil_div(entries, kManyChunk);
   int32_t* total = static_cast<int32_t*>(ws);
   int32_t* hist = total + E;
-  const unsigned grid = static_cast<unsigned>(chunks);
-  cudaError_t e = launch_pdl(sort_count_kernel, grid, kSortThreads, 0, s, 1, idx, entries, E, hist);
+  cudaError_t e = launch_pdl(sort_count_kernel, chunks, kManyThreads, 0, s, 1, idx, entries, E, hist);
+  if (e == cudaSuccess) e = launch_pdl(sort_scan_kernel, ceil_div(E, 32), 1024, 0, s, 1, hist, chunks, E, total);
   if (e == cudaSuccess)
-    e = launch_pdl(sort_scan_kernel, ceil_div(E, 32), 1024, 0, s, 1, hist, static_cast<int>(chunks), E, total);
-  if (e == cudaSuccess)
-    e = launch_pdl(sort_place_kernel, grid, kSortThreads, 0, s, 1, idx, entries, k, E, hist, total, offsets, perm_dst,
-                   perm_src);
+    e = launch_pdl(sort_place_kernel, chunks, kManyThreads, SortShared<kManyThreads>::bytes(E), s, 1, idx, entries, k, E, hist,
+                   total, offsets, perm_dst, perm_src);
   return e;
 }
 
 cudaError_t launch_permute(int elem_bytes, const void* x, long long ldx, void* y, long long ldy, const RowsArgs& a,
                            cudaStream_t s) {
+  const uintptr_t at = bits(x) | bits(y) | static_cast<uintptr_t>((ldx | ldy) * elem_bytes);
   const long long bytes = static_cast<long long>(a.cols) * elem_bytes;
-  ldx *= elem_bytes;
-  ldy *= elem_bytes;
-  const uintptr_t at = bits(x) | bits(y) | static_cast<uintptr_t>(ldx) | static_cast<uintptr_t>(ldy);
-  auto go = [&](auto unit) {
-    using U = decltype(unit);
-    return by_threads(bytes / static_cast<int>(sizeof(U)), [&](auto per) {
-      constexpr int PER = decltype(per)::value;
-      return launch_pdl(permute_kernel<U, PER>, row_grid(a, PER), kRowThreads, 0, s, 1, static_cast<const char*>(x), ldx,
-                        static_cast<char*>(y), ldy, bytes, a);
-    });
+  if (at % 16 == 0 && bytes >= 16) {
+    const RowLaunch r = row_launch(a.n, bytes / 16, kCopyUnits, true, kGridCtas);
+    return launch_pdl(permute_kernel, r.grid, r.block, 0, s, 1, static_cast<const char*>(x), ldx * elem_bytes,
+                      static_cast<char*>(y), ldy * elem_bytes, bytes, a);
+  }
+  auto any = [&](auto elem) {
+    using T = decltype(elem);
+    const RowLaunch r = row_launch(a.n, bytes / 16 + 2, kAnyUnits, true, kGridCtas);
+    return launch_pdl(permute_any_kernel<T>, r.grid, r.block, 0, s, 1, static_cast<const T*>(x), ldx, static_cast<T*>(y), ldy,
+                      a);
   };
-  if (at % 16 == 0) return go(uint4{});
-  if (at % 8 == 0) return go(uint2{});
-  if (at % 4 == 0) return go(0u);
-  if (at % 2 == 0) return go(uint16_t{});
-  return go(uint8_t{});
+  return elem_bytes == 4 ? any(uint32_t{}) : elem_bytes == 2 ? any(uint16_t{}) : any(uint8_t{});
 }
 
 cudaError_t launch_unpermute(int type, const void* y, long long ldy, void* out, long long ldo, const RowsArgs& a,
                              cudaStream_t s) {
   return by_type(type, [&](auto t) {
     using T = decltype(t);
-    const uintptr_t at = bits(y) | bits(out) | static_cast<uintptr_t>((ldy | ldo) * sizeof(T));
-    return by_alignment(at, sizeof(T), [&](auto cols) {
-      constexpr int N = decltype(cols)::value;
-      return by_threads(ceil_div(a.cols, N), [&](auto per) {
-        constexpr int PER = decltype(per)::value;
-        return launch_pdl(unpermute_kernel<T, N, PER>, row_grid(a, PER), kRowThreads, 0, s, 1, static_cast<const T*>(y),
-                          ldy, static_cast<T*>(out), ldo, a);
+    return by_alignment<T>(bits(y) | bits(out) | static_cast<uintptr_t>((ldy | ldo) * sizeof(T)), [&](auto access) {
+      return by_places(a.k, [&](auto places) {
+        constexpr bool ANY = decltype(access)::value == 0;
+        constexpr int N = (ANY ? 16 : decltype(access)::value) / static_cast<int>(sizeof(T));
+        constexpr int J = ANY ? std::min(4, decltype(places)::value) : decltype(places)::value;  // (registers)
+        constexpr int C = units_of(decltype(access)::value, J);
+        const RowLaunch r = row_launch(a.n, ceil_div(a.cols, N) + ANY, C, true, kSumGrid);
+        return launch_pdl(unpermute_kernel<T, N, J, C, ANY>, r.grid, r.block, 0, s, 1, static_cast<const T*>(y), ldy,
+                          static_cast<T*>(out), ldo, a);
       });
     });
   });
@@ -519,13 +900,14 @@ cudaError_t launch_unpermute_backward(int type, const void* d_out, long long ldo
     uintptr_t at = bits(d_out) | bits(y) | bits(d_y) | static_cast<uintptr_t>(ldo * sizeof(T));
     if (d_w) at |= static_cast<uintptr_t>(ldy * sizeof(T));
     if (d_y) at |= static_cast<uintptr_t>(ldd * sizeof(T));
-    return by_alignment(at, sizeof(T), [&](auto cols) {
-      constexpr int N = decltype(cols)::value;
-      return by_threads(ceil_div(a.cols, N), [&](auto per) {
-        constexpr int PER = decltype(per)::value;
-        return launch_pdl(unpermute_backward_kernel<T, N, PER>, row_grid(a, PER), kRowThreads, 0, s, 1,
-                          static_cast<const T*>(d_out), ldo, static_cast<const T*>(y), ldy, static_cast<T*>(d_y), ldd, d_w,
-                          a);
+    return by_alignment<T>(at, [&](auto access) {
+      return by_places(a.k, [&](auto places) {
+        constexpr bool ANY = decltype(access)::value == 0;
+        constexpr int N = (ANY ? 16 : decltype(access)::value) / static_cast<int>(sizeof(T));
+        constexpr int J = ANY ? std::min(4, decltype(places)::value) : decltype(places)::value;  // (registers)
+        const RowLaunch r = row_launch(a.n, ceil_div(a.cols, N) + ANY, 1, false, kGradGrid);  // (a row's sums meet in its CTA)
+        return launch_pdl(unpermute_backward_kernel<T, N, J, ANY>, r.grid, r.block, 0, s, 1, static_cast<const T*>(d_out), ldo,
+                          static_cast<const T*>(y), ldy, static_cast<T*>(d_y), ldd, d_w, a);
       });
     });
   });
@@ -535,16 +917,18 @@ cudaError_t launch_dequantize(int type, const void* q, long long ldq, const floa
                               long long ldy, const RowsArgs& a, cudaStream_t s) {
   return by_type(type, [&](auto t) {
     using T = decltype(t);
-    // (of q's rows only whether they start on 8 bytes counts)
-    const bool q8 = (bits(q) | static_cast<uintptr_t>(ldq)) % 8 == 0;
-    const uintptr_t at = q8 ? bits(y) | static_cast<uintptr_t>(ldy * sizeof(T)) : sizeof(T);
-    return by_alignment(at, sizeof(T), [&](auto cols) {
-      constexpr int N = decltype(cols)::value;
-      return by_threads(ceil_div(a.cols, N), [&](auto per) {
-        constexpr int PER = decltype(per)::value;
-        return launch_pdl(dequantize_kernel<T, N, PER>, row_grid(a, PER), kRowThreads, 0, s, 1,
-                          static_cast<const uint8_t*>(q), ldq, scales, lds, static_cast<T*>(y), ldy, a);
-      });
+    // (rows of q start on N bytes where rows of y start on 16)
+    const uintptr_t at = bits(y) | static_cast<uintptr_t>(ldy * sizeof(T)) | (bits(q) | static_cast<uintptr_t>(ldq)) * sizeof(T);
+    return by_alignment<T>(at, [&](auto access) {
+      constexpr bool ANY = decltype(access)::value == 0;
+      constexpr int N = (ANY ? 16 : decltype(access)::value) / static_cast<int>(sizeof(T));
+      const RowLaunch r = row_launch(a.n, ceil_div(a.cols, N) + ANY, ANY ? kAnyUnits : kDecodeUnits, true, kGridCtas);
+      if constexpr (ANY)
+        return launch_pdl(dequantize_any_kernel<T>, r.grid, r.block, 0, s, 1, static_cast<const uint8_t*>(q), ldq, scales,
+                          lds, static_cast<T*>(y), ldy, a);
+      else
+        return launch_pdl(dequantize_kernel<T, N>, r.grid, r.block, 0, s, 1, static_cast<const uint8_t*>(q), ldq, scales, lds,
+                          static_cast<T*>(y), ldy, a);
     });
   });
 }

@@ -9,8 +9,6 @@ namespace asap {
 enum ElemType { kElemBf16 = 0, kElemF16 = 1, kElemF32 = 2, kElemE4m3 = 3 };
 
 constexpr int kSortMaxExperts = 1024;
-constexpr int kSortThreads = 512;
-constexpr int kSortChunk = 4096;  // entries a CTA ranks
 
 size_t sort_workspace(long long entries, int experts);
 cudaError_t launch_sort(const int32_t* idx, long long entries, int k, int E, int32_t* offsets, int32_t* perm_dst,

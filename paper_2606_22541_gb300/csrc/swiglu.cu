@@ -26,8 +26,11 @@ constexpr int kThreads = 256;
 // with the e4m3 values decoded before the next loads are out, which takes the registers).
 // Grids of a few waves' CTAs, so that the SMs' ends are level: forward 4 to 50 CTAs for each SM make no difference, backward 10,
 // 20, 40 and all: 112, 104, 100, 110 us.
-constexpr int kSaveTeam = 8, kSaveCtas = 4, kSaveGrid = 16;  // lanes of a group, CTAs an SM, CTAs of the grid for each SM
+constexpr int kSaveCtas = 4, kSaveGrid = 16;  // CTAs an SM, CTAs of the grid for each SM
 constexpr int kGradCtas = 5, kGradGrid = 40;
+// Lanes of a group, by the columns of an access.
+__host__ __device__ constexpr int save_team(int v) { return v >= 4 ? 8 : 16; }
+__host__ __device__ constexpr int grad_team(int v) { return v == 8 ? 16 : 32; }
 
 // 1 / (1 + e^-g) of two columns.  fp32 results take expf and a division; 16-bit ones, whose rounding is 2^14 times
 // coarser, the fast exponential and reciprocal (relative 2^-22 and 2^-23 by their documentation, and |g| 2^-23 from the
@@ -50,79 +53,82 @@ __device__ __forceinline__ uint64_t sigmoid2(uint64_t g) {
   }
 }
 
-// A lane's kCols columns of a group, as kChunks chunks of V = 16 bytes (or what W columns an access make of it): chunk i
-// of lane l starts at column i kTeam V + l V, so that a team's accesses are contiguous.
-template <typename T, int W, int kTeam>
+// A lane's kCols columns of a group, as kChunks chunks of V columns, one access each (of V bytes in e4m3): chunk i of
+// lane l starts at column i kTeam V + l V, so that a team's accesses are contiguous.  V: 16 bytes, or as many columns as
+// the alignment of every row allows.
+template <typename T, int V, int kTeam>
 struct Lane {
-  static constexpr int kCols = 128 / kTeam, V = 16 / static_cast<int>(sizeof(T)), kChunks = kCols / V;
-  static constexpr int A = W < V ? W : V, kParts = V / A;
-  Cols<T, A> c[kChunks][kParts];
+  static constexpr int kCols = 128 / kTeam, kChunks = kCols / V;
+  Cols<T, V> c[kChunks];
   __device__ static __forceinline__ int column(int lane, int i) { return (i * kTeam + lane) * V; }
   // p: the group's first column, left: columns from there
   __device__ __forceinline__ void load(const T* p, int left, int lane) {
 #pragma unroll
-    for (int i = 0; i < kChunks; ++i)
-#pragma unroll
-      for (int j = 0; j < kParts; ++j) c[i][j].load(p + column(lane, i) + j * A, left - column(lane, i) - j * A);
+    for (int i = 0; i < kChunks; ++i) c[i].load(p + column(lane, i), left - column(lane, i));
   }
   __device__ __forceinline__ void to(float (&f)[kCols]) const {
 #pragma unroll
-    for (int i = 0; i < kChunks; ++i)
+    for (int i = 0; i < kChunks; ++i) {
+      float v[V];
+      c[i].to(v);
 #pragma unroll
-      for (int j = 0; j < kParts; ++j) {
-        float v[A];
-        c[i][j].to(v);
-#pragma unroll
-        for (int k = 0; k < A; ++k) f[i * V + j * A + k] = v[k];
-      }
+      for (int k = 0; k < V; ++k) f[i * V + k] = v[k];
+    }
   }
   __device__ static __forceinline__ void store(T* p, int left, int lane, const float (&f)[kCols]) {
 #pragma unroll
-    for (int i = 0; i < kChunks; ++i)
+    for (int i = 0; i < kChunks; ++i) {
+      float v[V];
 #pragma unroll
-      for (int j = 0; j < kParts; ++j) {
-        float v[A];
-#pragma unroll
-        for (int k = 0; k < A; ++k) v[k] = f[i * V + j * A + k];
-        Cols<T, A> o;
-        o.from(v);
-        const int at = column(lane, i) + j * A;
-        if (left > at) o.store(p + at, left - at);
-      }
+      for (int k = 0; k < V; ++k) v[k] = f[i * V + k];
+      Cols<T, V> o;
+      o.from(v);
+      const int at = column(lane, i);
+      if (left > at) o.store(p + at, left - at);
+    }
   }
   // The same columns in e4m3.
-  __device__ static __forceinline__ void store_q(uint8_t* p, bool wide, int left, int lane, const uint32_t (&w)[kCols / 4]) {
+  __device__ static __forceinline__ void store_q(uint8_t* p, int left, int lane, const uint32_t (&w)[kCols / 4]) {
 #pragma unroll
     for (int i = 0; i < kChunks; ++i) {
       const int at = column(lane, i);
-      if (wide && left - at >= V) {
+      if (left - at >= V) {
         if constexpr (V == 8)
           *reinterpret_cast<uint2*>(p + at) = make_uint2(w[2 * i], w[2 * i + 1]);
-        else
+        else if constexpr (V == 4)
           *reinterpret_cast<uint32_t*>(p + at) = w[i];
+        else if constexpr (V == 2)
+          *reinterpret_cast<uint16_t*>(p + at) = static_cast<uint16_t>(w[i / 2] >> (16 * (i & 1)));
+        else
+          p[at] = static_cast<uint8_t>(w[i / 4] >> (8 * (i & 3)));
       } else {
 #pragma unroll
         for (int j = 0; j < V; ++j)
-          if (at + j < left) p[at + j] = static_cast<uint8_t>(w[(i * V + j) >> 2] >> (8 * (j & 3)));
+          if (at + j < left) p[at + j] = static_cast<uint8_t>(w[(i * V + j) >> 2] >> (8 * ((i * V + j) & 3)));
       }
     }
   }
-  __device__ static __forceinline__ void load_q(const uint8_t* p, bool wide, int left, int lane, uint32_t (&w)[kCols / 4]) {
+  __device__ static __forceinline__ void load_q(const uint8_t* p, int left, int lane, uint32_t (&w)[kCols / 4]) {
+#pragma unroll
+    for (int i = 0; i < kCols / 4; ++i) w[i] = 0;
 #pragma unroll
     for (int i = 0; i < kChunks; ++i) {
       const int at = column(lane, i);
-      if (wide && left - at >= V) {
-        if constexpr (V == 8)
+      if (V > 1 && left - at >= V) {
+        if constexpr (V == 8) {
           asm volatile("ld.global.v2.b32 {%0, %1}, [%2];" : "=r"(w[2 * i]), "=r"(w[2 * i + 1]) : "l"(p + at));
-        else
+        } else if constexpr (V == 4) {
           asm volatile("ld.global.b32 %0, [%1];" : "=r"(w[i]) : "l"(p + at));
+        } else if constexpr (V == 2) {
+          uint16_t v;
+          asm volatile("ld.global.b16 %0, [%1];" : "=h"(v) : "l"(p + at));
+          w[i / 2] |= static_cast<uint32_t>(v) << (16 * (i & 1));
+        }
       } else {
-#pragma unroll
-        for (int j = 0; j < V / 4; ++j) w[i * (V / 4) + j] = 0;
 #pragma unroll
         for (int j = 0; j < V; ++j)
           if (at + j < left)
-            w[(i * V + j) >> 2] |= static_cast<uint32_t>(*const_cast<const volatile uint8_t*>(p + at + j)) << (8 * (j & 3));
+            w[(i * V + j) >> 2] |= static_cast<uint32_t>(*const_cast<const volatile uint8_t*>(p + at + j)) << (8 * ((i * V + j) & 3));
       }
     }
   }
@@ -161,9 +167,9 @@ __device__ __forceinline__ int filled(const SwigluArgs& a) {
 }
 // Largest magnitudes of a group of gate's and of up's columns (a NaN loses).
 // 16-bit values: gate's in the lower half of a register, up's in the upper, so that one exchange serves both.
-template <typename T, int W, int kTeam>
-__device__ __forceinline__ float2 amax(const Lane<T, W, kTeam>& gate, const Lane<T, W, kTeam>& up) {
-  using L = Lane<T, W, kTeam>;
+template <typename T, int V, int kTeam>
+__device__ __forceinline__ float2 amax(const Lane<T, V, kTeam>& gate, const Lane<T, V, kTeam>& up) {
+  using L = Lane<T, V, kTeam>;
   if constexpr (sizeof(T) == 4) {
     float g[L::kCols], u[L::kCols];
     gate.to(g);
@@ -188,10 +194,8 @@ __device__ __forceinline__ float2 amax(const Lane<T, W, kTeam>& gate, const Lane
 #pragma unroll
     for (int i = 0; i < L::kChunks; ++i)
 #pragma unroll
-      for (int j = 0; j < L::kParts; ++j)
-#pragma unroll
-        for (int k = 0; k < Cols<T, L::A>::kWords; ++k)
-          mg = larger(mg, gate.c[i][j].w[k] & kAbs), mu = larger(mu, up.c[i][j].w[k] & kAbs);
+      for (int k = 0; k < Cols<T, V>::kWords; ++k)
+        mg = larger(mg, gate.c[i].w[k] & kAbs), mu = larger(mu, up.c[i].w[k] & kAbs);
     uint32_t m = larger(__byte_perm(mg, mu, 0x5410), __byte_perm(mg, mu, 0x7632));
 #pragma unroll
     for (int o = kTeam / 2; o > 0; o >>= 1) m = larger(m, __shfl_xor_sync(kFull, m, o));
@@ -199,21 +203,21 @@ __device__ __forceinline__ float2 amax(const Lane<T, W, kTeam>& gate, const Lane
   }
 }
 
-template <typename T, int W>
+template <typename T, int V>
 __global__ void __launch_bounds__(kThreads, kSaveCtas)
-    swiglu_save_kernel(const T* gate, const T* up, long long ld, T* __restrict__ h, long long ldh, const SwigluArgs a,
-                       bool wide_q) {
-  using L = Lane<T, W, kSaveTeam>;
+    swiglu_save_kernel(const T* gate, const T* up, long long ld, T* __restrict__ h, long long ldh, const SwigluArgs a) {
+  constexpr int kTeam = save_team(V);
+  using L = Lane<T, V, kTeam>;
   pdl_wait();
   pdl_launch();
-  const int lane = threadIdx.x & (kSaveTeam - 1), rows = filled(a);
+  const int lane = threadIdx.x & (kTeam - 1), rows = filled(a);
   // (a warp's teams leave together: their shuffles name the whole warp)
-  for (Walk at(a.cols, kSaveTeam); __any_sync(kFull, at.row < rows); at.next()) {
+  for (Walk at(a.cols, kTeam); __any_sync(kFull, at.row < rows); at.next()) {
     const int c = at.grp * 128, left = at.row < rows ? a.cols - c : 0;
     L gl, ul;
     gl.load(gate + at.row * ld + c, left, lane);
     ul.load(up + at.row * ld + c, left, lane);
-    const float2 m = amax<T, W, kSaveTeam>(gl, ul);
+    const float2 m = amax<T, V, kTeam>(gl, ul);
     const GroupScale gs(m.x), us(m.y);
     if (left <= 0) continue;
     float g[L::kCols], u[L::kCols];
@@ -222,9 +226,9 @@ __global__ void __launch_bounds__(kThreads, kSaveCtas)
     uint32_t q[L::kCols / 4];
     const long long to = at.row * a.ldq + c;
     e4m3_pairs(gs, g, q);
-    L::store_q(a.gate_q + to, wide_q, left, lane, q);
+    L::store_q(a.gate_q + to, left, lane, q);
     e4m3_pairs(us, u, q);
-    L::store_q(a.up_q + to, wide_q, left, lane, q);
+    L::store_q(a.up_q + to, left, lane, q);
     if (lane == 0) {
       a.gate_s[at.row * a.lds + at.grp] = gs.s;
       a.up_s[at.row * a.lds + at.grp] = us.s;
@@ -240,12 +244,12 @@ __global__ void __launch_bounds__(kThreads, kSaveCtas)
   }
 }
 
-template <typename T, int W>
+template <typename T, int V>
 __global__ void __launch_bounds__(kThreads, kGradCtas)
     swiglu_backward_kernel(const T* d_h, long long ldd, T* __restrict__ d_gate, T* __restrict__ d_up, long long ldg,
-                           T* __restrict__ h, long long ldh, const SwigluArgs a, bool wide_q) {
-  constexpr int kTeam = 8 * sizeof(T);  // one chunk a lane
-  using L = Lane<T, W, kTeam>;
+                           T* __restrict__ h, long long ldh, const SwigluArgs a) {
+  constexpr int kTeam = grad_team(V);
+  using L = Lane<T, V, kTeam>;
   constexpr int N = L::kCols;
   pdl_wait();
   pdl_launch();
@@ -260,8 +264,8 @@ __global__ void __launch_bounds__(kThreads, kGradCtas)
     if (left <= L::column(lane, 0)) return;
     dn.load(d_h + at.row * ldd + c, left, lane);
     const long long from = at.row * a.ldq + c, scale = at.row * a.lds + at.grp;
-    L::load_q(a.gate_q + from, wide_q, left, lane, gn);
-    L::load_q(a.up_q + from, wide_q, left, lane, un);
+    L::load_q(a.gate_q + from, left, lane, gn);
+    L::load_q(a.up_q + from, left, lane, un);
     gsn = ld_dep(a.gate_s + scale);
     usn = ld_dep(a.up_s + scale);
   };
@@ -308,11 +312,15 @@ cudaError_t by_type(int type, F f) {
     default: return cudaErrorInvalidValue;
   }
 }
-// Columns per access, by the alignment (in bytes) of every row.
-template <typename F>
-cudaError_t by_alignment(uintptr_t at, int elem, F f) {
-  if (at % 16 == 0) return f(std::integral_constant<int, 8>{});
-  if (at % (4 * elem) == 0) return f(std::integral_constant<int, 4>{});
+// Columns an access, for rows of T whose addresses and strides make up ``at`` and the kept rows.
+template <typename T, typename F>
+cudaError_t by_alignment(uintptr_t at, const SwigluArgs& a, F f) {
+  const uintptr_t cols = at / sizeof(T) | bits(a.gate_q) | bits(a.up_q) | static_cast<uintptr_t>(a.ldq);
+  if constexpr (sizeof(T) == 2) {
+    if (cols % 8 == 0) return f(std::integral_constant<int, 8>{});
+  }
+  if (cols % 4 == 0) return f(std::integral_constant<int, 4>{});
+  if (cols % 2 == 0) return f(std::integral_constant<int, 2>{});
   return f(std::integral_constant<int, 1>{});
 }
 unsigned grid_of(const SwigluArgs& a, int team, int most) {
@@ -320,7 +328,6 @@ unsigned grid_of(const SwigluArgs& a, int team, int most) {
   const int teams = kThreads / team;
   return static_cast<unsigned>(std::min<long long>((groups + teams - 1) / teams, 152 * most));
 }
-bool wide(const SwigluArgs& a) { return ((bits(a.gate_q) | bits(a.up_q) | static_cast<uintptr_t>(a.ldq)) & 7u) == 0; }
 
 }  // namespace
 
@@ -329,9 +336,9 @@ cudaError_t launch_swiglu_save(int type, const void* gate, const void* up, long 
   return by_type(type, [&](auto t) {
     using T = decltype(t);
     const uintptr_t at = bits(gate) | bits(up) | bits(h) | static_cast<uintptr_t>((ld | ldh) * sizeof(T));
-    return by_alignment(at, sizeof(T), [&](auto w) {
-      return launch_pdl(swiglu_save_kernel<T, decltype(w)::value>, grid_of(a, kSaveTeam, kSaveGrid), kThreads, 0, s, 1,
-                        static_cast<const T*>(gate), static_cast<const T*>(up), ld, static_cast<T*>(h), ldh, a, wide(a));
+    return by_alignment<T>(at, a, [&](auto v) {
+      return launch_pdl(swiglu_save_kernel<T, decltype(v)::value>, grid_of(a, save_team(decltype(v)::value), kSaveGrid), kThreads, 0, s, 1,
+                        static_cast<const T*>(gate), static_cast<const T*>(up), ld, static_cast<T*>(h), ldh, a);
     });
   });
 }
@@ -342,10 +349,10 @@ cudaError_t launch_swiglu_backward(int type, const void* d_h, long long ldd, voi
     using T = decltype(t);
     uintptr_t at = bits(d_h) | bits(d_gate) | bits(d_up) | bits(h) | static_cast<uintptr_t>((ldd | ldg) * sizeof(T));
     if (h) at |= static_cast<uintptr_t>(ldh * sizeof(T));
-    return by_alignment(at, sizeof(T), [&](auto w) {
-      return launch_pdl(swiglu_backward_kernel<T, decltype(w)::value>, grid_of(a, 8 * sizeof(T), kGradGrid), kThreads, 0, s, 1,
+    return by_alignment<T>(at, a, [&](auto v) {
+      return launch_pdl(swiglu_backward_kernel<T, decltype(v)::value>, grid_of(a, grad_team(decltype(v)::value), kGradGrid), kThreads, 0, s, 1,
                         static_cast<const T*>(d_h), ldd, static_cast<T*>(d_gate), static_cast<T*>(d_up), ldg,
-                        static_cast<T*>(h), ldh, a, wide(a));
+                        static_cast<T*>(h), ldh, a);
     });
   });
 }
