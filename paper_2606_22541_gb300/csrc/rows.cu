@@ -8,6 +8,8 @@
 #include <cuda_fp8.h>
 
 #include <algorithm>
+#include <atomic>
+#include <utility>
 
 namespace asap {
 
@@ -257,8 +259,9 @@ static_assert(kClusterEntries <= 8 * 1024 * kSortRounds && kSmallEntries <= 512 
 // CTA; a thread has every blockDim.x-th unit of its row.  With few rows the
 // columns are spread over gridDim.y CTAs as well.
 constexpr int kRowThreads = 256;
-constexpr int kGridCtas = 32, kSumGrid = 8, kGradGrid = 16;  // CTAs of a grid for each SM at most; they take more rows in turn
-constexpr int kFewCtas = 152 * 4;  // below this many CTAs a call is short of work
+constexpr int kCopyWaves = 8, kSumWaves = 1, kAnySumWaves = 2, kGradWaves = 4;  // CTAs of a grid at most, in waves
+constexpr int kSms = 152;
+constexpr int kFewCtas = kSms * 4;  // below this many CTAs a call is short of work
 
 // Rows of a CTA: first_row() + threadIdx.y, and gridDim.x blockDim.y further on.
 __device__ __forceinline__ long long first_row() { return static_cast<long long>(blockIdx.x) * blockDim.y; }
@@ -490,13 +493,17 @@ __global__ void __launch_bounds__(kRowThreads, ANY ? 3 : kSumCtas)
 
 // d_y[place] = w d_out[t], d_w[t][j] = <d_out[t], y[place]> (fp32: per thread, then
 // over the lanes and the row's warps in a fixed tree).
-constexpr int kGradCtas = 4;
+// Threads of a CTA at most.  (Few rows have their laps side by side; where 64 registers are too few, whose limit that is,
+// CTAs stay small.)
+constexpr int kGradThreads = 1024;
+template <typename T, int J, bool ANY>
+constexpr int grad_threads = ANY || (J == 8 && std::is_same_v<T, __half>) ? kRowThreads : kGradThreads;
 // ANY: rows at any address, N columns as each row of d_y (of y without it) has them on 16 bytes.
 template <typename T, int N, int J, bool ANY>
-__global__ void __launch_bounds__(kRowThreads, ANY || (J == 8 && std::is_same_v<T, __half>) ? 3 : kGradCtas)
+__global__ void __launch_bounds__(grad_threads<T, J, ANY>, grad_threads<T, J, ANY> == kRowThreads ? 3 : 1)
     unpermute_backward_kernel(const T* d_out, long long ldo, const T* y, long long ldy, T* __restrict__ d_y, long long ldd,
                               float* __restrict__ d_w, const RowsArgs a) {
-  __shared__ float part[2][kRowThreads / 32][J];
+  __shared__ float part[2][kGradThreads / 32][J];
   pdl_wait();
   pdl_launch();
   const int width = team_width(), lane = threadIdx.x & (width - 1);
@@ -763,25 +770,38 @@ __global__ void __launch_bounds__(kRowThreads)
   }
 }
 
+// CTAs of this many threads that an SM holds (asked once: the library runs on one kind of GPU).
+template <auto KERNEL>
+int resident(int threads) {
+  static std::atomic<int> known[kGradThreads / 32 + 1];
+  std::atomic<int>& k = known[threads / 32];
+  int v = k.load(std::memory_order_relaxed);
+  if (v == 0) {
+    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&v, KERNEL, threads, 0) != cudaSuccess || v < 1) {
+      cudaGetLastError();
+      return 1;
+    }
+    k.store(v, std::memory_order_relaxed);
+  }
+  return v;
+}
+
 // Threads and CTAs for n rows of ``units`` units, C of them a thread at a time: as
 // few threads as a row needs, in equal laps where it needs more than a CTA has;
-// laps side by side while the rows alone would leave SMs without work.
-struct RowLaunch {
-  dim3 grid, block;
-};
-RowLaunch row_launch(long long n, long long units, int C, bool split, int grid) {
-  constexpr int most = kRowThreads;
+// laps side by side (split) while the rows alone would leave SMs without work.  CTAs of
+// ``waves`` full waves at most, which then take more rows in turn.
+template <auto KERNEL, typename... A>
+cudaError_t launch_rows(long long n, long long units, int C, bool split, int most, int waves, cudaStream_t s, A&&... args) {
+  if (n > kSms) most = kRowThreads;
   const long long need = std::max<long long>(1, (units + C - 1) / C);
   const long long laps = (need + most - 1) / most;
   const long long per = (need + laps - 1) / laps;
-  const unsigned x = per <= 8 ? 8 : per <= 16 ? 16 : static_cast<unsigned>((per + 31) / 32 * 32);
-  const unsigned y = std::max(1u, static_cast<unsigned>(kRowThreads) / x);
-  RowLaunch r;
-  r.block = dim3(x, y);
+  const int x = per <= 8 ? 8 : per <= 16 ? 16 : static_cast<int>((per + 31) / 32 * 32), y = std::max(1, kRowThreads / x);
   const long long ctas = (n + y - 1) / y;
-  r.grid = dim3(static_cast<unsigned>(std::min<long long>(ctas, 152 * grid)), 1);
-  if (split && ctas < kFewCtas) r.grid.y = static_cast<unsigned>(std::min<long long>(laps, 64));
-  return r;
+  dim3 grid(1, 1);
+  if (split && ctas < kFewCtas) grid.y = static_cast<unsigned>(std::min<long long>(laps, 64));
+  grid.x = static_cast<unsigned>(ctas <= kFewCtas ? ctas : std::min<long long>(ctas, static_cast<long long>(kSms) * resident<KERNEL>(x * y) * waves));
+  return launch_pdl(KERNEL, grid, dim3(x, y), 0, s, 1, std::forward<A>(args)...);
 }
 
 template <typename F>
@@ -862,14 +882,12 @@ cudaError_t launch_permute(int elem_bytes, const void* x, long long ldx, void* y
   const uintptr_t at = bits(x) | bits(y) | static_cast<uintptr_t>((ldx | ldy) * elem_bytes);
   const long long bytes = static_cast<long long>(a.cols) * elem_bytes;
   if (at % 16 == 0 && bytes >= 16) {
-    const RowLaunch r = row_launch(a.n, bytes / 16, kCopyUnits, true, kGridCtas);
-    return launch_pdl(permute_kernel, r.grid, r.block, 0, s, 1, static_cast<const char*>(x), ldx * elem_bytes,
+    return launch_rows<permute_kernel>(a.n, bytes / 16, kCopyUnits, true, kRowThreads, kCopyWaves, s, static_cast<const char*>(x), ldx * elem_bytes,
                       static_cast<char*>(y), ldy * elem_bytes, bytes, a);
   }
   auto any = [&](auto elem) {
     using T = decltype(elem);
-    const RowLaunch r = row_launch(a.n, bytes / 16 + 2, kAnyUnits, true, kGridCtas);
-    return launch_pdl(permute_any_kernel<T>, r.grid, r.block, 0, s, 1, static_cast<const T*>(x), ldx, static_cast<T*>(y), ldy,
+    return launch_rows<permute_any_kernel<T>>(a.n, bytes / 16 + 2, kAnyUnits, true, kRowThreads, kCopyWaves, s, static_cast<const T*>(x), ldx, static_cast<T*>(y), ldy,
                       a);
   };
   return elem_bytes == 4 ? any(uint32_t{}) : elem_bytes == 2 ? any(uint16_t{}) : any(uint8_t{});
@@ -885,8 +903,8 @@ cudaError_t launch_unpermute(int type, const void* y, long long ldy, void* out, 
         constexpr int N = (ANY ? 16 : decltype(access)::value) / static_cast<int>(sizeof(T));
         constexpr int J = ANY ? std::min(4, decltype(places)::value) : decltype(places)::value;  // (registers)
         constexpr int C = units_of(decltype(access)::value, J);
-        const RowLaunch r = row_launch(a.n, ceil_div(a.cols, N) + ANY, C, true, kSumGrid);
-        return launch_pdl(unpermute_kernel<T, N, J, C, ANY>, r.grid, r.block, 0, s, 1, static_cast<const T*>(y), ldy,
+        return launch_rows<unpermute_kernel<T, N, J, C, ANY>>(a.n, ceil_div(a.cols, N) + ANY, C, true, kRowThreads, ANY ? kAnySumWaves : kSumWaves, s,
+                           static_cast<const T*>(y), ldy,
                           static_cast<T*>(out), ldo, a);
       });
     });
@@ -905,8 +923,10 @@ cudaError_t launch_unpermute_backward(int type, const void* d_out, long long ldo
         constexpr bool ANY = decltype(access)::value == 0;
         constexpr int N = (ANY ? 16 : decltype(access)::value) / static_cast<int>(sizeof(T));
         constexpr int J = ANY ? std::min(4, decltype(places)::value) : decltype(places)::value;  // (registers)
-        const RowLaunch r = row_launch(a.n, ceil_div(a.cols, N) + ANY, 1, false, kGradGrid);  // (a row's sums meet in its CTA)
-        return launch_pdl(unpermute_backward_kernel<T, N, J, ANY>, r.grid, r.block, 0, s, 1, static_cast<const T*>(d_out), ldo,
+        // (a row's sums meet in its CTA)
+        return launch_rows<unpermute_backward_kernel<T, N, J, ANY>>(a.n, ceil_div(a.cols, N) + ANY, 1, false, grad_threads<T, J, ANY>,
+                           kGradWaves, s,
+                           static_cast<const T*>(d_out), ldo,
                           static_cast<const T*>(y), ldy, static_cast<T*>(d_y), ldd, d_w, a);
       });
     });
@@ -922,12 +942,12 @@ cudaError_t launch_dequantize(int type, const void* q, long long ldq, const floa
     return by_alignment<T>(at, [&](auto access) {
       constexpr bool ANY = decltype(access)::value == 0;
       constexpr int N = (ANY ? 16 : decltype(access)::value) / static_cast<int>(sizeof(T));
-      const RowLaunch r = row_launch(a.n, ceil_div(a.cols, N) + ANY, ANY ? kAnyUnits : kDecodeUnits, true, kGridCtas);
+      const int units = ceil_div(a.cols, N) + ANY;
       if constexpr (ANY)
-        return launch_pdl(dequantize_any_kernel<T>, r.grid, r.block, 0, s, 1, static_cast<const uint8_t*>(q), ldq, scales,
+        return launch_rows<dequantize_any_kernel<T>>(a.n, units, kAnyUnits, true, kRowThreads, kCopyWaves, s, static_cast<const uint8_t*>(q), ldq, scales,
                           lds, static_cast<T*>(y), ldy, a);
       else
-        return launch_pdl(dequantize_kernel<T, N>, r.grid, r.block, 0, s, 1, static_cast<const uint8_t*>(q), ldq, scales, lds,
+        return launch_rows<dequantize_kernel<T, N>>(a.n, units, kDecodeUnits, true, kRowThreads, kCopyWaves, s, static_cast<const uint8_t*>(q), ldq, scales, lds,
                           static_cast<T*>(y), ldy, a);
     });
   });
