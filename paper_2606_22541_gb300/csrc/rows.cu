@@ -259,6 +259,7 @@ static_assert(kClusterEntries <= 8 * 1024 * kSortRounds && kSmallEntries <= 512 
 // CTA; a thread has every blockDim.x-th unit of its row.  With few rows the
 // columns are spread over gridDim.y CTAs as well.
 constexpr int kRowThreads = 256;
+constexpr int kSumThreads = 128;  // of a CTA of the kernels that wait for several rows: more CTAs an SM, so that some always have loads out
 constexpr int kCopyWaves = 8, kSumWaves = 1, kAnySumWaves = 2, kGradWaves = 4;  // CTAs of a grid at most, in waves
 constexpr int kSms = 152;
 constexpr int kFewCtas = kSms * 4;  // below this many CTAs a call is short of work
@@ -792,11 +793,10 @@ int resident(int threads) {
 // ``waves`` full waves at most, which then take more rows in turn.
 template <auto KERNEL, typename... A>
 cudaError_t launch_rows(long long n, long long units, int C, bool split, int most, int waves, cudaStream_t s, A&&... args) {
-  if (n > kSms) most = kRowThreads;
   const long long need = std::max<long long>(1, (units + C - 1) / C);
   const long long laps = (need + most - 1) / most;
   const long long per = (need + laps - 1) / laps;
-  const int x = per <= 8 ? 8 : per <= 16 ? 16 : static_cast<int>((per + 31) / 32 * 32), y = std::max(1, kRowThreads / x);
+  const int x = per <= 8 ? 8 : per <= 16 ? 16 : static_cast<int>((per + 31) / 32 * 32), y = std::max(1, std::min(most, kRowThreads) / x);
   const long long ctas = (n + y - 1) / y;
   dim3 grid(1, 1);
   if (split && ctas < kFewCtas) grid.y = static_cast<unsigned>(std::min<long long>(laps, 64));
@@ -903,7 +903,8 @@ cudaError_t launch_unpermute(int type, const void* y, long long ldy, void* out, 
         constexpr int N = (ANY ? 16 : decltype(access)::value) / static_cast<int>(sizeof(T));
         constexpr int J = ANY ? std::min(4, decltype(places)::value) : decltype(places)::value;  // (registers)
         constexpr int C = units_of(decltype(access)::value, J);
-        return launch_rows<unpermute_kernel<T, N, J, C, ANY>>(a.n, ceil_div(a.cols, N) + ANY, C, true, kRowThreads, ANY ? kAnySumWaves : kSumWaves, s,
+        return launch_rows<unpermute_kernel<T, N, J, C, ANY>>(a.n, ceil_div(a.cols, N) + ANY, C, true, ANY ? kRowThreads : kSumThreads,
+                                                              ANY ? kAnySumWaves : kSumWaves, s,
                            static_cast<const T*>(y), ldy,
                           static_cast<T*>(out), ldo, a);
       });
@@ -923,9 +924,9 @@ cudaError_t launch_unpermute_backward(int type, const void* d_out, long long ldo
         constexpr bool ANY = decltype(access)::value == 0;
         constexpr int N = (ANY ? 16 : decltype(access)::value) / static_cast<int>(sizeof(T));
         constexpr int J = ANY ? std::min(4, decltype(places)::value) : decltype(places)::value;  // (registers)
-        // (a row's sums meet in its CTA)
-        return launch_rows<unpermute_backward_kernel<T, N, J, ANY>>(a.n, ceil_div(a.cols, N) + ANY, 1, false, grad_threads<T, J, ANY>,
-                           kGradWaves, s,
+        // (a row's sums meet in its CTA: few rows have wide ones)
+        const int threads = a.n <= kSms ? grad_threads<T, J, ANY> : a.n <= kFewCtas ? kRowThreads : kSumThreads;
+        return launch_rows<unpermute_backward_kernel<T, N, J, ANY>>(a.n, ceil_div(a.cols, N) + ANY, 1, false, threads, kGradWaves, s,
                            static_cast<const T*>(d_out), ldo,
                           static_cast<const T*>(y), ldy, static_cast<T*>(d_y), ldd, d_w, a);
       });
