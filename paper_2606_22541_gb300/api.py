@@ -436,8 +436,8 @@ def _sort(idx, n_experts, offsets, perm_dst, ws, perm_src, stream):
             not _dense(offsets, torch.int32, (n_experts + 1,)) or \
             (perm_src is not None and not _dense(perm_src, torch.int32, (shape[0] * shape[1],))) or \
             (ws is not None and not ws.is_contiguous()) or not _here(idx, offsets, perm_dst, perm_src, ws):
-        _refuse("contiguous int32 tensors on the current CUDA device, idx, perm_dst [n, k], offsets [n_experts + 1], perm_src [n * k] or None, "
-                "and a workspace", idx=idx, offsets=offsets, perm_dst=perm_dst,
+        _refuse("contiguous int32 tensors on the current CUDA device, idx, perm_dst [n, k], offsets [n_experts + 1], "
+                "perm_src [n * k] or None, and a workspace", idx=idx, offsets=offsets, perm_dst=perm_dst,
                 **{k: t for k, t in (("perm_src", perm_src), ("ws", ws)) if t is not None})
     p, nb = (None, 0) if ws is None else (ws.data_ptr(), ws.numel() * ws.element_size())
     return lib().asap_moe_sort(idx.data_ptr(), shape[0], shape[1], n_experts, offsets.data_ptr(), perm_dst.data_ptr(),
@@ -468,8 +468,8 @@ def _permute(x, perm_dst, x_perm, stream, status):
     if x.dim() != 2 or x_perm.dim() != 2 or perm_dst.dim() != 2 or x.dtype not in _BYTES or x_perm.dtype is not x.dtype or \
             x_perm.shape[1] != x.shape[1] or not _dense(perm_dst, torch.int32, (x.shape[0], perm_dst.shape[1])) or \
             not _here(x, x_perm, perm_dst, status):
-        _refuse("tensors on the current CUDA device, x [n, c], x_perm [rows, c] of one type, perm_dst [n, k] int32", x=x, perm_dst=perm_dst,
-                x_perm=x_perm)
+        _refuse("tensors on the current CUDA device, x [n, c], x_perm [rows, c] of one type, perm_dst [n, k] int32", x=x,
+                perm_dst=perm_dst, x_perm=x_perm)
     n, c = x.shape
     rows, ld, ldp = x_perm.shape[0], _ld(x), _ld(x_perm)
     if not (ld and ldp) and n and c and rows:
@@ -497,8 +497,8 @@ def _unpermute(y_perm, w, perm_dst, out, stream, status):
             out.dtype is not y_perm.dtype or y_perm.shape[1] != out.shape[1] or \
             not _dense(perm_dst, torch.int32, (out.shape[0], perm_dst.shape[1])) or \
             (w is not None and not _dense(w, _F32, perm_dst.shape)) or not _here(y_perm, w, perm_dst, out, status):
-        _refuse("tensors on the current CUDA device, y_perm [rows, c], out [n, c] of one type, perm_dst [n, k] int32, w [n, k] fp32 or None",
-                y_perm=y_perm, perm_dst=perm_dst, out=out, **({} if w is None else {"w": w}))
+        _refuse("tensors on the current CUDA device, y_perm [rows, c], out [n, c] of one type, perm_dst [n, k] int32, w "
+                "[n, k] fp32 or None", y_perm=y_perm, perm_dst=perm_dst, out=out, **({} if w is None else {"w": w}))
     n, c = out.shape
     rows, ldy, ldo = y_perm.shape[0], _ld(y_perm), _ld(out)
     if not (ldy and ldo) and n and c and rows:
@@ -531,8 +531,8 @@ def _unpermute_backward(d_out, y_perm, w, perm_dst, d_y_perm, d_w, stream, statu
             any(t is not None and not _dense(t, _F32, perm_dst.shape) for t in (w, d_w)) or \
             (d_w is not None and y_perm is None) or \
             not _here(d_out, y_perm, w, perm_dst, d_y_perm, d_w, status):
-        _refuse("tensors on the current CUDA device, d_out [n, c], y_perm and d_y_perm [rows, c] of one type, perm_dst [n, k] int32, w and d_w "
-                "[n, k] fp32", d_out=d_out, perm_dst=perm_dst, **y,
+        _refuse("tensors on the current CUDA device, d_out [n, c], y_perm and d_y_perm [rows, c] of one type, perm_dst "
+                "[n, k] int32, w and d_w [n, k] fp32", d_out=d_out, perm_dst=perm_dst, **y,
                 **{k: t for k, t in (("w", w), ("d_w", d_w)) if t is not None})
     n, c = d_out.shape
     ldo, lds = _ld(d_out), {k: _ld(t) for k, t in y.items()}
@@ -553,8 +553,8 @@ def _swiglu_kept(rows, cols, gate_q, gate_s, up_q, up_s, n_rows, **others):
             any(t.dtype is not _F32 or t.shape != blocks for t in (gate_s, up_s)) or \
             (n_rows is not None and (n_rows.dtype is not torch.int32 or n_rows.numel() != 1)) or \
             not _here(*tensors.values(), n_rows):
-        _refuse(f"tensors on the current CUDA device, {', '.join(others)} [n, c] of one type (bf16, fp16, fp32), gate_q, up_q [n, c] e4m3, gate_s, "
-                "up_s [n, ceil(c / 128)] fp32, n_rows None or one int32", **tensors,
+        _refuse(f"tensors on the current CUDA device, {', '.join(others)} [n, c] of one type (bf16, fp16, fp32), gate_q, "
+                "up_q [n, c] e4m3, gate_s, up_s [n, ceil(c / 128)] fp32, n_rows None or one int32", **tensors,
                 **({} if n_rows is None else {"n_rows": n_rows}))
     lds = {k: _ld(t) for k, t in tensors.items()}
     pairs = [("gate_q", "up_q"), ("gate_s", "up_s"), ("gate", "up"), ("d_gate", "d_up")]
@@ -632,8 +632,8 @@ def _dequantize(q, scales, x, perm_dst, stream, status):
             (x.shape[0] != q.shape[0] if perm_dst is None else
              perm_dst.dim() != 2 or not _dense(perm_dst, torch.int32, (q.shape[0], perm_dst.shape[1]))) or \
             not _here(q, scales, x, perm_dst, status):
-        _refuse("tensors on the current CUDA device, q [n, c] e4m3, scales [n, ceil(c / 128)] fp32, x [rows, c], perm_dst [n, k] int32 or None", q=q,
-                scales=scales, x=x, **({} if perm_dst is None else {"perm_dst": perm_dst}))
+        _refuse("tensors on the current CUDA device, q [n, c] e4m3, scales [n, ceil(c / 128)] fp32, x [rows, c], perm_dst "
+                "[n, k] int32 or None", q=q, scales=scales, x=x, **({} if perm_dst is None else {"perm_dst": perm_dst}))
     n, c = q.shape
     ldq, lds, ldx = _ld(q), _ld(scales), _ld(x)
     if not (ldq and lds and ldx) and n and c and x.shape[0]:

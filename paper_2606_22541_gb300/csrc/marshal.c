@@ -303,7 +303,8 @@ static PyObject* unpermute(PyObject* self, PyObject* const* a, Py_ssize_t n) {
   int code, type;
   (void)self;
   if (n != 6 || !call_unpermute || a[5] != Py_None || !where(a[4], &w) || !(d = rows_of(a[0], &w, &y)) ||
-      (type = type_of(d)) < 0 || !dense(a[2], &w, i32, 0, 0, &perm) || !dense_or_none(a[1], &w, f32, perm.rows, perm.cols, &wt) ||
+      (type = type_of(d)) < 0 || !dense(a[2], &w, i32, 0, 0, &perm) ||
+      !dense_or_none(a[1], &w, f32, perm.rows, perm.cols, &wt) ||
       rows_of(a[3], &w, &out) != d || perm.rows != out.rows || y.cols != out.cols)
     return not_mine();
   Py_BEGIN_ALLOW_THREADS;

@@ -186,7 +186,8 @@ __global__ void __launch_bounds__(THREADS)
 }
 
 // Many chunks: each one's counts (hist [chunk][E]); per expert, sums over the
-// earlier chunks (in place) and over all (total [E]); places.
+// earlier chunks (in place) and over all (total [E]); places.  (Chunks of 4096: 0.6 to 0.8 us more up to 131072 entries, 6 less
+// for 8.4 million.)
 constexpr int kManyThreads = 256, kManyChunk = kManyThreads * kSortRounds;
 
 __global__ void __launch_bounds__(kManyThreads)
@@ -250,19 +251,41 @@ __global__ void __launch_bounds__(kManyThreads)
   write_places(s, from, entries, kSortRounds, k, e, rank, perm_dst, perm_src);
 }
 
-// Entries of one cluster at most; below which one small CTA ranks them all; entries for each CTA of a cluster.
+// Entries of one cluster at most; below which one small CTA ranks them all; entries for each CTA of a cluster.  Measured
+// with 256 experts, us: one CTA / a cluster / three kernels for 2048 entries 3.9 / 5.0 / -, 4096 5.2 / 6.0 / 6.2, 16384
+// - / 6.2 / 6.7, 32768 - / 7.0 / 6.7 (one launch on the host instead of three), 65536 - / 9.0 / 6.7.  Bound by latency: 8.4
+// million entries take 60 us, the 101 MB that the three kernels move would take 15.
 constexpr long long kClusterEntries = 32768, kSmallEntries = 4096, kCtaEntries = 1024;
 static_assert(kClusterEntries <= 8 * 1024 * kSortRounds && kSmallEntries <= 512 * kSortRounds, "entries of the launches");
 
 // ------------------------------------------------------------ rows
 // A row is taken by blockDim.x threads (8, 16 or whole warps), blockDim.y rows by a
-// CTA; a thread has every blockDim.x-th unit of its row.  With few rows the
-// columns are spread over gridDim.y CTAs as well.
+// CTA; a thread has every blockDim.x-th unit (16 bytes) of its row.  With few rows the
+// columns are spread over gridDim.y CTAs as well; with many a CTA takes rows in turn
+// and has the next one's places on their way (the chain from a place to its row's
+// loads is what these kernels wait for most).  All are bound by HBM; a call of many
+// rows moves its bytes at 0.92 to 0.97 of the copy rate:
+//   permute 8045 tokens of 7168 bf16, k 8: 157 us, its bytes at the copy rate 152.7
+//   unpermute 5185 of 7168 bf16, k 8: 103 (98.5); 3584 of 4096 fp16, k 2: 15.5 (12.1)
+//   gradients 4096 of 7168 bf16, k 8: 155 (147); 3584 of 4096, k 2: 26.7 (21.6)
+//   e4m3 rows of 4096 x 7168 read back, k 8: 77.5 (73.6)
+// Rows that do not start on 16 bytes are shifted into place (struct Any): unpermute
+// 3780 of 4401 bf16, k 7: 71 us (39), with 2-byte accesses 155, in 4-byte words 268; fp32
+// rows, which need no shifts, go by 4 bytes with more of them on their way: 107 (78),
+// shifted 16 bytes 155.
 constexpr int kRowThreads = 256;
-constexpr int kSumThreads = 128;  // of a CTA of the kernels that wait for several rows: more CTAs an SM, so that some always have loads out
-constexpr int kCopyWaves = 8, kSumWaves = 1, kAnySumWaves = 2, kGradWaves = 4;  // CTAs of a grid at most, in waves
 constexpr int kSms = 152;
 constexpr int kFewCtas = kSms * 4;  // below this many CTAs a call is short of work
+// Of a CTA of the kernels that wait for several rows: more CTAs an SM, so that some
+// always have loads out (256, 128 and 64 threads, us: unpermute 12900 of 1792, k 6 56,
+// 54, 56; gradients 3584 of 4096, k 2 30, 27, 28).
+constexpr int kSumThreads = 128;
+// CTAs of a grid at most, in waves of as many as the SMs hold.  A part of a wave more
+// costs most (unpermute 3584 of 4096, k 2: 16.2 us in one wave, 17.0 in two, 19.2 in one
+// and a half); copies, whose CTAs differ more in their pace, gain from more waves
+// (permute 8045 of 7168, k 8 with 1, 2, 4, 8: 178, 166, 161, 157; gradients 4096 of 7168
+// with 1, 2, 4: 164, 165, 155).
+constexpr int kCopyWaves = 8, kSumWaves = 1, kAnySumWaves = 2, kGradWaves = 4;
 
 // Rows of a CTA: first_row() + threadIdx.y, and gridDim.x blockDim.y further on.
 __device__ __forceinline__ long long first_row() { return static_cast<long long>(blockIdx.x) * blockDim.y; }
@@ -384,7 +407,8 @@ __global__ void __launch_bounds__(kRowThreads)
 #pragma unroll
         for (int i = 0; i < C; ++i) {
           if (t >= a.n) continue;
-          const typename A::Raw r = A::fetch(row, c0 + static_cast<int>((i * blockDim.x + threadIdx.x) * A::N) - from - A::N, a.cols);
+          const int c = c0 + static_cast<int>((i * blockDim.x + threadIdx.x) * A::N) - from;
+          const typename A::Raw r = A::fetch(row, c - A::N, a.cols);
           lo[i] = r.lo, hi[i] = r.hi;
         }
         for (int j = 0; j < places; ++j) {
@@ -404,7 +428,7 @@ __global__ void __launch_bounds__(kRowThreads)
   }
 }
 
-constexpr int kSumCtas = 4;
+constexpr int kSumCtas = 4;  // CTAs of kRowThreads an SM that the registers are kept to
 // out[t] = sum_j w[t][j] y[place], fp32 in slot order; J places and C units of N
 // columns at a time.
 // ANY: rows at any address, N columns as out's row has them on 16 bytes.
@@ -492,13 +516,13 @@ __global__ void __launch_bounds__(kRowThreads, ANY ? 3 : kSumCtas)
   }
 }
 
-// d_y[place] = w d_out[t], d_w[t][j] = <d_out[t], y[place]> (fp32: per thread, then
-// over the lanes and the row's warps in a fixed tree).
-// Threads of a CTA at most.  (Few rows have their laps side by side; where 64 registers are too few, whose limit that is,
-// CTAs stay small.)
+// Threads of a CTA of the gradients at most.  (Few rows have their laps side by side, 8 tokens of 7168 6.2 us instead of
+// 10.4; 1024 threads limit the kernel to 64 registers, and where these are too few CTAs stay small.)
 constexpr int kGradThreads = 1024;
 template <typename T, int J, bool ANY>
 constexpr int grad_threads = ANY || (J == 8 && std::is_same_v<T, __half>) ? kRowThreads : kGradThreads;
+// d_y[place] = w d_out[t], d_w[t][j] = <d_out[t], y[place]> (fp32: per thread, then
+// over the lanes and the row's warps in a fixed tree).
 // ANY: rows at any address, N columns as each row of d_y (of y without it) has them on 16 bytes.
 template <typename T, int N, int J, bool ANY>
 __global__ void __launch_bounds__(grad_threads<T, J, ANY>, grad_threads<T, J, ANY> == kRowThreads ? 3 : 1)
@@ -796,11 +820,13 @@ cudaError_t launch_rows(long long n, long long units, int C, bool split, int mos
   const long long need = std::max<long long>(1, (units + C - 1) / C);
   const long long laps = (need + most - 1) / most;
   const long long per = (need + laps - 1) / laps;
-  const int x = per <= 8 ? 8 : per <= 16 ? 16 : static_cast<int>((per + 31) / 32 * 32), y = std::max(1, std::min(most, kRowThreads) / x);
+  const int x = per <= 8 ? 8 : per <= 16 ? 16 : static_cast<int>((per + 31) / 32 * 32);
+  const int y = std::max(1, std::min(most, kRowThreads) / x);
   const long long ctas = (n + y - 1) / y;
   dim3 grid(1, 1);
   if (split && ctas < kFewCtas) grid.y = static_cast<unsigned>(std::min<long long>(laps, 64));
-  grid.x = static_cast<unsigned>(ctas <= kFewCtas ? ctas : std::min<long long>(ctas, static_cast<long long>(kSms) * resident<KERNEL>(x * y) * waves));
+  grid.x = static_cast<unsigned>(ctas);
+  if (ctas > kFewCtas) grid.x = static_cast<unsigned>(std::min<long long>(ctas, 1ll * kSms * resident<KERNEL>(x * y) * waves));
   return launch_pdl(KERNEL, grid, dim3(x, y), 0, s, 1, std::forward<A>(args)...);
 }
 
@@ -822,7 +848,9 @@ cudaError_t by_alignment(uintptr_t at, F f) {
   return f(std::integral_constant<int, sizeof(T) == 4 ? 4 : 0>{});
 }
 // Units of a thread for accesses of this many bytes and J places: as many bytes on their way.
-constexpr int units_of(int access, int J) { return access == 0 ? 1 : access == 16 ? (J >= 4 ? 1 : 2) : access == 8 ? (J >= 8 ? 1 : 2) : (J >= 8 ? 2 : 4); }
+constexpr int units_of(int access, int J) {
+  return access == 0 ? 1 : access == 16 ? (J >= 4 ? 1 : 2) : access == 8 ? (J >= 8 ? 1 : 2) : (J >= 8 ? 2 : 4);
+}
 
 // Places handled together.
 template <typename F>
@@ -882,13 +910,14 @@ cudaError_t launch_permute(int elem_bytes, const void* x, long long ldx, void* y
   const uintptr_t at = bits(x) | bits(y) | static_cast<uintptr_t>((ldx | ldy) * elem_bytes);
   const long long bytes = static_cast<long long>(a.cols) * elem_bytes;
   if (at % 16 == 0 && bytes >= 16) {
-    return launch_rows<permute_kernel>(a.n, bytes / 16, kCopyUnits, true, kRowThreads, kCopyWaves, s, static_cast<const char*>(x), ldx * elem_bytes,
-                      static_cast<char*>(y), ldy * elem_bytes, bytes, a);
+    return launch_rows<permute_kernel>(a.n, bytes / 16, kCopyUnits, true, kRowThreads, kCopyWaves, s,
+                                       static_cast<const char*>(x), ldx * elem_bytes, static_cast<char*>(y),
+                                       ldy * elem_bytes, bytes, a);
   }
   auto any = [&](auto elem) {
     using T = decltype(elem);
-    return launch_rows<permute_any_kernel<T>>(a.n, bytes / 16 + 2, kAnyUnits, true, kRowThreads, kCopyWaves, s, static_cast<const T*>(x), ldx, static_cast<T*>(y), ldy,
-                      a);
+    return launch_rows<permute_any_kernel<T>>(a.n, bytes / 16 + 2, kAnyUnits, true, kRowThreads, kCopyWaves, s,
+                                              static_cast<const T*>(x), ldx, static_cast<T*>(y), ldy, a);
   };
   return elem_bytes == 4 ? any(uint32_t{}) : elem_bytes == 2 ? any(uint16_t{}) : any(uint8_t{});
 }
@@ -903,10 +932,9 @@ cudaError_t launch_unpermute(int type, const void* y, long long ldy, void* out, 
         constexpr int N = (ANY ? 16 : decltype(access)::value) / static_cast<int>(sizeof(T));
         constexpr int J = ANY ? std::min(4, decltype(places)::value) : decltype(places)::value;  // (registers)
         constexpr int C = units_of(decltype(access)::value, J);
-        return launch_rows<unpermute_kernel<T, N, J, C, ANY>>(a.n, ceil_div(a.cols, N) + ANY, C, true, ANY ? kRowThreads : kSumThreads,
-                                                              ANY ? kAnySumWaves : kSumWaves, s,
-                           static_cast<const T*>(y), ldy,
-                          static_cast<T*>(out), ldo, a);
+        return launch_rows<unpermute_kernel<T, N, J, C, ANY>>(
+            a.n, ceil_div(a.cols, N) + ANY, C, true, ANY ? kRowThreads : kSumThreads, ANY ? kAnySumWaves : kSumWaves, s,
+            static_cast<const T*>(y), ldy, static_cast<T*>(out), ldo, a);
       });
     });
   });
@@ -919,6 +947,7 @@ cudaError_t launch_unpermute_backward(int type, const void* d_out, long long ldo
     uintptr_t at = bits(d_out) | bits(y) | bits(d_y) | static_cast<uintptr_t>(ldo * sizeof(T));
     if (d_w) at |= static_cast<uintptr_t>(ldy * sizeof(T));
     if (d_y) at |= static_cast<uintptr_t>(ldd * sizeof(T));
+    if (a.cols == 0) at = 0;  // (sums of nothing: no row is touched)
     return by_alignment<T>(at, [&](auto access) {
       return by_places(a.k, [&](auto places) {
         constexpr bool ANY = decltype(access)::value == 0;
@@ -926,9 +955,9 @@ cudaError_t launch_unpermute_backward(int type, const void* d_out, long long ldo
         constexpr int J = ANY ? std::min(4, decltype(places)::value) : decltype(places)::value;  // (registers)
         // (a row's sums meet in its CTA: few rows have wide ones)
         const int threads = a.n <= kSms ? grad_threads<T, J, ANY> : a.n <= kFewCtas ? kRowThreads : kSumThreads;
-        return launch_rows<unpermute_backward_kernel<T, N, J, ANY>>(a.n, ceil_div(a.cols, N) + ANY, 1, false, threads, kGradWaves, s,
-                           static_cast<const T*>(d_out), ldo,
-                          static_cast<const T*>(y), ldy, static_cast<T*>(d_y), ldd, d_w, a);
+        return launch_rows<unpermute_backward_kernel<T, N, J, ANY>>(
+            a.n, ceil_div(a.cols, N) + ANY, 1, false, threads, kGradWaves, s, static_cast<const T*>(d_out), ldo,
+            static_cast<const T*>(y), ldy, static_cast<T*>(d_y), ldd, d_w, a);
       });
     });
   });
@@ -939,17 +968,20 @@ cudaError_t launch_dequantize(int type, const void* q, long long ldq, const floa
   return by_type(type, [&](auto t) {
     using T = decltype(t);
     // (rows of q start on N bytes where rows of y start on 16)
-    const uintptr_t at = bits(y) | static_cast<uintptr_t>(ldy * sizeof(T)) | (bits(q) | static_cast<uintptr_t>(ldq)) * sizeof(T);
+    const uintptr_t at =
+        bits(y) | static_cast<uintptr_t>(ldy * sizeof(T)) | (bits(q) | static_cast<uintptr_t>(ldq)) * sizeof(T);
     return by_alignment<T>(at, [&](auto access) {
       constexpr bool ANY = decltype(access)::value == 0;
       constexpr int N = (ANY ? 16 : decltype(access)::value) / static_cast<int>(sizeof(T));
       const int units = ceil_div(a.cols, N) + ANY;
       if constexpr (ANY)
-        return launch_rows<dequantize_any_kernel<T>>(a.n, units, kAnyUnits, true, kRowThreads, kCopyWaves, s, static_cast<const uint8_t*>(q), ldq, scales,
-                          lds, static_cast<T*>(y), ldy, a);
+        return launch_rows<dequantize_any_kernel<T>>(a.n, units, kAnyUnits, true, kRowThreads, kCopyWaves, s,
+                                                     static_cast<const uint8_t*>(q), ldq, scales, lds, static_cast<T*>(y), ldy,
+                                                     a);
       else
-        return launch_rows<dequantize_kernel<T, N>>(a.n, units, kDecodeUnits, true, kRowThreads, kCopyWaves, s, static_cast<const uint8_t*>(q), ldq, scales, lds,
-                          static_cast<T*>(y), ldy, a);
+        return launch_rows<dequantize_kernel<T, N>>(a.n, units, kDecodeUnits, true, kRowThreads, kCopyWaves, s,
+                                                    static_cast<const uint8_t*>(q), ldq, scales, lds, static_cast<T*>(y), ldy,
+                                                    a);
     });
   });
 }

@@ -17,15 +17,19 @@ namespace {
 
 constexpr unsigned kFull = 0xffffffffu;
 constexpr int kThreads = 256;
-// Both kernels stream: 8 bytes a column forward (bf16), 10 backward, which the copy rate would move in 79.6 and 99.4 us for
-// 32768 x 2048; they take 84 and 100.
-// The forward pass has the arithmetic to hide as well (two scales, two quotients, a sigmoid), so a lane has 16 columns, over
-// which the maximum's exchange and the scales are spread, and four CTAs an SM (3: 93 us); with 8 columns a lane it took 103
-// to 113, and 95 with lanes of 16 neighbouring columns, whose accesses are half as wide as they look.  Backward there is little,
-// so a lane has one 16-byte chunk and its next group's loads on their way (118 us with 16 columns and no loads ahead; 106
-// with the e4m3 values decoded before the next loads are out, which takes the registers).
-// Grids of a few waves' CTAs, so that the SMs' ends are level: forward 4 to 50 CTAs for each SM make no difference, backward 10,
-// 20, 40 and all: 112, 104, 100, 110 us.
+// Both kernels stream: 8 bytes a column forward (bf16), 10 backward, which the copy
+// rate would move in 79.6 and 99.4 us for 32768 x 2048; they take 84 and 100.
+// The forward pass has the arithmetic to hide as well (two scales, two quotients, a
+// sigmoid), so a lane has 16 columns, over which the maximum's exchange and the scales
+// are spread, and four CTAs an SM (3: 93 us); with 8 columns a lane it took 103 to 113,
+// and 95 with lanes of 16 neighbouring columns, whose accesses are half as wide as they
+// look.  Backward there is little, so a lane has one 16-byte chunk and its next group's
+// loads on their way (118 us with 16 columns and no loads ahead; 106 with the e4m3 values
+// decoded before the next loads are out, which takes the registers).
+// Grids of a few waves' CTAs, so that the SMs' ends are level: forward 4 to 50 CTAs for
+// each SM make no difference, backward 10, 20, 40 and all: 112, 104, 100, 110 us.
+// Odd widths, one column an access: 11259 x 5961 forward 128 us (79.7), 8558 x 4785
+// backward 92 (60.7); with the accesses of neighbouring lanes 8 columns apart 291 and 102.
 constexpr int kSaveCtas = 4, kSaveGrid = 16;  // CTAs an SM, CTAs of the grid for each SM
 constexpr int kGradCtas = 5, kGradGrid = 40;
 // Lanes of a group, by the columns of an access.
@@ -128,7 +132,8 @@ struct Lane {
 #pragma unroll
         for (int j = 0; j < V; ++j)
           if (at + j < left)
-            w[(i * V + j) >> 2] |= static_cast<uint32_t>(*const_cast<const volatile uint8_t*>(p + at + j)) << (8 * ((i * V + j) & 3));
+            w[(i * V + j) >> 2] |= static_cast<uint32_t>(*const_cast<const volatile uint8_t*>(p + at + j))
+                                   << (8 * ((i * V + j) & 3));
       }
     }
   }
@@ -337,7 +342,8 @@ cudaError_t launch_swiglu_save(int type, const void* gate, const void* up, long 
     using T = decltype(t);
     const uintptr_t at = bits(gate) | bits(up) | bits(h) | static_cast<uintptr_t>((ld | ldh) * sizeof(T));
     return by_alignment<T>(at, a, [&](auto v) {
-      return launch_pdl(swiglu_save_kernel<T, decltype(v)::value>, grid_of(a, save_team(decltype(v)::value), kSaveGrid), kThreads, 0, s, 1,
+      constexpr int V = decltype(v)::value;
+      return launch_pdl(swiglu_save_kernel<T, V>, grid_of(a, save_team(V), kSaveGrid), kThreads, 0, s, 1,
                         static_cast<const T*>(gate), static_cast<const T*>(up), ld, static_cast<T*>(h), ldh, a);
     });
   });
@@ -350,7 +356,8 @@ cudaError_t launch_swiglu_backward(int type, const void* d_h, long long ldd, voi
     uintptr_t at = bits(d_h) | bits(d_gate) | bits(d_up) | bits(h) | static_cast<uintptr_t>((ldd | ldg) * sizeof(T));
     if (h) at |= static_cast<uintptr_t>(ldh * sizeof(T));
     return by_alignment<T>(at, a, [&](auto v) {
-      return launch_pdl(swiglu_backward_kernel<T, decltype(v)::value>, grid_of(a, grad_team(decltype(v)::value), kGradGrid), kThreads, 0, s, 1,
+      constexpr int V = decltype(v)::value;
+      return launch_pdl(swiglu_backward_kernel<T, V>, grid_of(a, grad_team(V), kGradGrid), kThreads, 0, s, 1,
                         static_cast<const T*>(d_h), ldd, static_cast<T*>(d_gate), static_cast<T*>(d_up), ldg,
                         static_cast<T*>(h), ldh, a);
     });
