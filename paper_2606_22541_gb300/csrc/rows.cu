@@ -9,7 +9,6 @@
 
 #include <algorithm>
 #include <atomic>
-#include <utility>
 
 namespace asap {
 
@@ -815,19 +814,21 @@ int resident(int threads) {
 // few threads as a row needs, in equal laps where it needs more than a CTA has;
 // laps side by side (split) while the rows alone would leave SMs without work.  CTAs of
 // ``waves`` full waves at most, which then take more rows in turn.
-template <auto KERNEL, typename... A>
-cudaError_t launch_rows(long long n, long long units, int C, bool split, int most, int waves, cudaStream_t s, A&&... args) {
+struct RowLaunch {
+  dim3 grid, block;
+};
+template <auto KERNEL>
+RowLaunch row_launch(long long n, long long units, int C, bool split, int most, int waves) {
   const long long need = std::max<long long>(1, (units + C - 1) / C);
   const long long laps = (need + most - 1) / most;
   const long long per = (need + laps - 1) / laps;
   const int x = per <= 8 ? 8 : per <= 16 ? 16 : static_cast<int>((per + 31) / 32 * 32);
   const int y = std::max(1, std::min(most, kRowThreads) / x);
   const long long ctas = (n + y - 1) / y;
-  dim3 grid(1, 1);
+  dim3 grid(static_cast<unsigned>(ctas), 1);
   if (split && ctas < kFewCtas) grid.y = static_cast<unsigned>(std::min<long long>(laps, 64));
-  grid.x = static_cast<unsigned>(ctas);
   if (ctas > kFewCtas) grid.x = static_cast<unsigned>(std::min<long long>(ctas, 1ll * kSms * resident<KERNEL>(x * y) * waves));
-  return launch_pdl(KERNEL, grid, dim3(x, y), 0, s, 1, std::forward<A>(args)...);
+  return {grid, dim3(x, y)};
 }
 
 template <typename F>
@@ -910,14 +911,15 @@ cudaError_t launch_permute(int elem_bytes, const void* x, long long ldx, void* y
   const uintptr_t at = bits(x) | bits(y) | static_cast<uintptr_t>((ldx | ldy) * elem_bytes);
   const long long bytes = static_cast<long long>(a.cols) * elem_bytes;
   if (at % 16 == 0 && bytes >= 16) {
-    return launch_rows<permute_kernel>(a.n, bytes / 16, kCopyUnits, true, kRowThreads, kCopyWaves, s,
-                                       static_cast<const char*>(x), ldx * elem_bytes, static_cast<char*>(y),
-                                       ldy * elem_bytes, bytes, a);
+    const RowLaunch r = row_launch<permute_kernel>(a.n, bytes / 16, kCopyUnits, true, kRowThreads, kCopyWaves);
+    return launch_pdl(permute_kernel, r.grid, r.block, 0, s, 1, static_cast<const char*>(x), ldx * elem_bytes,
+                      static_cast<char*>(y), ldy * elem_bytes, bytes, a);
   }
   auto any = [&](auto elem) {
     using T = decltype(elem);
-    return launch_rows<permute_any_kernel<T>>(a.n, bytes / 16 + 2, kAnyUnits, true, kRowThreads, kCopyWaves, s,
-                                              static_cast<const T*>(x), ldx, static_cast<T*>(y), ldy, a);
+    const RowLaunch r = row_launch<permute_any_kernel<T>>(a.n, bytes / 16 + 2, kAnyUnits, true, kRowThreads, kCopyWaves);
+    return launch_pdl(permute_any_kernel<T>, r.grid, r.block, 0, s, 1, static_cast<const T*>(x), ldx, static_cast<T*>(y), ldy,
+                      a);
   };
   return elem_bytes == 4 ? any(uint32_t{}) : elem_bytes == 2 ? any(uint16_t{}) : any(uint8_t{});
 }
@@ -932,9 +934,10 @@ cudaError_t launch_unpermute(int type, const void* y, long long ldy, void* out, 
         constexpr int N = (ANY ? 16 : decltype(access)::value) / static_cast<int>(sizeof(T));
         constexpr int J = ANY ? std::min(4, decltype(places)::value) : decltype(places)::value;  // (registers)
         constexpr int C = units_of(decltype(access)::value, J);
-        return launch_rows<unpermute_kernel<T, N, J, C, ANY>>(
-            a.n, ceil_div(a.cols, N) + ANY, C, true, ANY ? kRowThreads : kSumThreads, ANY ? kAnySumWaves : kSumWaves, s,
-            static_cast<const T*>(y), ldy, static_cast<T*>(out), ldo, a);
+        const RowLaunch r = row_launch<unpermute_kernel<T, N, J, C, ANY>>(
+            a.n, ceil_div(a.cols, N) + ANY, C, true, ANY ? kRowThreads : kSumThreads, ANY ? kAnySumWaves : kSumWaves);
+        return launch_pdl(unpermute_kernel<T, N, J, C, ANY>, r.grid, r.block, 0, s, 1, static_cast<const T*>(y), ldy,
+                          static_cast<T*>(out), ldo, a);
       });
     });
   });
@@ -955,9 +958,10 @@ cudaError_t launch_unpermute_backward(int type, const void* d_out, long long ldo
         constexpr int J = ANY ? std::min(4, decltype(places)::value) : decltype(places)::value;  // (registers)
         // (a row's sums meet in its CTA: few rows have wide ones)
         const int threads = a.n <= kSms ? grad_threads<T, J, ANY> : a.n <= kFewCtas ? kRowThreads : kSumThreads;
-        return launch_rows<unpermute_backward_kernel<T, N, J, ANY>>(
-            a.n, ceil_div(a.cols, N) + ANY, 1, false, threads, kGradWaves, s, static_cast<const T*>(d_out), ldo,
-            static_cast<const T*>(y), ldy, static_cast<T*>(d_y), ldd, d_w, a);
+        const RowLaunch r = row_launch<unpermute_backward_kernel<T, N, J, ANY>>(a.n, ceil_div(a.cols, N) + ANY, 1, false,
+                                                                                threads, kGradWaves);
+        return launch_pdl(unpermute_backward_kernel<T, N, J, ANY>, r.grid, r.block, 0, s, 1, static_cast<const T*>(d_out),
+                          ldo, static_cast<const T*>(y), ldy, static_cast<T*>(d_y), ldd, d_w, a);
       });
     });
   });
@@ -974,14 +978,15 @@ cudaError_t launch_dequantize(int type, const void* q, long long ldq, const floa
       constexpr bool ANY = decltype(access)::value == 0;
       constexpr int N = (ANY ? 16 : decltype(access)::value) / static_cast<int>(sizeof(T));
       const int units = ceil_div(a.cols, N) + ANY;
-      if constexpr (ANY)
-        return launch_rows<dequantize_any_kernel<T>>(a.n, units, kAnyUnits, true, kRowThreads, kCopyWaves, s,
-                                                     static_cast<const uint8_t*>(q), ldq, scales, lds, static_cast<T*>(y), ldy,
-                                                     a);
-      else
-        return launch_rows<dequantize_kernel<T, N>>(a.n, units, kDecodeUnits, true, kRowThreads, kCopyWaves, s,
-                                                    static_cast<const uint8_t*>(q), ldq, scales, lds, static_cast<T*>(y), ldy,
-                                                    a);
+      if constexpr (ANY) {
+        const RowLaunch r = row_launch<dequantize_any_kernel<T>>(a.n, units, kAnyUnits, true, kRowThreads, kCopyWaves);
+        return launch_pdl(dequantize_any_kernel<T>, r.grid, r.block, 0, s, 1, static_cast<const uint8_t*>(q), ldq, scales, lds,
+                          static_cast<T*>(y), ldy, a);
+      } else {
+        const RowLaunch r = row_launch<dequantize_kernel<T, N>>(a.n, units, kDecodeUnits, true, kRowThreads, kCopyWaves);
+        return launch_pdl(dequantize_kernel<T, N>, r.grid, r.block, 0, s, 1, static_cast<const uint8_t*>(q), ldq, scales, lds,
+                          static_cast<T*>(y), ldy, a);
+      }
     });
   });
 }
