@@ -166,7 +166,9 @@ struct Any {
     return v;
   }
   // The N columns ``pre`` before those of hi, lo being the N before it.
-  __device__ static __forceinline__ V before(const V& lo, const V& hi, int pre) { return shifted(lo, hi, 16 - pre * kSize); }
+  __device__ static __forceinline__ V before(const V& lo, const V& hi, int pre) {
+    return pre == 0 ? hi : shifted(lo, hi, 16 - pre * kSize);
+  }
 
   // Columns c .. c + N - 1 of a row (cols > 0, c > -N) in two steps, so that several rows' loads are on their way before the
   // first is looked at: the two aligned 16 bytes that hold them, then the columns.  Of the 16 bytes only those that hold
@@ -186,7 +188,8 @@ struct Any {
     return r;
   }
   __device__ static __forceinline__ V columns(const Raw& r, const T* row, int c) {
-    return shifted(r.lo, r.hi, static_cast<int>(reinterpret_cast<uintptr_t>(row + c) & 15));
+    const int o = static_cast<int>(reinterpret_cast<uintptr_t>(row + c) & 15);
+    return o == 0 ? r.lo : shifted(r.lo, r.hi, o);
   }
   // Columns c .. c + N - 1 back into a row, c on a boundary: those inside it.
   __device__ static __forceinline__ void store(T* row, int c, int cols, const V& v) {
