@@ -295,7 +295,7 @@ __global__ void __launch_bounds__(kThreads, kGradCtas)
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         const float s = j ? s2.y : s2.x, t = g[i + j] * s;
-        dg[i + j] = d[i + j] * u[i + j] * fmaf(t, 1.0f - s, s);
+        dg[i + j] = d[i + j] * fmaf(t, 1.0f - s, s) * u[i + j];  // (d u alone may pass fp32 where the slope is 0)
         du[i + j] = d[i + j] * t;
         u[i + j] *= t;
       }

@@ -72,6 +72,22 @@ def test_widest_rows(c):
     assert torch.equal(near[0], out[:, -tail.shape[1]:]) and torch.equal(near[1], d_up[:, -tail.shape[1]:])
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_closed_gates_under_the_largest_values(dtype):
+    """A gate far below zero closes whatever stands beside it: results and gradients of 0, not of infinity times 0."""
+    n, c = 3, 300
+    big = torch.finfo(dtype).max / 4
+    g = torch.full((n, c), -1e5, device=DEV).to(dtype)
+    u = torch.full((n, c), big, device=DEV).to(dtype)
+    d = torch.full((n, c), 100.0, device=DEV).to(dtype)
+    q, s = [torch.empty((n, c), dtype=F8, device=DEV) for _ in range(2)], [torch.empty((n, 3), device=DEV) for _ in range(2)]
+    h, dg, du, h2 = (torch.full((n, c), 5.0, device=DEV).to(dtype) for _ in range(4))
+    api.asap_moe_swiglu_save(g, u, h, q[0], s[0], q[1], s[1])
+    api.asap_moe_swiglu_backward(d, q[0], s[0], q[1], s[1], dg, du, h2)
+    for t in (h, dg, du, h2):
+        assert (t == 0).all()
+
+
 FIRST = """
 import torch
 from paper_2606_22541_gb300 import api
