@@ -125,7 +125,8 @@ def fast():
             _marshal.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
                 L.asap_moe_fp8_quantize, L.asap_moe_fp8_swiglu_quantize, L.asap_moe_fp8_matmul)),
                 torch.bfloat16, torch.float32, torch.float8_e4m3fn, torch.uint8,
-                torch.cuda.current_device, torch._C._cuda_getCurrentRawStream)
+                # (torch.cuda.current_device without its check that CUDA has started, 0.1 us: the tensors are on the GPU)
+                torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream)
             _marshal.bind_rows(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
                 L.asap_moe_sort, L.asap_moe_permute, L.asap_moe_unpermute, L.asap_moe_unpermute_backward,
                 L.asap_moe_swiglu_save, L.asap_moe_swiglu_backward, L.asap_moe_fp8_dequantize)),
