@@ -466,10 +466,11 @@ int asap_moe_fp8_matmul(const void* a, int64_t lda, const float* a_scales, int64
  * sorted by expert and back with the gradients of both, and SwiGLU whose
  * activations are kept for the backward pass in e4m3.  No handle; they launch
  * on the caller's current device and only enqueue.  Strides (ld*) are in
- * elements between rows and at least the rows' length; no extent may exceed
- * 2^30, n * k stays below 2^31, k >= 1.  Any column count, stride and alignment
- * (rows that start on 16-byte boundaries are the fast ones).  Outputs must not
- * overlap inputs or each other.  The same call gives the same bits each time.
+ * elements between rows and at least the rows' length; no extent (n, k, rows,
+ * cols) may exceed 2^30, n * k stays below 2^31, k >= 1.  Any column count, stride
+ * and alignment (rows that start on 16-byte boundaries are the fast ones).  Outputs
+ * must not overlap inputs or each other.  The same call gives the same bits each
+ * time.
  *
  * perm_dst [n, k] int32: the row of (token t, slot j) among the rows of x_perm or
  * y_perm, -1 where no expert takes the entry.  A row outside [0, rows) is treated

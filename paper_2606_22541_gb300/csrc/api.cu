@@ -1574,7 +1574,9 @@ int check_rows(int32_t n, int32_t k, int32_t rows, int32_t cols, const int32_t* 
                const uint32_t* status) {
   if (n < 0 || rows < 0 || cols < 0 || n > kMaxExtent || rows > kMaxExtent || cols > kMaxExtent)
     return fail(ASAP_ERR_INVALID, "n, rows and cols must be in [0, 2^30]");
-  if (k < 1 || static_cast<long long>(n) * k > INT32_MAX) return fail(ASAP_ERR_INVALID, "k must be at least 1, n * k below 2^31");
+  // (the loops over a token's places count in int, with a step beyond the last)
+  if (k < 1 || k > kMaxExtent || static_cast<long long>(n) * k > INT32_MAX)
+    return fail(ASAP_ERR_INVALID, "k must be in [1, 2^30], n * k below 2^31");
   if (n > 0 && !perm_dst) return fail(ASAP_ERR_INVALID, "NULL tensor");
   if (!on(perm_dst, 4) || !on(w, 4) || !on(status, 4))
     return fail(ASAP_ERR_INVALID, "tensors must be aligned to their elements");
@@ -1608,8 +1610,8 @@ asap::RowsArgs rows_args(const int32_t* perm_dst, int32_t n, int32_t k, int32_t 
 }
 
 int check_sort(int32_t n, int32_t k, int32_t n_experts) {
-  if (n < 0 || k < 1 || n > kMaxExtent || static_cast<long long>(n) * k > INT32_MAX)
-    return fail(ASAP_ERR_INVALID, "n must be in [0, 2^30], k at least 1, n * k below 2^31");
+  if (n < 0 || k < 1 || n > kMaxExtent || k > kMaxExtent || static_cast<long long>(n) * k > INT32_MAX)
+    return fail(ASAP_ERR_INVALID, "n must be in [0, 2^30], k in [1, 2^30], n * k below 2^31");
   if (n_experts < 1 || n_experts > asap::kSortMaxExperts)
     return fail(ASAP_ERR_INVALID, "n_experts must be in [1, " + std::to_string(asap::kSortMaxExperts) + "]");
   return ASAP_OK;
