@@ -294,8 +294,13 @@ __global__ void __launch_bounds__(kThreads, kGradCtas)
       const float2 s2 = unpair(sigmoid2<T>(pair(g[i], g[i + 1])));
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        const float s = j ? s2.y : s2.x, t = g[i + j] * s;
-        dg[i + j] = d[i + j] * fmaf(t, 1.0f - s, s) * u[i + j];  // (d u alone may pass fp32 where the slope is 0)
+        const float s = j ? s2.y : s2.x, t = g[i + j] * s, slope = fmaf(t, 1.0f - s, s), p = d[i + j] * u[i + j];
+        // The slope is at most 1.1, so (d u) slope loses bits only where the result is below 2^-126.  Where d u passes
+        // fp32 the slope goes before u: it may be 0, and a closed gate's gradient meets no infinity.  (d slope always
+        // first lost results whose d slope is below 2^-126; it took 0.2 us less of 101 for 32768 x 2048, 0.6 of 45 for
+        // 1996 x 14336, 0.9 of 21 for 31962 x 288.)
+        dg[i + j] = p * slope;
+        if (isinf(p)) dg[i + j] = d[i + j] * slope * u[i + j];
         du[i + j] = d[i + j] * t;
         u[i + j] *= t;
       }
