@@ -527,18 +527,19 @@ int asap_moe_unpermute_backward(int32_t type, const void* d_out, int64_t ldo, co
 
 /* h = silu(gate) * up (fp32, rounded to the type), and gate and up kept for
  * asap_moe_swiglu_backward in e4m3 with a scale per row per 128 columns, as
- * asap_moe_fp8_quantize would quantise them.  gate, up [rows, cols] with one
- * stride (the halves of a product's rows, or two tensors), gate_q, up_q [rows,
- * cols] and gate_s, up_s [rows, ceil(cols/128)] likewise.  n_rows: NULL, or a
- * device int32 (offsets[n_experts] of the sort): only that many rows are read and
- * written. */
+ * asap_moe_fp8_quantize would quantise them.  1 / (1 + exp(-gate)) counts as 0
+ * where the exponential passes its range: gate below -87.3 in bf16 and fp16, -88.7
+ * in fp32.  gate, up [rows, cols] with one stride (the halves of a product's rows,
+ * or two tensors), gate_q, up_q [rows, cols] and gate_s, up_s [rows,
+ * ceil(cols/128)] likewise.  n_rows: NULL, or a device int32 (offsets[n_experts] of
+ * the sort): only that many rows are read and written. */
 int asap_moe_swiglu_save(int32_t type, const void* gate, const void* up, int64_t ld, int32_t rows,
                          int32_t cols, const int32_t* n_rows, void* h, int64_t ldh, void* gate_q,
                          void* up_q, int64_t ldq, float* gate_s, float* up_s, int64_t lds,
                          void* stream);
 
 /* The gradients of silu(gate) * up at what was kept (G, U: e4m3 times scale; S =
- * 1 / (1 + exp(-G))):
+ * 1 / (1 + exp(-G)), 0 below the same bounds):
  *   d_gate = d_h U (S + G S (1 - S)),  d_up = d_h G S
  * and h = G S U for the gradient of the next product's weight (NULL: not wanted).
  * d_gate, d_up [rows, cols] with one stride; n_rows as above. */

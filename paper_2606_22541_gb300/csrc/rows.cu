@@ -252,8 +252,9 @@ __global__ void __launch_bounds__(kManyThreads)
 
 // Entries of one cluster at most; below which one small CTA ranks them all; entries for each CTA of a cluster.  Measured
 // with 256 experts, us: one CTA / a cluster / three kernels for 2048 entries 3.9 / 5.0 / -, 4096 5.2 / 6.0 / 6.2, 16384
-// - / 6.2 / 6.7, 32768 - / 7.0 / 6.7 (one launch on the host instead of three), 65536 - / 9.0 / 6.7.  Bound by latency: 8.4
-// million entries take 60 us, the 101 MB that the three kernels move would take 15.
+// - / 6.2 / 6.7, 32768 - / 7.0 / 6.7 (one launch on the host instead of three), 65536 - / 9.0 / 6.7: bound by latency.
+// Millions of entries are bound by the kernels' own work: 8.4 million take 62 us, the 101 MB that the three kernels move
+// would take 15.  Alone they take 10 (count), 25 (scan: E / 32 CTAs, which read the counts twice) and 36 (votes and places).
 constexpr long long kClusterEntries = 32768, kSmallEntries = 4096, kCtaEntries = 1024;
 static_assert(kClusterEntries <= 8 * 1024 * kSortRounds && kSmallEntries <= 512 * kSortRounds, "entries of the launches");
 
@@ -262,16 +263,22 @@ static_assert(kClusterEntries <= 8 * 1024 * kSortRounds && kSmallEntries <= 512 
 // CTA; a thread has every blockDim.x-th unit (16 bytes) of its row.  With few rows the
 // columns are spread over gridDim.y CTAs as well; with many a CTA takes rows in turn
 // and has the next one's places on their way (the chain from a place to its row's
-// loads is what these kernels wait for most).  All are bound by HBM; a call of many
-// rows moves its bytes at 0.92 to 0.97 of the copy rate:
+// loads is what these kernels wait for most).  A call of many wide rows is bound by
+// HBM and moves its bytes at 0.94 to 0.97 of the copy rate:
 //   permute 8045 tokens of 7168 bf16, k 8: 157 us, its bytes at the copy rate 152.7
-//   unpermute 5185 of 7168 bf16, k 8: 103 (98.5); 3584 of 4096 fp16, k 2: 15.5 (12.1)
-//   gradients 4096 of 7168 bf16, k 8: 155 (147); 3584 of 4096, k 2: 26.7 (21.6)
+//   unpermute 5185 of 7168 bf16, k 8: 104 (98.5)
+//   gradients 4096 of 7168 bf16, k 8: 156 (147)
 //   e4m3 rows of 4096 x 7168 read back, k 8: 77.5 (73.6)
-// Rows that do not start on 16 bytes are shifted into place (struct Any): unpermute
-// 3780 of 4401 bf16, k 7: 71 us (39), with 2-byte accesses 155, in 4-byte words 268; fp32
-// rows, which need no shifts, go by 4 bytes with more of them on their way: 107 (78),
-// shifted 16 bytes 155.
+// Calls of 10 to 50 us are at about 0.8, held up by that chain and the launch's ends:
+//   unpermute 3584 of 4096 fp16, k 2: 15.5 (12.1); gradients 3584 of 4096, k 2: 26.7 (21.6)
+// The gradients of narrow rows, whose next row has only its places ahead, at 0.34 to 0.67:
+//   4431 of 1152 bf16, k 4: 20.3 (13.6); 4044 of 272, k 3: 6.2 (2.3); 5994 of 144, k 5: 8.3 (2.9)
+// 16-bit rows that do not start on 8 bytes are shifted into place (struct Any), with two
+// loads for every 16 bytes, 0.45 to 0.55 for sums and gradients:
+//   unpermute 3780 of 4401 bf16, k 7: 73 us (39), with 2-byte accesses 155, in 4-byte words 268;
+//   14762 of 2254, k 7: 142 (78); gradients of those: 268 (147); 3406 of 1909, k 7: 63 (29)
+// fp32 rows, which need no shifts, go by 4 bytes with more of them on their way: 3780 of
+// 4401, k 7: 107 (78), shifted 16 bytes 155.
 constexpr int kRowThreads = 256;
 constexpr int kSms = 152;
 constexpr int kFewCtas = kSms * 4;  // below this many CTAs a call is short of work
